@@ -567,6 +567,133 @@ int32_t ps_stack_stats(ps_stack *st, ps_stats *out);
 int32_t ps_stack_op_time(ps_stack *st, uint32_t i, double *start_ms, double *dur_ms);
 void ps_stack_destroy(ps_stack *st);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators of a step that answers several drafted tokens at once.  A draft (a small model, a table of
+ * earlier text) proposes a TREE of tokens: node 0 is the last known token, every other node follows its
+ * parent; the stack answers all of them in one forward, the drafts that the answers bear out are kept.
+ * Each operator stands alone on device tensors of any decoder, and the stack uses them for its own
+ * forwards (ps_stack_set_rotation, ps_stack_set_tree, ps_stack_verify_tree, ps_stack_keep_path).
+ *
+ * All pointers are device memory of the stream's device, which must be the current one; strides count
+ * elements.  Calls are asynchronous on `stream`, allocate nothing, write no memory but their outputs and
+ * the caller's workspace, and can be captured into a HIP graph (kernel nodes only).  Two calls that may
+ * overlap in time, replays of captured ones among them, need workspaces of their own.
+ * A batch of n_seq sequences has its tokens one after the other: sequence s owns rows first[s] ..
+ * first[s + 1] - 1 of the token arrays; rows from first[n_seq] on (a padded batch) are neither read nor
+ * written.  Values of these arrays cannot be checked by the host, so the kernels bound them: first is
+ * clamped to 0 .. n_tokens, a sequence's tokens beyond max_tree are left out, context is clamped to
+ * 0 .. max_context, and a parent that does not lie in front of its node counts as none (-1). */
+#define PS_TYPE_F16 0u
+#define PS_TYPE_BF16 1u
+#define PS_TYPE_F32 2u
+#define PS_TREE_MAX 256u /* tokens of one sequence's tree */
+
+/* RMS norm of every query and key head and the rotation of positions, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * gain      (norm = 0: y = x)
+ *   the first rot_dim dimensions in pairs (a, b), pair i turned by the angle positions[t] * inv_freq[i]:
+ *   (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin);  the others stay y
+ * pairs = 0: pair i is dimensions (i, i + rot_dim / 2); 1: (2 i, 2 i + 1).  Sums and products in fp32, the
+ * angle in 64 bits (a position of a million times a frequency of 1 keeps its fraction), one rounding at the end.
+ *  type F16, BF16 or F32: of q, k, the gains and the outputs.  q [n_tokens][n_q_heads][head_dim], k [n_tokens]
+ *  [n_k_heads][head_dim] with the strides below (dimensions lie together); n_q_heads or n_k_heads may be 0.
+ *  head_dim 1 .. 512, rot_dim even, 0 .. head_dim (0: no rotation, inv_freq and positions are not read).
+ *  q_gain, k_gain [head_dim] or NULL (gain 1).  q_out may be q and k_out k, with the same strides (in place);
+ *  otherwise outputs may not overlap inputs or each other.  Alignment of an element is enough; rows whose
+ *  addresses and strides are multiples of 16 bytes are faster. */
+typedef struct ps_qk_norm_rope_args {
+    uint32_t type, n_tokens, n_q_heads, n_k_heads, head_dim, rot_dim, pairs, norm;
+    float eps;
+    uint32_t reserved;
+    const void *q, *k;
+    void *q_out, *k_out;
+    uint64_t q_token, q_head, k_token, k_head;
+    uint64_t q_out_token, q_out_head, k_out_token, k_out_head;
+    const void *q_gain, *k_gain;
+    const int32_t *positions; /* [n_tokens] */
+    const float *inv_freq;    /* [rot_dim / 2] */
+} ps_qk_norm_rope_args;
+int32_t ps_qk_norm_rope(const ps_qk_norm_rope_args *args, void *stream);
+
+/* Attention of the trees' tokens: token t of sequence s sees the cached positions 0 .. context[s] - 1 of its
+ * sequence, itself and its ancestors in the tree, and nothing else:
+ *   out[t][h] = sum_j w_j v_j,  w = softmax(scale q[t][h] . k_j),  kv head h / (n_q_heads / n_kv_heads)
+ * parent[t]: the parent's number within the sequence's tree, -1 for a node that follows the cache directly (there
+ * may be several).  A chain (parent[t] = t - 1) is causal attention of a chunk.
+ *  type F16 or BF16; head_dim 64 or 128; max_tree <= PS_TREE_MAX.  q, out [n_tokens][n_q_heads][head_dim]; k_new,
+ *  v_new [n_tokens][n_kv_heads][head_dim]; k_cache, v_cache [n_seq][n_kv_heads][capacity][head_dim], all with the
+ *  strides below.  Every address and stride in bytes is a multiple of 16 (PS_E_ARG otherwise), and 64 rows of the
+ *  cache or of new tokens span less than 2 GiB.  max_context: a bound on context[], <= capacity; work is dealt out by it.
+ *  append = 1: the tokens' K and V rows are also written to the cache, row context[s] + t (max_context + max_tree
+ *  <= capacity); each sequence's cache must then be its own.  out may not overlap any input.
+ * Scores, softmax and sums in fp32; the weights of the value product are rounded to `type`, and the weights' sum is
+ * taken of the rounded ones.  ps_tree_attention_workspace: the workspace bytes of these arguments (a function of
+ * the sizes, not of pointers or device values); 256-byte aligned. */
+typedef struct ps_tree_attention_args {
+    uint32_t type, n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim;
+    uint32_t max_context, max_tree, capacity, append;
+    float scale;
+    uint32_t reserved;
+    const void *q, *k_new, *v_new;
+    void *k_cache, *v_cache; /* written with append only */
+    void *out;
+    uint64_t q_token, q_head, k_new_token, k_new_head, v_new_token, v_new_head;
+    uint64_t k_seq, k_head, k_row, v_seq, v_head, v_row;
+    uint64_t out_token, out_head;
+    const int32_t *first;   /* [n_seq + 1] */
+    const int32_t *context; /* [n_seq]     */
+    const int32_t *parent;  /* [n_tokens]  */
+} ps_tree_attention_args;
+int32_t ps_tree_attention_workspace(const ps_tree_attention_args *args, uint64_t *bytes);
+int32_t ps_tree_attention(const ps_tree_attention_args *args, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Which drafts the target model accepts, from given random numbers, so that every token kept or drawn is
+ * distributed as if the target alone had drawn it.  Rows p = softmax(target_logits[t] / T), q = softmax(
+ * draft_logits[t] / T): the distributions BEHIND node t, T = temperature[s] of its sequence (NULL: 1).  From node 0,
+ * a node's children are tried in the order of their numbers, the k-th (token x, random number u = u_accept[its row]):
+ *   with draft_logits (the children were drawn one by one from q):  accepted if  p(x) > (c_k + u W_k) q(x),
+ *     c_0 = 0, W_0 = 1, c_(k+1) = c_k + W_k, W_(k+1) = sum over the vocabulary of max(p - c_(k+1) q, 0):
+ *     what is left after a refusal, max(p_k - q, 0) scaled to sum 1, written with p and q of the node;
+ *   without (the children are given tokens):  p_k is p without the refused tokens, accepted if  p_k(x) > u sum(p_k).
+ * The walk goes on from the first accepted child.  Where none is accepted the next token is drawn from what is
+ * left: the first index whose running sum passes u_sample[s] times the sum (nothing left: from p).  T <= 0 or not a
+ * number: no sampling, p is 1 at the largest logit (the lowest index among equals), q is not read.  Random numbers
+ * lie in [0, 1).  A logit that is no number counts as -inf, +inf as the largest finite number; a row of -inf alone
+ * accepts nothing and its token is -1.  A token outside the vocabulary has probability 0.
+ * At most max_children children of a node are tried (1 .. 256; with draft_logits each costs a launch); parents of nodes other than 0
+ * that count as none are never reached.  Sums and exponentials are in 64 bits: a border of the running sum lies among
+ * a hundred thousand others, and the same inputs give the same tokens whatever the launch.
+ *  type F16, BF16 or F32 of the logits; rows [n_tokens][vocab] with the strides below, dimensions together;
+ *  vocab 1 .. 2^24, alignment of an element is enough.
+ *  path [n_seq][max_tree] (path_seq elements apart): the accepted nodes, node 0 first, then -1; count [n_seq]: how
+ *  many (0: the sequence has no token); next_token [n_seq].  */
+typedef struct ps_verify_tree_args {
+    uint32_t type, n_seq, n_tokens, vocab, max_tree, max_children;
+    const void *target_logits, *draft_logits;
+    uint64_t target_row, draft_row, path_seq;
+    const int32_t *first, *token, *parent;
+    const float *u_accept, *u_sample, *temperature;
+    int32_t *path, *count, *next_token;
+} ps_verify_tree_args;
+int32_t ps_verify_tree_workspace(const ps_verify_tree_args *args, uint64_t *bytes);
+int32_t ps_verify_tree(const ps_verify_tree_args *args, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Keep the accepted path's rows of a cache: row context[s] + path[s][i] of every plane moves to row context[s] + i,
+ * for i < count[s] (at most max_tree).  All rows of a plane are read before one is written, so any path may be
+ * given, the same node twice too; an entry outside 0 .. max_tree - 1, or a row outside 0 .. capacity - 1, is left
+ * out (its place keeps what it holds).  cache: n_planes planes of `capacity` rows of row_bytes bytes for each
+ * sequence (every layer's and kv head's K and V are planes), strides in BYTES; everything a multiple of 16, row_bytes
+ * 16 .. 4096, max_tree <= PS_TREE_MAX.  Rows that are not moved to are left as they were. */
+typedef struct ps_cache_keep_args {
+    uint32_t n_seq, n_planes, capacity, row_bytes, max_tree, reserved;
+    void *cache;
+    uint64_t seq_stride, plane_stride, row_stride;
+    uint64_t path_seq;      /* elements between two sequences' paths */
+    const int32_t *path;    /* [n_seq][max_tree] */
+    const int32_t *count;   /* [n_seq] */
+    const int32_t *context; /* [n_seq] */
+} ps_cache_keep_args;
+int32_t ps_cache_keep(const ps_cache_keep_args *args, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

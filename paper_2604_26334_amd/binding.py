@@ -90,7 +90,44 @@ class ps_op_info(C.Structure):
                 ("slot_offset", C.c_uint64), ("bytes", C.c_uint64)]
 
 
-EXPORTS = ["ps_stack_create_tiers", "ps_stack_set_tier", "ps_stack_tier", "ps_stack_forward_noalloc", "ps_plan_num_shards", "ps_stack_forward_chunked", "ps_last_error", "ps_tier_tokens", "ps_tier_for_tokens", "ps_packed_bytes", "ps_plan_create",
+PS_TYPE_F16, PS_TYPE_BF16, PS_TYPE_F32 = 0, 1, 2
+PS_TREE_MAX = 256
+
+
+class ps_qk_norm_rope_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "n_tokens", "n_q_heads", "n_k_heads", "head_dim", "rot_dim", "pairs", "norm")] + \
+               [("eps", C.c_float), ("reserved", C.c_uint32)] + \
+               [(n, C.c_void_p) for n in ("q", "k", "q_out", "k_out")] + \
+               [(n, C.c_uint64) for n in ("q_token", "q_head", "k_token", "k_head", "q_out_token", "q_out_head", "k_out_token", "k_out_head")] + \
+               [(n, C.c_void_p) for n in ("q_gain", "k_gain", "positions", "inv_freq")]
+
+
+class ps_tree_attention_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "n_seq", "n_tokens", "n_q_heads", "n_kv_heads", "head_dim", "max_context",
+                                          "max_tree", "capacity", "append")] + \
+               [("scale", C.c_float), ("reserved", C.c_uint32)] + \
+               [(n, C.c_void_p) for n in ("q", "k_new", "v_new", "k_cache", "v_cache", "out")] + \
+               [(n, C.c_uint64) for n in ("q_token", "q_head", "k_new_token", "k_new_head", "v_new_token", "v_new_head", "k_seq",
+                                          "k_head", "k_row", "v_seq", "v_head", "v_row", "out_token", "out_head")] + \
+               [(n, C.c_void_p) for n in ("first", "context", "parent")]
+
+
+class ps_verify_tree_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "n_seq", "n_tokens", "vocab", "max_tree", "max_children")] + \
+               [(n, C.c_void_p) for n in ("target_logits", "draft_logits")] + \
+               [(n, C.c_uint64) for n in ("target_row", "draft_row", "path_seq")] + \
+               [(n, C.c_void_p) for n in ("first", "token", "parent", "u_accept", "u_sample", "temperature", "path", "count",
+                                          "next_token")]
+
+
+class ps_cache_keep_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("n_seq", "n_planes", "capacity", "row_bytes", "max_tree", "reserved")] + \
+               [("cache", C.c_void_p)] + [(n, C.c_uint64) for n in ("seq_stride", "plane_stride", "row_stride", "path_seq")] + \
+               [(n, C.c_void_p) for n in ("path", "count", "context")]
+
+
+EXPORTS = ["ps_qk_norm_rope", "ps_tree_attention", "ps_tree_attention_workspace", "ps_verify_tree", "ps_verify_tree_workspace",
+           "ps_cache_keep", "ps_stack_create_tiers", "ps_stack_set_tier", "ps_stack_tier", "ps_stack_forward_noalloc", "ps_plan_num_shards", "ps_stack_forward_chunked", "ps_last_error", "ps_tier_tokens", "ps_tier_for_tokens", "ps_packed_bytes", "ps_plan_create",
            "ps_plan_summary", "ps_plan_get_shard", "ps_plan_destroy", "ps_schedule_create",
            "ps_schedule_num_ops", "ps_schedule_get_op", "ps_schedule_validate", "ps_schedule_destroy",
            "ps_route_host", "ps_profile_measure", "ps_stack_create", "ps_stack_load_matrix",
@@ -174,6 +211,12 @@ def lib():
             "ps_stack_load_kv": [vp, u32, u32, vp, vp, u32],
             "ps_stack_set_context": [vp, u32],
             "ps_stack_set_logits_out": [vp, vp, u32, u32],
+            "ps_qk_norm_rope": [C.POINTER(ps_qk_norm_rope_args), vp],
+            "ps_tree_attention_workspace": [C.POINTER(ps_tree_attention_args), C.POINTER(u64)],
+            "ps_tree_attention": [C.POINTER(ps_tree_attention_args), vp, u64, vp],
+            "ps_verify_tree_workspace": [C.POINTER(ps_verify_tree_args), C.POINTER(u64)],
+            "ps_verify_tree": [C.POINTER(ps_verify_tree_args), vp, u64, vp],
+            "ps_cache_keep": [C.POINTER(ps_cache_keep_args), vp],
             "ps_cpu_matmul": [vp, u32, u32, i32, vp, u32, C.c_float, vp, vp, u32],
         }
         for name, args in sig.items():
@@ -672,3 +715,178 @@ def load_synthetic(stacks, cfg, seed, threads=8, lookahead=12, progress=None):
             if progress and (done % progress == 0 or done == len(todo)):
                 import sys
                 print("  loaded %d / %d matrices" % (done, len(todo)), file=sys.stderr, flush=True)
+
+
+# ---------------------------------------------------------------- operators on device tensors
+# Thin forms of ps_qk_norm_rope, ps_tree_attention, ps_verify_tree and ps_cache_keep: torch CUDA tensors in, launched on the
+# current stream of their device; outputs (and workspaces, unless given) come from torch's allocator on that stream.
+
+_TYPE = {}
+
+
+def _type_of(t):
+    if not _TYPE:
+        import torch
+        _TYPE.update({torch.float16: PS_TYPE_F16, torch.bfloat16: PS_TYPE_BF16, torch.float32: PS_TYPE_F32})
+    if t.dtype not in _TYPE:
+        raise PshardError(PS_E_ARG, "float16, bfloat16 or float32 tensors are taken, not %s" % t.dtype)
+    return _TYPE[t.dtype]
+
+
+def _want(ok, text):
+    if not ok:
+        raise PshardError(PS_E_ARG, text)
+
+
+def _same(name, t, shape, dtype, device):
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
+        raise PshardError(PS_E_ARG, "%s must be %s %s on %s (got %s %s on %s)" % (
+            name, dtype, list(shape), device, t.dtype, list(t.shape), t.device))
+
+
+def _rows(name, t):
+    """Strides of a tensor whose last dimension lies together (a dimension of one element may have any stride)."""
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] > 1:
+        raise PshardError(PS_E_ARG, "%s: the last dimension must be contiguous" % name)
+    if min(st) < 0:
+        raise PshardError(PS_E_ARG, "%s: negative strides" % name)
+    return st
+
+
+def _table(name, t, n, dtype, device):
+    """A contiguous 1-d tensor of n elements, as its address."""
+    _same(name, t, (n,), dtype, device)
+    if n > 1 and t.stride(0) != 1:
+        raise PshardError(PS_E_ARG, "%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+def _on(device):
+    """The device made current (if it is not) and its current stream."""
+    import torch
+    if device.type != "cuda":
+        raise PshardError(PS_E_ARG, "tensors on a GPU are taken, not on %s" % device)
+    return torch.cuda.device(device), torch.cuda.current_stream(device).cuda_stream
+
+
+def _workspace(need, given, device):
+    import torch
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _want(given.dtype == torch.uint8 and given.is_contiguous() and given.device == device, "workspace must be contiguous uint8 on %s" % device)
+    return given
+
+
+def qk_norm_rope(q, k, positions, inv_freq, q_gain=None, k_gain=None, eps=1e-6, norm=True, pairs=False, q_out=None, k_out=None):
+    """ps_qk_norm_rope.  q [tokens, q heads, dim], k [tokens, k heads, dim] of one type (last dimension contiguous, other strides
+    free); positions int32 [tokens] and inv_freq float32 [rotated / 2], or both None (no rotation).  Returns (q_out, k_out): new
+    tensors, or the given ones (q_out = q, k_out = k: in place)."""
+    import torch
+    _want(q.dim() == 3 and k.dim() == 3, "q and k are [tokens, heads, dim]")
+    n, hq, d = q.shape
+    hk, dev, dt = k.shape[1], q.device, q.dtype
+    ty = _type_of(q)
+    _same("k", k, (n, hk, d), dt, dev)
+    q_out = torch.empty((n, hq, d), dtype=dt, device=dev) if q_out is None else q_out
+    k_out = torch.empty((n, hk, d), dtype=dt, device=dev) if k_out is None else k_out
+    _same("q_out", q_out, (n, hq, d), dt, dev)
+    _same("k_out", k_out, (n, hk, d), dt, dev)
+    _want((positions is None) == (inv_freq is None), "positions and inv_freq come together")
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    s = [_rows(name, t) for name, t in (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out))]
+    a = ps_qk_norm_rope_args(
+        ty, n, hq, hk, d, rot, int(bool(pairs)), int(bool(norm)), eps, 0, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
+        s[0][0], s[0][1], s[1][0], s[1][1], s[2][0], s[2][1], s[3][0], s[3][1],
+        None if q_gain is None else _table("q_gain", q_gain, d, dt, dev), None if k_gain is None else _table("k_gain", k_gain, d, dt, dev),
+        None if positions is None else _table("positions", positions, n, torch.int32, dev),
+        None if inv_freq is None else _table("inv_freq", inv_freq, rot // 2, torch.float32, dev))
+    here, stream = _on(dev)
+    with here:
+        _check(lib().ps_qk_norm_rope(C.byref(a), stream))
+    return q_out, k_out
+
+
+def tree_attention(q, k_new, v_new, k_cache, v_cache, first, context, parent, max_context, max_tree, scale=None, append=False, out=None,
+                   workspace=None):
+    """ps_tree_attention.  q [tokens, q heads, dim], k_new / v_new [tokens, kv heads, dim], k_cache / v_cache [sequences, kv heads,
+    capacity, dim] of one type (last dimension contiguous, other strides free); first int32 [sequences + 1], context int32
+    [sequences], parent int32 [tokens].  max_context, max_tree: bounds on context and on the tokens of a sequence.  Returns out
+    [tokens, q heads, dim]: the given tensor, or a new one (whose rows of no sequence hold anything)."""
+    import torch
+    _want(q.dim() == 3 and k_new.dim() == 3 and k_cache.dim() == 4, "q, k_new are [tokens, heads, dim], the caches [sequences, heads, capacity, dim]")
+    n, hq, d = q.shape
+    hk, dev, dt = k_new.shape[1], q.device, q.dtype
+    ty = _type_of(q)
+    b, cap = k_cache.shape[0], k_cache.shape[2]
+    _same("k_new", k_new, (n, hk, d), dt, dev)
+    _same("v_new", v_new, (n, hk, d), dt, dev)
+    _same("k_cache", k_cache, (b, hk, cap, d), dt, dev)
+    _same("v_cache", v_cache, (b, hk, cap, d), dt, dev)
+    out = torch.empty((n, hq, d), dtype=dt, device=dev) if out is None else out
+    _same("out", out, (n, hq, d), dt, dev)
+    sq, sk, sv, ck, cv, so = (_rows(name, t) for name, t in (("q", q), ("k_new", k_new), ("v_new", v_new), ("k_cache", k_cache),
+                                                             ("v_cache", v_cache), ("out", out)))
+    a = ps_tree_attention_args(
+        ty, b, n, hq, hk, d, int(max_context), int(max_tree), cap, int(bool(append)), d ** -0.5 if scale is None else scale, 0,
+        q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(),
+        sq[0], sq[1], sk[0], sk[1], sv[0], sv[1], ck[0], ck[1], ck[2], cv[0], cv[1], cv[2], so[0], so[1],
+        _table("first", first, b + 1, torch.int32, dev), _table("context", context, b, torch.int32, dev),
+        _table("parent", parent, n, torch.int32, dev))
+    here, stream = _on(dev)
+    with here:
+        need = C.c_uint64()
+        _check(lib().ps_tree_attention_workspace(C.byref(a), C.byref(need)))
+        ws = _workspace(need.value, workspace, dev)
+        _check(lib().ps_tree_attention(C.byref(a), ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, stream))
+    return out
+
+
+def verify_tree(target_logits, token, parent, first, u_accept, u_sample, draft_logits=None, temperature=None, max_tree=PS_TREE_MAX,
+                max_children=PS_TREE_MAX, path=None, count=None, next_token=None, workspace=None):
+    """ps_verify_tree.  target_logits (and draft_logits) [tokens, vocab] of one type; token, parent int32 [tokens]; first int32
+    [sequences + 1]; u_accept float32 [tokens], u_sample float32 [sequences], temperature float32 [sequences] or None.  Returns
+    (path int32 [sequences, max_tree], count int32 [sequences], next_token int32 [sequences])."""
+    import torch
+    _want(target_logits.dim() == 2, "logits are [tokens, vocab]")
+    n, v = target_logits.shape
+    dev, dt, b = target_logits.device, target_logits.dtype, u_sample.numel()
+    ty = _type_of(target_logits)
+    if draft_logits is not None:
+        _same("draft_logits", draft_logits, (n, v), dt, dev)
+    i32 = torch.int32
+    path = torch.empty((b, int(max_tree)), dtype=i32, device=dev) if path is None else path
+    count = torch.empty(b, dtype=i32, device=dev) if count is None else count
+    next_token = torch.empty(b, dtype=i32, device=dev) if next_token is None else next_token
+    _same("path", path, (b, int(max_tree)), i32, dev)
+    a = ps_verify_tree_args(
+        ty, b, n, v, int(max_tree), int(max_children), target_logits.data_ptr(), None if draft_logits is None else draft_logits.data_ptr(),
+        _rows("target_logits", target_logits)[0], 0 if draft_logits is None else _rows("draft_logits", draft_logits)[0], _rows("path", path)[0],
+        _table("first", first, b + 1, i32, dev), _table("token", token, n, i32, dev), _table("parent", parent, n, i32, dev),
+        _table("u_accept", u_accept, n, torch.float32, dev), _table("u_sample", u_sample, b, torch.float32, dev),
+        None if temperature is None else _table("temperature", temperature, b, torch.float32, dev),
+        path.data_ptr(), _table("count", count, b, i32, dev), _table("next_token", next_token, b, i32, dev))
+    here, stream = _on(dev)
+    with here:
+        need = C.c_uint64()
+        _check(lib().ps_verify_tree_workspace(C.byref(a), C.byref(need)))
+        ws = _workspace(need.value, workspace, dev)
+        _check(lib().ps_verify_tree(C.byref(a), ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, stream))
+    return path, count, next_token
+
+
+def cache_keep(cache, path, count, context):
+    """ps_cache_keep, in place.  cache [sequences, planes, capacity, dim] of any type (rows contiguous, other strides free); path int32
+    [sequences, max_tree], count, context int32 [sequences], as verify_tree and tree_attention have them.  Returns cache."""
+    import torch
+    _want(cache.dim() == 4 and path.dim() == 2, "cache is [sequences, planes, capacity, dim], path [sequences, max_tree]")
+    b, planes, cap, d = cache.shape
+    dev, e = cache.device, cache.element_size()
+    _same("path", path, (b, path.shape[1]), torch.int32, dev)
+    st = _rows("cache", cache)
+    a = ps_cache_keep_args(b, planes, cap, d * e, path.shape[1], 0, cache.data_ptr(), st[0] * e, st[1] * e, st[2] * e, _rows("path", path)[0],
+                           path.data_ptr(), _table("count", count, b, torch.int32, dev), _table("context", context, b, torch.int32, dev))
+    here, stream = _on(dev)
+    with here:
+        _check(lib().ps_cache_keep(C.byref(a), stream))
+    return cache
