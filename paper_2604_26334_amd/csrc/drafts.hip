@@ -5,7 +5,9 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "ps_internal.h"
 
@@ -15,6 +17,8 @@ namespace {
 
 typedef _Float16 f16_t;
 typedef __bf16 bf16_t;
+typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u2_t __attribute__((ext_vector_type(2)));
 
 constexpr float kFloatMax = 3.402823466e38f;
 
@@ -66,44 +70,422 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(ps_qk_norm_rope_args 
 }
 
 // ------------------------------------------------------------------------------------ tree attention
-// A wave per (sequence, token, query head): one position after the other, running maximum and sum.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void tree_attention_kernel(ps_tree_attention_args a) {
-    const uint32_t s = blockIdx.z, h = blockIdx.y, lane = threadIdx.x;
+// Score rows are (token, query head of the kv group) pairs.  A workgroup of four waves holds a block of NT x 16 rows of one kv
+// head and a run of 32-position tiles; its waves take the tiles in turn, each with a running maximum, weight sum and value sums
+// of its own, and meet in LDS at the end: no barrier in the walk.
+//  scores, transposed: S^T = K Q^T, A = 16 positions x 32 dims of K straight from memory into registers, B = 16 rows of
+//   queries (registers, loaded once): lane (row j, c) then holds four positions of row j for each of two tiles;
+//  weights x values, transposed: O^T = V^T P^T, B = the weights exactly as the score accumulators hold them (the two
+//   16-position tiles are numbered so that lane group c owns 8 consecutive positions: 4 from each), A = 16 dims x 32 positions of V
+//   by LDS transpose reads of the wave's own stage; and the weights' sum by one more product, with ones.
+// The next tile's K and V are requested as soon as the scores have used this one's K and its V lies in LDS.  They go through
+// registers: in front of a transpose read the compiler waits for every load into LDS, the next tile's too.
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef f16_t f16x8_t __attribute__((ext_vector_type(8)));
+typedef bf16_t bf16x8_t __attribute__((ext_vector_type(8)));
+
+template <typename T> struct Mfma;
+template <> struct Mfma<f16_t> {
+    typedef f16x8_t v8;
+    static constexpr uint32_t kInf = 0x7C007C00u;
+    static __device__ __forceinline__ f4_t mul(v8 a, v8 b, f4_t c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+#else
+        return c;
+#endif
+    }
+};
+template <> struct Mfma<bf16_t> {
+    typedef bf16x8_t v8;
+    static constexpr uint32_t kInf = 0x7F807F80u;
+    static __device__ __forceinline__ f4_t mul(v8 a, v8 b, f4_t c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+#else
+        return c;
+#endif
+    }
+};
+
+// A operand of 16 dims x 32 positions from rows staged in LDS: two transpose reads, four rows (hi bytes) apart
+__device__ __forceinline__ u4_t transposed(const unsigned char *p, uint32_t hi) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s4_t;
+    typedef __attribute__((address_space(3))) s4_t lds_s4_t;
+    const u2_t a = __builtin_bit_cast(u2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t *)(p)));
+    const u2_t b = __builtin_bit_cast(u2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t *)(p + hi)));
+    return u4_t{a.x, a.y, b.x, b.y};
+#else
+    return u4_t{};
+#endif
+}
+// largest value of the four lanes that share a row (lane, lane ^ 16, ^ 32, ^ 48)
+__device__ __forceinline__ float row_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+// 16-byte piece u of a staged V row lies in slot u ^ swizzle: even swizzles keep the pair of pieces that a transpose read takes
+// together, and the eight rows of half a wave (8 c + 0 .. 3) lie in different banks
+template <int D> __device__ __forceinline__ uint32_t v_swizzle(uint32_t row) {
+    return D == 128 ? ((row & 3u) | (((row >> 3) & 1u) << 2)) << 1 : (((row >> 1) & 1u) | (((row >> 3) & 1u) << 1)) << 1;
+}
+
+constexpr uint32_t kTile = 32;           // positions of a tile
+constexpr uint32_t kMaskWords = PS_TREE_MAX / 32;
+
+struct TreeDeal { uint32_t nt, blocks, nsplit; };
+
+template <int D, int NT> constexpr uint32_t tree_lds() {
+    const uint32_t stages = 4 * kTile * D * 2, meet = 4 * NT * 16 * (D + 4) * 4 + 4 * NT * 16 * 2 * 4;
+    return std::max(stages, meet) + PS_TREE_MAX * kMaskWords * 4 + PS_TREE_MAX * 4 + 16;
+}
+
+// Tiles of sequence: the cache's, then the tree's own; each split takes `per` of them
+__device__ __forceinline__ uint32_t tiles_per_split(uint32_t tiles, uint32_t nsplit) { return ((tiles + nsplit - 1) / nsplit + 3) & ~3u; }
+
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attention_args a, uint32_t blocks, uint32_t nsplit, float *part) {
+    using M = Mfma<T>;
+    using v8 = typename M::v8;
+    constexpr int KK = D / 32, DT = D / 16, RB = NT * 16, OP = D + 4;
+    constexpr uint32_t kStage = kTile * D * 2, kRowPieces = D / 8, kVLoads = kStage / 1024;
+    extern __shared__ u4_t tree_lds_mem[];
+    unsigned char *const lds = reinterpret_cast<unsigned char *>(tree_lds_mem);
+    constexpr uint32_t kTables = tree_lds<D, NT>() - (PS_TREE_MAX * kMaskWords * 4 + PS_TREE_MAX * 4 + 16);
+    uint32_t *const anc = reinterpret_cast<uint32_t *>(lds + kTables);           // [token][word]: itself and its ancestors
+    int *const up = reinterpret_cast<int *>(anc + PS_TREE_MAX * kMaskWords);
+    int *const wild = up + PS_TREE_MAX;                                          // some own value is infinite or no number
+
+    // blocks of the same positions lie 8 workgroups apart: on one XCD, whose L2 they share
+    const uint32_t units = a.n_seq * a.n_kv_heads * nsplit;
+    const uint32_t unit = blockIdx.x / 8 / blocks * 8 + blockIdx.x % 8, rb = blockIdx.x / 8 % blocks;
+    if (unit >= units) return;
+    const uint32_t z = unit % nsplit, hk = unit / nsplit % a.n_kv_heads, s = unit / nsplit / a.n_kv_heads;
     const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
-    const int t = blockIdx.x;
-    if (t >= sr.n) return;
-    const int ctx = clampi(a.context[s], 0, (int)a.max_context);
-    const uint32_t hk = h / (a.n_q_heads / a.n_kv_heads);
-    constexpr int E = D / 64;
-    float q[E], o[E];
-    const size_t row = (size_t)sr.row0 + t;
-    for (int e = 0; e < E; ++e) { q[e] = to_f(static_cast<const T *>(a.q)[row * a.q_token + h * a.q_head + lane * E + e]); o[e] = 0.f; }
-    float m = -INFINITY, l = 0.f;
-    auto see = [&](const T *k, const T *v) {
-        float d = 0.f;
-        for (int e = 0; e < E; ++e) d = fmaf(q[e], to_f(k[lane * E + e]), d);
-        for (int x = 32; x; x >>= 1) d += __shfl_xor(d, x, 64);
-        d *= a.scale;
-        const float mn = fmaxf(m, d), r = m == -INFINITY ? 0.f : __expf(m - mn), w = mn == -INFINITY ? 0.f : __expf(d - mn);
-        m = mn;
-        l = l * r + w;
-        for (int e = 0; e < E; ++e) o[e] = o[e] * r + w * to_f(v[lane * E + e]);
+    const uint32_t ctx = clampi(a.context[s], 0, (int)a.max_context), t_n = sr.n, G = a.n_q_heads / a.n_kv_heads;
+    const uint32_t R = t_n * G, row0 = rb * RB;
+    if (row0 >= R) return;
+    const uint32_t nc = (ctx + kTile - 1) / kTile, tiles = nc + (t_n + kTile - 1) / kTile, per = tiles_per_split(tiles, nsplit);
+    const uint32_t lo = z * per, hi = min(tiles, lo + per);
+    if (lo >= hi) return;               // (the merge knows how many splits a sequence has)
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t i = lane & 15, c = lane >> 4;
+
+    const char *kc = reinterpret_cast<const char *>(static_cast<const T *>(a.k_cache) + s * a.k_seq + hk * a.k_head);
+    const char *vc = reinterpret_cast<const char *>(static_cast<const T *>(a.v_cache) + s * a.v_seq + hk * a.v_head);
+    const T *kn = static_cast<const T *>(a.k_new) + (size_t)sr.row0 * a.k_new_token + hk * a.k_new_head;
+    const T *vn = static_cast<const T *>(a.v_new) + (size_t)sr.row0 * a.v_new_token + hk * a.v_new_head;
+    unsigned char *const stage = lds + wave * kStage;
+    // K: lane i of position tile Tt takes row 8 (i / 4) + i % 4 + 4 Tt; V: lane l fills slot l of four (D = 64: eight) rows
+    const uint32_t krow = 8 * (i >> 2) + (i & 3), vrow = lane / kRowPieces;
+    u4_t kreg[2][KK], vreg[kVLoads];
+    auto request = [&](uint32_t tile) {
+        const bool own = tile >= nc;
+        const uint32_t P0 = (own ? tile - nc : tile) * kTile, last = min(kTile, (own ? t_n : ctx) - P0) - 1;
+        const uint32_t krow_b = (uint32_t)(own ? a.k_new_token : a.k_row) * 2, vrow_b = (uint32_t)(own ? a.v_new_token : a.v_row) * 2;
+        // (rows past the last lie past the buffer's range: zeros)
+        const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((own ? reinterpret_cast<const char *>(kn) : kc) + (size_t)P0 * krow_b), 0,
+                                                                            (int)(last * krow_b + D * 2), 0x00020000);
+        const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((own ? reinterpret_cast<const char *>(vn) : vc) + (size_t)P0 * vrow_b), 0,
+                                                                            (int)(last * vrow_b + D * 2), 0x00020000);
+#pragma unroll
+        for (int Tt = 0; Tt < 2; ++Tt)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+                kreg[Tt][kk] = __builtin_bit_cast(u4_t, __builtin_amdgcn_raw_buffer_load_b128(kb, (krow + 4 * Tt) * krow_b + c * 16 + kk * 64, 0, 0));
+#pragma unroll
+        for (uint32_t u = 0; u < kVLoads; ++u) {
+            const uint32_t row = u * (64 / kRowPieces) + vrow;
+            vreg[u] = __builtin_bit_cast(u4_t, __builtin_amdgcn_raw_buffer_load_b128(vb, row * vrow_b + ((lane % kRowPieces) ^ v_swizzle<D>(row)) * 16, 0, 0));
+        }
     };
-    const T *kc = static_cast<const T *>(a.k_cache) + s * a.k_seq + hk * a.k_head, *vc = static_cast<const T *>(a.v_cache) + s * a.v_seq + hk * a.v_head;
-    for (int j = 0; j < ctx; ++j) see(kc + j * a.k_row, vc + j * a.v_row);
-    for (int j = t; j >= 0; j = parent_of(a.parent[sr.row0 + j], j))
-        see(static_cast<const T *>(a.k_new) + ((size_t)sr.row0 + j) * a.k_new_token + hk * a.k_new_head,
-            static_cast<const T *>(a.v_new) + ((size_t)sr.row0 + j) * a.v_new_token + hk * a.v_new_head);
-    for (int e = 0; e < E; ++e) static_cast<T *>(a.out)[row * a.out_token + h * a.out_head + lane * E + e] = (T)(o[e] / l);
-    if (a.append && h % (a.n_q_heads / a.n_kv_heads) == 0) {
-        T *kd = static_cast<T *>(a.k_cache) + s * a.k_seq + hk * a.k_head + ((size_t)ctx + t) * a.k_row;
-        T *vd = static_cast<T *>(a.v_cache) + s * a.v_seq + hk * a.v_head + ((size_t)ctx + t) * a.v_row;
-        for (int e = 0; e < E; ++e) {
-            kd[lane * E + e] = static_cast<const T *>(a.k_new)[row * a.k_new_token + hk * a.k_new_head + lane * E + e];
-            vd[lane * E + e] = static_cast<const T *>(a.v_new)[row * a.v_new_token + hk * a.v_new_head + lane * E + e];
+    if (lo + wave < hi) request(lo + wave);
+
+    // own tiles: which tokens each token sees
+    const bool own = hi > nc;
+    if (own) {
+        int link = -1;
+        uint32_t m[kMaskWords];
+        if (tid == 0) *wild = 0;
+        if (tid < t_n) {
+            link = parent_of(a.parent[sr.row0 + tid], (int)tid);
+#pragma unroll
+            for (uint32_t w = 0; w < kMaskWords; ++w) anc[tid * kMaskWords + w] = tid / 32 == w ? 1u << (tid % 32) : 0u;
+            up[tid] = link;
+        }
+        // every step doubles how far back a token's mask reaches
+        while (__syncthreads_or(link >= 0)) {
+            int next = -1;
+            if (link >= 0) {
+#pragma unroll
+                for (uint32_t w = 0; w < kMaskWords; ++w) m[w] = anc[link * kMaskWords + w];
+                next = up[link];
+            }
+            __syncthreads();
+            if (link >= 0) {
+#pragma unroll
+                for (uint32_t w = 0; w < kMaskWords; ++w) anc[tid * kMaskWords + w] |= m[w];
+                up[tid] = next;
+            }
+            link = next;
         }
     }
+    if (a.append && z == 0) {            // rows context and up, which nobody reads: each block moves the tokens whose first row it holds
+        const uint32_t t0 = (row0 + G - 1) / G, t1 = min(t_n, (row0 + RB + G - 1) / G);
+        T *kd = static_cast<T *>(a.k_cache) + s * a.k_seq + hk * a.k_head, *vd = static_cast<T *>(a.v_cache) + s * a.v_seq + hk * a.v_head;
+        for (uint32_t u = tid; u < (t1 - t0) * kRowPieces * 2; u += 256) {
+            const uint32_t t = t0 + u / (2 * kRowPieces), e = u % kRowPieces * 8;
+            const bool v = u / kRowPieces & 1;
+            *reinterpret_cast<u4_t *>(v ? vd + ((size_t)ctx + t) * a.v_row + e : kd + ((size_t)ctx + t) * a.k_row + e) =
+                *reinterpret_cast<const u4_t *>(v ? vn + (size_t)t * a.v_new_token + e : kn + (size_t)t * a.k_new_token + e);
+        }
+    }
+
+    // the block's rows of queries; a negative scale turns their signs
+    const float scale_abs = fabsf(a.scale);
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+    const float c2 = fmaxf(scale_abs * 1.4426950408889634f, 1e-30f);     // weights are 2^(c2 (s - m))
+    const float slack = 8.f / c2;      // a row is rescaled only where its weights would pass 2^8
+    uint32_t tok[NT];
+    v8 q[NT][KK];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const uint32_t rho = min(row0 + t * 16 + i, R - 1);
+        tok[t] = rho / G;
+        const T *qr = static_cast<const T *>(a.q) + ((size_t)sr.row0 + tok[t]) * a.q_token + (size_t)(hk * G + rho % G) * a.q_head + c * 8;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            u4_t v = *reinterpret_cast<const u4_t *>(qr + kk * 32);
+            v.x ^= sign; v.y ^= sign; v.z ^= sign; v.w ^= sign;
+            q[t][kk] = __builtin_bit_cast(v8, v);
+        }
+    }
+    float m_run[NT];
+    f4_t O[NT][DT], L[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m_run[t] = -INFINITY;
+        L[t] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) O[t][dt] = f4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    v8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (T)1.f;
+    uint32_t vread[DT];
+    {
+        const uint32_t row = 8 * c + (i >> 2);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vread[dt] = row * (D * 2) + (((2 * dt + ((i & 3) >> 1)) ^ v_swizzle<D>(row)) << 4) + (i & 1) * 8;
+    }
+    for (uint32_t tile = lo + wave; tile < hi; tile += 4) {
+        const bool mine = tile >= nc;                                   // (uniform) one of the tree's own tiles
+        const uint32_t P0 = (mine ? tile - nc : tile) * kTile;
+        f4_t S[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int Tt = 0; Tt < 2; ++Tt)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) S[t][Tt] = M::mul(__builtin_bit_cast(v8, kreg[Tt][kk]), q[t][kk], S[t][Tt]);
+        if (mine) {
+            // An infinite value or one that is no number must not meet the zero weight of a row that does not see it: the
+            // product takes zero in its place, and rows that do see it get it at the end.
+            bool odd = false;
+#pragma unroll
+            for (uint32_t u = 0; u < kVLoads; ++u) {
+                uint32_t d[4] = {vreg[u].x, vreg[u].y, vreg[u].z, vreg[u].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool l16 = (d[e] & M::kInf & 0xFFFFu) == (M::kInf & 0xFFFFu), h16 = (d[e] & M::kInf & 0xFFFF0000u) == (M::kInf & 0xFFFF0000u);
+                    odd |= l16 || h16;
+                    d[e] = (l16 ? 0u : d[e] & 0xFFFFu) | (h16 ? 0u : d[e] & 0xFFFF0000u);
+                }
+                vreg[u] = u4_t{d[0], d[1], d[2], d[3]};
+            }
+            if (odd) *wild = 1;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kVLoads; ++u) *reinterpret_cast<u4_t *>(stage + u * 1024 + lane * 16) = vreg[u];
+        if (tile + 4 < hi) request(tile + 4);
+        if (mine) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const uint32_t word = anc[tok[t] * kMaskWords + P0 / 32] >> (8 * c);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = word >> e & 1 ? S[t][e >> 2][e & 3] : -INFINITY;
+            }
+        } else if (ctx - P0 < kTile) {      // the cache's last tile
+            asm volatile("");
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = P0 + 8 * c + e < ctx ? S[t][e >> 2][e & 3] : -INFINITY;
+        }
+        v8 P[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float mx = fmaxf(fmaxf(fmaxf(S[t][0][0], S[t][0][1]), fmaxf(S[t][0][2], S[t][0][3])), fmaxf(fmaxf(S[t][1][0], S[t][1][1]), fmaxf(S[t][1][2], S[t][1][3])));
+            if (__any(mx > m_run[t] + slack)) {
+                mx = row_max(mx);
+                mx = mx > m_run[t] + slack ? mx : m_run[t];
+                const float resc = m_run[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[t] - mx) * c2);
+                m_run[t] = mx;
+                L[t] = L[t] * resc;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) O[t][dt] = O[t][dt] * resc;
+            }
+            const float ms = m_run[t] == -INFINITY ? 0.f : m_run[t] * c2;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) P[t][e] = (T)__builtin_amdgcn_exp2f(fmaf(S[t][e >> 2][e & 3], c2, -ms));
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const v8 vr = __builtin_bit_cast(v8, transposed(stage + vread[dt], 4 * D * 2));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) O[t][dt] = M::mul(vr, P[t], O[t][dt]);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) L[t] = M::mul(ones, P[t], L[t]);
+    }
+    // the four waves meet
+    __syncthreads();
+    float *ob = reinterpret_cast<float *>(lds), *om = ob + 4 * RB * OP, *ol = om + 4 * RB;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const uint32_t row = t * 16 + i;
+        float *dst = ob + (wave * RB + row) * OP + 4 * c;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4_t *>(dst + 16 * dt) = O[t][dt];
+        if (c == 0) { om[wave * RB + row] = m_run[t]; ol[wave * RB + row] = L[t][0]; }
+    }
+    __syncthreads();
+    constexpr uint32_t kPiece = 4, kPerRow = D / kPiece;
+    for (uint32_t u = tid; u < RB * kPerRow; u += 256) {
+        const uint32_t row = u / kPerRow, d0 = u % kPerRow * kPiece, rho = row0 + row;
+        if (rho >= R) break;
+        float mx = om[row];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) mx = fmaxf(mx, om[w * RB + row]);
+        float l = 0.f;
+        f4_t o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float mw = om[w * RB + row];
+            if (mw == -INFINITY && mx != -INFINITY) continue;            // (a wave that saw nothing of this row)
+            const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mw - mx) * c2);
+            l = fmaf(f, ol[w * RB + row], l);
+            const f4_t v = *reinterpret_cast<const f4_t *>(ob + (w * RB + row) * OP + d0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[e], o[e]);
+        }
+        const uint32_t t = rho / G, h = hk * G + rho % G;
+        if (own && *wild) {
+            for (uint32_t j = (max(lo, nc) - nc) * kTile; j < min(t_n, (hi - nc) * kTile); ++j) {
+                if (!(anc[t * kMaskWords + j / 32] >> (j % 32) & 1)) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = to_f(vn[(size_t)j * a.v_new_token + d0 + e]);
+                    if (!(fabsf(v) < INFINITY)) o[e] += v;
+                }
+            }
+        }
+        const size_t token = (size_t)sr.row0 + t;
+        if (nsplit > 1) {
+            float *dst = part + ((token * a.n_q_heads + h) * nsplit + z) * OP;
+            *reinterpret_cast<f4_t *>(dst + d0) = o;
+            if (d0 == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(mx * c2, l);
+        } else {
+            T r[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = (T)(o[e] / l);
+            *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + token * a.out_token + h * a.out_head + d0) = *reinterpret_cast<const uint2 *>(r);
+        }
+    }
+}
+
+// A wave per (token, query head) merges the records of its sequence's splits, in their order: value sums, then maximum (in
+// powers of two) and weight sum.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args a, uint32_t nsplit, const float *part) {
+    constexpr int E = D / 64, OP = D + 4;
+    const uint32_t lane = threadIdx.x & 63, h = blockIdx.x * 4 + (threadIdx.x >> 6), t = blockIdx.y, s = blockIdx.z;
+    const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
+    if (h >= a.n_q_heads || (int)t >= sr.n) return;
+    const uint32_t ctx = clampi(a.context[s], 0, (int)a.max_context);
+    const uint32_t tiles = (ctx + kTile - 1) / kTile + (sr.n + kTile - 1) / kTile, per = tiles_per_split(tiles, nsplit), n = (tiles + per - 1) / per;
+    const size_t token = (size_t)sr.row0 + t;
+    const float *p = part + (token * a.n_q_heads + h) * nsplit * OP;
+    float mx = -INFINITY, l = 0.f, o[E] = {};
+    for (uint32_t z0 = 0; z0 < n; z0 += 8) {
+        float mv[8], lv[8], ov[8][E], m8 = mx;
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) {
+            const float *r = p + (size_t)min(z0 + u, n - 1) * OP;
+            mv[u] = r[D];
+            lv[u] = r[D + 1];
+#pragma unroll
+            for (int e = 0; e < E; ++e) ov[u][e] = r[lane * E + e];
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) m8 = fmaxf(m8, mv[u]);
+        const float ms = m8 == -INFINITY ? 0.f : m8, resc = __builtin_amdgcn_exp2f(mx - ms);
+        l *= resc;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= resc;
+        mx = m8;
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) {
+            const bool in = z0 + u < n && (mv[u] != -INFINITY || m8 == -INFINITY);     // left out, not weighed with zero: a sum may be infinite
+            const float w = mv[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mv[u] - ms);
+            l = in ? fmaf(w, lv[u], l) : l;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = in ? fmaf(w, ov[u][e], o[e]) : o[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) static_cast<T *>(a.out)[token * a.out_token + h * a.out_head + lane * E + e] = (T)(o[e] / l);
+}
+
+// How the work is dealt out: rows in blocks of 16 or 32 (64 rows a wave take more than 256 registers, and the compiler then
+// moves the value sums between its two kinds of them in every tile); positions in as many splits as bring the launch to the
+// workgroups the chip holds at once (two per CU, by registers), none of less than 8 tiles
+TreeDeal tree_deal(const ps_tree_attention_args &a) {
+    TreeDeal d;
+    const uint32_t rows = std::max(1u, a.max_tree) * (a.n_q_heads / a.n_kv_heads);
+    d.nt = rows <= 16 ? 1 : 2;
+    d.blocks = (rows + d.nt * 16 - 1) / (d.nt * 16);
+    const uint64_t wgs = std::max<uint64_t>(1, (uint64_t)a.n_seq * a.n_kv_heads * d.blocks);
+    const uint32_t tiles = (a.max_context + kTile - 1) / kTile + (a.max_tree + kTile - 1) / kTile, room = 512;
+    d.nsplit = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(room / wgs, tiles / 8));
+    return d;
+}
+
+template <typename T, int D, int NT>
+hipError_t launch_tree_k(const ps_tree_attention_args &a, const TreeDeal &d, float *part, hipStream_t st) {
+    constexpr uint32_t lds = tree_lds<D, NT>();
+    static std::atomic<uint64_t> done{0};        // devices this kernel's LDS size has been announced on
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev >= 64 || !(done.load(std::memory_order_relaxed) >> dev & 1)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_attention_kernel<T, D, NT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+        if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
+    const uint32_t units = a.n_seq * a.n_kv_heads * d.nsplit;
+    hipLaunchKernelGGL((tree_attention_kernel<T, D, NT>), dim3((units + 7) / 8 * 8 * d.blocks), dim3(256), lds, st, a, d.blocks, d.nsplit, part);
+    return hipGetLastError();
+}
+template <typename T, int D>
+hipError_t launch_tree(const ps_tree_attention_args &a, const TreeDeal &d, float *part, hipStream_t st) {
+    hipError_t e = d.nt == 1 ? launch_tree_k<T, D, 1>(a, d, part, st) : launch_tree_k<T, D, 2>(a, d, part, st);
+    if (e != hipSuccess || d.nsplit == 1) return e;
+    hipLaunchKernelGGL((tree_merge_kernel<T, D>), dim3((a.n_q_heads + 3) / 4, a.max_tree, a.n_seq), dim3(256), 0, st, a, d.nsplit, part);
+    return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------ verification
@@ -264,7 +646,7 @@ __global__ __launch_bounds__(256) void cache_keep_kernel(ps_cache_keep_args a, u
     char *base = static_cast<char *>(a.cache) + s * a.seq_stride + plane * a.plane_stride;
     const uint32_t units = a.row_bytes / 16;
     for (uint32_t c0 = 0; c0 < units; c0 += seg) {
-        uint4 v[16];
+        u4_t v[16];
         bool ok[16];
 #pragma unroll
         for (int u = 0; u < 16; ++u) {
@@ -274,14 +656,14 @@ __global__ __launch_bounds__(256) void cache_keep_kernel(ps_cache_keep_args a, u
                 const int node = path[i];
                 const int64_t from = ctx + node, to = ctx + i;
                 ok[u] = node >= 0 && node < (int)a.max_tree && from >= 0 && from < a.capacity && to >= 0 && to < a.capacity;
-                if (ok[u]) v[u] = *reinterpret_cast<const uint4 *>(base + from * a.row_stride + col * 16);
+                if (ok[u]) v[u] = *reinterpret_cast<const u4_t *>(base + from * a.row_stride + col * 16);
             }
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
         for (int u = 0; u < 16; ++u) {
             const uint32_t idx = u * 64 + lane, i = idx / seg, col = c0 + idx % seg;
-            if (ok[u]) *reinterpret_cast<uint4 *>(base + (ctx + i) * a.row_stride + col * 16) = v[u];
+            if (ok[u]) *reinterpret_cast<u4_t *>(base + (ctx + i) * a.row_stride + col * 16) = v[u];
         }
     }
 }
@@ -356,7 +738,8 @@ int32_t ps_tree_attention_workspace(const ps_tree_attention_args *a, uint64_t *b
     PS_WANT(bytes, "NULL argument");
     const int32_t rc = check_tree(a);
     if (rc) return rc;
-    *bytes = 0;
+    const TreeDeal d = tree_deal(*a);
+    *bytes = d.nsplit > 1 ? align_up((uint64_t)a->n_tokens * a->n_q_heads * d.nsplit * (a->head_dim + 4) * 4, kAlign) : 0;
     return PS_OK;
 }
 
@@ -377,16 +760,12 @@ int32_t ps_tree_attention(const ps_tree_attention_args *a, void *workspace, uint
         PS_WANT(n <= (1ull << 30) / 64, "64 rows must span less than 2 GiB (stride of %llu elements)", (unsigned long long)n);
     for (const int32_t *p : {a->first, a->context, a->parent}) PS_WANT(aligned(p, 4), "first, context and parent must be aligned to 4 bytes");
     PS_WANT(workspace_bytes >= need && (need == 0 || (workspace && aligned(workspace, kAlign))), "a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need);
-    const dim3 grid(a->max_tree, a->n_q_heads, a->n_seq);
+    const TreeDeal d = tree_deal(*a);
+    PS_WANT((uint64_t)a->n_seq * a->n_kv_heads * d.nsplit * d.blocks < 1ull << 28, "too many sequences and heads for one call");
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a->type == PS_TYPE_F16) {
-        if (a->head_dim == 64) hipLaunchKernelGGL((tree_attention_kernel<f16_t, 64>), grid, dim3(64), 0, st, *a);
-        else hipLaunchKernelGGL((tree_attention_kernel<f16_t, 128>), grid, dim3(64), 0, st, *a);
-    } else {
-        if (a->head_dim == 64) hipLaunchKernelGGL((tree_attention_kernel<bf16_t, 64>), grid, dim3(64), 0, st, *a);
-        else hipLaunchKernelGGL((tree_attention_kernel<bf16_t, 128>), grid, dim3(64), 0, st, *a);
-    }
-    PS_TRY(hipGetLastError());
+    float *part = static_cast<float *>(workspace);
+    if (a->type == PS_TYPE_F16) PS_TRY(a->head_dim == 64 ? (launch_tree<f16_t, 64>(*a, d, part, st)) : (launch_tree<f16_t, 128>(*a, d, part, st)));
+    else PS_TRY(a->head_dim == 64 ? (launch_tree<bf16_t, 64>(*a, d, part, st)) : (launch_tree<bf16_t, 128>(*a, d, part, st)));
     return PS_OK;
 }
 
