@@ -489,149 +489,531 @@ hipError_t launch_tree(const ps_tree_attention_args &a, const TreeDeal &d, float
 }
 
 // ------------------------------------------------------------------------------------ verification
-// A workgroup per sequence walks down the tree; every row is read by the whole workgroup.
+// Rows are cut into chunks (rules in verify_shape).  Launches, in order:
+//  verify_rows_kernel   chunk maximum and sum of exponentials of every row that a decision needs: the nodes with children, target and
+//                       draft; without sampling the largest logit's index instead
+//  verify_left_kernel   with drafts, for the k-th child (k = 1 ..): chunk sums W_k = sum max(p - c_k q, 0) of the nodes whose first k
+//                       children are refused and that the walk may still reach
+//  verify_draw_kernel   every workgroup works out the same walk; chunk sums of what is left to draw from behind its last node
+//  verify_pick_kernel   the chunk that the random number falls into, and the index in it
+// Exponentials and sums are in 64 bits: with fp32's 2^-24 a border of the running sum moves by as much as a hundred thousandth of
+// the vocabulary's entries weigh.  A 64-bit multiply-add costs this machine what a 32-bit one does; an exponential here is about
+// 18 of them, which in a large batch takes as long as the row's bytes do.  No result depends on the order of workgroups.
+constexpr uint32_t kVerThreads = 256, kMaxChunks = 32;
+struct RowPart { double z; float m; int best; };                 // one chunk of a row
+struct DrawHead { double c, ip, iq; float m, mq; int row, kind; };   // what is left behind the last node, for the pick
+enum { DRAW_NONE = 0, DRAW_BEST = 1, DRAW_LEAF = 2, DRAW_LEFT = 3, DRAW_GIVEN = 4 };
+struct VerifyShape { uint32_t chunk, nchunk, loop; };
+struct VerifyWork { RowPart *parts; double *left; RowPart *recs; DrawHead *heads; };   // [token][target, draft][chunk], [token][chunk], [seq][chunk], [seq]
+
 __device__ __forceinline__ float sane(float v) { return v != v ? -INFINITY : fminf(v, kFloatMax); }
 
-constexpr int kVerThreads = 1024;
+// 2^t for t <= 0, to 3e-13 of its value: t = n + f, |f| <= 1/2, the exponential series of f ln 2 to the tenth power (the next term
+// is (ln 2 / 2)^11 / 11! = 2e-13)
+__device__ __forceinline__ double pow2_neg(double t) {
+    t = fmax(t, -1100.0);
+    const double n = rint(t), f = t - n;
+    double p = 7.054911620801121e-09;                            // (ln 2)^i / i!, i = 10 .. 0
+    p = fma(p, f, 1.0178086009239696e-07);
+    p = fma(p, f, 1.3215486790144305e-06);
+    p = fma(p, f, 1.5252733804059838e-05);
+    p = fma(p, f, 1.5403530393381606e-04);
+    p = fma(p, f, 1.3333558146428441e-03);
+    p = fma(p, f, 9.618129107628477e-03);
+    p = fma(p, f, 5.5504108664821576e-02);
+    p = fma(p, f, 2.402265069591007e-01);
+    p = fma(p, f, 6.931471805599453e-01);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)n);
+}
+// exp((x - m) / T) with k = log2(e) / T; a row of -inf alone has no probabilities
+__device__ __forceinline__ double weight(float x, float m, double k) { return pow2_neg(((double)x - (double)m) * k); }
+__device__ __forceinline__ double rate_of(float temp) { return 1.4426950408889634 / (double)fminf(temp, 1e30f); }
 
+// logits i .. i + 7 of a row (past the end: -inf); rows may start anywhere
 template <typename T>
-struct Row { const T *x; float m; double z, k; int best; };     // probabilities exp((x - m) k) / z
+__device__ __forceinline__ void load8(const T *x, uint32_t i, uint32_t end, float (&v)[8]) {
+    if (i + 8 <= end) {
+        T t[8];
+        __builtin_memcpy(t, x + i, sizeof(t));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = sane(to_f(t[e]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = i + e < end ? sane(to_f(x[i + e])) : -INFINITY;
+    }
+}
 
-__device__ double block_sum(double v, double *buf) {
+__device__ __forceinline__ double block_sum(double v, double *buf) {     // every thread gets the sum
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
     __syncthreads();
-    double r = 0;
-    for (int w = 0; w < kVerThreads / 64; ++w) r += buf[w];
-    return r;
+    return (buf[0] + buf[1]) + (buf[2] + buf[3]);
 }
-
-template <typename T>
-__device__ double chance(const Row<T> &r, int x, uint32_t V, float temp) {
-    if (x < 0 || x >= (int)V || r.m == -INFINITY) return 0.0;
-    if (!(temp > 0.f)) return x == r.best ? 1.0 : 0.0;
-    return exp(((double)sane(to_f(r.x[x])) - (double)r.m) * r.k) / r.z;
+__device__ __forceinline__ float block_max(float v, float *buf) {
+    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return fmaxf(fmaxf(buf[0], buf[1]), fmaxf(buf[2], buf[3]));
 }
+__device__ __forceinline__ int block_min(int v, int *buf) {
+    for (int o = 32; o; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return min(min(buf[0], buf[1]), min(buf[2], buf[3]));
+}
+struct BlockBuf { double d[4]; float f[4]; int i[4]; };
 
+// One chunk [lo, hi) of a row: its maximum, and the sum of exp((x - max) k), or (greedy) the first index of the maximum.
+// A chunk is a multiple of 2048 long: kVec vectors of 8 to a thread at a time, all of them requested before the first is used
+constexpr uint32_t kVec = 2, kSpan = kVec * kVerThreads * 8;
 template <typename T>
-__device__ Row<T> read_row(const T *x, uint32_t V, float temp, double *buf) {
-    Row<T> r{x, -INFINITY, 0.0, 0.0, -1};
-    float m = -INFINITY;
-    int best = 0x7FFFFFFF;
-    for (uint32_t i = threadIdx.x; i < V; i += kVerThreads) { const float v = sane(to_f(x[i])); if (v > m) { m = v; best = i; } }
-    for (int o = 32; o; o >>= 1) {
-        const float m2 = __shfl_xor(m, o, 64);
-        const int b2 = __shfl_xor(best, o, 64);
-        if (m2 > m || (m2 == m && b2 < best)) { m = m2; best = b2; }
+__device__ RowPart chunk_part(const T *x, uint32_t lo, uint32_t hi, double k, bool greedy, BlockBuf &b) {
+    RowPart r{0.0, -INFINITY, 0x7FFFFFFF};
+    for (uint32_t s0 = lo; s0 < hi; s0 += kSpan) {
+        float v[kVec][8], mx = -INFINITY;
+#pragma unroll
+        for (uint32_t u = 0; u < kVec; ++u) load8(x, s0 + (u * kVerThreads + threadIdx.x) * 8, hi, v[u]);
+#pragma unroll
+        for (uint32_t u = 0; u < kVec; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mx = fmaxf(mx, v[u][e]);
+        mx = block_max(mx, b.f);
+        if (mx == -INFINITY) continue;
+        if (greedy) {
+            int at = 0x7FFFFFFF;
+#pragma unroll
+            for (uint32_t u = 0; u < kVec; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (v[u][e] == mx) at = min(at, (int)(s0 + (u * kVerThreads + threadIdx.x) * 8 + e));
+            at = block_min(at, b.i);
+            if (mx > r.m) r.best = at;
+            r.m = fmaxf(r.m, mx);
+            continue;
+        }
+        const float m = fmaxf(r.m, mx);
+        double z = 0;
+#pragma unroll
+        for (uint32_t u = 0; u < kVec; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z += weight(v[u][e], m, k);
+        z = block_sum(z, b.d);
+        r.z = (r.m == -INFINITY ? 0.0 : r.z * weight(r.m, m, k)) + z;
+        r.m = m;
     }
-    __shared__ float wm[kVerThreads / 64];
-    __shared__ int wb[kVerThreads / 64];
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) { wm[threadIdx.x >> 6] = m; wb[threadIdx.x >> 6] = best; }
-    __syncthreads();
-    for (int w = 0; w < kVerThreads / 64; ++w)
-        if (w == 0 || wm[w] > m || (wm[w] == m && wb[w] < best)) { m = wm[w]; best = wb[w]; }
-    r.m = m;
-    r.best = best;
-    r.k = 1.0 / (double)fminf(temp, 1e30f);
-    if (m == -INFINITY || !(temp > 0.f)) return r;
-    double z = 0;
-    for (uint32_t i = threadIdx.x; i < V; i += kVerThreads) z += exp(((double)sane(to_f(x[i])) - (double)m) * r.k);
-    r.z = block_sum(z, buf);
+    return r;
+}
+
+struct RowSum { double z; float m; int best; };
+__device__ __forceinline__ RowSum row_sum(const RowPart *p, uint32_t n, double k, bool greedy) {
+    RowSum r{0.0, -INFINITY, -1};
+    for (uint32_t i = 0; i < n; ++i) {
+        const float m = p[i].m;
+        if (m > r.m) { r.m = m; r.best = p[i].best; }
+    }
+    if (greedy || r.m == -INFINITY) return r;
+    for (uint32_t i = 0; i < n; ++i)
+        if (p[i].m != -INFINITY) r.z += p[i].z * weight(p[i].m, r.m, k);
     return r;
 }
 
 template <typename T>
-__global__ __launch_bounds__(kVerThreads) void verify_tree_kernel(ps_verify_tree_args a) {
-    __shared__ double buf[kVerThreads / 64];
-    __shared__ int up[PS_TREE_MAX], refused[PS_TREE_MAX];
-    __shared__ double part[kVerThreads];
-    const uint32_t s = blockIdx.x, tid = threadIdx.x, V = a.vocab;
+__global__ __launch_bounds__(kVerThreads) void verify_rows_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
+    __shared__ BlockBuf b;
+    __shared__ unsigned char parent[PS_TREE_MAX];
+    const uint32_t tid = threadIdx.x, s = blockIdx.z, chunk = blockIdx.x;
     const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
-    int32_t *path = a.path + s * a.path_seq;
-    for (uint32_t i = tid; i < a.max_tree; i += kVerThreads) path[i] = -1;
+    if (sr.n < 2) return;
+    const float temp = a.temperature ? a.temperature[s] : 1.f;
+    const bool greedy = !(temp > 0.f);
+    const double k = greedy ? 0.0 : rate_of(temp);
+    parent[tid] = 0;
+    __syncthreads();
+    if ((int)tid < sr.n) {
+        const int up = parent_of(a.parent[sr.row0 + tid], tid);
+        if (up >= 0) parent[up] = 1;
+    }
+    __syncthreads();
+    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    uint32_t seen = 0;
+    for (int i = 0; i < sr.n; ++i) {
+        if (!parent[i] || seen++ % gridDim.y != blockIdx.y) continue;
+        const size_t row = (size_t)sr.row0 + i;
+        const RowPart p = chunk_part(static_cast<const T *>(a.target_logits) + row * a.target_row, lo, hi, k, greedy, b);
+        if (tid == 0) w.parts[row * 2 * sh.nchunk + chunk] = p;
+        if (!a.draft_logits || greedy) continue;
+        const RowPart q = chunk_part(static_cast<const T *>(a.draft_logits) + row * a.draft_row, lo, hi, k, false, b);
+        if (tid == 0) w.parts[(row * 2 + 1) * sh.nchunk + chunk] = q;
+    }
+}
+
+// Decisions of a sequence's nodes, as far as they are known: by one thread for each node
+struct Walk {
+    RowSum p[PS_TREE_MAX], q[PS_TREE_MAX];     // of nodes with children
+    double px[PS_TREE_MAX], left[PS_TREE_MAX]; // of a node as its parent's child: p(token), W (or what is left without the refused)
+    double c[PS_TREE_MAX];                     // c in front of this child
+    int up[PS_TREE_MAX], rank[PS_TREE_MAX], token[PS_TREE_MAX], went[PS_TREE_MAX], kids[PS_TREE_MAX];
+    bool dup[PS_TREE_MAX];
+};
+
+// known: children up to this rank are decided (their W has been summed)
+template <typename T>
+__device__ void decide(const ps_verify_tree_args &a, const VerifyShape &sh, const VerifyWork &w, const SeqRows &sr, float temp, uint32_t known, Walk &k) {
+    const int tid = threadIdx.x;
+    const bool greedy = !(temp > 0.f), drafts = a.draft_logits && !greedy, in = tid < sr.n;
+    const double rate = greedy ? 0.0 : rate_of(temp);
+    k.kids[tid] = 0;
+    k.went[tid] = 0x7FFFFFFF;
+    int up = -1, token = -1;
+    float u = 0.f;
+    const size_t row = (size_t)sr.row0 + tid;
+    if (in) { up = parent_of(a.parent[row], tid); token = a.token[row]; u = a.u_accept[row]; }
+    k.up[tid] = in ? up : -1;
+    k.token[tid] = token;
+    __syncthreads();
+    if (up >= 0) atomicAdd(&k.kids[up], 1);
+    int rank = 0;
+    bool dup = false;
+    for (int j = 1; j < tid && up >= 0; ++j)
+        if (k.up[j] == up) { ++rank; dup |= k.token[j] == token; }
+    k.rank[tid] = rank;
+    k.dup[tid] = dup;
+    __syncthreads();
+    if (in && k.kids[tid]) {
+        k.p[tid] = row_sum(w.parts + row * 2 * sh.nchunk, sh.nchunk, rate, greedy);
+        if (drafts) k.q[tid] = row_sum(w.parts + (row * 2 + 1) * sh.nchunk, sh.nchunk, rate, false);
+    }
+    double sum = 1.0;
+    if (up >= 0 && drafts && rank > 0 && rank <= (int)known && rank < (int)a.max_children) {
+        sum = 0;
+        for (uint32_t i = 0; i < sh.nchunk; ++i) sum += w.left[row * sh.nchunk + i];
+    }
+    k.left[tid] = sum;
+    __syncthreads();
+    double px = 0, qx = 0;
+    const bool inside = token >= 0 && token < (int)a.vocab;
+    if (up >= 0 && inside) {
+        const size_t at = (size_t)sr.row0 + up;
+        if (greedy) px = token == k.p[up].best ? 1.0 : 0.0;
+        else if (k.p[up].m != -INFINITY) px = weight(sane(to_f(static_cast<const T *>(a.target_logits)[at * a.target_row + token])), k.p[up].m, rate) / k.p[up].z;
+        if (drafts && k.q[up].m != -INFINITY) qx = weight(sane(to_f(static_cast<const T *>(a.draft_logits)[at * a.draft_row + token])), k.q[up].m, rate) / k.q[up].z;
+    }
+    k.px[tid] = px;
+    __syncthreads();
+    if (up >= 0) {
+        double c = 0, rest = 1.0;
+        for (int j = 1; j < tid; ++j) {
+            if (k.up[j] != up) continue;
+            if (drafts) c += k.left[j];
+            else if (!greedy && !k.dup[j]) rest -= k.px[j];
+        }
+        k.c[tid] = c;
+        const bool yes = drafts ? px > (c + (double)u * k.left[tid]) * qx : (greedy || !dup) && px > (double)u * rest;
+        if (yes && rank < (int)a.max_children && (!drafts || rank <= (int)known)) atomicMin(&k.went[up], tid);
+    }
+    __syncthreads();
+}
+
+template <typename T>
+__global__ __launch_bounds__(kVerThreads) void verify_left_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w, uint32_t k) {
+    __shared__ Walk walk;
+    __shared__ BlockBuf b;
+    __shared__ int list[PS_TREE_MAX], n;
+    const uint32_t s = blockIdx.y, chunk = blockIdx.x;
+    const int tid = threadIdx.x;
+    const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
+    const float temp = a.temperature ? a.temperature[s] : 1.f;
+    if (sr.n < 2 || !(temp > 0.f)) return;
+    decide<T>(a, sh, w, sr, temp, k - 1, walk);
+    if (tid == 0) n = 0;
+    __syncthreads();
+    // a child of rank k whose parent has accepted none before it, where no edge above is known to be refused
+    bool ok = tid < sr.n && walk.up[tid] >= 0 && walk.rank[tid] == (int)k && walk.went[walk.up[tid]] == 0x7FFFFFFF;
+    if (ok) {
+        int i = walk.up[tid];
+        for (; i > 0; i = walk.up[i]) {
+            const int up = walk.up[i];
+            if (up < 0 || (walk.went[up] != i && (walk.went[up] != 0x7FFFFFFF || walk.rank[i] < (int)k))) break;
+        }
+        ok = i == 0;
+    }
+    if (ok) list[atomicAdd(&n, 1)] = tid;      // (any order: each is worked on alone)
+    __syncthreads();
+    const double rate = rate_of(temp);
+    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    for (int j = 0; j < n; ++j) {
+        const int child = list[j], up = walk.up[child];
+        const size_t row = (size_t)sr.row0 + up;
+        const RowSum p = walk.p[up], q = walk.q[up];
+        // the child's c holds W of those in front of it, all known
+        const double c = walk.c[child], ip = p.m == -INFINITY ? 0.0 : 1.0 / p.z, iq = q.m == -INFINITY ? 0.0 : c / q.z;
+        double sum = 0;
+        for (uint32_t i = lo + tid * 8; i < hi; i += kVerThreads * 8) {
+            float x[8], y[8];
+            load8(static_cast<const T *>(a.target_logits) + row * a.target_row, i, hi, x);
+            load8(static_cast<const T *>(a.draft_logits) + row * a.draft_row, i, hi, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double pv = ip > 0 ? weight(x[e], p.m, rate) * ip : 0.0, qv = iq > 0 ? weight(y[e], q.m, rate) * iq : 0.0;
+                sum += fmax(pv - qv, 0.0);
+            }
+        }
+        sum = block_sum(sum, b.d);
+        if (tid == 0) w.left[((size_t)sr.row0 + child) * sh.nchunk + chunk] = sum;
+    }
+}
+
+// Entries i .. i + 7 of what is left to draw from (DRAW_LEFT, DRAW_GIVEN, DRAW_LEAF with its chunk's or row's maximum in m)
+template <typename T>
+__device__ __forceinline__ void left8(const ps_verify_tree_args &a, const DrawHead &h, int kind, double rate, uint32_t i, uint32_t hi, const int *refused, int nref,
+                                      double (&r)[8]) {
+    float x[8];
+    load8(static_cast<const T *>(a.target_logits) + (size_t)h.row * a.target_row, i, hi, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = weight(x[e], h.m, rate) * h.ip;
+    if (kind == DRAW_LEFT) {
+        load8(static_cast<const T *>(a.draft_logits) + (size_t)h.row * a.draft_row, i, hi, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = fmax(r[e] - (h.iq > 0 ? weight(x[e], h.mq, rate) * h.iq : 0.0), 0.0);
+    }
+    if (kind == DRAW_GIVEN)
+        for (int j = 0; j < nref; ++j) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] = refused[j] == (int)(i + e) ? 0.0 : r[e];
+        }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
+    __shared__ Walk walk;
+    __shared__ BlockBuf b;
+    __shared__ int path[PS_TREE_MAX], refused[PS_TREE_MAX], n, nref, last;
+    const uint32_t s = blockIdx.y, chunk = blockIdx.x;
+    const int tid = threadIdx.x;
+    const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
     if (sr.n == 0) {
-        if (tid == 0) { a.count[s] = 0; a.next_token[s] = -1; }
+        if (chunk) return;
+        if (tid < (int)a.max_tree) a.path[s * a.path_seq + tid] = -1;
+        if (tid == 0) { a.count[s] = 0; w.heads[s].kind = DRAW_NONE; }
         return;
     }
-    for (int i = tid; i < sr.n; i += kVerThreads) up[i] = parent_of(a.parent[sr.row0 + i], i);
-    __syncthreads();
     const float temp = a.temperature ? a.temperature[s] : 1.f;
     const bool greedy = !(temp > 0.f), drafts = a.draft_logits && !greedy;
-    int here = 0, n = 0;
-    for (;;) {
-        if (tid == 0) path[n] = here;
-        ++n;
-        const Row<T> p = read_row(static_cast<const T *>(a.target_logits) + ((size_t)sr.row0 + here) * a.target_row, V, temp, buf);
-        Row<T> q{};
-        if (drafts) q = read_row(static_cast<const T *>(a.draft_logits) + ((size_t)sr.row0 + here) * a.draft_row, V, temp, buf);
-        double c = 0, w = 1;
-        int went = -1, nref = 0, tried = 0;
-        for (int i = here + 1; i < sr.n && went < 0 && tried < (int)a.max_children; ++i) {
-            if (up[i] != here) continue;
-            ++tried;
-            const int x = a.token[sr.row0 + i];
-            const double u = a.u_accept[sr.row0 + i], px = chance(p, x, V, temp);
-            if (drafts) {
-                if (px > (c + u * w) * chance(q, x, V, temp)) { went = i; break; }
-                c += w;
-                double left = 0;
-                for (uint32_t j = tid; j < V; j += kVerThreads) left += fmax(chance(p, j, V, temp) - c * chance(q, j, V, temp), 0.0);
-                w = block_sum(left, buf);
-            } else {
-                bool again = false;
-                for (int r = 0; r < nref; ++r) again |= refused[r] == x;
-                if (!again && px > u * w) { went = i; break; }
-                if (!again && !greedy) {
-                    __syncthreads();
-                    if (tid == 0) refused[nref] = x;
-                    __syncthreads();
-                    ++nref;
-                    w -= px;
-                }
+    const double rate = greedy ? 0.0 : rate_of(temp);
+    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    int kids = 0;
+    if (sr.n > 1) {
+        decide<T>(a, sh, w, sr, temp, a.max_children, walk);
+        if (tid == 0) {
+            int here = 0, m = 0;
+            for (;;) {
+                path[m++] = here;
+                const int next = walk.went[here];
+                if (next == 0x7FFFFFFF) break;
+                here = next;
             }
+            n = m;
+            last = here;
+            nref = 0;
         }
-        if (went >= 0) { here = went; continue; }
-        // draw: every thread sums a run of the vocabulary, thread 0 looks for the run, then for the index
-        const uint32_t per = (V + kVerThreads - 1) / kVerThreads;
-        for (int again = 0; again < 2; ++again) {
-            auto left = [&](uint32_t j) {
-                const double v = chance(p, j, V, temp);
-                if (again) return v;
-                for (int r = 0; r < nref; ++r) if (refused[r] == (int)j) return 0.0;
-                return drafts ? fmax(v - c * chance(q, j, V, temp), 0.0) : v;
-            };
-            double sum = 0;
-            for (uint32_t j = tid * per; j < min(V, (tid + 1) * per); ++j) sum += left(j);
-            __syncthreads();
-            part[tid] = sum;
-            __syncthreads();
-            double total = 0;
-            for (int k = 0; k < kVerThreads; ++k) total += part[k];
-            if (total <= 0 && !again) continue;
-            if (tid == 0) {
-                int pick = -1, last = -1;
-                const double goal = (double)a.u_sample[s] * total;
-                double run = 0;
-                for (int k = 0; k < kVerThreads && pick < 0 && total > 0; ++k) {
-                    if (run + part[k] <= goal && k + 1 < kVerThreads) { run += part[k]; continue; }
-                    double r = run;
-                    for (uint32_t j = k * per; j < min(V, (k + 1) * per); ++j) {
-                        const double v = left(j);
-                        if (v > 0) last = j;
-                        r += v;
-                        if (r > goal) { pick = j; break; }
-                    }
-                    run += part[k];
-                }
-                a.next_token[s] = pick >= 0 ? pick : last;
-                a.count[s] = n;
-            }
-            break;
+        __syncthreads();
+        kids = walk.kids[last];
+    } else {
+        if (tid == 0) { path[0] = 0; n = 1; last = 0; nref = 0; }
+        __syncthreads();
+    }
+    DrawHead h{};
+    h.row = sr.row0 + last;
+    h.m = h.mq = -INFINITY;
+    if (kids) {
+        const RowSum p = walk.p[last];
+        h.m = p.m;
+        h.kind = p.m == -INFINITY ? DRAW_NONE : greedy ? DRAW_BEST : drafts ? DRAW_LEFT : DRAW_GIVEN;
+        h.ip = h.kind >= DRAW_LEAF ? 1.0 / p.z : 0.0;
+        if (drafts) {      // c behind the last child tried
+            const bool tried = tid < sr.n && walk.up[tid] == last && walk.rank[tid] < (int)a.max_children;
+            h.c = block_sum(tried ? walk.left[tid] : 0.0, b.d);
+            h.mq = walk.q[last].m;
+            h.iq = h.mq == -INFINITY ? 0.0 : h.c / walk.q[last].z;
+        } else if (tid < sr.n && walk.up[tid] == last && walk.rank[tid] < (int)a.max_children && !walk.dup[tid]) {
+            // (only those of this chunk)
+            const int x = walk.token[tid];
+            if (x >= (int)lo && x < (int)hi) refused[atomicAdd(&nref, 1)] = x;
         }
+        __syncthreads();
+    } else {
+        h.kind = DRAW_LEAF;
+    }
+    if (chunk == 0) {
+        if (tid < (int)a.max_tree) a.path[s * a.path_seq + tid] = tid < n ? path[tid] : -1;
+        if (tid == 0) {
+            a.count[s] = n;
+            w.heads[s] = h;
+            if (h.kind == DRAW_BEST) w.recs[s * sh.nchunk].best = walk.p[last].best;
+        }
+    }
+    if (h.kind < DRAW_LEAF) return;
+    RowPart r{0.0, h.m, 0};
+    if (h.kind == DRAW_LEAF) {
+        r = chunk_part(static_cast<const T *>(a.target_logits) + (size_t)h.row * a.target_row, lo, hi, rate, greedy, b);
+    } else {
+        double sum = 0;
+        for (uint32_t i = lo + tid * 8; i < hi; i += kVerThreads * 8) {
+            double v[8];
+            left8<T>(a, h, h.kind, rate, i, hi, refused, nref, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += v[e];
+        }
+        r.z = block_sum(sum, b.d);
+    }
+    if (tid == 0) w.recs[s * sh.nchunk + chunk] = r;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kVerThreads) void verify_pick_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
+    __shared__ double sums[kMaxChunks], runs[4];
+    __shared__ int refused[PS_TREE_MAX], nref, pick[2];
+    const uint32_t s = blockIdx.x;
+    const int tid = threadIdx.x;
+    DrawHead h = w.heads[s];
+    if (h.kind <= DRAW_BEST) {
+        if (tid == 0) a.next_token[s] = h.kind == DRAW_BEST ? w.recs[s * sh.nchunk].best : -1;
         return;
     }
+    const float temp = a.temperature ? a.temperature[s] : 1.f;
+    const bool greedy = !(temp > 0.f);
+    const double rate = greedy ? 0.0 : rate_of(temp);
+    const RowPart *recs = w.recs + s * sh.nchunk;
+    int kind = h.kind;
+    if (kind == DRAW_LEAF) {
+        const RowSum r = row_sum(recs, sh.nchunk, rate, greedy);
+        if (r.m == -INFINITY || greedy) {
+            if (tid == 0) a.next_token[s] = r.m == -INFINITY ? -1 : r.best;
+            return;
+        }
+        h.m = r.m;
+        h.ip = 1.0;
+    }
+    auto chunk_sums = [&](const RowPart *p) {       // relative to the row's maximum
+        __syncthreads();
+        for (uint32_t i = tid; i < sh.nchunk; i += kVerThreads) sums[i] = p[i].m == -INFINITY ? 0.0 : kind == DRAW_LEAF ? p[i].z * weight(p[i].m, h.m, rate) : p[i].z;
+        __syncthreads();
+    };
+    if (tid == 0) nref = 0;
+    chunk_sums(recs);
+    double total = 0;
+    for (uint32_t i = 0; i < sh.nchunk; ++i) total += sums[i];
+    if (kind == DRAW_GIVEN) {
+        const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
+        const int last = h.row - sr.row0;
+        __shared__ int up[PS_TREE_MAX];
+        up[tid] = tid < sr.n ? parent_of(a.parent[sr.row0 + tid], tid) : -1;
+        __syncthreads();
+        if (tid < sr.n && up[tid] == last) {
+            int rank = 0;
+            for (int j = 1; j < tid; ++j) rank += up[j] == last;
+            if (rank < (int)a.max_children) refused[atomicAdd(&nref, 1)] = a.token[sr.row0 + tid];
+        }
+        __syncthreads();
+    }
+    if (!(total > 0)) {      // nothing left: the target's own row
+        kind = DRAW_LEAF;
+        h.ip = 1.0;
+        chunk_sums(w.parts + (size_t)h.row * 2 * sh.nchunk);
+        total = 0;
+        for (uint32_t i = 0; i < sh.nchunk; ++i) total += sums[i];
+    }
+    const double goal = (double)a.u_sample[s] * total;
+    // the first chunk whose running sum passes the goal (or the last one that holds anything)
+    double run = 0, before = 0;
+    uint32_t chunk = 0;
+    for (uint32_t i = 0; i < sh.nchunk; ++i) {
+        if (sums[i] > 0) { chunk = i; before = run; }
+        run += sums[i];
+        if (run > goal) break;
+    }
+    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    // in it, a run of consecutive entries to a thread
+    const uint32_t per = sh.chunk / kVerThreads, i0 = lo + tid * per;
+    double mine = 0;
+    int some = -1;
+    for (uint32_t i = i0; i < min(hi, i0 + per); i += 8) {
+        double v[8];
+        left8<T>(a, h, kind, rate, i, hi, refused, nref, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { mine += v[e]; some = v[e] > 0 ? (int)(i + e) : some; }
+    }
+    double upto = mine;
+    for (int o = 1; o < 64; o <<= 1) {
+        const double v = __shfl_up(upto, o, 64);
+        if ((tid & 63) >= o) upto += v;
+    }
+    if ((tid & 63) == 63) runs[tid >> 6] = upto;
+    if (tid < 2) pick[tid] = tid ? -1 : 0x7FFFFFFF;
+    __syncthreads();
+    double base = before;
+    for (int i = 0; i < tid >> 6; ++i) base += runs[i];
+    const double prior = __shfl_up(upto, 1, 64);
+    const double from = (tid & 63) ? base + prior : base, to = base + upto;
+    if (to > goal && mine > 0) atomicMin(&pick[0], tid);
+    if (some >= 0) atomicMax(&pick[1], some);
+    __syncthreads();
+    if (pick[0] == 0x7FFFFFFF) {
+        if (tid == 0) a.next_token[s] = pick[1];
+        return;
+    }
+    if (tid != pick[0]) return;
+    double r = from;
+    int found = some;
+    for (uint32_t i = i0; i < min(hi, i0 + per); i += 8) {
+        double v[8];
+        left8<T>(a, h, kind, rate, i, hi, refused, nref, v);
+        bool done = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            r += v[e];
+            if (!done && v[e] > 0 && r > goal) { found = i + e; done = true; }
+        }
+        if (done) break;
+    }
+    a.next_token[s] = found;
+}
+
+// Chunks of a multiple of 2048 entries, at most kMaxChunks: a chunk of 4096 keeps a workgroup for about 3 us, as long as a launch's ends take.
+// Row passes: as many workgroups as keep the chip busy, each takes the nodes in turn.
+VerifyShape verify_shape(const ps_verify_tree_args &a) {
+    VerifyShape sh;
+    const uint32_t unit = kSpan / kVec, want = std::max(kSpan, (a.vocab + kMaxChunks - 1) / kMaxChunks);
+    sh.chunk = (want + unit - 1) / unit * unit;
+    sh.nchunk = (a.vocab + sh.chunk - 1) / sh.chunk;
+    sh.loop = (uint32_t)std::min<uint64_t>(std::max(1u, a.max_tree), std::max<uint64_t>(1, 4096 / std::max<uint64_t>(1, (uint64_t)sh.nchunk * a.n_seq)));
+    return sh;
+}
+uint64_t verify_work(const ps_verify_tree_args &a, const VerifyShape &sh, uint8_t *base, VerifyWork *w) {
+    uint64_t off = 0;
+    auto take = [&](uint64_t bytes) { uint8_t *p = base ? base + off : nullptr; off = align_up(off + bytes, kAlign); return p; };
+    w->parts = reinterpret_cast<RowPart *>(take((uint64_t)a.n_tokens * 2 * sh.nchunk * sizeof(RowPart)));
+    w->left = reinterpret_cast<double *>(take(a.draft_logits ? (uint64_t)a.n_tokens * sh.nchunk * 8 : 0));
+    w->recs = reinterpret_cast<RowPart *>(take((uint64_t)a.n_seq * sh.nchunk * sizeof(RowPart)));
+    w->heads = reinterpret_cast<DrawHead *>(take((uint64_t)a.n_seq * sizeof(DrawHead)));
+    return off;
+}
+
+template <typename T>
+hipError_t launch_verify(const ps_verify_tree_args &a, const VerifyShape &sh, const VerifyWork &w, hipStream_t st) {
+    if (a.n_tokens && a.max_tree > 1) {
+        hipLaunchKernelGGL(verify_rows_kernel<T>, dim3(sh.nchunk, sh.loop, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
+        if (a.draft_logits)
+            for (uint32_t k = 1; k < std::min(a.max_children, a.max_tree - 1); ++k)
+                hipLaunchKernelGGL(verify_left_kernel<T>, dim3(sh.nchunk, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w, k);
+    }
+    hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(sh.nchunk, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
+    hipLaunchKernelGGL(verify_pick_kernel<T>, dim3(a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
+    return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------ kept rows
@@ -776,7 +1158,8 @@ int32_t ps_verify_tree_workspace(const ps_verify_tree_args *a, uint64_t *bytes) 
     PS_WANT(a->max_tree <= PS_TREE_MAX, "trees of up to %u tokens (got %u)", PS_TREE_MAX, a->max_tree);
     PS_WANT(a->max_children >= 1 && a->max_children <= PS_TREE_MAX, "max_children 1 .. %u (got %u)", PS_TREE_MAX, a->max_children);
     PS_WANT(a->n_seq <= 65535 && a->n_tokens <= 0x7FFFFFFF, "%u sequences, %u tokens: too many", a->n_seq, a->n_tokens);
-    *bytes = 0;
+    VerifyWork w;
+    *bytes = verify_work(*a, verify_shape(*a), nullptr, &w);
     return PS_OK;
 }
 
@@ -795,11 +1178,12 @@ int32_t ps_verify_tree(const ps_verify_tree_args *a, void *workspace, uint64_t w
         PS_WANT(aligned(p, 4), "tables, random numbers and outputs must be aligned to 4 bytes");
     PS_WANT(workspace_bytes >= need && (need == 0 || (workspace && aligned(workspace, kAlign))), "a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid(a->n_seq);
-    if (a->type == PS_TYPE_F16) hipLaunchKernelGGL(verify_tree_kernel<f16_t>, grid, dim3(kVerThreads), 0, st, *a);
-    else if (a->type == PS_TYPE_BF16) hipLaunchKernelGGL(verify_tree_kernel<bf16_t>, grid, dim3(kVerThreads), 0, st, *a);
-    else hipLaunchKernelGGL(verify_tree_kernel<float>, grid, dim3(kVerThreads), 0, st, *a);
-    PS_TRY(hipGetLastError());
+    const VerifyShape sh = verify_shape(*a);
+    VerifyWork w;
+    verify_work(*a, sh, static_cast<uint8_t *>(workspace), &w);
+    if (a->type == PS_TYPE_F16) PS_TRY(launch_verify<f16_t>(*a, sh, w, st));
+    else if (a->type == PS_TYPE_BF16) PS_TRY(launch_verify<bf16_t>(*a, sh, w, st));
+    else PS_TRY(launch_verify<float>(*a, sh, w, st));
     return PS_OK;
 }
 
