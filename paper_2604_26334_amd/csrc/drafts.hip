@@ -498,51 +498,74 @@ hipError_t launch_tree(const ps_tree_attention_args &a, const TreeDeal &d, float
 //  verify_pick_kernel   the chunk that the random number falls into, and the index in it
 // Exponentials and sums are in 64 bits: with fp32's 2^-24 a border of the running sum moves by as much as a hundred thousandth of
 // the vocabulary's entries weigh.  A 64-bit multiply-add costs this machine what a 32-bit one does; an exponential here is about
-// 18 of them, which in a large batch takes as long as the row's bytes do.  No result depends on the order of workgroups.
+// 17 of them, which in a large batch takes longer than the row's bytes do.  No result depends on the order of workgroups.
 constexpr uint32_t kVerThreads = 256, kMaxChunks = 32;
-struct RowPart { double z; float m; int best; };                 // one chunk of a row
-struct DrawHead { double c, ip, iq; float m, mq; int row, kind; };   // what is left behind the last node, for the pick
+struct RowPart { double z; float m; int best; };                 // one chunk of a row: sum of exp((x - m) k), m about its maximum (greedy: m its maximum, at `best`)
+struct DrawHead { double c, ip, iq; float m, mq; int row, kind, nref, pad; };   // what is left behind the last node, for the pick
 enum { DRAW_NONE = 0, DRAW_BEST = 1, DRAW_LEAF = 2, DRAW_LEFT = 3, DRAW_GIVEN = 4 };
-struct VerifyShape { uint32_t chunk, nchunk, loop; };
-struct VerifyWork { RowPart *parts; double *left; RowPart *recs; DrawHead *heads; };   // [token][target, draft][chunk], [token][chunk], [seq][chunk], [seq]
+struct VerifyShape { uint32_t chunk, nchunk, loop, dchunk, ndraw; };   // rows in chunks; what is drawn from in chunks of its own
+struct VerifyWork { RowPart *parts; double *left; RowPart *recs; DrawHead *heads; int *refused; };   // [token][target, draft][chunk], [token][draw chunk], [seq][draw chunk], [seq], [seq][max_tree]
 
-__device__ __forceinline__ float sane(float v) { return v != v ? -INFINITY : fminf(v, kFloatMax); }
+// no number: -inf (the larger of the two that is one); +inf: the largest finite number
+__device__ __forceinline__ float sane(float v) { return fminf(fmaxf(v, -INFINITY), kFloatMax); }
 
-// 2^t for t <= 0, to 3e-13 of its value: t = n + f, |f| <= 1/2, the exponential series of f ln 2 to the tenth power (the next term
-// is (ln 2 / 2)^11 / 11! = 2e-13)
-__device__ __forceinline__ double pow2_neg(double t) {
+// 2^t for t below 1000, to 8e-13 of its value: t = n + f, |f| <= 1/2, and the polynomial of degree 8 whose largest relative error on
+// that range is least (its ten extrema found by exchange; the exponential series takes two terms more for this)
+__device__ __forceinline__ double pow2_of(double t) {
     t = fmax(t, -1100.0);
     const double n = rint(t), f = t - n;
-    double p = 7.054911620801121e-09;                            // (ln 2)^i / i!, i = 10 .. 0
-    p = fma(p, f, 1.0178086009239696e-07);
-    p = fma(p, f, 1.3215486790144305e-06);
-    p = fma(p, f, 1.5252733804059838e-05);
-    p = fma(p, f, 1.5403530393381606e-04);
-    p = fma(p, f, 1.3333558146428441e-03);
-    p = fma(p, f, 9.618129107628477e-03);
-    p = fma(p, f, 5.5504108664821576e-02);
-    p = fma(p, f, 2.402265069591007e-01);
-    p = fma(p, f, 6.931471805599453e-01);
-    p = fma(p, f, 1.0);
+    double p = 1.317587152556586e-06;
+    p = fma(p, f, 1.53097370386769e-05);
+    p = fma(p, f, 0.000154038516881703);
+    p = fma(p, f, 0.0013333452064018458);
+    p = fma(p, f, 0.009618128542944679);
+    p = fma(p, f, 0.05550410939339462);
+    p = fma(p, f, 0.24022650698879996);
+    p = fma(p, f, 0.6931471805465148);
+    p = fma(p, f, 0.9999999999997624);
     return ldexp(p, (int)n);
 }
-// exp((x - m) / T) with k = log2(e) / T; a row of -inf alone has no probabilities
-__device__ __forceinline__ double weight(float x, float m, double k) { return pow2_neg(((double)x - (double)m) * k); }
+// exp((x - m) / T) with k = log2(e) / T; a row of -inf alone has no probabilities.  (x k - m k in one operation would lose everything
+// where m is the largest finite number)
+__device__ __forceinline__ double weight(float x, float m, double k) { return pow2_of(((double)x - (double)m) * k); }
 __device__ __forceinline__ double rate_of(float temp) { return 1.4426950408889634 / (double)fminf(temp, 1e30f); }
 
-// logits i .. i + 7 of a row (past the end: -inf); rows may start anywhere
+// Eight logits of a row, which may start anywhere, as they lie in memory (past the end -inf), taken out two at a time
 template <typename T>
-__device__ __forceinline__ void load8(const T *x, uint32_t i, uint32_t end, float (&v)[8]) {
-    if (i + 8 <= end) {
-        T t[8];
-        __builtin_memcpy(t, x + i, sizeof(t));
+struct Oct {
+    static constexpr int N = sizeof(T) * 2;
+    uint32_t d[N];
+    __device__ __forceinline__ void fill(const T *x, uint32_t i) { __builtin_memcpy(d, x + i, sizeof(d)); }
+    __device__ __forceinline__ void fill(const T *x, uint32_t i, uint32_t end) {
+        if (i + 8 <= end) { fill(x, i); return; }
+#pragma unroll 1
+        for (uint32_t e = i; e < i + 8; ++e) {
+            const T v = e < end ? x[e] : (T)-INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = sane(to_f(t[e]));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = i + e < end ? sane(to_f(x[i + e])) : -INFINITY;
+            for (int j = 0; j < N; ++j) {
+                const uint32_t from = j + 1 < N ? d[j + 1] : sizeof(T) == 2 ? (uint32_t)__builtin_bit_cast(uint16_t, (uint16_t)bits(v)) : bits(v);
+                d[j] = sizeof(T) == 2 ? d[j] >> 16 | from << 16 : from;
+            }
+        }
     }
-}
+    static __device__ __forceinline__ uint32_t bits(T v) {
+        if constexpr (sizeof(T) == 2) return __builtin_bit_cast(uint16_t, v);
+        else return __builtin_bit_cast(uint32_t, v);
+    }
+    __device__ __forceinline__ void take(float &a, float &b) {
+        if constexpr (sizeof(T) == 2) {
+            a = sane(to_f(__builtin_bit_cast(T, (uint16_t)d[0])));
+            b = sane(to_f(__builtin_bit_cast(T, (uint16_t)(d[0] >> 16))));
+#pragma unroll
+            for (int j = 0; j + 1 < N; ++j) d[j] = d[j + 1];
+        } else {
+            a = sane(__builtin_bit_cast(float, d[0]));
+            b = sane(__builtin_bit_cast(float, d[1]));
+#pragma unroll
+            for (int j = 0; j + 2 < N; ++j) d[j] = d[j + 2];
+        }
+    }
+};
 
 __device__ __forceinline__ double block_sum(double v, double *buf) {     // every thread gets the sum
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -566,65 +589,90 @@ __device__ __forceinline__ int block_min(int v, int *buf) {
     return min(min(buf[0], buf[1]), min(buf[2], buf[3]));
 }
 struct BlockBuf { double d[4]; float f[4]; int i[4]; };
+// the numbers of the threads that `have`, in order; how many
+__device__ __forceinline__ uint32_t listed(bool have, unsigned char *list, uint32_t (&cnt)[4]) {
+    const uint64_t all = __ballot(have);
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0) cnt[wave] = __popcll(all);
+    __syncthreads();
+    uint32_t at = __popcll(all & ((1ull << lane) - 1)), n = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) { at += i < wave ? cnt[i] : 0u; n += cnt[i]; }
+    if (have) list[at] = (unsigned char)threadIdx.x;
+    __syncthreads();
+    return n;
+}
 
-// One chunk [lo, hi) of a row: its maximum, and the sum of exp((x - max) k), or (greedy) the first index of the maximum.
-// A chunk is a multiple of 2048 long: kVec vectors of 8 to a thread at a time, all of them requested before the first is used
-constexpr uint32_t kVec = 2, kSpan = kVec * kVerThreads * 8;
+// One chunk [lo, hi) of a row (see RowPart).
+// A thread takes eight at a time with the next eight on their way, and keeps a running maximum and sum.
+// The sum is relative to the first maximum a thread meets: 64 bits hold 2^800 times as much beside it, and only a larger value
+// moves it (`slack`: how far a logit may lie above it).
+struct Running { float m; double z; int best; };
 template <typename T>
-__device__ RowPart chunk_part(const T *x, uint32_t lo, uint32_t hi, double k, bool greedy, BlockBuf &b) {
-    RowPart r{0.0, -INFINITY, 0x7FFFFFFF};
-    for (uint32_t s0 = lo; s0 < hi; s0 += kSpan) {
-        float v[kVec][8], mx = -INFINITY;
+__device__ __forceinline__ void take8(Running &r, Oct<T> &o, uint32_t i, double k, float slack, bool greedy) {
+    float v[8], mx = -INFINITY;
 #pragma unroll
-        for (uint32_t u = 0; u < kVec; ++u) load8(x, s0 + (u * kVerThreads + threadIdx.x) * 8, hi, v[u]);
-#pragma unroll
-        for (uint32_t u = 0; u < kVec; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) mx = fmaxf(mx, v[u][e]);
-        mx = block_max(mx, b.f);
-        if (mx == -INFINITY) continue;
-        if (greedy) {
-            int at = 0x7FFFFFFF;
-#pragma unroll
-            for (uint32_t u = 0; u < kVec; ++u)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (v[u][e] == mx) at = min(at, (int)(s0 + (u * kVerThreads + threadIdx.x) * 8 + e));
-            at = block_min(at, b.i);
-            if (mx > r.m) r.best = at;
-            r.m = fmaxf(r.m, mx);
-            continue;
-        }
-        const float m = fmaxf(r.m, mx);
-        double z = 0;
-#pragma unroll
-        for (uint32_t u = 0; u < kVec; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z += weight(v[u][e], m, k);
-        z = block_sum(z, b.d);
-        r.z = (r.m == -INFINITY ? 0.0 : r.z * weight(r.m, m, k)) + z;
-        r.m = m;
+    for (int e = 0; e < 8; e += 2) {
+        o.take(v[e], v[e + 1]);
+        mx = fmaxf(mx, fmaxf(v[e], v[e + 1]));
     }
-    return r;
+    if (mx > r.m + slack) {
+        r.z = r.m == -INFINITY ? 0.0 : r.z * weight(r.m, mx, k);
+        r.m = mx;
+        if (greedy)
+#pragma unroll
+            for (int e = 7; e >= 0; --e) r.best = v[e] == mx ? (int)(i + e) : r.best;
+    }
+    if (greedy) return;
+    const float m = fmaxf(r.m, -kFloatMax);           // (-inf alone so far: weights of zero)
+    double z[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e & 3] += weight(v[e], m, k);
+    r.z += (z[0] + z[1]) + (z[2] + z[3]);
+}
+template <typename T>
+__device__ __forceinline__ RowPart chunk_part(const T *x, uint32_t lo, uint32_t hi, double k, bool greedy, BlockBuf &b) {
+    Running r{-INFINITY, 0.0, 0x7FFFFFFF};
+    const float slack = greedy ? 0.f : (float)fmin(800.0 / k, 1e38);
+    const uint32_t step = kVerThreads * 8;
+    Oct<T> next;
+    uint32_t i = lo + threadIdx.x * 8;
+    if (i < hi) next.fill(x, i, hi);
+#pragma unroll 1
+    for (; i < hi; i += step) {
+        Oct<T> o = next;
+        if (i + step + 8 <= hi) next.fill(x, i + step);
+        else if (i + step < hi) next.fill(x, i + step, hi);
+        take8(r, o, i, k, slack, greedy);
+    }
+    RowPart p{0.0, block_max(r.m, b.f), 0x7FFFFFFF};
+    if (p.m == -INFINITY) return p;
+    if (greedy) p.best = block_min(r.m == p.m ? r.best : 0x7FFFFFFF, b.i);
+    else p.z = block_sum(r.m == -INFINITY ? 0.0 : r.z * weight(r.m, p.m, k), b.d);
+    return p;
 }
 
 struct RowSum { double z; float m; int best; };
-__device__ __forceinline__ RowSum row_sum(const RowPart *p, uint32_t n, double k, bool greedy) {
-    RowSum r{0.0, -INFINITY, -1};
-    for (uint32_t i = 0; i < n; ++i) {
-        const float m = p[i].m;
-        if (m > r.m) { r.m = m; r.best = p[i].best; }
+// the parts of a row put together by `g` lanes (a power of two) with one each; every lane of them gets the sum
+__device__ __forceinline__ RowSum row_sum(const RowPart &mine, uint32_t g, double k, bool greedy) {
+    RowSum r{0.0, mine.m, 0x7FFFFFFF};
+    for (int o = g / 2; o; o >>= 1) r.m = fmaxf(r.m, __shfl_xor(r.m, o, 64));
+    if (greedy) {
+        r.best = mine.m == r.m && r.m != -INFINITY ? mine.best : 0x7FFFFFFF;
+        for (int o = g / 2; o; o >>= 1) r.best = min(r.best, __shfl_xor(r.best, o, 64));
+        return r;
     }
-    if (greedy || r.m == -INFINITY) return r;
-    for (uint32_t i = 0; i < n; ++i)
-        if (p[i].m != -INFINITY) r.z += p[i].z * weight(p[i].m, r.m, k);
+    r.z = mine.m == -INFINITY ? 0.0 : mine.z * weight(mine.m, r.m, k);
+    for (int o = g / 2; o; o >>= 1) r.z += __shfl_xor(r.z, o, 64);
     return r;
 }
+__device__ __forceinline__ uint32_t lanes_for(uint32_t n) { return n <= 1 ? 1u : 1u << (32 - __clz(n - 1)); }
 
 template <typename T>
 __global__ __launch_bounds__(kVerThreads) void verify_rows_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
     __shared__ BlockBuf b;
-    __shared__ unsigned char parent[PS_TREE_MAX];
+    __shared__ unsigned char parent[PS_TREE_MAX], list[PS_TREE_MAX];
+    __shared__ uint32_t cnt[4];
     const uint32_t tid = threadIdx.x, s = blockIdx.z, chunk = blockIdx.x;
     const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
     if (sr.n < 2) return;
@@ -638,16 +686,16 @@ __global__ __launch_bounds__(kVerThreads) void verify_rows_kernel(ps_verify_tree
         if (up >= 0) parent[up] = 1;
     }
     __syncthreads();
+    const uint32_t count = listed(parent[tid] != 0, list, cnt);
     const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
-    uint32_t seen = 0;
-    for (int i = 0; i < sr.n; ++i) {
-        if (!parent[i] || seen++ % gridDim.y != blockIdx.y) continue;
-        const size_t row = (size_t)sr.row0 + i;
-        const RowPart p = chunk_part(static_cast<const T *>(a.target_logits) + row * a.target_row, lo, hi, k, greedy, b);
-        if (tid == 0) w.parts[row * 2 * sh.nchunk + chunk] = p;
-        if (!a.draft_logits || greedy) continue;
-        const RowPart q = chunk_part(static_cast<const T *>(a.draft_logits) + row * a.draft_row, lo, hi, k, false, b);
-        if (tid == 0) w.parts[(row * 2 + 1) * sh.nchunk + chunk] = q;
+    for (uint32_t j = blockIdx.y; j < count; j += gridDim.y) {
+        const size_t row = (size_t)sr.row0 + list[j];
+#pragma unroll 1
+        for (uint32_t which = 0; which < (a.draft_logits && !greedy ? 2u : 1u); ++which) {
+            const T *x = which ? static_cast<const T *>(a.draft_logits) + row * a.draft_row : static_cast<const T *>(a.target_logits) + row * a.target_row;
+            const RowPart p = chunk_part(x, lo, hi, k, greedy, b);
+            if (tid == 0) w.parts[(row * 2 + which) * sh.nchunk + chunk] = p;
+        }
     }
 }
 
@@ -658,58 +706,83 @@ struct Walk {
     double c[PS_TREE_MAX];                     // c in front of this child
     int up[PS_TREE_MAX], rank[PS_TREE_MAX], token[PS_TREE_MAX], went[PS_TREE_MAX], kids[PS_TREE_MAX];
     bool dup[PS_TREE_MAX];
+    unsigned char list[PS_TREE_MAX];
+    uint32_t cnt[4];
 };
 
 // known: children up to this rank are decided (their W has been summed)
 template <typename T>
-__device__ void decide(const ps_verify_tree_args &a, const VerifyShape &sh, const VerifyWork &w, const SeqRows &sr, float temp, uint32_t known, Walk &k) {
+__device__ __forceinline__ void decide(const ps_verify_tree_args &a, const VerifyShape &sh, const VerifyWork &w, const SeqRows &sr, float temp, uint32_t known, Walk &k) {
     const int tid = threadIdx.x;
     const bool greedy = !(temp > 0.f), drafts = a.draft_logits && !greedy, in = tid < sr.n;
     const double rate = greedy ? 0.0 : rate_of(temp);
     k.kids[tid] = 0;
     k.went[tid] = 0x7FFFFFFF;
+    k.left[tid] = 1.0;
     int up = -1, token = -1;
-    float u = 0.f;
+    float u = 0.f, x = -INFINITY, y = -INFINITY;
     const size_t row = (size_t)sr.row0 + tid;
     if (in) { up = parent_of(a.parent[row], tid); token = a.token[row]; u = a.u_accept[row]; }
-    k.up[tid] = in ? up : -1;
+    const bool inside = up >= 0 && token >= 0 && token < (int)a.vocab;
+    if (inside) {       // (on their way while the rows are put together)
+        x = to_f(static_cast<const T *>(a.target_logits)[((size_t)sr.row0 + up) * a.target_row + token]);
+        if (drafts) y = to_f(static_cast<const T *>(a.draft_logits)[((size_t)sr.row0 + up) * a.draft_row + token]);
+    }
+    k.up[tid] = up;
     k.token[tid] = token;
     __syncthreads();
     if (up >= 0) atomicAdd(&k.kids[up], 1);
     int rank = 0;
     bool dup = false;
-    for (int j = 1; j < tid && up >= 0; ++j)
-        if (k.up[j] == up) { ++rank; dup |= k.token[j] == token; }
+    if (up >= 0) {
+#pragma unroll 4
+        for (int j = 1; j < tid; ++j) {
+            const bool same = k.up[j] == up;
+            rank += same;
+            dup |= same && k.token[j] == token;
+        }
+    }
     k.rank[tid] = rank;
     k.dup[tid] = dup;
     __syncthreads();
-    if (in && k.kids[tid]) {
-        k.p[tid] = row_sum(w.parts + row * 2 * sh.nchunk, sh.nchunk, rate, greedy);
-        if (drafts) k.q[tid] = row_sum(w.parts + (row * 2 + 1) * sh.nchunk, sh.nchunk, rate, false);
+    // a few lanes to a row: the rows with children, target and draft; then the W of children behind a node's first
+    const uint32_t rows = listed(k.kids[tid] > 0, k.list, k.cnt) * (drafts ? 2 : 1), g = lanes_for(sh.nchunk);
+    for (uint32_t j0 = 0; j0 < rows; j0 += kVerThreads / g) {
+        const uint32_t j = j0 + tid / g, part = tid % g;
+        const int i = j < rows ? k.list[drafts ? j >> 1 : j] : 0;
+        const bool which = drafts && (j & 1);
+        RowPart mine{0.0, -INFINITY, 0x7FFFFFFF};
+        if (j < rows && part < sh.nchunk) mine = w.parts[(((size_t)sr.row0 + i) * 2 + which) * sh.nchunk + part];
+        const RowSum r = row_sum(mine, g, rate, greedy);
+        if (j < rows && part == 0) (which ? k.q : k.p)[i] = r;
     }
-    double sum = 1.0;
-    if (up >= 0 && drafts && rank > 0 && rank <= (int)known && rank < (int)a.max_children) {
-        sum = 0;
-        for (uint32_t i = 0; i < sh.nchunk; ++i) sum += w.left[row * sh.nchunk + i];
+    if (drafts && known) {
+        __syncthreads();
+        const uint32_t later = listed(up >= 0 && rank > 0 && rank <= (int)known && rank < (int)a.max_children, k.list, k.cnt);
+        for (uint32_t j = tid >> 5; j < later; j += kVerThreads / 32) {
+            const int i = k.list[j];
+            double sum = (tid & 31) < (int)sh.ndraw ? w.left[((size_t)sr.row0 + i) * sh.ndraw + (tid & 31)] : 0.0;
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor(sum, o, 32);
+            if ((tid & 31) == 0) k.left[i] = sum;
+        }
     }
-    k.left[tid] = sum;
     __syncthreads();
     double px = 0, qx = 0;
-    const bool inside = token >= 0 && token < (int)a.vocab;
-    if (up >= 0 && inside) {
-        const size_t at = (size_t)sr.row0 + up;
+    if (inside) {
         if (greedy) px = token == k.p[up].best ? 1.0 : 0.0;
-        else if (k.p[up].m != -INFINITY) px = weight(sane(to_f(static_cast<const T *>(a.target_logits)[at * a.target_row + token])), k.p[up].m, rate) / k.p[up].z;
-        if (drafts && k.q[up].m != -INFINITY) qx = weight(sane(to_f(static_cast<const T *>(a.draft_logits)[at * a.draft_row + token])), k.q[up].m, rate) / k.q[up].z;
+        else if (k.p[up].m != -INFINITY) px = weight(sane(x), k.p[up].m, rate) / k.p[up].z;
+        if (drafts && k.q[up].m != -INFINITY) qx = weight(sane(y), k.q[up].m, rate) / k.q[up].z;
     }
     k.px[tid] = px;
     __syncthreads();
     if (up >= 0) {
         double c = 0, rest = 1.0;
-        for (int j = 1; j < tid; ++j) {
-            if (k.up[j] != up) continue;
-            if (drafts) c += k.left[j];
-            else if (!greedy && !k.dup[j]) rest -= k.px[j];
+        if (drafts) {
+#pragma unroll 4
+            for (int j = 1; j < tid; ++j) c += k.up[j] == up ? k.left[j] : 0.0;
+        } else if (!greedy) {
+#pragma unroll 4
+            for (int j = 1; j < tid; ++j) rest -= k.up[j] == up && !k.dup[j] ? k.px[j] : 0.0;
         }
         k.c[tid] = c;
         const bool yes = drafts ? px > (c + (double)u * k.left[tid]) * qx : (greedy || !dup) && px > (double)u * rest;
@@ -717,6 +790,34 @@ __device__ void decide(const ps_verify_tree_args &a, const VerifyShape &sh, cons
     }
     __syncthreads();
 }
+
+// Eight entries of what is left to draw from, two at a time: max(p - c q, 0), p without the refused, or p, times ip
+template <typename T>
+struct Left8 {
+    Oct<T> p, q;
+    __device__ __forceinline__ void fill(const ps_verify_tree_args &a, const DrawHead &h, int kind, uint32_t i, uint32_t hi) {
+        p.fill(static_cast<const T *>(a.target_logits) + (size_t)h.row * a.target_row, i, hi);
+        if (kind == DRAW_LEFT) q.fill(static_cast<const T *>(a.draft_logits) + (size_t)h.row * a.draft_row, i, hi);
+    }
+    __device__ __forceinline__ void take(const DrawHead &h, int kind, double rate, uint32_t i, const int *refused, int nref, double &u, double &v) {
+        float x, y;
+        p.take(x, y);
+        const float m = fmaxf(h.m, -kFloatMax), mq = fmaxf(h.mq, -kFloatMax);       // (rows of -inf alone: weights of zero)
+        u = weight(x, m, rate) * h.ip;
+        v = weight(y, m, rate) * h.ip;
+        if (kind == DRAW_LEFT) {
+            q.take(x, y);
+            u = fmax(u - weight(x, mq, rate) * h.iq, 0.0);
+            v = fmax(v - weight(y, mq, rate) * h.iq, 0.0);
+        }
+        if (kind == DRAW_GIVEN)
+#pragma unroll 1
+            for (int j = 0; j < nref; ++j) {
+                u = refused[j] == (int)i ? 0.0 : u;
+                v = refused[j] == (int)i + 1 ? 0.0 : v;
+            }
+    }
+};
 
 template <typename T>
 __global__ __launch_bounds__(kVerThreads) void verify_left_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w, uint32_t k) {
@@ -744,54 +845,38 @@ __global__ __launch_bounds__(kVerThreads) void verify_left_kernel(ps_verify_tree
     if (ok) list[atomicAdd(&n, 1)] = tid;      // (any order: each is worked on alone)
     __syncthreads();
     const double rate = rate_of(temp);
-    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    const uint32_t lo = chunk * sh.dchunk, hi = min(a.vocab, lo + sh.dchunk);
     for (int j = 0; j < n; ++j) {
         const int child = list[j], up = walk.up[child];
         const size_t row = (size_t)sr.row0 + up;
         const RowSum p = walk.p[up], q = walk.q[up];
         // the child's c holds W of those in front of it, all known
         const double c = walk.c[child], ip = p.m == -INFINITY ? 0.0 : 1.0 / p.z, iq = q.m == -INFINITY ? 0.0 : c / q.z;
+        DrawHead h{};
+        h.row = row;
+        h.m = p.m; h.mq = q.m; h.ip = ip; h.iq = iq;
         double sum = 0;
+#pragma unroll 1
         for (uint32_t i = lo + tid * 8; i < hi; i += kVerThreads * 8) {
-            float x[8], y[8];
-            load8(static_cast<const T *>(a.target_logits) + row * a.target_row, i, hi, x);
-            load8(static_cast<const T *>(a.draft_logits) + row * a.draft_row, i, hi, y);
+            Left8<T> l;
+            l.fill(a, h, DRAW_LEFT, i, hi);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const double pv = ip > 0 ? weight(x[e], p.m, rate) * ip : 0.0, qv = iq > 0 ? weight(y[e], q.m, rate) * iq : 0.0;
-                sum += fmax(pv - qv, 0.0);
+            for (uint32_t e = 0; e < 8; e += 2) {
+                double u, v;
+                l.take(h, DRAW_LEFT, rate, i + e, nullptr, 0, u, v);
+                sum += u + v;
             }
         }
         sum = block_sum(sum, b.d);
-        if (tid == 0) w.left[((size_t)sr.row0 + child) * sh.nchunk + chunk] = sum;
+        if (tid == 0) w.left[((size_t)sr.row0 + child) * sh.ndraw + chunk] = sum;
     }
-}
-
-// Entries i .. i + 7 of what is left to draw from (DRAW_LEFT, DRAW_GIVEN, DRAW_LEAF with its chunk's or row's maximum in m)
-template <typename T>
-__device__ __forceinline__ void left8(const ps_verify_tree_args &a, const DrawHead &h, int kind, double rate, uint32_t i, uint32_t hi, const int *refused, int nref,
-                                      double (&r)[8]) {
-    float x[8];
-    load8(static_cast<const T *>(a.target_logits) + (size_t)h.row * a.target_row, i, hi, x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = weight(x[e], h.m, rate) * h.ip;
-    if (kind == DRAW_LEFT) {
-        load8(static_cast<const T *>(a.draft_logits) + (size_t)h.row * a.draft_row, i, hi, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = fmax(r[e] - (h.iq > 0 ? weight(x[e], h.mq, rate) * h.iq : 0.0), 0.0);
-    }
-    if (kind == DRAW_GIVEN)
-        for (int j = 0; j < nref; ++j) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] = refused[j] == (int)(i + e) ? 0.0 : r[e];
-        }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
     __shared__ Walk walk;
     __shared__ BlockBuf b;
-    __shared__ int path[PS_TREE_MAX], refused[PS_TREE_MAX], n, nref, last;
+    __shared__ int path[PS_TREE_MAX], refused[PS_TREE_MAX], n, nref, all, last;
     const uint32_t s = blockIdx.y, chunk = blockIdx.x;
     const int tid = threadIdx.x;
     const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
@@ -804,7 +889,7 @@ __global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree
     const float temp = a.temperature ? a.temperature[s] : 1.f;
     const bool greedy = !(temp > 0.f), drafts = a.draft_logits && !greedy;
     const double rate = greedy ? 0.0 : rate_of(temp);
-    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    const uint32_t lo = chunk * sh.dchunk, hi = min(a.vocab, lo + sh.dchunk);
     int kids = 0;
     if (sr.n > 1) {
         decide<T>(a, sh, w, sr, temp, a.max_children, walk);
@@ -818,12 +903,12 @@ __global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree
             }
             n = m;
             last = here;
-            nref = 0;
+            nref = all = 0;
         }
         __syncthreads();
         kids = walk.kids[last];
     } else {
-        if (tid == 0) { path[0] = 0; n = 1; last = 0; nref = 0; }
+        if (tid == 0) { path[0] = 0; n = 1; last = 0; nref = all = 0; }
         __syncthreads();
     }
     DrawHead h{};
@@ -840,11 +925,12 @@ __global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree
             h.mq = walk.q[last].m;
             h.iq = h.mq == -INFINITY ? 0.0 : h.c / walk.q[last].z;
         } else if (tid < sr.n && walk.up[tid] == last && walk.rank[tid] < (int)a.max_children && !walk.dup[tid]) {
-            // (only those of this chunk)
             const int x = walk.token[tid];
-            if (x >= (int)lo && x < (int)hi) refused[atomicAdd(&nref, 1)] = x;
+            if (chunk == 0) w.refused[s * a.max_tree + atomicAdd(&all, 1)] = x;
+            if (x >= (int)lo && x < (int)hi) refused[atomicAdd(&nref, 1)] = x;       // (those of this chunk)
         }
         __syncthreads();
+        h.nref = all;
     } else {
         h.kind = DRAW_LEAF;
     }
@@ -853,7 +939,7 @@ __global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree
         if (tid == 0) {
             a.count[s] = n;
             w.heads[s] = h;
-            if (h.kind == DRAW_BEST) w.recs[s * sh.nchunk].best = walk.p[last].best;
+            if (h.kind == DRAW_BEST) w.recs[s * sh.ndraw].best = walk.p[last].best;
         }
     }
     if (h.kind < DRAW_LEAF) return;
@@ -862,144 +948,160 @@ __global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree
         r = chunk_part(static_cast<const T *>(a.target_logits) + (size_t)h.row * a.target_row, lo, hi, rate, greedy, b);
     } else {
         double sum = 0;
+#pragma unroll 1
         for (uint32_t i = lo + tid * 8; i < hi; i += kVerThreads * 8) {
-            double v[8];
-            left8<T>(a, h, h.kind, rate, i, hi, refused, nref, v);
+            Left8<T> l;
+            l.fill(a, h, h.kind, i, hi);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += v[e];
+            for (uint32_t e = 0; e < 8; e += 2) {
+                double u, v;
+                l.take(h, h.kind, rate, i + e, refused, nref, u, v);
+                sum += u + v;
+            }
         }
         r.z = block_sum(sum, b.d);
     }
-    if (tid == 0) w.recs[s * sh.nchunk + chunk] = r;
+    if (tid == 0) w.recs[s * sh.ndraw + chunk] = r;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kVerThreads) void verify_pick_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
-    __shared__ double sums[kMaxChunks], runs[4];
-    __shared__ int refused[PS_TREE_MAX], nref, pick[2];
+    __shared__ double runs[4];
+    __shared__ int refused[PS_TREE_MAX], pick[2];
     const uint32_t s = blockIdx.x;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, half = tid & 31;
     DrawHead h = w.heads[s];
+    const RowPart *recs = w.recs + s * sh.ndraw;
+    RowPart mine = half < (int)sh.ndraw ? recs[half] : RowPart{0.0, -INFINITY, 0x7FFFFFFF};     // every half wave holds them all
+    const int mine_refused = tid < (int)a.max_tree ? w.refused[s * a.max_tree + tid] : -1;       // (those that there are: see the head)
     if (h.kind <= DRAW_BEST) {
-        if (tid == 0) a.next_token[s] = h.kind == DRAW_BEST ? w.recs[s * sh.nchunk].best : -1;
+        if (tid == 0) a.next_token[s] = h.kind == DRAW_BEST ? mine.best : -1;
         return;
     }
-    const float temp = a.temperature ? a.temperature[s] : 1.f;
+    const float temp = a.temperature ? a.temperature[s] : 1.f, u = a.u_sample[s];
     const bool greedy = !(temp > 0.f);
     const double rate = greedy ? 0.0 : rate_of(temp);
-    const RowPart *recs = w.recs + s * sh.nchunk;
+    refused[tid] = tid < h.nref ? mine_refused : -1;
+    __syncthreads();
+    const int nref = h.nref;
     int kind = h.kind;
+    uint32_t chunk_len = sh.dchunk;
     if (kind == DRAW_LEAF) {
-        const RowSum r = row_sum(recs, sh.nchunk, rate, greedy);
+        const RowSum r = row_sum(mine, 32, rate, greedy);
         if (r.m == -INFINITY || greedy) {
             if (tid == 0) a.next_token[s] = r.m == -INFINITY ? -1 : r.best;
             return;
         }
         h.m = r.m;
         h.ip = 1.0;
+        mine.z = mine.m == -INFINITY ? 0.0 : mine.z * weight(mine.m, h.m, rate);
     }
-    auto chunk_sums = [&](const RowPart *p) {       // relative to the row's maximum
-        __syncthreads();
-        for (uint32_t i = tid; i < sh.nchunk; i += kVerThreads) sums[i] = p[i].m == -INFINITY ? 0.0 : kind == DRAW_LEAF ? p[i].z * weight(p[i].m, h.m, rate) : p[i].z;
-        __syncthreads();
-    };
-    if (tid == 0) nref = 0;
-    chunk_sums(recs);
-    double total = 0;
-    for (uint32_t i = 0; i < sh.nchunk; ++i) total += sums[i];
-    if (kind == DRAW_GIVEN) {
-        const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
-        const int last = h.row - sr.row0;
-        __shared__ int up[PS_TREE_MAX];
-        up[tid] = tid < sr.n ? parent_of(a.parent[sr.row0 + tid], tid) : -1;
-        __syncthreads();
-        if (tid < sr.n && up[tid] == last) {
-            int rank = 0;
-            for (int j = 1; j < tid; ++j) rank += up[j] == last;
-            if (rank < (int)a.max_children) refused[atomicAdd(&nref, 1)] = a.token[sr.row0 + tid];
+    auto running = [&](double v) {           // over the chunks, in their order
+        for (int o = 1; o < 32; o <<= 1) {
+            const double t = __shfl_up(v, o, 32);
+            if (half >= o) v += t;
         }
-        __syncthreads();
-    }
-    if (!(total > 0)) {      // nothing left: the target's own row
+        return v;
+    };
+    double run = running(mine.z), total = __shfl(run, 31, 32);
+    if (!(total > 0)) {      // nothing left: the target's own row, whose parts are chunks of their own
         kind = DRAW_LEAF;
         h.ip = 1.0;
-        chunk_sums(w.parts + (size_t)h.row * 2 * sh.nchunk);
-        total = 0;
-        for (uint32_t i = 0; i < sh.nchunk; ++i) total += sums[i];
+        chunk_len = sh.chunk;
+        mine = half < (int)sh.nchunk ? w.parts[(size_t)h.row * 2 * sh.nchunk + half] : RowPart{0.0, -INFINITY, 0x7FFFFFFF};
+        mine.z = mine.m == -INFINITY ? 0.0 : mine.z * weight(mine.m, h.m, rate);
+        run = running(mine.z);
+        total = __shfl(run, 31, 32);
     }
-    const double goal = (double)a.u_sample[s] * total;
     // the first chunk whose running sum passes the goal (or the last one that holds anything)
-    double run = 0, before = 0;
-    uint32_t chunk = 0;
-    for (uint32_t i = 0; i < sh.nchunk; ++i) {
-        if (sums[i] > 0) { chunk = i; before = run; }
-        run += sums[i];
-        if (run > goal) break;
-    }
-    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
-    // in it, a run of consecutive entries to a thread
-    const uint32_t per = sh.chunk / kVerThreads, i0 = lo + tid * per;
-    double mine = 0;
-    int some = -1;
-    for (uint32_t i = i0; i < min(hi, i0 + per); i += 8) {
-        double v[8];
-        left8<T>(a, h, kind, rate, i, hi, refused, nref, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { mine += v[e]; some = v[e] > 0 ? (int)(i + e) : some; }
-    }
-    double upto = mine;
-    for (int o = 1; o < 64; o <<= 1) {
-        const double v = __shfl_up(upto, o, 64);
-        if ((tid & 63) >= o) upto += v;
-    }
-    if ((tid & 63) == 63) runs[tid >> 6] = upto;
-    if (tid < 2) pick[tid] = tid ? -1 : 0x7FFFFFFF;
-    __syncthreads();
+    const double goal = (double)u * total;
+    const uint32_t passes = (uint32_t)__ballot(run > goal && mine.z > 0), some_left = (uint32_t)__ballot(mine.z > 0);
+    const int chunk = passes ? __ffs(passes) - 1 : 31 - __clz(some_left);
+    const double prior_run = __shfl_up(run, 1, 32);
+    const double before = chunk ? __shfl(prior_run, chunk, 32) : 0.0;
+    // in it, threads take vectors of 8 entries in turn, 2048 entries at a time
+    const uint32_t lo = chunk * chunk_len, hi = min(a.vocab, lo + chunk_len);
     double base = before;
-    for (int i = 0; i < tid >> 6; ++i) base += runs[i];
-    const double prior = __shfl_up(upto, 1, 64);
-    const double from = (tid & 63) ? base + prior : base, to = base + upto;
-    if (to > goal && mine > 0) atomicMin(&pick[0], tid);
-    if (some >= 0) atomicMax(&pick[1], some);
-    __syncthreads();
-    if (pick[0] == 0x7FFFFFFF) {
-        if (tid == 0) a.next_token[s] = pick[1];
-        return;
-    }
-    if (tid != pick[0]) return;
-    double r = from;
-    int found = some;
-    for (uint32_t i = i0; i < min(hi, i0 + per); i += 8) {
-        double v[8];
-        left8<T>(a, h, kind, rate, i, hi, refused, nref, v);
-        bool done = false;
+    int last_some = -1;
+    Left8<T> none;
+    none.p.fill(nullptr, 0, 0);
+    none.q.fill(nullptr, 0, 0);
+    for (uint32_t i0 = lo; i0 < hi; i0 += kVerThreads * 8) {
+        const uint32_t i = i0 + tid * 8;
+        Left8<T> all, l;
+        if (i < hi) all.fill(a, h, kind, i, hi);
+        else all = none;
+        l = all;
+        double sum = 0;
+        int some = -1;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            r += v[e];
-            if (!done && v[e] > 0 && r > goal) { found = i + e; done = true; }
+        for (uint32_t e = 0; e < 8; e += 2) {
+            double x, y;
+            l.take(h, kind, rate, i + e, refused, nref, x, y);
+            sum += x + y;
+            some = y > 0 ? (int)(i + e + 1) : x > 0 ? (int)(i + e) : some;
         }
-        if (done) break;
+        double upto = sum;
+        for (int o = 1; o < 64; o <<= 1) {
+            const double t = __shfl_up(upto, o, 64);
+            if ((tid & 63) >= o) upto += t;
+        }
+        __syncthreads();
+        if ((tid & 63) == 63) runs[tid >> 6] = upto;
+        if (tid < 2) pick[tid] = tid ? -1 : 0x7FFFFFFF;
+        __syncthreads();
+        double from = base;
+        for (int j = 0; j < tid >> 6; ++j) from += runs[j];
+        const double to = from + upto, prior = __shfl_up(upto, 1, 64);
+        if (tid & 63) from += prior;
+        if (to > goal && sum > 0) atomicMin(&pick[0], tid);
+        if (some >= 0) atomicMax(&pick[1], some);
+        __syncthreads();
+        if (pick[0] != 0x7FFFFFFF) {
+            if (tid != pick[0]) return;
+            int found = -1;
+            double r = from;
+#pragma unroll 1
+            for (uint32_t e = 0; e < 8; e += 2) {
+                double x, y;
+                all.take(h, kind, rate, i + e, refused, nref, x, y);
+                if (found < 0 && x > 0 && r + x > goal) found = i + e;
+                if (found < 0 && y > 0 && r + (x + y) > goal) found = i + e + 1;
+                r += x + y;
+            }
+            a.next_token[s] = found >= 0 ? found : some;
+            return;
+        }
+        last_some = max(last_some, pick[1]);
+        base = ((base + runs[0]) + runs[1]) + runs[2] + runs[3];
     }
-    a.next_token[s] = found;
+    if (tid == 0) a.next_token[s] = last_some;      // the goal lies within the last sum's rounding
 }
 
-// Chunks of a multiple of 2048 entries, at most kMaxChunks: a chunk of 4096 keeps a workgroup for about 3 us, as long as a launch's ends take.
-// Row passes: as many workgroups as keep the chip busy, each takes the nodes in turn.
+// Chunks are multiples of 2048 entries, 4096 at least and at most kMaxChunks of a row.  Row passes: as few chunks as keep about 2048
+// workgroups, counting half of the nodes (each workgroup takes several in turn where there are more): every chunk ends in two reductions, and its part is read by
+// every workgroup that works out the walk.  What is drawn from is one row of each sequence: about 1024 workgroups.
 VerifyShape verify_shape(const ps_verify_tree_args &a) {
     VerifyShape sh;
-    const uint32_t unit = kSpan / kVec, want = std::max(kSpan, (a.vocab + kMaxChunks - 1) / kMaxChunks);
-    sh.chunk = (want + unit - 1) / unit * unit;
-    sh.nchunk = (a.vocab + sh.chunk - 1) / sh.chunk;
-    sh.loop = (uint32_t)std::min<uint64_t>(std::max(1u, a.max_tree), std::max<uint64_t>(1, 4096 / std::max<uint64_t>(1, (uint64_t)sh.nchunk * a.n_seq)));
+    auto cut = [&](uint64_t chunks, uint32_t *len, uint32_t *n) {
+        chunks = std::max<uint64_t>(1, std::min<uint64_t>(chunks, kMaxChunks));
+        *len = (uint32_t)((std::max<uint64_t>(4096, (a.vocab + chunks - 1) / chunks) + 2047) / 2048 * 2048);
+        *n = (a.vocab + *len - 1) / *len;
+    };
+    const uint64_t seqs = std::max(1u, a.n_seq), nodes = std::max(1u, a.max_tree / 2);
+    cut((2048 + seqs * nodes - 1) / (seqs * nodes), &sh.chunk, &sh.nchunk);
+    cut((1024 + seqs - 1) / seqs, &sh.dchunk, &sh.ndraw);
+    sh.loop = (uint32_t)std::min<uint64_t>(std::max(1u, a.max_tree - 1), std::max<uint64_t>(1, 4096 / (sh.nchunk * seqs)));
     return sh;
 }
 uint64_t verify_work(const ps_verify_tree_args &a, const VerifyShape &sh, uint8_t *base, VerifyWork *w) {
     uint64_t off = 0;
     auto take = [&](uint64_t bytes) { uint8_t *p = base ? base + off : nullptr; off = align_up(off + bytes, kAlign); return p; };
     w->parts = reinterpret_cast<RowPart *>(take((uint64_t)a.n_tokens * 2 * sh.nchunk * sizeof(RowPart)));
-    w->left = reinterpret_cast<double *>(take(a.draft_logits ? (uint64_t)a.n_tokens * sh.nchunk * 8 : 0));
-    w->recs = reinterpret_cast<RowPart *>(take((uint64_t)a.n_seq * sh.nchunk * sizeof(RowPart)));
+    w->left = reinterpret_cast<double *>(take(a.draft_logits ? (uint64_t)a.n_tokens * sh.ndraw * 8 : 0));
+    w->recs = reinterpret_cast<RowPart *>(take((uint64_t)a.n_seq * sh.ndraw * sizeof(RowPart)));
     w->heads = reinterpret_cast<DrawHead *>(take((uint64_t)a.n_seq * sizeof(DrawHead)));
+    w->refused = reinterpret_cast<int *>(take((uint64_t)a.n_seq * a.max_tree * 4));
     return off;
 }
 
@@ -1009,9 +1111,9 @@ hipError_t launch_verify(const ps_verify_tree_args &a, const VerifyShape &sh, co
         hipLaunchKernelGGL(verify_rows_kernel<T>, dim3(sh.nchunk, sh.loop, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
         if (a.draft_logits)
             for (uint32_t k = 1; k < std::min(a.max_children, a.max_tree - 1); ++k)
-                hipLaunchKernelGGL(verify_left_kernel<T>, dim3(sh.nchunk, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w, k);
+                hipLaunchKernelGGL(verify_left_kernel<T>, dim3(sh.ndraw, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w, k);
     }
-    hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(sh.nchunk, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
+    hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(sh.ndraw, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
     hipLaunchKernelGGL(verify_pick_kernel<T>, dim3(a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
     return hipGetLastError();
 }
