@@ -35,7 +35,106 @@ __device__ __forceinline__ int parent_of(int p, int i) { return p >= 0 && p < i 
 template <typename T> __device__ __forceinline__ float to_f(T v) { return (float)v; }
 
 // ------------------------------------------------------------------------------------ norms and rotation
-// A wave per (token, head); lane l holds the pairs l, l + 64, ...
+// Bound by memory: every element is read and written once.  The angle's product and its fraction of a turn are worked out in 64
+// bits, sine and cosine of the fraction in 32.
+struct Turn { float c, s; };
+__device__ __forceinline__ Turn turn_of(double pos, float freq) {
+    const double turns = pos * (double)freq * 0.15915494309189535;        // 1 / (2 pi)
+    Turn t;
+    const float f = (float)(turns - rint(turns)) * 2.f;                    // half turns, |f| <= 1
+    sincospif(f, &t.s, &t.c);
+    return t;
+}
+
+// head_dim and rot_dim multiples of 16 (rows may start anywhere: this machine's wide loads and stores take any element's address).  A lane
+// holds 16 dimensions of a head: with halves 8 of the first half and the 8 they turn with (beyond the rotated ones: 16 of the rest),
+// with pairs 16 in a row; so no value moves between lanes, and a head is a group of L = head_dim / 16 lanes (rounded up to a power of
+// two), which its sum of squares goes over.  A wave takes a token, all its heads in turn or (few tokens) a share of them, the next ones
+// on their way; a lane's sines and cosines, half of the arithmetic, are worked out once for all of these.
+template <typename T> struct Vec8 { T v[8]; };
+template <typename T>
+__global__ __launch_bounds__(256) void qk_norm_rope_wide_kernel(ps_qk_norm_rope_args a, uint32_t L, uint32_t splits) {
+    const uint32_t lane = threadIdx.x & 63, l = lane % L, groups = 64 / L, heads = a.n_q_heads + a.n_k_heads;
+    const uint32_t half = a.rot_dim / 2, nrot = a.pairs ? 0 : half / 8;
+    const bool live = l * 16 < a.head_dim;
+    // the first dimensions of the lane's two runs of 8
+    const bool across = !a.pairs && l < nrot;
+    const uint32_t d0 = across ? l * 8 : l * 16, d1 = across ? half + l * 8 : l * 16 + 8;
+    Vec8<T> gain[2][2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const T *g = static_cast<const T *>(w ? a.k_gain : a.q_gain);
+        if (a.norm && g && live) {
+            gain[w][0] = *reinterpret_cast<const Vec8<T> *>(g + d0);
+            gain[w][1] = *reinterpret_cast<const Vec8<T> *>(g + d1);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) gain[w][0].v[e] = gain[w][1].v[e] = (T)1.f;
+        }
+    }
+    auto at = [&](const void *q, const void *k, uint64_t q_token, uint64_t q_head, uint64_t k_token, uint64_t k_head, uint64_t t, uint32_t hh) {
+        return hh < a.n_q_heads ? static_cast<const T *>(q) + t * q_token + hh * q_head : static_cast<const T *>(k) + t * k_token + (hh - a.n_q_heads) * k_head;
+    };
+    const uint64_t items = (uint64_t)a.n_tokens * splits;
+    for (uint64_t item = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (uint64_t)gridDim.x * 4) {
+        const uint64_t t = item / splits;
+        const uint32_t h0 = (uint32_t)(item % splits) * groups + lane / L;
+        Vec8<T> u, v;
+        auto request = [&](uint32_t hh) {
+            if (!live || hh >= heads) return;
+            const T *p = at(a.q, a.k, a.q_token, a.q_head, a.k_token, a.k_head, t, hh);
+            u = *reinterpret_cast<const Vec8<T> *>(p + d0);
+            v = *reinterpret_cast<const Vec8<T> *>(p + d1);
+        };
+        request(h0);
+        Turn w[8];
+        if (live && half) {
+            const double pos = (double)a.positions[t];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t i = a.pairs ? d0 / 2 + e : l * 8 + e;
+                w[e] = i < half ? turn_of(pos, a.inv_freq[i]) : Turn{1.f, 0.f};
+            }
+        }
+        for (uint32_t hh = h0; hh - lane / L < heads; hh += groups * splits) {      // (the same number of turns for all lanes)
+            const bool on = live && hh < heads, isq = hh < a.n_q_heads;
+            float x[16];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { x[e] = on ? to_f(u.v[e]) : 0.f; x[8 + e] = on ? to_f(v.v[e]) : 0.f; }
+            request(hh + groups * splits);
+            if (a.norm) {
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+                for (uint32_t o = L / 2; o; o >>= 1) ss += __shfl_xor(ss, o, 64);
+                const float rinv = 1.0f / sqrtf(ss / (float)a.head_dim + a.eps);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = x[e] * rinv * to_f(isq ? gain[0][0].v[e] : gain[1][0].v[e]);
+                    x[8 + e] = x[8 + e] * rinv * to_f(isq ? gain[0][1].v[e] : gain[1][1].v[e]);
+                }
+            }
+            if (!on) continue;
+            if (a.pairs ? d0 < a.rot_dim : across) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float p = a.pairs ? x[2 * e] : x[e], q = a.pairs ? x[2 * e + 1] : x[8 + e];
+                    const float pr = p * w[e].c - q * w[e].s, qr = q * w[e].c + p * w[e].s;
+                    if (a.pairs) { x[2 * e] = pr; x[2 * e + 1] = qr; }
+                    else { x[e] = pr; x[8 + e] = qr; }
+                }
+            }
+            T *y = const_cast<T *>(at(a.q_out, a.k_out, a.q_out_token, a.q_out_head, a.k_out_token, a.k_out_head, t, hh));
+            Vec8<T> r, z;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { r.v[e] = (T)x[e]; z.v[e] = (T)x[8 + e]; }
+            *reinterpret_cast<Vec8<T> *>(y + d0) = r;
+            *reinterpret_cast<Vec8<T> *>(y + d1) = z;
+        }
+    }
+}
+
+// Any other layout: a wave per (token, head), lane l holds the pairs l, l + 64, ...
 template <typename T>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(ps_qk_norm_rope_args a) {
     const uint32_t lane = threadIdx.x & 63, heads = a.n_q_heads + a.n_k_heads;
@@ -60,13 +159,27 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(ps_qk_norm_rope_args 
         const uint32_t da = a.pairs ? 2 * i : i, db = a.pairs ? 2 * i + 1 : i + half;
         const float ga = a.norm && gain ? to_f(gain[da]) : 1.f, gb = a.norm && gain ? to_f(gain[db]) : 1.f;
         const float va = to_f(x[da]) * rinv * ga, vb = to_f(x[db]) * rinv * gb;
-        const double turn = pos * (double)a.inv_freq[i];
-        const float c = (float)cos(turn), s = (float)sin(turn);
-        y[da] = (T)(va * c - vb * s);
-        y[db] = (T)(vb * c + va * s);
+        const Turn w = turn_of(pos, a.inv_freq[i]);
+        y[da] = (T)(va * w.c - vb * w.s);
+        y[db] = (T)(vb * w.c + va * w.s);
     }
     for (uint32_t d = a.rot_dim + lane; d < a.head_dim; d += 64)
         y[d] = (T)(to_f(x[d]) * rinv * (a.norm && gain ? to_f(gain[d]) : 1.f));
+}
+
+template <typename T>
+hipError_t launch_rope(const ps_qk_norm_rope_args &a, hipStream_t st) {
+    const uint32_t heads = a.n_q_heads + a.n_k_heads;
+    if (a.head_dim % 16 || a.rot_dim % 16) {
+        hipLaunchKernelGGL(qk_norm_rope_kernel<T>, dim3((uint32_t)(((uint64_t)a.n_tokens * heads + 3) / 4)), dim3(256), 0, st, a);
+        return hipGetLastError();
+    }
+    uint32_t L = 1;
+    while (L * 16 < a.head_dim) L *= 2;
+    // a wave to a token, and below 4096 tokens (four waves a SIMD) its heads shared out as far as that takes
+    const uint32_t rounds = (heads * L + 63) / 64, splits = (uint32_t)std::min<uint64_t>(rounds, (4095ull + a.n_tokens) / a.n_tokens);
+    hipLaunchKernelGGL(qk_norm_rope_wide_kernel<T>, dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * splits + 3) / 4, 1u << 24)), dim3(256), 0, st, a, L, splits);
+    return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------ tree attention
@@ -1209,12 +1322,10 @@ int32_t ps_qk_norm_rope(const ps_qk_norm_rope_args *a, void *stream) {
         PS_WANT(a->k != a->k_out || (a->k_token == a->k_out_token && a->k_head == a->k_out_head), "in place: k and k_out must have the same strides");
     }
     PS_WANT(!a->rot_dim || (a->positions && a->inv_freq && aligned(a->positions, 4) && aligned(a->inv_freq, 4)), "positions or inv_freq is NULL or unaligned");
-    const dim3 grid((uint32_t)((items + 3) / 4));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a->type == PS_TYPE_F16) hipLaunchKernelGGL(qk_norm_rope_kernel<f16_t>, grid, dim3(256), 0, st, *a);
-    else if (a->type == PS_TYPE_BF16) hipLaunchKernelGGL(qk_norm_rope_kernel<bf16_t>, grid, dim3(256), 0, st, *a);
-    else hipLaunchKernelGGL(qk_norm_rope_kernel<float>, grid, dim3(256), 0, st, *a);
-    PS_TRY(hipGetLastError());
+    if (a->type == PS_TYPE_F16) PS_TRY(launch_rope<f16_t>(*a, st));
+    else if (a->type == PS_TYPE_BF16) PS_TRY(launch_rope<bf16_t>(*a, st));
+    else PS_TRY(launch_rope<float>(*a, st));
     return PS_OK;
 }
 
