@@ -728,9 +728,10 @@ def _type_of(t):
     if not _TYPE:
         import torch
         _TYPE.update({torch.float16: PS_TYPE_F16, torch.bfloat16: PS_TYPE_BF16, torch.float32: PS_TYPE_F32})
-    if t.dtype not in _TYPE:
+    ty = _TYPE.get(t.dtype)
+    if ty is None:
         raise PshardError(PS_E_ARG, "float16, bfloat16 or float32 tensors are taken, not %s" % t.dtype)
-    return _TYPE[t.dtype]
+    return ty
 
 
 def _want(ok, text):
@@ -739,7 +740,7 @@ def _want(ok, text):
 
 
 def _same(name, t, shape, dtype, device):
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
+    if t.shape != shape or t.dtype != dtype or t.device != device:
         raise PshardError(PS_E_ARG, "%s must be %s %s on %s (got %s %s on %s)" % (
             name, dtype, list(shape), device, t.dtype, list(t.shape), t.device))
 
@@ -749,8 +750,6 @@ def _rows(name, t):
     st = t.stride()
     if st[-1] != 1 and t.shape[-1] > 1:
         raise PshardError(PS_E_ARG, "%s: the last dimension must be contiguous" % name)
-    if min(st) < 0:
-        raise PshardError(PS_E_ARG, "%s: negative strides" % name)
     return st
 
 
@@ -762,20 +761,31 @@ def _table(name, t, n, dtype, device):
     return t.data_ptr()
 
 
-def _on(device):
-    """The device made current (if it is not) and its current stream."""
+def _launch(device, call, *args):
+    """call(*args, stream): with the device made current if it is not, on its current stream"""
     import torch
     if device.type != "cuda":
         raise PshardError(PS_E_ARG, "tensors on a GPU are taken, not on %s" % device)
-    return torch.cuda.device(device), torch.cuda.current_stream(device).cuda_stream
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        rc = call(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, stream)
+    if rc != PS_OK:
+        _check(rc)
 
 
 def _workspace(need, given, device):
+    """(address, bytes, tensor) of the workspace: the given one, or one from torch's allocator"""
     import torch
     if given is None:
-        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    _want(given.dtype == torch.uint8 and given.is_contiguous() and given.device == device, "workspace must be contiguous uint8 on %s" % device)
-    return given
+        if not need:
+            return None, 0, None
+        given = torch.empty(need, dtype=torch.uint8, device=device)
+    else:
+        _want(given.dtype == torch.uint8 and given.is_contiguous() and given.device == device, "workspace must be contiguous uint8 on %s" % device)
+    return given.data_ptr(), given.numel(), given
 
 
 def qk_norm_rope(q, k, positions, inv_freq, q_gain=None, k_gain=None, eps=1e-6, norm=True, pairs=False, q_out=None, k_out=None):
@@ -794,16 +804,14 @@ def qk_norm_rope(q, k, positions, inv_freq, q_gain=None, k_gain=None, eps=1e-6, 
     _same("k_out", k_out, (n, hk, d), dt, dev)
     _want((positions is None) == (inv_freq is None), "positions and inv_freq come together")
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    s = [_rows(name, t) for name, t in (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out))]
+    sq, sk, so, sp = _rows("q", q), _rows("k", k), _rows("q_out", q_out), _rows("k_out", k_out)
     a = ps_qk_norm_rope_args(
         ty, n, hq, hk, d, rot, int(bool(pairs)), int(bool(norm)), eps, 0, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
-        s[0][0], s[0][1], s[1][0], s[1][1], s[2][0], s[2][1], s[3][0], s[3][1],
+        sq[0], sq[1], sk[0], sk[1], so[0], so[1], sp[0], sp[1],
         None if q_gain is None else _table("q_gain", q_gain, d, dt, dev), None if k_gain is None else _table("k_gain", k_gain, d, dt, dev),
         None if positions is None else _table("positions", positions, n, torch.int32, dev),
         None if inv_freq is None else _table("inv_freq", inv_freq, rot // 2, torch.float32, dev))
-    here, stream = _on(dev)
-    with here:
-        _check(lib().ps_qk_norm_rope(C.byref(a), stream))
+    _launch(dev, lib().ps_qk_norm_rope, C.byref(a))
     return q_out, k_out
 
 
@@ -825,20 +833,18 @@ def tree_attention(q, k_new, v_new, k_cache, v_cache, first, context, parent, ma
     _same("v_cache", v_cache, (b, hk, cap, d), dt, dev)
     out = torch.empty((n, hq, d), dtype=dt, device=dev) if out is None else out
     _same("out", out, (n, hq, d), dt, dev)
-    sq, sk, sv, ck, cv, so = (_rows(name, t) for name, t in (("q", q), ("k_new", k_new), ("v_new", v_new), ("k_cache", k_cache),
-                                                             ("v_cache", v_cache), ("out", out)))
+    sq, sk, sv = _rows("q", q), _rows("k_new", k_new), _rows("v_new", v_new)
+    ck, cv, so = _rows("k_cache", k_cache), _rows("v_cache", v_cache), _rows("out", out)
     a = ps_tree_attention_args(
         ty, b, n, hq, hk, d, int(max_context), int(max_tree), cap, int(bool(append)), d ** -0.5 if scale is None else scale, 0,
         q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(),
         sq[0], sq[1], sk[0], sk[1], sv[0], sv[1], ck[0], ck[1], ck[2], cv[0], cv[1], cv[2], so[0], so[1],
         _table("first", first, b + 1, torch.int32, dev), _table("context", context, b, torch.int32, dev),
         _table("parent", parent, n, torch.int32, dev))
-    here, stream = _on(dev)
-    with here:
-        need = C.c_uint64()
-        _check(lib().ps_tree_attention_workspace(C.byref(a), C.byref(need)))
-        ws = _workspace(need.value, workspace, dev)
-        _check(lib().ps_tree_attention(C.byref(a), ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, stream))
+    need = C.c_uint64()
+    _check(lib().ps_tree_attention_workspace(C.byref(a), C.byref(need)))
+    at, size, _held = _workspace(need.value, workspace, dev)
+    _launch(dev, lib().ps_tree_attention, C.byref(a), at, size)
     return out
 
 
@@ -866,12 +872,10 @@ def verify_tree(target_logits, token, parent, first, u_accept, u_sample, draft_l
         _table("u_accept", u_accept, n, torch.float32, dev), _table("u_sample", u_sample, b, torch.float32, dev),
         None if temperature is None else _table("temperature", temperature, b, torch.float32, dev),
         path.data_ptr(), _table("count", count, b, i32, dev), _table("next_token", next_token, b, i32, dev))
-    here, stream = _on(dev)
-    with here:
-        need = C.c_uint64()
-        _check(lib().ps_verify_tree_workspace(C.byref(a), C.byref(need)))
-        ws = _workspace(need.value, workspace, dev)
-        _check(lib().ps_verify_tree(C.byref(a), ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, stream))
+    need = C.c_uint64()
+    _check(lib().ps_verify_tree_workspace(C.byref(a), C.byref(need)))
+    at, size, _held = _workspace(need.value, workspace, dev)
+    _launch(dev, lib().ps_verify_tree, C.byref(a), at, size)
     return path, count, next_token
 
 
@@ -886,7 +890,5 @@ def cache_keep(cache, path, count, context):
     st = _rows("cache", cache)
     a = ps_cache_keep_args(b, planes, cap, d * e, path.shape[1], 0, cache.data_ptr(), st[0] * e, st[1] * e, st[2] * e, _rows("path", path)[0],
                            path.data_ptr(), _table("count", count, b, torch.int32, dev), _table("context", context, b, torch.int32, dev))
-    here, stream = _on(dev)
-    with here:
-        _check(lib().ps_cache_keep(C.byref(a), stream))
+    _launch(dev, lib().ps_cache_keep, C.byref(a))
     return cache
