@@ -694,6 +694,46 @@ typedef struct ps_cache_keep_args {
 } ps_cache_keep_args;
 int32_t ps_cache_keep(const ps_cache_keep_args *args, void *stream);
 
+/* The same inside a stack's forward (stacks with a KV cache; every plan kind and tier, pinned or streamed caches alike).
+ *
+ * ps_stack_set_rotation: from now on every forward normalises the queries and keys of each layer head by head and turns them
+ * by their positions (ps_qk_norm_rope) between the QKV projection and the attention, so the cache holds turned keys; NULL: no
+ * longer.  A token's position is the context + its number in the forward, or + its depth in the tree.  rot_dim a multiple
+ * of 16, up to head_dim; norm = 1: RMS norm per head with the model's rms_eps and gains fp16 [n_layers][head_dim] (NULL: 1).
+ * Device arrays, caller-owned, valid and unchanged until the setting changes.  Waits for the compute stream and drops captured
+ * replays.  PS_E_STATE without a KV cache. */
+typedef struct ps_rotation {
+    uint32_t rot_dim, pairs, norm, reserved;
+    const float *inv_freq;  /* device [rot_dim / 2] */
+    const void *q_gain, *k_gain;
+} ps_rotation;
+int32_t ps_stack_set_rotation(ps_stack *st, const ps_rotation *rotation);
+/* ps_stack_set_tree: the rows of the following ps_stack_forward calls are a tree of n tokens instead of a chunk: parents (host,
+ * copied) as ps_tree_attention has them, parents[i] in -1 .. i - 1 (PS_E_ARG otherwise).  n <= the plan's token count and
+ * <= PS_TREE_MAX; x_in, x_out are [n][hidden], router logits [n_layers][n][n_experts], logits of every token [n][vocab].
+ * n = 0: chunks again; ps_stack_set_tier does the same.  ps_stack_forward_chunked returns PS_E_STATE meanwhile.  All n rows are appended
+ * to the cache, node i at position context + i; ps_stack_keep_path puts the accepted ones in place. */
+int32_t ps_stack_set_tree(ps_stack *st, const int32_t *parents, uint32_t n);
+/* ps_stack_verify_tree: ps_verify_tree over the logits of the last forward (ps_stack_set_logits_out with every token; with one
+ * token: that token's row alone, i.e. the draw of the next token), the tree that ps_stack_set_tree set or, without one, the
+ * chain of the forward's tokens.  Device pointers: token int32 [n], draft_logits fp16 [n][vocab] or NULL, u_accept fp32 [n],
+ * u_sample, temperature (NULL: 1) fp32 [1]; path int32 [n], count, next_token int32 [1].  On the compute stream, asynchronous.
+ * PS_E_STATE before a forward with logits. */
+typedef struct ps_stack_verify_args {
+    const int32_t *token;
+    const void *draft_logits;
+    const float *u_accept, *u_sample, *temperature;
+    int32_t *path, *count, *next_token;
+    uint32_t max_children, reserved;
+} ps_stack_verify_args;
+int32_t ps_stack_verify_workspace(const ps_stack *st, const ps_stack_verify_args *args, uint64_t *bytes);
+int32_t ps_stack_verify_tree(ps_stack *st, const ps_stack_verify_args *args, void *workspace, uint64_t workspace_bytes);
+/* ps_stack_keep_path: ps_cache_keep over every layer's and kv head's cache, wherever it lives: row context + path[i] of the
+ * last ps_stack_forward moves to row context + i for i < *count (device int32 [n] and [1], as ps_stack_verify_tree leaves
+ * them).  On the compute stream, asynchronous; the next step's ps_stack_set_context is context + *count.  Once per
+ * forward (PS_E_STATE otherwise). */
+int32_t ps_stack_keep_path(ps_stack *st, const int32_t *path, const int32_t *count);
+
 #ifdef __cplusplus
 }
 #endif

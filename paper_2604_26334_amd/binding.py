@@ -126,7 +126,16 @@ class ps_cache_keep_args(C.Structure):
                [(n, C.c_void_p) for n in ("path", "count", "context")]
 
 
-EXPORTS = ["ps_qk_norm_rope", "ps_tree_attention", "ps_tree_attention_workspace", "ps_verify_tree", "ps_verify_tree_workspace",
+class ps_rotation(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("rot_dim", "pairs", "norm", "reserved")] + [(n, C.c_void_p) for n in ("inv_freq", "q_gain", "k_gain")]
+
+
+class ps_stack_verify_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("token", "draft_logits", "u_accept", "u_sample", "temperature", "path", "count", "next_token")] + \
+               [("max_children", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+EXPORTS = ["ps_stack_set_rotation", "ps_stack_set_tree", "ps_stack_verify_workspace", "ps_stack_verify_tree", "ps_stack_keep_path", "ps_qk_norm_rope", "ps_tree_attention", "ps_tree_attention_workspace", "ps_verify_tree", "ps_verify_tree_workspace",
            "ps_cache_keep", "ps_stack_create_tiers", "ps_stack_set_tier", "ps_stack_tier", "ps_stack_forward_noalloc", "ps_plan_num_shards", "ps_stack_forward_chunked", "ps_last_error", "ps_tier_tokens", "ps_tier_for_tokens", "ps_packed_bytes", "ps_plan_create",
            "ps_plan_summary", "ps_plan_get_shard", "ps_plan_destroy", "ps_schedule_create",
            "ps_schedule_num_ops", "ps_schedule_get_op", "ps_schedule_validate", "ps_schedule_destroy",
@@ -217,6 +226,11 @@ def lib():
             "ps_verify_tree_workspace": [C.POINTER(ps_verify_tree_args), C.POINTER(u64)],
             "ps_verify_tree": [C.POINTER(ps_verify_tree_args), vp, u64, vp],
             "ps_cache_keep": [C.POINTER(ps_cache_keep_args), vp],
+            "ps_stack_set_rotation": [vp, C.POINTER(ps_rotation)],
+            "ps_stack_set_tree": [vp, vp, u32],
+            "ps_stack_verify_workspace": [vp, C.POINTER(ps_stack_verify_args), C.POINTER(u64)],
+            "ps_stack_verify_tree": [vp, C.POINTER(ps_stack_verify_args), vp, u64],
+            "ps_stack_keep_path": [vp, vp, vp],
             "ps_cpu_matmul": [vp, u32, u32, i32, vp, u32, C.c_float, vp, vp, u32],
         }
         for name, args in sig.items():
@@ -522,6 +536,7 @@ class Stack:
         self.plan = plan
         s = plan.summary()
         self.M = s.n_tokens
+        self.tree_rows = self.logits_rows = 0
         self.H = plan.cfg["hidden"]
         self.arena = torch.empty(int(s.budget_bytes), dtype=torch.uint8, device=self.device)
         self.device_index = self.arena.device.index
@@ -543,6 +558,7 @@ class Stack:
             _check(lib().ps_stack_set_tier(self.h, int(tier), C.byref(up)))
         self.plan = self.table.plan(tier)
         self.M = self.plan.summary().n_tokens
+        self.tree_rows = 0
         return up.value
 
     def tier(self):
@@ -569,6 +585,60 @@ class Stack:
     def set_context(self, context):
         _check(lib().ps_stack_set_context(self.h, int(context)))
 
+    def set_rotation(self, inv_freq=None, q_gain=None, k_gain=None, pairs=False, norm=False):
+        """ps_stack_set_rotation: inv_freq float32 [rotated / 2], gains float16 [layers, head_dim] (norm; None: 1), kept alive
+        here; no argument: no rotation and no norm."""
+        torch, cfg = self.torch, self.plan.cfg
+        r = ps_rotation(0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(pairs)), int(bool(norm)), 0, None, None, None)
+        if inv_freq is not None:
+            r.inv_freq = _table("inv_freq", inv_freq, inv_freq.numel(), torch.float32, self.arena.device)
+        for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
+            if t is not None:
+                _same(name, t, (cfg["n_layers"], cfg["head_dim"]), torch.float16, self.arena.device)
+                _want(t.is_contiguous(), "%s must be contiguous" % name)
+                setattr(r, name, t.data_ptr())
+        with torch.cuda.device(self.device):
+            _check(lib().ps_stack_set_rotation(self.h, C.byref(r)))
+        self.rotation = (inv_freq, q_gain, k_gain)
+
+    def set_tree(self, parents=()):
+        """ps_stack_set_tree: the following forwards take a tree of len(parents) rows; nothing: chunks again."""
+        p = np.ascontiguousarray(parents, dtype=np.int32)
+        _check(lib().ps_stack_set_tree(self.h, _ptr(p) if len(p) else None, len(p)))
+        self.tree_rows = len(p)
+
+    def verify_tree(self, token, u_accept, u_sample, draft_logits=None, temperature=None, max_children=PS_TREE_MAX, path=None, count=None,
+                    next_token=None, workspace=None):
+        """ps_stack_verify_tree over the last forward's logits, on self.compute: token int32, u_accept float32 [rows], u_sample, temperature
+        float32 [1] (CUDA tensors, ready on self.compute), draft_logits float16 [rows, vocab].  Returns (path [rows], count [1], next_token [1])."""
+        torch, dev, n, i32 = self.torch, self.arena.device, token.numel(), self.torch.int32
+        with torch.cuda.device(dev), torch.cuda.stream(self.compute):
+            path = torch.empty(n, dtype=i32, device=dev) if path is None else path
+            count = torch.empty(1, dtype=i32, device=dev) if count is None else count
+            next_token = torch.empty(1, dtype=i32, device=dev) if next_token is None else next_token
+            if draft_logits is not None:
+                _same("draft_logits", draft_logits, (n, self.plan.cfg["vocab"]), torch.float16, dev)
+                _want(draft_logits.is_contiguous(), "draft_logits must be contiguous")
+            a = ps_stack_verify_args(_table("token", token, n, i32, dev), None if draft_logits is None else draft_logits.data_ptr(),
+                                     _table("u_accept", u_accept, n, torch.float32, dev), _table("u_sample", u_sample, 1, torch.float32, dev),
+                                     None if temperature is None else _table("temperature", temperature, 1, torch.float32, dev),
+                                     _table("path", path, n, i32, dev), _table("count", count, 1, i32, dev),
+                                     _table("next_token", next_token, 1, i32, dev), int(max_children), 0)
+            need = C.c_uint64()
+            _check(lib().ps_stack_verify_workspace(self.h, C.byref(a), C.byref(need)))
+            _want(n == (1 if self.logits_rows == 1 else self.tree_rows or self.M), "one token per row of logits (got %d)" % n)
+            at, size, _held = _workspace(need.value, workspace, dev)
+            _check(lib().ps_stack_verify_tree(self.h, C.byref(a), at, size))
+        return path, count, next_token
+
+    def keep_path(self, path, count):
+        """ps_stack_keep_path: path int32 [rows of the last forward], count int32 [1], as verify_tree returns them."""
+        n = self.tree_rows or self.M
+        _table("path", path, n, self.torch.int32, self.arena.device)
+        _table("count", count, 1, self.torch.int32, self.arena.device)
+        with self.torch.cuda.device(self.device):
+            _check(lib().ps_stack_keep_path(self.h, path.data_ptr(), count.data_ptr()))
+
     def set_cpu_threads(self, threads):
         _check(lib().ps_stack_set_cpu_threads(self.h, int(threads)))
 
@@ -579,13 +649,14 @@ class Stack:
             assert logits.dtype == self.torch.float16 and logits.is_contiguous()
             assert logits.numel() == rows * self.plan.cfg["vocab"]
         _check(lib().ps_stack_set_logits_out(self.h, logits.data_ptr() if rows else None, int(first_token), int(rows)))
+        self.logits_rows = int(rows)
 
     def forward(self, x_in, x_out, router_logits=None, router_logits_dev=None):
         """x_in, x_out: torch fp16 CUDA tensors [M][H]; asynchronous on self.compute.
         router_logits_dev: optional torch fp32 CUDA tensor holding the same values as router_logits."""
         assert x_in.dtype == self.torch.float16 and x_out.dtype == self.torch.float16
         assert x_in.is_contiguous() and x_out.is_contiguous()
-        shape = (self.M, self.H)
+        shape = (self.tree_rows or self.M, self.H)
         assert x_in.shape == shape and x_out.shape == shape
         lg = None if router_logits is None else np.ascontiguousarray(router_logits, dtype=np.float32)
         ld = None

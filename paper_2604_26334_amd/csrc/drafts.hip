@@ -9,6 +9,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "drafts.h"
 #include "ps_internal.h"
 
 namespace ps {
@@ -31,6 +32,7 @@ __device__ __forceinline__ SeqRows rows_of(const int32_t *first, uint32_t s, uin
     return {a, clampi(b - a, 0, (int)max_tree)};
 }
 __device__ __forceinline__ int parent_of(int p, int i) { return p >= 0 && p < i ? p : -1; }
+__device__ __forceinline__ uint32_t byte_of(const TreeBytes &t, uint32_t i) { return t.w[i / 4] >> (i % 4 * 8) & 0xFFu; }
 
 template <typename T> __device__ __forceinline__ float to_f(T v) { return (float)v; }
 
@@ -52,8 +54,18 @@ __device__ __forceinline__ Turn turn_of(double pos, float freq) {
 // two), which its sum of squares goes over.  A wave takes a token, all its heads in turn or (few tokens) a share of them, the next ones
 // on their way; a lane's sines and cosines, half of the arithmetic, are worked out once for all of these.
 template <typename T> struct Vec8 { T v[8]; };
-template <typename T>
-__global__ __launch_bounds__(256) void qk_norm_rope_wide_kernel(ps_qk_norm_rope_args a, uint32_t L, uint32_t splits) {
+struct GivenPositions {
+    const int32_t *p;
+    __device__ __forceinline__ double operator()(uint64_t t) const { return (double)p[t]; }
+};
+struct StackPositions {       // of a forward's tokens: see launch_stack_rotation
+    const uint32_t *ctx_dev;
+    uint32_t ctx, tree;
+    TreeBytes depth;
+    __device__ __forceinline__ double operator()(uint64_t t) const { return (double)((ctx_dev ? *ctx_dev : ctx) + (tree ? byte_of(depth, (uint32_t)t) : (uint32_t)t)); }
+};
+template <typename T, class P>
+__global__ __launch_bounds__(256) void qk_norm_rope_wide_kernel(ps_qk_norm_rope_args a, P position, uint32_t L, uint32_t splits) {
     const uint32_t lane = threadIdx.x & 63, l = lane % L, groups = 64 / L, heads = a.n_q_heads + a.n_k_heads;
     const uint32_t half = a.rot_dim / 2, nrot = a.pairs ? 0 : half / 8;
     const bool live = l * 16 < a.head_dim;
@@ -89,7 +101,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_wide_kernel(ps_qk_norm_rope_
         request(h0);
         Turn w[8];
         if (live && half) {
-            const double pos = (double)a.positions[t];
+            const double pos = position(t);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const uint32_t i = a.pairs ? d0 / 2 + e : l * 8 + e;
@@ -167,18 +179,20 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(ps_qk_norm_rope_args 
         y[d] = (T)(to_f(x[d]) * rinv * (a.norm && gain ? to_f(gain[d]) : 1.f));
 }
 
-template <typename T>
-hipError_t launch_rope(const ps_qk_norm_rope_args &a, hipStream_t st) {
-    const uint32_t heads = a.n_q_heads + a.n_k_heads;
-    if (a.head_dim % 16 || a.rot_dim % 16) {
-        hipLaunchKernelGGL(qk_norm_rope_kernel<T>, dim3((uint32_t)(((uint64_t)a.n_tokens * heads + 3) / 4)), dim3(256), 0, st, a);
-        return hipGetLastError();
-    }
+template <typename T, class P>
+hipError_t launch_rope_wide(const ps_qk_norm_rope_args &a, const P &position, hipStream_t st) {
     uint32_t L = 1;
     while (L * 16 < a.head_dim) L *= 2;
     // a wave to a token, and below 4096 tokens (four waves a SIMD) its heads shared out as far as that takes
-    const uint32_t rounds = (heads * L + 63) / 64, splits = (uint32_t)std::min<uint64_t>(rounds, (4095ull + a.n_tokens) / a.n_tokens);
-    hipLaunchKernelGGL(qk_norm_rope_wide_kernel<T>, dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * splits + 3) / 4, 1u << 24)), dim3(256), 0, st, a, L, splits);
+    const uint32_t rounds = ((a.n_q_heads + a.n_k_heads) * L + 63) / 64, splits = (uint32_t)std::min<uint64_t>(rounds, (4095ull + a.n_tokens) / a.n_tokens);
+    hipLaunchKernelGGL((qk_norm_rope_wide_kernel<T, P>), dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * splits + 3) / 4, 1u << 24)), dim3(256), 0, st, a,
+                       position, L, splits);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_rope(const ps_qk_norm_rope_args &a, hipStream_t st) {
+    if (a.head_dim % 16 == 0 && a.rot_dim % 16 == 0) return launch_rope_wide<T>(a, GivenPositions{a.positions}, st);
+    hipLaunchKernelGGL(qk_norm_rope_kernel<T>, dim3((uint32_t)(((uint64_t)a.n_tokens * (a.n_q_heads + a.n_k_heads) + 3) / 4)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
@@ -257,8 +271,32 @@ template <int D, int NT> constexpr uint32_t tree_lds() {
 // Tiles of sequence: the cache's, then the tree's own; each split takes `per` of them
 __device__ __forceinline__ uint32_t tiles_per_split(uint32_t tiles, uint32_t nsplit) { return ((tiles + nsplit - 1) / nsplit + 3) & ~3u; }
 
-template <typename T, int D, int NT>
-__global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attention_args a, uint32_t blocks, uint32_t nsplit, float *part) {
+// Where a launch's tables are: in device memory (a batch of sequences), or in its arguments (a stack's own forward: one sequence, some
+// of the model's heads, rows appended through a table of addresses)
+struct BatchTrees {
+    static constexpr bool kStack = false;
+};
+struct StackTree {
+    static constexpr bool kStack = true;
+    const uint64_t *home;
+    uint32_t cap, heads, head0;          // query heads of the model, the launch's first one
+    TreeBytes up;
+};
+struct TreeSeq { SeqRows rows; uint32_t ctx; };
+template <class S>
+__device__ __forceinline__ TreeSeq sequence_of(const ps_tree_attention_args &a, const S &, uint32_t s) {
+    if constexpr (S::kStack) return {{0, (int)a.n_tokens}, a.max_context};
+    else return {rows_of(a.first, s, a.n_tokens, a.max_tree), (uint32_t)clampi(a.context[s], 0, (int)a.max_context)};
+}
+// where the records of a token's query head start
+template <class S>
+__device__ __forceinline__ size_t record_of(const ps_tree_attention_args &a, const S &w, size_t token, uint32_t h, uint32_t nsplit) {
+    if constexpr (S::kStack) return (token * w.heads + w.head0 + h) * nsplit;
+    else return (token * a.n_q_heads + h) * nsplit;
+}
+
+template <typename T, int D, int NT, class Where>
+__global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attention_args a, Where where, uint32_t blocks, uint32_t nsplit, float *part) {
     using M = Mfma<T>;
     using v8 = typename M::v8;
     constexpr int KK = D / 32, DT = D / 16, RB = NT * 16, OP = D + 4;
@@ -275,8 +313,9 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     const uint32_t unit = blockIdx.x / 8 / blocks * 8 + blockIdx.x % 8, rb = blockIdx.x / 8 % blocks;
     if (unit >= units) return;
     const uint32_t z = unit % nsplit, hk = unit / nsplit % a.n_kv_heads, s = unit / nsplit / a.n_kv_heads;
-    const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
-    const uint32_t ctx = clampi(a.context[s], 0, (int)a.max_context), t_n = sr.n, G = a.n_q_heads / a.n_kv_heads;
+    const TreeSeq seq = sequence_of(a, where, s);
+    const SeqRows sr = seq.rows;
+    const uint32_t ctx = seq.ctx, t_n = sr.n, G = a.n_q_heads / a.n_kv_heads;
     const uint32_t R = t_n * G, row0 = rb * RB;
     if (row0 >= R) return;
     const uint32_t nc = (ctx + kTile - 1) / kTile, tiles = nc + (t_n + kTile - 1) / kTile, per = tiles_per_split(tiles, nsplit);
@@ -322,7 +361,8 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
         uint32_t m[kMaskWords];
         if (tid == 0) *wild = 0;
         if (tid < t_n) {
-            link = parent_of(a.parent[sr.row0 + tid], (int)tid);
+            if constexpr (Where::kStack) link = (int)byte_of(where.up, tid) - 1;
+            else link = parent_of(a.parent[sr.row0 + tid], (int)tid);
 #pragma unroll
             for (uint32_t w = 0; w < kMaskWords; ++w) anc[tid * kMaskWords + w] = tid / 32 == w ? 1u << (tid % 32) : 0u;
             up[tid] = link;
@@ -347,6 +387,10 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     if (a.append && z == 0) {            // rows context and up, which nobody reads: each block moves the tokens whose first row it holds
         const uint32_t t0 = (row0 + G - 1) / G, t1 = min(t_n, (row0 + RB + G - 1) / G);
         T *kd = static_cast<T *>(a.k_cache) + s * a.k_seq + hk * a.k_head, *vd = static_cast<T *>(a.v_cache) + s * a.v_seq + hk * a.v_head;
+        if constexpr (Where::kStack) {
+            kd = reinterpret_cast<T *>(where.home[hk]);
+            vd = kd + (size_t)where.cap * D;
+        }
         for (uint32_t u = tid; u < (t1 - t0) * kRowPieces * 2; u += 256) {
             const uint32_t t = t0 + u / (2 * kRowPieces), e = u % kRowPieces * 8;
             const bool v = u / kRowPieces & 1;
@@ -508,7 +552,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
         }
         const size_t token = (size_t)sr.row0 + t;
         if (nsplit > 1) {
-            float *dst = part + ((token * a.n_q_heads + h) * nsplit + z) * OP;
+            float *dst = part + (record_of(a, where, token, h, nsplit) + z) * OP;
             *reinterpret_cast<f4_t *>(dst + d0) = o;
             if (d0 == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(mx * c2, l);
         } else {
@@ -522,16 +566,17 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
 
 // A wave per (token, query head) merges the records of its sequence's splits, in their order: value sums, then maximum (in
 // powers of two) and weight sum.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args a, uint32_t nsplit, const float *part) {
+template <typename T, int D, class S>
+__global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args a, S where, uint32_t nsplit, const float *part) {
     constexpr int E = D / 64, OP = D + 4;
     const uint32_t lane = threadIdx.x & 63, h = blockIdx.x * 4 + (threadIdx.x >> 6), t = blockIdx.y, s = blockIdx.z;
-    const SeqRows sr = rows_of(a.first, s, a.n_tokens, a.max_tree);
+    const TreeSeq seq = sequence_of(a, where, s);
+    const SeqRows sr = seq.rows;
     if (h >= a.n_q_heads || (int)t >= sr.n) return;
-    const uint32_t ctx = clampi(a.context[s], 0, (int)a.max_context);
+    const uint32_t ctx = seq.ctx;
     const uint32_t tiles = (ctx + kTile - 1) / kTile + (sr.n + kTile - 1) / kTile, per = tiles_per_split(tiles, nsplit), n = (tiles + per - 1) / per;
     const size_t token = (size_t)sr.row0 + t;
-    const float *p = part + (token * a.n_q_heads + h) * nsplit * OP;
+    const float *p = part + record_of(a, where, token, h, nsplit) * OP;
     float mx = -INFINITY, l = 0.f, o[E] = {};
     for (uint32_t z0 = 0; z0 < n; z0 += 8) {
         float mv[8], lv[8], ov[8][E], m8 = mx;
@@ -577,28 +622,35 @@ TreeDeal tree_deal(const ps_tree_attention_args &a) {
     return d;
 }
 
-template <typename T, int D, int NT>
-hipError_t launch_tree_k(const ps_tree_attention_args &a, const TreeDeal &d, float *part, hipStream_t st) {
+template <typename T, int D, int NT, class S>
+hipError_t launch_tree_k(const ps_tree_attention_args &a, const S &where, const TreeDeal &d, float *part, hipStream_t st) {
     constexpr uint32_t lds = tree_lds<D, NT>();
     static std::atomic<uint64_t> done{0};        // devices this kernel's LDS size has been announced on
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev >= 64 || !(done.load(std::memory_order_relaxed) >> dev & 1)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_attention_kernel<T, D, NT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_attention_kernel<T, D, NT, S>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
         if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     const uint32_t units = a.n_seq * a.n_kv_heads * d.nsplit;
-    hipLaunchKernelGGL((tree_attention_kernel<T, D, NT>), dim3((units + 7) / 8 * 8 * d.blocks), dim3(256), lds, st, a, d.blocks, d.nsplit, part);
+    hipLaunchKernelGGL((tree_attention_kernel<T, D, NT, S>), dim3((units + 7) / 8 * 8 * d.blocks), dim3(256), lds, st, a, where, d.blocks, d.nsplit, part);
+    return hipGetLastError();
+}
+template <typename T, int D, class S>
+hipError_t launch_tree(const ps_tree_attention_args &a, const S &where, const TreeDeal &d, float *part, hipStream_t st) {
+    return d.nt == 1 ? launch_tree_k<T, D, 1>(a, where, d, part, st) : launch_tree_k<T, D, 2>(a, where, d, part, st);
+}
+template <typename T, int D, class S>
+hipError_t launch_merge(const ps_tree_attention_args &a, const S &where, uint32_t nsplit, const float *part, hipStream_t st) {
+    hipLaunchKernelGGL((tree_merge_kernel<T, D, S>), dim3((a.n_q_heads + 3) / 4, a.max_tree, a.n_seq), dim3(256), 0, st, a, where, nsplit, part);
     return hipGetLastError();
 }
 template <typename T, int D>
-hipError_t launch_tree(const ps_tree_attention_args &a, const TreeDeal &d, float *part, hipStream_t st) {
-    hipError_t e = d.nt == 1 ? launch_tree_k<T, D, 1>(a, d, part, st) : launch_tree_k<T, D, 2>(a, d, part, st);
-    if (e != hipSuccess || d.nsplit == 1) return e;
-    hipLaunchKernelGGL((tree_merge_kernel<T, D>), dim3((a.n_q_heads + 3) / 4, a.max_tree, a.n_seq), dim3(256), 0, st, a, d.nsplit, part);
-    return hipGetLastError();
+hipError_t launch_trees(const ps_tree_attention_args &a, const TreeDeal &d, float *part, hipStream_t st) {
+    const hipError_t e = launch_tree<T, D>(a, BatchTrees{}, d, part, st);
+    return e != hipSuccess || d.nsplit == 1 ? e : launch_merge<T, D>(a, BatchTrees{}, d.nsplit, part, st);
 }
 
 // ------------------------------------------------------------------------------------ verification
@@ -1232,37 +1284,59 @@ hipError_t launch_verify(const ps_verify_tree_args &a, const VerifyShape &sh, co
 }
 
 // ------------------------------------------------------------------------------------ kept rows
-// A wave per plane of a sequence: it reads up to 16 x 64 pieces of 16 bytes (all rows of a run of columns) before it
-// writes any, so rows may move onto rows that others are read from.
-__global__ __launch_bounds__(256) void cache_keep_kernel(ps_cache_keep_args a, uint32_t seg) {
+// A wave per plane of a sequence, run of columns by run: kKeep pieces of 16 bytes a lane hold all rows of a run, and are all read before
+// one is written, so rows may move onto rows that others are read from.  Rows that stay where they are are not touched.
+constexpr uint32_t kKeep = 4;
+struct BatchPlanes {
+    __device__ __forceinline__ char *operator()(const ps_cache_keep_args &a, uint32_t s, uint32_t plane) const {
+        return static_cast<char *>(a.cache) + s * a.seq_stride + plane * a.plane_stride;
+    }
+    __device__ __forceinline__ int64_t context(const ps_cache_keep_args &a, uint32_t s) const { return a.context[s]; }
+};
+struct StackPlanes {       // home[plane / 2]: K rows, then V rows
+    const uint64_t *home;
+    uint32_t ctx;
+    __device__ __forceinline__ char *operator()(const ps_cache_keep_args &a, uint32_t, uint32_t plane) const {
+        return reinterpret_cast<char *>(home[plane / 2]) + (plane & 1 ? (uint64_t)a.capacity * a.row_stride : 0);
+    }
+    __device__ __forceinline__ int64_t context(const ps_cache_keep_args &, uint32_t) const { return ctx; }
+};
+template <class S>
+__global__ __launch_bounds__(256) void cache_keep_kernel(ps_cache_keep_args a, S where) {
     const uint32_t lane = threadIdx.x & 63, plane = blockIdx.x * 4 + (threadIdx.x >> 6), s = blockIdx.y;
     if (plane >= a.n_planes) return;
     const int n = clampi(a.count[s], 0, (int)a.max_tree);
-    const int64_t ctx = a.context[s];
+    const int64_t ctx = where.context(a, s);
     const int32_t *path = a.path + s * a.path_seq;
-    char *base = static_cast<char *>(a.cache) + s * a.seq_stride + plane * a.plane_stride;
+    char *base = where(a, s, plane);
     const uint32_t units = a.row_bytes / 16;
+    // columns of a run: as many (a power of two) as leave room for all rows
+    const uint32_t shift = 31 - __clz(64 * kKeep / (uint32_t)max(n, 1)), seg = 1u << shift;
+    if (n == 0) return;
     for (uint32_t c0 = 0; c0 < units; c0 += seg) {
-        u4_t v[16];
-        bool ok[16];
+        u4_t v[kKeep];
+        bool ok[kKeep];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            const uint32_t idx = u * 64 + lane, i = idx / seg, col = c0 + idx % seg;
-            ok[u] = (int)i < n && col < units;
-            if (ok[u]) {
-                const int node = path[i];
-                const int64_t from = ctx + node, to = ctx + i;
-                ok[u] = node >= 0 && node < (int)a.max_tree && from >= 0 && from < a.capacity && to >= 0 && to < a.capacity;
-                if (ok[u]) v[u] = *reinterpret_cast<const u4_t *>(base + from * a.row_stride + col * 16);
-            }
+        for (uint32_t u = 0; u < kKeep; ++u) {
+            const uint32_t idx = u * 64 + lane, i = idx >> shift, col = c0 + (idx & (seg - 1));
+            const int node = (int)i < n && col < units ? path[i] : -1;
+            const int64_t from = ctx + node, to = ctx + i;
+            ok[u] = node >= 0 && node < (int)a.max_tree && node != (int)i && from >= 0 && from < a.capacity && to >= 0 && to < a.capacity;
+            if (ok[u]) v[u] = *reinterpret_cast<const u4_t *>(base + from * a.row_stride + col * 16);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            const uint32_t idx = u * 64 + lane, i = idx / seg, col = c0 + idx % seg;
+        for (uint32_t u = 0; u < kKeep; ++u) {
+            const uint32_t idx = u * 64 + lane, i = idx >> shift, col = c0 + (idx & (seg - 1));
             if (ok[u]) *reinterpret_cast<u4_t *>(base + (ctx + i) * a.row_stride + col * 16) = v[u];
         }
     }
+}
+
+__global__ __launch_bounds__(PS_TREE_MAX) void tree_tables_kernel(int32_t *first, int32_t *parent, StackTreeNodes tree, uint32_t n) {
+    const uint32_t t = threadIdx.x;
+    if (t < 2) first[t] = t ? (int32_t)n : 0;
+    if (t < n) parent[t] = tree.n ? (int32_t)byte_of(tree.up, t) - 1 : (int32_t)t - 1;
 }
 
 #define PS_TRY(call)                                                                                    \
@@ -1293,6 +1367,91 @@ int32_t check_tree(const ps_tree_attention_args *a) {
 }
 
 }  // namespace
+
+bool make_tree_nodes(const int32_t *parent, uint32_t n, StackTreeNodes *out) {
+    *out = StackTreeNodes{};
+    uint8_t *up = reinterpret_cast<uint8_t *>(out->up.w), *depth = reinterpret_cast<uint8_t *>(out->depth.w);
+    for (uint32_t i = 0; i < n; ++i) {
+        if (parent[i] < -1 || parent[i] >= (int32_t)i) { set_error("node %u cannot follow node %d: a parent comes before its children", i, parent[i]); return false; }
+        up[i] = (uint8_t)(parent[i] + 1);
+        depth[i] = parent[i] < 0 ? 0 : (uint8_t)(depth[parent[i]] + 1);
+    }
+    out->n = n;
+    return true;
+}
+
+hipError_t launch_stack_rotation(const StackRotation &r, uint32_t layer, __half *qkv, uint32_t qkv_w, uint32_t n_q, uint32_t n_kv, uint32_t n_tokens,
+                                 uint32_t ctx, const uint32_t *ctx_dev, const StackTreeNodes &tree, hipStream_t st) {
+    if (n_tokens == 0) return hipSuccess;
+    if (r.rot_dim % 16 || r.rot_dim > 128 || (tree.n && n_tokens > tree.n)) return hipErrorInvalidValue;
+    ps_qk_norm_rope_args a{};
+    a.type = PS_TYPE_F16; a.n_tokens = n_tokens; a.n_q_heads = n_q; a.n_k_heads = n_kv; a.head_dim = 128; a.rot_dim = r.rot_dim;
+    a.pairs = r.pairs; a.norm = r.norm; a.eps = r.eps;
+    a.q = a.q_out = qkv;
+    a.k = a.k_out = qkv + (size_t)n_q * 128;
+    a.q_token = a.k_token = a.q_out_token = a.k_out_token = qkv_w;
+    a.q_head = a.k_head = a.q_out_head = a.k_out_head = 128;
+    a.q_gain = r.q_gain ? r.q_gain + (size_t)layer * 128 : nullptr;
+    a.k_gain = r.k_gain ? r.k_gain + (size_t)layer * 128 : nullptr;
+    a.inv_freq = r.inv_freq;
+    return launch_rope_wide<f16_t>(a, StackPositions{ctx_dev, ctx, tree.n, tree.depth}, st);
+}
+
+static ps_tree_attention_args stack_tree_call(const StackTreeArgs &s, uint32_t n_tokens, uint32_t nheads) {
+    ps_tree_attention_args a{};
+    const uint32_t G = s.n_q / s.n_kv;
+    a.type = PS_TYPE_F16; a.n_seq = 1; a.n_tokens = a.max_tree = n_tokens; a.n_kv_heads = nheads; a.n_q_heads = nheads * G; a.head_dim = 128;
+    a.max_context = s.ctx; a.capacity = s.cap; a.append = s.home ? 1 : 0; a.scale = 0.08838834764831845f;
+    const uint32_t head0 = nheads == s.n_kv ? 0 : s.head0;
+    a.q = s.qkv + (size_t)head0 * G * 128;
+    a.k_new = s.qkv + (size_t)(s.n_q + head0) * 128;
+    a.v_new = s.qkv + (size_t)(s.n_q + s.n_kv + head0) * 128;
+    a.q_token = a.k_new_token = a.v_new_token = s.qkv_w;
+    a.q_head = a.k_new_head = a.v_new_head = 128;
+    a.k_cache = const_cast<__half *>(s.k_base);
+    a.v_cache = const_cast<__half *>(s.k_base + (size_t)s.cap * 128);
+    a.k_head = a.v_head = s.head_stride / 2;
+    a.k_row = a.v_row = 128;
+    a.out = s.out + (size_t)head0 * G * 128;
+    a.out_token = (uint64_t)s.n_q * 128;
+    a.out_head = 128;
+    return a;
+}
+uint32_t stack_tree_splits(uint32_t n_q, uint32_t n_kv, uint32_t ctx, uint32_t n_tokens, uint64_t part_bytes) {
+    ps_tree_attention_args a{};
+    a.n_seq = 1; a.max_tree = n_tokens; a.n_q_heads = n_q; a.n_kv_heads = n_kv; a.max_context = ctx;
+    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(tree_deal(a).nsplit, part_bytes / ((uint64_t)n_tokens * n_q * (128 + 4) * 4)));
+}
+static TreeDeal stack_deal(const StackTreeArgs &s, uint32_t n_tokens) {
+    ps_tree_attention_args a{};
+    a.n_seq = 1; a.max_tree = n_tokens; a.n_q_heads = s.n_q; a.n_kv_heads = s.n_kv; a.max_context = s.ctx;
+    TreeDeal d = tree_deal(a);
+    d.nsplit = s.splits;
+    return d;
+}
+hipError_t launch_stack_tree(const StackTreeArgs &s, const StackTreeNodes &tree, hipStream_t st) {
+    if (s.nheads == 0 || tree.n == 0) return hipSuccess;
+    if (s.splits == 0 || tree.n > PS_TREE_MAX || (s.home ? (uint64_t)s.ctx + tree.n > s.cap : s.ctx > s.cap)) return hipErrorInvalidValue;
+    const StackTree where{s.home ? s.home + s.head0 : nullptr, s.cap, s.n_q, s.head0 * (s.n_q / s.n_kv), tree.up};
+    ps_tree_attention_args a = stack_tree_call(s, tree.n, s.nheads);
+    return launch_tree<f16_t, 128>(a, where, stack_deal(s, tree.n), s.part, st);
+}
+hipError_t launch_stack_tree_merge(const StackTreeArgs &s, uint32_t n_tokens, hipStream_t st) {
+    return launch_merge<f16_t, 128>(stack_tree_call(s, n_tokens, s.n_kv), StackTree{nullptr, s.cap, s.n_q, 0, {}}, s.splits, s.part, st);
+}
+hipError_t launch_tree_tables(int32_t *first, int32_t *parent, uint32_t n, const StackTreeNodes &tree, hipStream_t st) {
+    if (n > PS_TREE_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(tree_tables_kernel, dim3(1), dim3(PS_TREE_MAX), 0, st, first, parent, tree, n);
+    return hipGetLastError();
+}
+hipError_t launch_stack_keep(const uint64_t *home, uint32_t n_homes, uint32_t cap, uint32_t ctx, uint32_t width, const int32_t *path, const int32_t *count,
+                             hipStream_t st) {
+    ps_cache_keep_args a{};
+    a.n_seq = 1; a.n_planes = 2 * n_homes; a.capacity = cap; a.row_bytes = 256; a.max_tree = width; a.row_stride = 256;
+    a.path = path; a.count = count;
+    hipLaunchKernelGGL(cache_keep_kernel<StackPlanes>, dim3((a.n_planes + 3) / 4), dim3(256), 0, st, a, StackPlanes{home, ctx});
+    return hipGetLastError();
+}
 }  // namespace ps
 
 using namespace ps;
@@ -1359,8 +1518,8 @@ int32_t ps_tree_attention(const ps_tree_attention_args *a, void *workspace, uint
     PS_WANT((uint64_t)a->n_seq * a->n_kv_heads * d.nsplit * d.blocks < 1ull << 28, "too many sequences and heads for one call");
     hipStream_t st = static_cast<hipStream_t>(stream);
     float *part = static_cast<float *>(workspace);
-    if (a->type == PS_TYPE_F16) PS_TRY(a->head_dim == 64 ? (launch_tree<f16_t, 64>(*a, d, part, st)) : (launch_tree<f16_t, 128>(*a, d, part, st)));
-    else PS_TRY(a->head_dim == 64 ? (launch_tree<bf16_t, 64>(*a, d, part, st)) : (launch_tree<bf16_t, 128>(*a, d, part, st)));
+    if (a->type == PS_TYPE_F16) PS_TRY(a->head_dim == 64 ? (launch_trees<f16_t, 64>(*a, d, part, st)) : (launch_trees<f16_t, 128>(*a, d, part, st)));
+    else PS_TRY(a->head_dim == 64 ? (launch_trees<bf16_t, 64>(*a, d, part, st)) : (launch_trees<bf16_t, 128>(*a, d, part, st)));
     return PS_OK;
 }
 
@@ -1410,8 +1569,7 @@ int32_t ps_cache_keep(const ps_cache_keep_args *a, void *stream) {
     PS_WANT(aligned(a->cache, 16) && a->seq_stride % 16 == 0 && a->plane_stride % 16 == 0 && a->row_stride % 16 == 0, "the cache and its strides must be multiples of 16 bytes");
     PS_WANT(a->row_stride >= a->row_bytes || a->capacity == 1, "rows of %u bytes lie %llu bytes apart", a->row_bytes, (unsigned long long)a->row_stride);
     PS_WANT(aligned(a->path, 4) && aligned(a->count, 4) && aligned(a->context, 4), "path, count and context must be aligned to 4 bytes");
-    const uint32_t seg = std::max(1u, std::min(a->row_bytes / 16, 1024 / a->max_tree));
-    hipLaunchKernelGGL(cache_keep_kernel, dim3((a->n_planes + 3) / 4, a->n_seq), dim3(256), 0, static_cast<hipStream_t>(stream), *a, seg);
+    hipLaunchKernelGGL(cache_keep_kernel<BatchPlanes>, dim3((a->n_planes + 3) / 4, a->n_seq), dim3(256), 0, static_cast<hipStream_t>(stream), *a, BatchPlanes{});
     PS_TRY(hipGetLastError());
     return PS_OK;
 }

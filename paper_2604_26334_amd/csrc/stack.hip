@@ -17,6 +17,7 @@
 #include <tuple>
 
 #include "cpu_backend.h"
+#include "drafts.h"
 #include "kernels.h"
 #include "ps_internal.h"
 
@@ -90,6 +91,10 @@ struct ps_stack {
     bool step_pending = false;
     bool kv_copied = false;                   // some kv shard is not resident: the copy stream reads appended rows
     uint32_t kv_rows = 0;                     // cache positions written so far (loaded or appended): what a tier switch moves
+    bool rotate = false;                      // queries and keys are normalised and turned in front of the attention
+    ps::StackRotation rotation{};
+    ps::StackTreeNodes tree{};                // n > 0: the rows of a forward are a tree
+    uint32_t step_rows = 0, step_ctx = 0;     // rows and context of the last ps_stack_forward (0: none since its rows were kept, or the tier changed)
     bool profiling = false;
     bool own_rinv_launch = false;             // decode mode 2: RMS factors always from rinv_kernel
     const void *rinv_of = nullptr;            // rows whose RMS factors the last residual epilogue or combine left in the workspace
@@ -296,6 +301,15 @@ int32_t issue_kernel(ps_stack *st, const ps_schedule &sc, const Op &op, const __
         return a;
     };
 
+    auto tree_args = [&](const __half *k_base, uint32_t head0, uint32_t nheads) {
+        StackTreeArgs t{};
+        t.k_base = k_base; t.head_stride = g.kv_shard_bytes; t.cap = m.kv_context; t.ctx = st->ctx;
+        t.head0 = head0; t.nheads = nheads; t.n_q = m.n_q_heads; t.n_kv = m.n_kv_heads;
+        t.qkv = qkv; t.qkv_w = g.qkv_w; t.out = reinterpret_cast<__half *>(WS + p.ws.attn); t.part = reinterpret_cast<float *>(WS + p.ws.apart);
+        t.home = st->timing ? nullptr : reinterpret_cast<const uint64_t *>(WS + p.ws.kvhome) + (size_t)l * m.n_kv_heads;
+        t.splits = stack_tree_splits(m.n_q_heads, m.n_kv_heads, st->ctx, st->tree.n, p.ws.kvhome - p.ws.apart);
+        return t;
+    };
     // The routing tables are on their way in front of everything but the first layer's RMS factors and QKV, whose launches take them
     // along: that of the factors whatever there is, that of a QKV in planes (whose factors have no launch) what it has threads for
     const bool factors_take = op.info.kernel == PS_K_RINV && op.info.shard0 == 0 && g.has_attn;
@@ -468,6 +482,14 @@ int32_t issue_kernel(ps_stack *st, const ps_schedule &sc, const Op &op, const __
         }
         case PS_K_ATTN: {
             const Shard &s = p.shards[op.info.shard0];
+            if (st->rotate && s.expert == 0 && !st->timing)      // in front of the layer's first run of heads
+                PS_LAUNCH(launch_stack_rotation(st->rotation, l, qkv, g.qkv_w, m.n_q_heads, m.n_kv_heads, M, st->ctx,
+                                                st->use_graph ? reinterpret_cast<const uint32_t *>(WS + p.ws.ctx) : nullptr, st->tree, cs));
+            if (st->tree.n) {
+                const StackTreeArgs t = tree_args(reinterpret_cast<const __half *>(wptr(op)), s.expert, op.info.nshards);
+                PS_LAUNCH(launch_stack_tree(t, st->tree, cs));
+                return PS_OK;
+            }
             if (MP > 1) {   // a chunk of tokens: the cached positions of this run of kv heads and the chunk's own rows
                 AttnChunkArgs c{};
                 c.k_base = reinterpret_cast<const __half *>(wptr(op)); c.head_stride = g.kv_shard_bytes;
@@ -495,6 +517,11 @@ int32_t issue_kernel(ps_stack *st, const ps_schedule &sc, const Op &op, const __
             return PS_OK;
         }
         case PS_K_ATTN_COMBINE:
+            if (st->tree.n) {
+                const StackTreeArgs t = tree_args(nullptr, 0, m.n_kv_heads);
+                if (t.splits > 1) PS_LAUNCH(launch_stack_tree_merge(t, st->tree.n, cs));
+                return PS_OK;
+            }
             if (MP > 1) {
                 const uint64_t *home = reinterpret_cast<const uint64_t *>(WS + p.ws.kvhome) + (size_t)l * m.n_kv_heads;
                 uint32_t nsplit, per;
@@ -1299,6 +1326,8 @@ int32_t ps_stack_set_tier(ps_stack *st, uint32_t tier, uint64_t *uploaded_bytes)
     // no forward of the old tier may be in flight while its workspace moves and shards are pinned again
     PS_HIP(hipStreamSynchronize(st->copy));
     PS_HIP(hipStreamSynchronize(st->compute));
+    st->tree = ps::StackTreeNodes{};
+    st->step_rows = 0;
     if (tier == st->active_tier) return PS_OK;
     for (auto &g : st->graphs) (void)hipGraphExecDestroy(g.second.exec);
     st->graphs.clear();
@@ -1521,6 +1550,100 @@ int32_t ps_stack_set_logits_out(ps_stack *st, void *logits_dev, uint32_t first_t
     return PS_OK;
 }
 
+int32_t ps_stack_set_rotation(ps_stack *st, const ps_rotation *r) {
+    if (!st) { ps::set_error("NULL argument"); return PS_E_ARG; }
+    const ps_plan &p = st->plan;
+    if (!p.g.kv) { ps::set_error("this stack has no KV cache (kv_context is 0)"); return PS_E_STATE; }
+    if (r && (r->rot_dim % 16 || r->rot_dim > p.g.m.head_dim || r->pairs > 1 || r->norm > 1)) {
+        ps::set_error("rot_dim must be a multiple of 16 up to %u, pairs and norm 0 or 1 (got %u, %u, %u)", p.g.m.head_dim, r->rot_dim, r->pairs, r->norm);
+        return PS_E_ARG;
+    }
+    if (r && ((r->rot_dim && !r->inv_freq) || (uintptr_t)r->inv_freq % 4 || (uintptr_t)r->q_gain % 2 || (uintptr_t)r->k_gain % 2)) {
+        ps::set_error("inv_freq is NULL, or an array is not aligned to its elements"); return PS_E_ARG;
+    }
+    // captured steps hold the former setting
+    PS_HIP(hipStreamSynchronize(st->compute));
+    for (auto &g : st->graphs) (void)hipGraphExecDestroy(g.second.exec);
+    st->graphs.clear();
+    st->rotate = r && (r->rot_dim || r->norm);
+    st->rotation = ps::StackRotation{};
+    if (r) {
+        st->rotation = ps::StackRotation{r->inv_freq, static_cast<const __half *>(r->norm ? r->q_gain : nullptr),
+                                         static_cast<const __half *>(r->norm ? r->k_gain : nullptr), r->rot_dim, r->pairs, r->norm, p.g.m.rms_eps};
+    }
+    return pick_replay(st);
+}
+
+int32_t ps_stack_set_tree(ps_stack *st, const int32_t *parents, uint32_t n) {
+    if (!st || (n && !parents)) { ps::set_error("NULL argument"); return PS_E_ARG; }
+    const ps_plan &p = st->plan;
+    if (n == 0) { st->tree = ps::StackTreeNodes{}; return PS_OK; }
+    if (!p.g.kv) { ps::set_error("this stack has no KV cache (kv_context is 0)"); return PS_E_STATE; }
+    if (p.M < 2) { ps::set_error("the installed plan takes one token"); return PS_E_STATE; }
+    if (n > p.M || n > PS_TREE_MAX) { ps::set_error("a tree of %u tokens (the plan takes %u, a tree %u)", n, p.M, PS_TREE_MAX); return PS_E_ARG; }
+    ps::StackTreeNodes t;
+    if (!ps::make_tree_nodes(parents, n, &t)) return PS_E_ARG;
+    st->tree = t;
+    return PS_OK;
+}
+
+// ps_stack_verify_tree as a call of ps_verify_tree; its tables (first, parents) lie in front of the operator's workspace
+static int32_t stack_verify_call(const ps_stack *st, const ps_stack_verify_args *v, ps_verify_tree_args *a, uint64_t *tables, uint64_t *bytes) {
+    if (!st || !v) { ps::set_error("NULL argument"); return PS_E_ARG; }
+    const ps_plan &p = st->plan;
+    if (!st->head_rows || !st->logits || !st->step_rows) { ps::set_error("verification needs the logits of a forward (ps_stack_set_logits_out, ps_stack_forward)"); return PS_E_STATE; }
+    const uint32_t n = st->head_rows == 1 ? 1 : st->step_rows;
+    if (n > PS_TREE_MAX) { ps::set_error("trees of up to %u tokens (the forward had %u)", PS_TREE_MAX, n); return PS_E_ARG; }
+    *a = ps_verify_tree_args{};
+    a->type = PS_TYPE_F16; a->n_seq = 1; a->n_tokens = n; a->vocab = p.g.m.vocab; a->max_tree = n; a->max_children = v->max_children;
+    a->target_logits = st->logits; a->draft_logits = v->draft_logits;
+    a->target_row = a->draft_row = p.g.m.vocab;
+    a->path_seq = n;
+    a->token = v->token; a->u_accept = v->u_accept; a->u_sample = v->u_sample; a->temperature = v->temperature;
+    a->path = v->path; a->count = v->count; a->next_token = v->next_token;
+    *tables = ps::align_up((2ull + n) * 4, ps::kAlign);
+    const int32_t rc = ps_verify_tree_workspace(a, bytes);
+    if (rc == PS_OK) *bytes += *tables;
+    return rc;
+}
+
+int32_t ps_stack_verify_workspace(const ps_stack *st, const ps_stack_verify_args *args, uint64_t *bytes) {
+    if (!bytes) { ps::set_error("NULL argument"); return PS_E_ARG; }
+    ps_verify_tree_args a;
+    uint64_t tables;
+    return stack_verify_call(st, args, &a, &tables, bytes);
+}
+
+int32_t ps_stack_verify_tree(ps_stack *st, const ps_stack_verify_args *args, void *workspace, uint64_t workspace_bytes) {
+    ps_verify_tree_args a;
+    uint64_t tables, need;
+    const int32_t rc = stack_verify_call(st, args, &a, &tables, &need);
+    if (rc) return rc;
+    if (!workspace || (uintptr_t)workspace % ps::kAlign || workspace_bytes < need) {
+        ps::set_error("a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need); return PS_E_ARG;
+    }
+    int32_t *first = static_cast<int32_t *>(workspace), *parent = first + 2;
+    PS_HIP(ps::launch_tree_tables(first, parent, a.n_tokens, st->head_rows == 1 ? ps::StackTreeNodes{} : st->tree, st->compute));
+    a.first = first;
+    a.parent = parent;
+    return ps_verify_tree(&a, static_cast<uint8_t *>(workspace) + tables, workspace_bytes - tables, st->compute);
+}
+
+int32_t ps_stack_keep_path(ps_stack *st, const int32_t *path, const int32_t *count) {
+    if (!st || !path || !count) { ps::set_error("NULL argument"); return PS_E_ARG; }
+    const ps_plan &p = st->plan;
+    if (!p.g.kv) { ps::set_error("this stack has no KV cache (kv_context is 0)"); return PS_E_STATE; }
+    if (!st->step_rows) { ps::set_error("a path is kept once after a forward"); return PS_E_STATE; }
+    if ((uintptr_t)path % 4 || (uintptr_t)count % 4) { ps::set_error("path and count must be aligned to 4 bytes"); return PS_E_ARG; }
+    if (st->step_rows > PS_TREE_MAX) { ps::set_error("paths of up to %u entries (the forward had %u rows)", PS_TREE_MAX, st->step_rows); return PS_E_ARG; }
+    PS_HIP(ps::launch_stack_keep(reinterpret_cast<const uint64_t *>(st->ws_base + p.ws.kvhome), p.g.m.n_layers * p.g.m.n_kv_heads, p.g.m.kv_context, st->step_ctx,
+                                 st->step_rows, path, count, st->compute));
+    st->step_rows = 0;
+    // the next step's cache copies read the rows that moved
+    if (st->kv_copied) { PS_HIP(hipEventRecord(st->ev_step, st->compute)); st->step_pending = true; }
+    return PS_OK;
+}
+
 int32_t ps_stack_set_cpu_threads(ps_stack *st, uint32_t threads) {
     if (!st || threads == 0 || threads > 64) { ps::set_error("threads must be 1..64"); return PS_E_ARG; }
     if (!st->plan.cpu_bytes) { ps::set_error("this plan has no CPU shard"); return PS_E_STATE; }
@@ -1624,7 +1747,11 @@ int32_t ps_stack_forward(ps_stack *st, const void *x_in, void *x_out, const floa
     const int32_t rc = forward_checks(st, x_in, x_out);
     if (rc) return rc;
     const ps_plan &p = st->plan;
-    return forward_impl(st, x_in, x_out, router_logits, router_logits_dev, (uint64_t)p.M * p.g.m.n_experts, p.M);
+    const uint32_t n = st->tree.n ? st->tree.n : p.M;
+    st->step_rows = 0;
+    const int32_t rcf = forward_impl(st, x_in, x_out, router_logits, router_logits_dev, (uint64_t)n * p.g.m.n_experts, n);
+    if (rcf == PS_OK) { st->step_rows = n; st->step_ctx = st->ctx; }
+    return rcf;
 }
 
 int32_t ps_stack_forward_noalloc(ps_stack *st, const void *x_in, void *x_out) {
@@ -1657,6 +1784,8 @@ int32_t ps_stack_forward_chunked(ps_stack *st, const void *x_in, void *x_out, ui
     int32_t rc = forward_checks(st, x_in, x_out);
     if (rc) return rc;
     if (n_tokens == 0) { ps::set_error("n_tokens is 0"); return PS_E_ARG; }
+    if (st->tree.n) { ps::set_error("a tree is set: its rows go through ps_stack_forward"); return PS_E_STATE; }
+    st->step_rows = 0;
     const ps_plan &p = st->plan;
     if (last_logits_dev && !p.g.m.vocab) { ps::set_error("this stack has no output head (vocab is 0)"); return PS_E_STATE; }
     if (last_logits_dev && (uintptr_t)last_logits_dev % 16) { ps::set_error("logits buffer must be 16-byte aligned"); return PS_E_ARG; }
