@@ -258,18 +258,27 @@ template <int D> __device__ __forceinline__ uint32_t v_swizzle(uint32_t row) {
     return D == 128 ? ((row & 3u) | (((row >> 3) & 1u) << 2)) << 1 : (((row >> 1) & 1u) | (((row >> 3) & 1u) << 1)) << 1;
 }
 
-constexpr uint32_t kTile = 32;           // positions of a tile
-constexpr uint32_t kMaskWords = PS_TREE_MAX / 32;
-
-struct TreeDeal { uint32_t nt, blocks, nsplit; };
-
-template <int D, int NT> constexpr uint32_t tree_lds() {
-    const uint32_t stages = 4 * kTile * D * 2, meet = 4 * NT * 16 * (D + 4) * 4 + 4 * NT * 16 * 2 * 4;
-    return std::max(stages, meet) + PS_TREE_MAX * kMaskWords * 4 + PS_TREE_MAX * 4 + 16;
+// K rows, read 16 at a time (8 (i / 4) + i % 4): their swizzles are all different (D = 64: two rows share the banks, those eight of a kind are)
+template <int D> __device__ __forceinline__ uint32_t k_swizzle(uint32_t row) {
+    return D == 128 ? (row & 3u) | (((row >> 3) & 3u) << 2) : ((row >> 1) & 1u) | (((row >> 3) & 3u) << 1);
 }
 
-// Tiles of sequence: the cache's, then the tree's own; each split takes `per` of them
-__device__ __forceinline__ uint32_t tiles_per_split(uint32_t tiles, uint32_t nsplit) { return ((tiles + nsplit - 1) / nsplit + 3) & ~3u; }
+constexpr uint32_t kTile = 32;           // positions of a tile
+constexpr uint32_t kStep = 64;           // positions of a step of the kernel for many rows
+constexpr uint32_t kMaskWords = PS_TREE_MAX / 32;
+
+struct TreeDeal { uint32_t nt, blocks, nsplit, unit; };       // nt 0: the kernel for many rows; unit: positions that a split is a multiple of
+
+constexpr uint32_t kTreeTables = PS_TREE_MAX * kMaskWords * 4 + PS_TREE_MAX * 4 + 16;
+template <int D, int NT> constexpr uint32_t tree_lds() {
+    const uint32_t stages = 4 * kTile * D * 2, meet = 4 * NT * 16 * (D + 4) * 4 + 4 * NT * 16 * 2 * 4;
+    return std::max(stages, meet) + kTreeTables;
+}
+template <int D> constexpr uint32_t tree_rows_lds() { return 2 * 2 * kStep * D * 2 + kTreeTables; }
+
+// Units of a sequence's positions: the cache's, then the tree's own; each split takes `per` of them
+__device__ __forceinline__ uint32_t units_of(uint32_t ctx, uint32_t t_n, uint32_t unit) { return (ctx + unit - 1) / unit + (t_n + unit - 1) / unit; }
+__device__ __forceinline__ uint32_t units_per_split(uint32_t units, uint32_t nsplit) { return (units + nsplit - 1) / nsplit; }
 
 // Where a launch's tables are: in device memory (a batch of sequences), or in its arguments (a stack's own forward: one sequence, some
 // of the model's heads, rows appended through a table of addresses)
@@ -295,6 +304,107 @@ __device__ __forceinline__ size_t record_of(const ps_tree_attention_args &a, con
     else return (token * a.n_q_heads + h) * nsplit;
 }
 
+// anc[token][word]: a bit for the token itself and each of its ancestors; every thread of the workgroup calls it.  Every step doubles how far back a
+// token's mask reaches.  Up to 64 tokens one wave does it in registers.
+template <class Where>
+__device__ __forceinline__ void ancestors(const ps_tree_attention_args &a, const Where &where, const SeqRows &sr, uint32_t *anc, int *up) {
+    const uint32_t tid = threadIdx.x, t_n = sr.n;
+    int link = -1;
+    if (tid < t_n) {
+        if constexpr (Where::kStack) link = (int)byte_of(where.up, tid) - 1;
+        else link = parent_of(a.parent[sr.row0 + tid], (int)tid);
+    }
+    if (t_n <= 64) {
+        if (tid < 64) {
+            uint32_t m0 = tid < 32 ? 1u << tid : 0u, m1 = tid < 32 ? 0u : 1u << (tid - 32);
+            while (__any(link >= 0)) {
+                const int from = max(link, 0);
+                const uint32_t u0 = __shfl(m0, from, 64), u1 = __shfl(m1, from, 64);
+                const int next = __shfl(link, from, 64);
+                if (link >= 0) { m0 |= u0; m1 |= u1; link = next; }
+            }
+            if (tid < t_n) { anc[tid * kMaskWords] = m0; anc[tid * kMaskWords + 1] = m1; }
+        }
+        __syncthreads();
+        return;
+    }
+    if (tid < t_n) {
+#pragma unroll
+        for (uint32_t w = 0; w < kMaskWords; ++w) anc[tid * kMaskWords + w] = tid / 32 == w ? 1u << (tid % 32) : 0u;
+        up[tid] = link;
+    }
+    uint32_t m[kMaskWords];
+    while (__syncthreads_or(link >= 0)) {
+        int next = -1;
+        if (link >= 0) {
+#pragma unroll
+            for (uint32_t w = 0; w < kMaskWords; ++w) m[w] = anc[link * kMaskWords + w];
+            next = up[link];
+        }
+        __syncthreads();
+        if (link >= 0) {
+#pragma unroll
+            for (uint32_t w = 0; w < kMaskWords; ++w) anc[tid * kMaskWords + w] |= m[w];
+            up[tid] = next;
+        }
+        link = next;
+    }
+}
+
+// rows context and up, which nobody reads: each block moves the tokens whose first row it holds
+template <typename T, int D, class Where>
+__device__ __forceinline__ void append_rows(const ps_tree_attention_args &a, const Where &where, uint32_t s, uint32_t hk, uint32_t ctx, uint32_t t0, uint32_t t1, const T *kn, const T *vn) {
+    constexpr uint32_t kRowPieces = D / 8;
+    T *kd = static_cast<T *>(a.k_cache) + s * a.k_seq + hk * a.k_head, *vd = static_cast<T *>(a.v_cache) + s * a.v_seq + hk * a.v_head;
+    if constexpr (Where::kStack) {
+        kd = reinterpret_cast<T *>(where.home[hk]);
+        vd = kd + (size_t)where.cap * D;
+    }
+    for (uint32_t u = threadIdx.x; u < (t1 - t0) * kRowPieces * 2; u += 256) {
+        const uint32_t t = t0 + u / (2 * kRowPieces), e = u % kRowPieces * 8;
+        const bool v = u / kRowPieces & 1;
+        *reinterpret_cast<u4_t *>(v ? vd + ((size_t)ctx + t) * a.v_row + e : kd + ((size_t)ctx + t) * a.k_row + e) =
+            *reinterpret_cast<const u4_t *>(v ? vn + (size_t)t * a.v_new_token + e : kn + (size_t)t * a.k_new_token + e);
+    }
+}
+
+// An infinite value or one that is no number must not meet the zero weight of a row that does not see it: the product takes
+// zero in its place (and rows that do see it get it at the end); whether there was one
+template <typename T>
+__device__ __forceinline__ bool made_finite(u4_t &v) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t d = v[e];
+        const bool l16 = (d & Mfma<T>::kInf & 0xFFFFu) == (Mfma<T>::kInf & 0xFFFFu), h16 = (d & Mfma<T>::kInf & 0xFFFF0000u) == (Mfma<T>::kInf & 0xFFFF0000u);
+        odd |= l16 || h16;
+        v[e] = (l16 ? 0u : d & 0xFFFFu) | (h16 ? 0u : d & 0xFFFF0000u);
+    }
+    return odd;
+}
+
+// Scores of a tile (S, hidden positions -inf) to weights P relative to the running maximum, which a row raises only where its
+// weights would pass 2^8: each row by its own scores alone, so its result does not depend on its neighbours
+template <typename T, int NT, int DT>
+__device__ __forceinline__ void weigh(const f4_t (&S)[NT][2], float (&m_run)[NT], f4_t (&L)[NT], f4_t (&O)[NT][DT], typename Mfma<T>::v8 (&P)[NT], float c2, float slack) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        float mx = fmaxf(fmaxf(fmaxf(S[t][0][0], S[t][0][1]), fmaxf(S[t][0][2], S[t][0][3])), fmaxf(fmaxf(S[t][1][0], S[t][1][1]), fmaxf(S[t][1][2], S[t][1][3])));
+        if (__any(mx > m_run[t] + slack)) {
+            mx = row_max(mx);
+            mx = mx > m_run[t] + slack ? mx : m_run[t];
+            const float resc = m_run[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[t] - mx) * c2);
+            m_run[t] = mx;
+            L[t] = L[t] * resc;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) O[t][dt] = O[t][dt] * resc;
+        }
+        const float ms = m_run[t] == -INFINITY ? 0.f : m_run[t] * c2;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) P[t][e] = (T)__builtin_amdgcn_exp2f(fmaf(S[t][e >> 2][e & 3], c2, -ms));
+    }
+}
+
 template <typename T, int D, int NT, class Where>
 __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attention_args a, Where where, uint32_t blocks, uint32_t nsplit, float *part) {
     using M = Mfma<T>;
@@ -303,7 +413,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     constexpr uint32_t kStage = kTile * D * 2, kRowPieces = D / 8, kVLoads = kStage / 1024;
     extern __shared__ u4_t tree_lds_mem[];
     unsigned char *const lds = reinterpret_cast<unsigned char *>(tree_lds_mem);
-    constexpr uint32_t kTables = tree_lds<D, NT>() - (PS_TREE_MAX * kMaskWords * 4 + PS_TREE_MAX * 4 + 16);
+    constexpr uint32_t kTables = tree_lds<D, NT>() - kTreeTables;
     uint32_t *const anc = reinterpret_cast<uint32_t *>(lds + kTables);           // [token][word]: itself and its ancestors
     int *const up = reinterpret_cast<int *>(anc + PS_TREE_MAX * kMaskWords);
     int *const wild = up + PS_TREE_MAX;                                          // some own value is infinite or no number
@@ -318,7 +428,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     const uint32_t ctx = seq.ctx, t_n = sr.n, G = a.n_q_heads / a.n_kv_heads;
     const uint32_t R = t_n * G, row0 = rb * RB;
     if (row0 >= R) return;
-    const uint32_t nc = (ctx + kTile - 1) / kTile, tiles = nc + (t_n + kTile - 1) / kTile, per = tiles_per_split(tiles, nsplit);
+    const uint32_t nc = (ctx + kTile - 1) / kTile, tiles = units_of(ctx, t_n, kTile), per = units_per_split(tiles, nsplit);
     const uint32_t lo = z * per, hi = min(tiles, lo + per);
     if (lo >= hi) return;               // (the merge knows how many splits a sequence has)
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -357,47 +467,10 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     // own tiles: which tokens each token sees
     const bool own = hi > nc;
     if (own) {
-        int link = -1;
-        uint32_t m[kMaskWords];
         if (tid == 0) *wild = 0;
-        if (tid < t_n) {
-            if constexpr (Where::kStack) link = (int)byte_of(where.up, tid) - 1;
-            else link = parent_of(a.parent[sr.row0 + tid], (int)tid);
-#pragma unroll
-            for (uint32_t w = 0; w < kMaskWords; ++w) anc[tid * kMaskWords + w] = tid / 32 == w ? 1u << (tid % 32) : 0u;
-            up[tid] = link;
-        }
-        // every step doubles how far back a token's mask reaches
-        while (__syncthreads_or(link >= 0)) {
-            int next = -1;
-            if (link >= 0) {
-#pragma unroll
-                for (uint32_t w = 0; w < kMaskWords; ++w) m[w] = anc[link * kMaskWords + w];
-                next = up[link];
-            }
-            __syncthreads();
-            if (link >= 0) {
-#pragma unroll
-                for (uint32_t w = 0; w < kMaskWords; ++w) anc[tid * kMaskWords + w] |= m[w];
-                up[tid] = next;
-            }
-            link = next;
-        }
+        ancestors(a, where, sr, anc, up);
     }
-    if (a.append && z == 0) {            // rows context and up, which nobody reads: each block moves the tokens whose first row it holds
-        const uint32_t t0 = (row0 + G - 1) / G, t1 = min(t_n, (row0 + RB + G - 1) / G);
-        T *kd = static_cast<T *>(a.k_cache) + s * a.k_seq + hk * a.k_head, *vd = static_cast<T *>(a.v_cache) + s * a.v_seq + hk * a.v_head;
-        if constexpr (Where::kStack) {
-            kd = reinterpret_cast<T *>(where.home[hk]);
-            vd = kd + (size_t)where.cap * D;
-        }
-        for (uint32_t u = tid; u < (t1 - t0) * kRowPieces * 2; u += 256) {
-            const uint32_t t = t0 + u / (2 * kRowPieces), e = u % kRowPieces * 8;
-            const bool v = u / kRowPieces & 1;
-            *reinterpret_cast<u4_t *>(v ? vd + ((size_t)ctx + t) * a.v_row + e : kd + ((size_t)ctx + t) * a.k_row + e) =
-                *reinterpret_cast<const u4_t *>(v ? vn + (size_t)t * a.v_new_token + e : kn + (size_t)t * a.k_new_token + e);
-        }
-    }
+    if (a.append && z == 0) append_rows<T, D>(a, where, s, hk, ctx, (row0 + G - 1) / G, min(t_n, (row0 + RB + G - 1) / G), kn, vn);
 
     // the block's rows of queries; a negative scale turns their signs
     const float scale_abs = fabsf(a.scale);
@@ -449,20 +522,9 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
 #pragma unroll
                 for (int t = 0; t < NT; ++t) S[t][Tt] = M::mul(__builtin_bit_cast(v8, kreg[Tt][kk]), q[t][kk], S[t][Tt]);
         if (mine) {
-            // An infinite value or one that is no number must not meet the zero weight of a row that does not see it: the
-            // product takes zero in its place, and rows that do see it get it at the end.
             bool odd = false;
 #pragma unroll
-            for (uint32_t u = 0; u < kVLoads; ++u) {
-                uint32_t d[4] = {vreg[u].x, vreg[u].y, vreg[u].z, vreg[u].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool l16 = (d[e] & M::kInf & 0xFFFFu) == (M::kInf & 0xFFFFu), h16 = (d[e] & M::kInf & 0xFFFF0000u) == (M::kInf & 0xFFFF0000u);
-                    odd |= l16 || h16;
-                    d[e] = (l16 ? 0u : d[e] & 0xFFFFu) | (h16 ? 0u : d[e] & 0xFFFF0000u);
-                }
-                vreg[u] = u4_t{d[0], d[1], d[2], d[3]};
-            }
+            for (uint32_t u = 0; u < kVLoads; ++u) odd |= made_finite<T>(vreg[u]);
             if (odd) *wild = 1;
         }
 #pragma unroll
@@ -483,22 +545,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
                 for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = P0 + 8 * c + e < ctx ? S[t][e >> 2][e & 3] : -INFINITY;
         }
         v8 P[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float mx = fmaxf(fmaxf(fmaxf(S[t][0][0], S[t][0][1]), fmaxf(S[t][0][2], S[t][0][3])), fmaxf(fmaxf(S[t][1][0], S[t][1][1]), fmaxf(S[t][1][2], S[t][1][3])));
-            if (__any(mx > m_run[t] + slack)) {
-                mx = row_max(mx);
-                mx = mx > m_run[t] + slack ? mx : m_run[t];
-                const float resc = m_run[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[t] - mx) * c2);
-                m_run[t] = mx;
-                L[t] = L[t] * resc;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) O[t][dt] = O[t][dt] * resc;
-            }
-            const float ms = m_run[t] == -INFINITY ? 0.f : m_run[t] * c2;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) P[t][e] = (T)__builtin_amdgcn_exp2f(fmaf(S[t][e >> 2][e & 3], c2, -ms));
-        }
+        weigh<T>(S, m_run, L, O, P, c2, slack);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
             const v8 vr = __builtin_bit_cast(v8, transposed(stage + vread[dt], 4 * D * 2));
@@ -564,17 +611,225 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     }
 }
 
+// The kernel for more than 64 rows of a kv head: a workgroup of four waves with 32 rows each walks its positions in steps of 64, whose
+// K and V rows all four read from LDS: a quarter of the memory traffic, which at 512 rows bounds the kernel above (16 KB a wave and tile from the L2:
+// 64 tokens over 131072 positions, 8 query heads a kv head: 316 us so, 186 here = 740 TFLOP/s).  Products as above, K's operands from LDS as well.  Two stages, one barrier
+// a step; a step's rows are requested two steps ahead, into registers, and written one ahead.
+template <typename T, int D, class Where>
+__global__ __launch_bounds__(256, 2) void tree_rows_kernel(ps_tree_attention_args a, Where where, uint32_t blocks, uint32_t nsplit, float *part) {
+    using M = Mfma<T>;
+    using v8 = typename M::v8;
+    constexpr int KK = D / 32, DT = D / 16, NT = 2, RB = 4 * NT * 16, OP = D + 4;
+    constexpr uint32_t kHalf = kStep * D * 2, kRowPieces = D / 8, kLoads = kStep * kRowPieces / 256;     // a step's K (or V) rows; pieces a thread moves of them
+    extern __shared__ u4_t tree_lds_mem[];
+    unsigned char *const lds = reinterpret_cast<unsigned char *>(tree_lds_mem);
+    uint32_t *const anc = reinterpret_cast<uint32_t *>(lds + 4 * kHalf);
+    int *const up = reinterpret_cast<int *>(anc + PS_TREE_MAX * kMaskWords);
+    int *const wild = up + PS_TREE_MAX;
+
+    const uint32_t units = a.n_seq * a.n_kv_heads * nsplit;
+    const uint32_t unit = blockIdx.x / 8 / blocks * 8 + blockIdx.x % 8, rb = blockIdx.x / 8 % blocks;
+    if (unit >= units) return;
+    const uint32_t z = unit % nsplit, hk = unit / nsplit % a.n_kv_heads, s = unit / nsplit / a.n_kv_heads;
+    const TreeSeq seq = sequence_of(a, where, s);
+    const SeqRows sr = seq.rows;
+    const uint32_t ctx = seq.ctx, t_n = sr.n, G = a.n_q_heads / a.n_kv_heads;
+    const uint32_t R = t_n * G, row0 = rb * RB;
+    if (row0 >= R) return;
+    const uint32_t nc = (ctx + kStep - 1) / kStep, steps = units_of(ctx, t_n, kStep), per = units_per_split(steps, nsplit);
+    const uint32_t lo = z * per, hi = min(steps, lo + per);
+    if (lo >= hi) return;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t i = lane & 15, c = lane >> 4;
+    const char *kc = reinterpret_cast<const char *>(static_cast<const T *>(a.k_cache) + s * a.k_seq + hk * a.k_head);
+    const char *vc = reinterpret_cast<const char *>(static_cast<const T *>(a.v_cache) + s * a.v_seq + hk * a.v_head);
+    const T *kn = static_cast<const T *>(a.k_new) + (size_t)sr.row0 * a.k_new_token + hk * a.k_new_head;
+    const T *vn = static_cast<const T *>(a.v_new) + (size_t)sr.row0 * a.v_new_token + hk * a.v_new_head;
+
+    u4_t kreg[kLoads], vreg[kLoads];
+    auto request = [&](uint32_t step) {
+        const bool mine = step >= nc;
+        const uint32_t P0 = (mine ? step - nc : step) * kStep, last = min(kStep, (mine ? t_n : ctx) - P0) - 1;
+        const uint32_t krow_b = (uint32_t)(mine ? a.k_new_token : a.k_row) * 2, vrow_b = (uint32_t)(mine ? a.v_new_token : a.v_row) * 2;
+        // (rows past the last lie past the buffer's range: zeros)
+        const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((mine ? reinterpret_cast<const char *>(kn) : kc) + (size_t)P0 * krow_b), 0,
+                                                                            (int)(last * krow_b + D * 2), 0x00020000);
+        const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((mine ? reinterpret_cast<const char *>(vn) : vc) + (size_t)P0 * vrow_b), 0,
+                                                                            (int)(last * vrow_b + D * 2), 0x00020000);
+#pragma unroll
+        for (uint32_t u = 0; u < kLoads; ++u) {
+            const uint32_t row = (u * 256 + tid) / kRowPieces, slot = tid % kRowPieces;
+            kreg[u] = __builtin_bit_cast(u4_t, __builtin_amdgcn_raw_buffer_load_b128(kb, row * krow_b + (slot ^ k_swizzle<D>(row)) * 16, 0, 0));
+            vreg[u] = __builtin_bit_cast(u4_t, __builtin_amdgcn_raw_buffer_load_b128(vb, row * vrow_b + (slot ^ v_swizzle<D>(row)) * 16, 0, 0));
+        }
+    };
+    auto store = [&](uint32_t step, uint32_t buf) {
+        if (step >= nc) {
+            bool odd = false;
+#pragma unroll
+            for (uint32_t u = 0; u < kLoads; ++u) odd |= made_finite<T>(vreg[u]);
+            if (odd) *wild = 1;
+        }
+        unsigned char *to = lds + buf * 2 * kHalf;
+#pragma unroll
+        for (uint32_t u = 0; u < kLoads; ++u) {
+            *reinterpret_cast<u4_t *>(to + (u * 256 + tid) * 16) = kreg[u];
+            *reinterpret_cast<u4_t *>(to + kHalf + (u * 256 + tid) * 16) = vreg[u];
+        }
+    };
+    request(lo);
+    const bool own = hi > nc;
+    if (own) {
+        if (tid == 0) *wild = 0;
+        ancestors(a, where, sr, anc, up);
+    }
+    if (a.append && z == 0) append_rows<T, D>(a, where, s, hk, ctx, (row0 + G - 1) / G, min(t_n, (row0 + RB + G - 1) / G), kn, vn);
+
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+    const float c2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
+    const float slack = 8.f / c2;
+    const uint32_t mine0 = row0 + wave * (NT * 16);      // the wave's rows
+    const bool rows = mine0 < R;
+    uint32_t tok[NT], head[NT];
+    v8 q[NT][KK];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const uint32_t rho = min(mine0 + t * 16 + i, R - 1);
+        tok[t] = rho / G;
+        head[t] = hk * G + rho % G;
+        const T *qr = static_cast<const T *>(a.q) + ((size_t)sr.row0 + tok[t]) * a.q_token + (size_t)head[t] * a.q_head + c * 8;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) q[t][kk] = __builtin_bit_cast(v8, *reinterpret_cast<const u4_t *>(qr + kk * 32) ^ u4_t{sign, sign, sign, sign});
+    }
+    float m_run[NT];
+    f4_t O[NT][DT], L[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m_run[t] = -INFINITY;
+        L[t] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) O[t][dt] = f4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    v8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (T)1.f;
+    // LDS byte offsets of this lane's operand pieces in a stage's first tile (a tile further: 32 rows, whose swizzles are the same)
+    uint32_t kread[KK], vread[DT];
+    {
+        const uint32_t row = 8 * (i >> 2) + (i & 3);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kread[kk] = row * (D * 2) + (((4 * kk + c) ^ k_swizzle<D>(row)) << 4);
+        const uint32_t vrow = 8 * c + (i >> 2);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vread[dt] = kHalf + vrow * (D * 2) + (((2 * dt + ((i & 3) >> 1)) ^ v_swizzle<D>(vrow)) << 4) + (i & 1) * 8;
+    }
+    auto meet = [] {      // everyone's LDS accesses are done (loads from memory stay on their way)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    store(lo, 0);
+    if (lo + 1 < hi) request(lo + 1);
+    meet();
+    for (uint32_t step = lo; step < hi; ++step) {
+        const bool mine = step >= nc;
+        const uint32_t P0 = (mine ? step - nc : step) * kStep, left = (mine ? t_n : ctx) - P0;
+        const unsigned char *st = lds + ((step - lo) & 1) * 2 * kHalf;
+        if (rows) {
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+                if (left <= h * kTile) break;            // (uniform)
+                const unsigned char *tile = st + h * kTile * D * 2;
+                f4_t S[NT][2];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int Tt = 0; Tt < 2; ++Tt)
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk) {
+                        // (rows 4 further have the same swizzle)
+                        const v8 kr = __builtin_bit_cast(v8, *reinterpret_cast<const u4_t *>(tile + kread[kk] + Tt * 4 * D * 2));
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) S[t][Tt] = M::mul(kr, q[t][kk], S[t][Tt]);
+                    }
+                if (mine) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint32_t word = anc[tok[t] * kMaskWords + P0 / 32 + h] >> (8 * c);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = word >> e & 1 ? S[t][e >> 2][e & 3] : -INFINITY;
+                    }
+                } else if (left - h * kTile < kTile) {
+                    asm volatile("");
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = h * kTile + 8 * c + e < left ? S[t][e >> 2][e & 3] : -INFINITY;
+                }
+                v8 P[NT];
+                weigh<T>(S, m_run, L, O, P, c2, slack);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    const v8 vr = __builtin_bit_cast(v8, transposed(tile + vread[dt], 4 * D * 2));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) O[t][dt] = M::mul(vr, P[t], O[t][dt]);
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) L[t] = M::mul(ones, P[t], L[t]);
+            }
+        }
+        if (step + 1 < hi) {
+            store(step + 1, (step + 1 - lo) & 1);
+            if (step + 2 < hi) request(step + 2);
+        }
+        meet();
+    }
+    if (!rows) return;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (mine0 + t * 16 + i >= R) continue;
+        const size_t token = (size_t)sr.row0 + tok[t];
+        if (own && *wild) {
+            for (uint32_t j = (max(lo, nc) - nc) * kStep; j < min(t_n, (hi - nc) * kStep); ++j) {
+                if (!(anc[tok[t] * kMaskWords + j / 32] >> (j % 32) & 1)) continue;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = to_f(vn[(size_t)j * a.v_new_token + 16 * dt + 4 * c + e]);
+                        if (!(fabsf(v) < INFINITY)) O[t][dt][e] += v;
+                    }
+            }
+        }
+        if (nsplit > 1) {
+            float *dst = part + (record_of(a, where, token, head[t], nsplit) + z) * OP;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4_t *>(dst + 16 * dt + 4 * c) = O[t][dt];
+            if (c == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(m_run[t] * c2, L[t][0]);
+        } else {
+            T *dst = static_cast<T *>(a.out) + token * a.out_token + (size_t)head[t] * a.out_head + 4 * c;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                T r[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = (T)(O[t][dt][e] / L[t][0]);
+                *reinterpret_cast<u2_t *>(dst + 16 * dt) = *reinterpret_cast<const u2_t *>(r);
+            }
+        }
+    }
+}
+
 // A wave per (token, query head) merges the records of its sequence's splits, in their order: value sums, then maximum (in
 // powers of two) and weight sum.
 template <typename T, int D, class S>
-__global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args a, S where, uint32_t nsplit, const float *part) {
+__global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args a, S where, uint32_t nsplit, uint32_t unit, const float *part) {
     constexpr int E = D / 64, OP = D + 4;
     const uint32_t lane = threadIdx.x & 63, h = blockIdx.x * 4 + (threadIdx.x >> 6), t = blockIdx.y, s = blockIdx.z;
     const TreeSeq seq = sequence_of(a, where, s);
     const SeqRows sr = seq.rows;
     if (h >= a.n_q_heads || (int)t >= sr.n) return;
     const uint32_t ctx = seq.ctx;
-    const uint32_t tiles = (ctx + kTile - 1) / kTile + (sr.n + kTile - 1) / kTile, per = tiles_per_split(tiles, nsplit), n = (tiles + per - 1) / per;
+    const uint32_t units = units_of(ctx, sr.n, unit), per = units_per_split(units, nsplit), n = (units + per - 1) / per;
     const size_t token = (size_t)sr.row0 + t;
     const float *p = part + record_of(a, where, token, h, nsplit) * OP;
     float mx = -INFINITY, l = 0.f, o[E] = {};
@@ -608,49 +863,54 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args 
     for (int e = 0; e < E; ++e) static_cast<T *>(a.out)[token * a.out_token + h * a.out_head + lane * E + e] = (T)(o[e] / l);
 }
 
-// How the work is dealt out: rows in blocks of 16 or 32 (64 rows a wave take more than 256 registers, and the compiler then
-// moves the value sums between its two kinds of them in every tile); positions in as many splits as bring the launch to the
-// workgroups the chip holds at once (two per CU, by registers), none of less than 8 tiles
+// How the work is dealt out.  Rows of a kv head: up to 16 or 32 in one block of the first kernel, up to 64 in two of them, more in
+// blocks of 128 of the second (the first one with 64 rows a wave takes more than 256 registers, and the compiler then moves the value
+// sums between its two kinds of them in every tile).  Positions: as many splits as bring the launch to the workgroups the chip holds
+// at once (two per CU, by registers), none of less than four units of 32 or two of 64.
 TreeDeal tree_deal(const ps_tree_attention_args &a) {
     TreeDeal d;
     const uint32_t rows = std::max(1u, a.max_tree) * (a.n_q_heads / a.n_kv_heads);
-    d.nt = rows <= 16 ? 1 : 2;
-    d.blocks = (rows + d.nt * 16 - 1) / (d.nt * 16);
+    d.nt = rows <= 16 ? 1 : rows <= 64 ? 2 : 0;
+    d.unit = d.nt ? kTile : kStep;
+    const uint32_t block = d.nt ? d.nt * 16 : 128;
+    d.blocks = (rows + block - 1) / block;
     const uint64_t wgs = std::max<uint64_t>(1, (uint64_t)a.n_seq * a.n_kv_heads * d.blocks);
-    const uint32_t tiles = (a.max_context + kTile - 1) / kTile + (a.max_tree + kTile - 1) / kTile, room = 512;
-    d.nsplit = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(room / wgs, tiles / 8));
+    const uint32_t units = (a.max_context + d.unit - 1) / d.unit + (a.max_tree + d.unit - 1) / d.unit, least = d.nt ? 4 : 2;
+    d.nsplit = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / wgs, units / least));
     return d;
 }
 
-template <typename T, int D, int NT, class S>
-hipError_t launch_tree_k(const ps_tree_attention_args &a, const S &where, const TreeDeal &d, float *part, hipStream_t st) {
-    constexpr uint32_t lds = tree_lds<D, NT>();
-    static std::atomic<uint64_t> done{0};        // devices this kernel's LDS size has been announced on
+// a kernel that takes more LDS than a launch gets by itself: announced once per device
+template <class K, class S>
+hipError_t launch_tree_k(K kernel, uint32_t lds, std::atomic<uint64_t> &done, const ps_tree_attention_args &a, const S &where, const TreeDeal &d, float *part, hipStream_t st) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev >= 64 || !(done.load(std::memory_order_relaxed) >> dev & 1)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_attention_kernel<T, D, NT, S>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
         if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     const uint32_t units = a.n_seq * a.n_kv_heads * d.nsplit;
-    hipLaunchKernelGGL((tree_attention_kernel<T, D, NT, S>), dim3((units + 7) / 8 * 8 * d.blocks), dim3(256), lds, st, a, where, d.blocks, d.nsplit, part);
+    hipLaunchKernelGGL(kernel, dim3((units + 7) / 8 * 8 * d.blocks), dim3(256), lds, st, a, where, d.blocks, d.nsplit, part);
     return hipGetLastError();
 }
 template <typename T, int D, class S>
 hipError_t launch_tree(const ps_tree_attention_args &a, const S &where, const TreeDeal &d, float *part, hipStream_t st) {
-    return d.nt == 1 ? launch_tree_k<T, D, 1>(a, where, d, part, st) : launch_tree_k<T, D, 2>(a, where, d, part, st);
+    static std::atomic<uint64_t> done[3];
+    if (d.nt == 0) return launch_tree_k(&tree_rows_kernel<T, D, S>, tree_rows_lds<D>(), done[0], a, where, d, part, st);
+    if (d.nt == 1) return launch_tree_k(&tree_attention_kernel<T, D, 1, S>, tree_lds<D, 1>(), done[1], a, where, d, part, st);
+    return launch_tree_k(&tree_attention_kernel<T, D, 2, S>, tree_lds<D, 2>(), done[2], a, where, d, part, st);
 }
 template <typename T, int D, class S>
-hipError_t launch_merge(const ps_tree_attention_args &a, const S &where, uint32_t nsplit, const float *part, hipStream_t st) {
-    hipLaunchKernelGGL((tree_merge_kernel<T, D, S>), dim3((a.n_q_heads + 3) / 4, a.max_tree, a.n_seq), dim3(256), 0, st, a, where, nsplit, part);
+hipError_t launch_merge(const ps_tree_attention_args &a, const S &where, const TreeDeal &d, const float *part, hipStream_t st) {
+    hipLaunchKernelGGL((tree_merge_kernel<T, D, S>), dim3((a.n_q_heads + 3) / 4, a.max_tree, a.n_seq), dim3(256), 0, st, a, where, d.nsplit, d.unit, part);
     return hipGetLastError();
 }
 template <typename T, int D>
 hipError_t launch_trees(const ps_tree_attention_args &a, const TreeDeal &d, float *part, hipStream_t st) {
     const hipError_t e = launch_tree<T, D>(a, BatchTrees{}, d, part, st);
-    return e != hipSuccess || d.nsplit == 1 ? e : launch_merge<T, D>(a, BatchTrees{}, d.nsplit, part, st);
+    return e != hipSuccess || d.nsplit == 1 ? e : launch_merge<T, D>(a, BatchTrees{}, d, part, st);
 }
 
 // ------------------------------------------------------------------------------------ verification
@@ -1437,7 +1697,7 @@ hipError_t launch_stack_tree(const StackTreeArgs &s, const StackTreeNodes &tree,
     return launch_tree<f16_t, 128>(a, where, stack_deal(s, tree.n), s.part, st);
 }
 hipError_t launch_stack_tree_merge(const StackTreeArgs &s, uint32_t n_tokens, hipStream_t st) {
-    return launch_merge<f16_t, 128>(stack_tree_call(s, n_tokens, s.n_kv), StackTree{nullptr, s.cap, s.n_q, 0, {}}, s.splits, s.part, st);
+    return launch_merge<f16_t, 128>(stack_tree_call(s, n_tokens, s.n_kv), StackTree{nullptr, s.cap, s.n_q, 0, {}}, stack_deal(s, n_tokens), s.part, st);
 }
 hipError_t launch_tree_tables(int32_t *first, int32_t *parent, uint32_t n, const StackTreeNodes &tree, hipStream_t st) {
     if (n > PS_TREE_MAX) return hipErrorInvalidValue;
