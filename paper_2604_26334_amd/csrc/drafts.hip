@@ -464,14 +464,6 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     };
     if (lo + wave < hi) request(lo + wave);
 
-    // own tiles: which tokens each token sees
-    const bool own = hi > nc;
-    if (own) {
-        if (tid == 0) *wild = 0;
-        ancestors(a, where, sr, anc, up);
-    }
-    if (a.append && z == 0) append_rows<T, D>(a, where, s, hk, ctx, (row0 + G - 1) / G, min(t_n, (row0 + RB + G - 1) / G), kn, vn);
-
     // the block's rows of queries; a negative scale turns their signs
     const float scale_abs = fabsf(a.scale);
     const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
@@ -491,6 +483,14 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
             q[t][kk] = __builtin_bit_cast(v8, v);
         }
     }
+    // own tiles: which tokens each token sees
+    const bool own = hi > nc;
+    if (own) {
+        if (tid == 0) *wild = 0;
+        ancestors(a, where, sr, anc, up);
+    }
+    if (a.append && z == 0) append_rows<T, D>(a, where, s, hk, ctx, (row0 + G - 1) / G, min(t_n, (row0 + RB + G - 1) / G), kn, vn);
+
     float m_run[NT];
     f4_t O[NT][DT], L[NT];
 #pragma unroll
@@ -611,7 +611,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     }
 }
 
-// The kernel for more than 64 rows of a kv head: a workgroup of four waves with 32 rows each walks its positions in steps of 64, whose
+// The kernel for more than 32 rows of a kv head: a workgroup of four waves with 32 rows each walks its positions in steps of 64, whose
 // K and V rows all four read from LDS: a quarter of the memory traffic, which at 512 rows bounds the kernel above (16 KB a wave and tile from the L2:
 // 64 tokens over 131072 positions, 8 query heads a kv head: 316 us so, 186 here = 740 TFLOP/s).  Products as above, K's operands from LDS as well.  Two stages, one barrier
 // a step; a step's rows are requested two steps ahead, into registers, and written one ahead.
@@ -678,13 +678,6 @@ __global__ __launch_bounds__(256, 2) void tree_rows_kernel(ps_tree_attention_arg
         }
     };
     request(lo);
-    const bool own = hi > nc;
-    if (own) {
-        if (tid == 0) *wild = 0;
-        ancestors(a, where, sr, anc, up);
-    }
-    if (a.append && z == 0) append_rows<T, D>(a, where, s, hk, ctx, (row0 + G - 1) / G, min(t_n, (row0 + RB + G - 1) / G), kn, vn);
-
     const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
     const float c2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
     const float slack = 8.f / c2;
@@ -701,6 +694,13 @@ __global__ __launch_bounds__(256, 2) void tree_rows_kernel(ps_tree_attention_arg
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) q[t][kk] = __builtin_bit_cast(v8, *reinterpret_cast<const u4_t *>(qr + kk * 32) ^ u4_t{sign, sign, sign, sign});
     }
+    const bool own = hi > nc;
+    if (own) {
+        if (tid == 0) *wild = 0;
+        ancestors(a, where, sr, anc, up);
+    }
+    if (a.append && z == 0) append_rows<T, D>(a, where, s, hk, ctx, (row0 + G - 1) / G, min(t_n, (row0 + RB + G - 1) / G), kn, vn);
+
     float m_run[NT];
     f4_t O[NT][DT], L[NT];
 #pragma unroll
@@ -863,20 +863,21 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args 
     for (int e = 0; e < E; ++e) static_cast<T *>(a.out)[token * a.out_token + h * a.out_head + lane * E + e] = (T)(o[e] / l);
 }
 
-// How the work is dealt out.  Rows of a kv head: up to 16 or 32 in one block of the first kernel, up to 64 in two of them, more in
-// blocks of 128 of the second (the first one with 64 rows a wave takes more than 256 registers, and the compiler then moves the value
+// How the work is dealt out.  Rows of a kv head: up to 16 or 32 in one block of the first kernel, more in blocks of 128 of the second (48
+// rows, 8 sequences of 8190: 72 us in two blocks of the first, 62 so; with 64 rows a wave the first takes more than 256 registers, and the compiler then moves the value
 // sums between its two kinds of them in every tile).  Positions: as many splits as bring the launch to the workgroups the chip holds
-// at once (two per CU, by registers), none of less than four units of 32 or two of 64.
+// at once (two per CU, by registers), none of less than four units of 32 or two of 64; for several sequences, whose lengths differ, twice as many
+// (16 sequences of 17 tokens, lengths of 600 to 8190, 57 -> 48 us, 32 of 8 tokens 87 -> 82; eight of one length 62 -> 70).
 TreeDeal tree_deal(const ps_tree_attention_args &a) {
     TreeDeal d;
     const uint32_t rows = std::max(1u, a.max_tree) * (a.n_q_heads / a.n_kv_heads);
-    d.nt = rows <= 16 ? 1 : rows <= 64 ? 2 : 0;
+    d.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
     d.unit = d.nt ? kTile : kStep;
     const uint32_t block = d.nt ? d.nt * 16 : 128;
     d.blocks = (rows + block - 1) / block;
     const uint64_t wgs = std::max<uint64_t>(1, (uint64_t)a.n_seq * a.n_kv_heads * d.blocks);
     const uint32_t units = (a.max_context + d.unit - 1) / d.unit + (a.max_tree + d.unit - 1) / d.unit, least = d.nt ? 4 : 2;
-    d.nsplit = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / wgs, units / least));
+    d.nsplit = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((a.n_seq > 1 ? 1024 : 512) / wgs, units / least));
     return d;
 }
 
