@@ -55,10 +55,12 @@ __device__ __forceinline__ Turn turn_of(double pos, float freq) {
 // on their way; a lane's sines and cosines, half of the arithmetic, are worked out once for all of these.
 template <typename T> struct Vec8 { T v[8]; };
 struct GivenPositions {
+    static constexpr uint32_t kLds = 0;
     const int32_t *p;
     __device__ __forceinline__ double operator()(uint64_t t) const { return (double)p[t]; }
 };
 struct StackPositions {       // of a forward's tokens: see launch_stack_rotation
+    static constexpr uint32_t kLds = 16;       // keeps a stack's launch off the CUs that a gather copy holds with their whole LDS
     const uint32_t *ctx_dev;
     uint32_t ctx, tree;
     TreeBytes depth;
@@ -185,7 +187,7 @@ hipError_t launch_rope_wide(const ps_qk_norm_rope_args &a, const P &position, hi
     while (L * 16 < a.head_dim) L *= 2;
     // a wave to a token, and below 4096 tokens (four waves a SIMD) its heads shared out as far as that takes
     const uint32_t rounds = ((a.n_q_heads + a.n_k_heads) * L + 63) / 64, splits = (uint32_t)std::min<uint64_t>(rounds, (4095ull + a.n_tokens) / a.n_tokens);
-    hipLaunchKernelGGL((qk_norm_rope_wide_kernel<T, P>), dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * splits + 3) / 4, 1u << 24)), dim3(256), 0, st, a,
+    hipLaunchKernelGGL((qk_norm_rope_wide_kernel<T, P>), dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * splits + 3) / 4, 1u << 24)), dim3(256), P::kLds, st, a,
                        position, L, splits);
     return hipGetLastError();
 }
@@ -905,7 +907,7 @@ hipError_t launch_tree(const ps_tree_attention_args &a, const S &where, const Tr
 }
 template <typename T, int D, class S>
 hipError_t launch_merge(const ps_tree_attention_args &a, const S &where, const TreeDeal &d, const float *part, hipStream_t st) {
-    hipLaunchKernelGGL((tree_merge_kernel<T, D, S>), dim3((a.n_q_heads + 3) / 4, a.max_tree, a.n_seq), dim3(256), 0, st, a, where, d.nsplit, d.unit, part);
+    hipLaunchKernelGGL((tree_merge_kernel<T, D, S>), dim3((a.n_q_heads + 3) / 4, a.max_tree, a.n_seq), dim3(256), S::kStack ? 16 : 0, st, a, where, d.nsplit, d.unit, part);
     return hipGetLastError();
 }
 template <typename T, int D>

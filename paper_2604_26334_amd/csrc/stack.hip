@@ -1577,13 +1577,14 @@ int32_t ps_stack_set_rotation(ps_stack *st, const ps_rotation *r) {
 int32_t ps_stack_set_tree(ps_stack *st, const int32_t *parents, uint32_t n) {
     if (!st || (n && !parents)) { ps::set_error("NULL argument"); return PS_E_ARG; }
     const ps_plan &p = st->plan;
-    if (n == 0) { st->tree = ps::StackTreeNodes{}; return PS_OK; }
+    if (n == 0) { st->tree = ps::StackTreeNodes{}; st->step_rows = 0; return PS_OK; }
     if (!p.g.kv) { ps::set_error("this stack has no KV cache (kv_context is 0)"); return PS_E_STATE; }
     if (p.M < 2) { ps::set_error("the installed plan takes one token"); return PS_E_STATE; }
     if (n > p.M || n > PS_TREE_MAX) { ps::set_error("a tree of %u tokens (the plan takes %u, a tree %u)", n, p.M, PS_TREE_MAX); return PS_E_ARG; }
     ps::StackTreeNodes t;
     if (!ps::make_tree_nodes(parents, n, &t)) return PS_E_ARG;
     st->tree = t;
+    st->step_rows = 0;      // (the rows of the last forward were another tree's)
     return PS_OK;
 }
 
