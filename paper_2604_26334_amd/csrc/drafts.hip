@@ -937,25 +937,36 @@ struct VerifyWork { RowPart *parts; double *left; RowPart *recs; DrawHead *heads
 // no number: -inf (the larger of the two that is one); +inf: the largest finite number
 __device__ __forceinline__ float sane(float v) { return fminf(fmaxf(v, -INFINITY), kFloatMax); }
 
-// 2^t for t below 1000, to 8e-13 of its value: t = n + f, |f| <= 1/2, and the polynomial of degree 8 whose largest relative error on
-// that range is least (its ten extrema found by exchange; the exponential series takes two terms more for this)
-__device__ __forceinline__ double pow2_of(double t) {
-    t = fmax(t, -1100.0);
-    const double n = rint(t), f = t - n;
-    double p = 1.317587152556586e-06;
-    p = fma(p, f, 1.53097370386769e-05);
-    p = fma(p, f, 0.000154038516881703);
-    p = fma(p, f, 0.0013333452064018458);
-    p = fma(p, f, 0.009618128542944679);
-    p = fma(p, f, 0.05550410939339462);
-    p = fma(p, f, 0.24022650698879996);
-    p = fma(p, f, 0.6931471805465148);
-    p = fma(p, f, 0.9999999999997624);
-    return ldexp(p, (int)n);
+// exp((x - m) / T) with k = log2(e) / T, for N values in step (one after the other they are a chain of 17 operations each, which few
+// waves cannot hide): 2^t, t = n + f, |f| <= 1/2, and the polynomial of degree 8 whose largest relative error on that range is least (8e-13;
+// its ten extrema found by exchange; the exponential series takes two terms more for this).  t below 1000; -inf gives 0, where m is
+// finite.  (x k - m k in one operation would lose everything where m is the largest finite number)
+template <int N>
+__device__ __forceinline__ void weights(const float (&x)[N], float m, double k, double (&w)[N]) {
+    constexpr double c[9] = {1.317587152556586e-06, 1.53097370386769e-05, 0.000154038516881703, 0.0013333452064018458, 0.009618128542944679,
+                             0.05550410939339462, 0.24022650698879996, 0.6931471805465148, 0.9999999999997624};
+    double f[N];
+    int n[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const double t = fmax(((double)x[e] - (double)m) * k, -1100.0), r = rint(t);
+        f[e] = t - r;
+        n[e] = (int)r;
+        w[e] = c[0];
+    }
+#pragma unroll
+    for (int j = 1; j < 9; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = fma(w[e], f[e], c[j]);
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] = ldexp(w[e], n[e]);
 }
-// exp((x - m) / T) with k = log2(e) / T; a row of -inf alone has no probabilities.  (x k - m k in one operation would lose everything
-// where m is the largest finite number)
-__device__ __forceinline__ double weight(float x, float m, double k) { return pow2_of(((double)x - (double)m) * k); }
+__device__ __forceinline__ double weight(float x, float m, double k) {
+    const float v[1] = {x};
+    double w[1];
+    weights(v, m, k, w);
+    return w[0];
+}
 __device__ __forceinline__ double rate_of(float temp) { return 1.4426950408889634 / (double)fminf(temp, 1e30f); }
 
 // Eight logits of a row, which may start anywhere, as they lie in memory (past the end -inf), taken out two at a time
@@ -1035,6 +1046,7 @@ __device__ __forceinline__ uint32_t listed(bool have, unsigned char *list, uint3
 // A thread takes eight at a time with the next eight on their way, and keeps a running maximum and sum.
 // The sum is relative to the first maximum a thread meets: 64 bits hold 2^800 times as much beside it, and only a larger value
 // moves it (`slack`: how far a logit may lie above it).
+__device__ __forceinline__ double sum8(const double (&r)[8]) { return ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7])); }
 struct Running { float m; double z; int best; };
 template <typename T>
 __device__ __forceinline__ void take8(Running &r, Oct<T> &o, uint32_t i, double k, float slack, bool greedy) {
@@ -1053,10 +1065,9 @@ __device__ __forceinline__ void take8(Running &r, Oct<T> &o, uint32_t i, double 
     }
     if (greedy) return;
     const float m = fmaxf(r.m, -kFloatMax);           // (-inf alone so far: weights of zero)
-    double z[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e & 3] += weight(v[e], m, k);
-    r.z += (z[0] + z[1]) + (z[2] + z[3]);
+    double w[8];
+    weights(v, m, k, w);
+    r.z += sum8(w);
 }
 template <typename T>
 __device__ __forceinline__ RowPart chunk_part(const T *x, uint32_t lo, uint32_t hi, double k, bool greedy, BlockBuf &b) {
@@ -1219,34 +1230,35 @@ __device__ __forceinline__ void decide(const ps_verify_tree_args &a, const Verif
     __syncthreads();
 }
 
-// Eight entries of what is left to draw from, two at a time: max(p - c q, 0), p without the refused, or p, times ip
+// Eight entries i .. i + 7 of what is left to draw from: max(p - c q, 0), p without the refused, or p, times ip
 template <typename T>
-struct Left8 {
+__device__ __forceinline__ void left8(const ps_verify_tree_args &a, const DrawHead &h, int kind, double rate, uint32_t i, uint32_t hi, const int *refused, int nref,
+                                      double (&r)[8]) {
     Oct<T> p, q;
-    __device__ __forceinline__ void fill(const ps_verify_tree_args &a, const DrawHead &h, int kind, uint32_t i, uint32_t hi) {
-        p.fill(static_cast<const T *>(a.target_logits) + (size_t)h.row * a.target_row, i, hi);
-        if (kind == DRAW_LEFT) q.fill(static_cast<const T *>(a.draft_logits) + (size_t)h.row * a.draft_row, i, hi);
+    p.fill(static_cast<const T *>(a.target_logits) + (size_t)h.row * a.target_row, i, hi);
+    if (kind == DRAW_LEFT) q.fill(static_cast<const T *>(a.draft_logits) + (size_t)h.row * a.draft_row, i, hi);
+    const float m = fmaxf(h.m, -kFloatMax), mq = fmaxf(h.mq, -kFloatMax);       // (rows of -inf alone: weights of zero)
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) p.take(x[e], x[e + 1]);
+    weights(x, m, rate, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] *= h.ip;
+    if (kind == DRAW_LEFT) {
+        double w[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) q.take(x[e], x[e + 1]);
+        weights(x, mq, rate, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = fmax(r[e] - w[e] * h.iq, 0.0);
     }
-    __device__ __forceinline__ void take(const DrawHead &h, int kind, double rate, uint32_t i, const int *refused, int nref, double &u, double &v) {
-        float x, y;
-        p.take(x, y);
-        const float m = fmaxf(h.m, -kFloatMax), mq = fmaxf(h.mq, -kFloatMax);       // (rows of -inf alone: weights of zero)
-        u = weight(x, m, rate) * h.ip;
-        v = weight(y, m, rate) * h.ip;
-        if (kind == DRAW_LEFT) {
-            q.take(x, y);
-            u = fmax(u - weight(x, mq, rate) * h.iq, 0.0);
-            v = fmax(v - weight(y, mq, rate) * h.iq, 0.0);
+    if (kind == DRAW_GIVEN)
+        for (int j = 0; j < nref; ++j) {
+            const uint32_t at = (uint32_t)refused[j] - i;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e) r[e] = at == e ? 0.0 : r[e];
         }
-        if (kind == DRAW_GIVEN)
-#pragma unroll 1
-            for (int j = 0; j < nref; ++j) {
-                u = refused[j] == (int)i ? 0.0 : u;
-                v = refused[j] == (int)i + 1 ? 0.0 : v;
-            }
-    }
-};
-
+}
 template <typename T>
 __global__ __launch_bounds__(kVerThreads) void verify_left_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w, uint32_t k) {
     __shared__ Walk walk;
@@ -1286,14 +1298,9 @@ __global__ __launch_bounds__(kVerThreads) void verify_left_kernel(ps_verify_tree
         double sum = 0;
 #pragma unroll 1
         for (uint32_t i = lo + tid * 8; i < hi; i += kVerThreads * 8) {
-            Left8<T> l;
-            l.fill(a, h, DRAW_LEFT, i, hi);
-#pragma unroll
-            for (uint32_t e = 0; e < 8; e += 2) {
-                double u, v;
-                l.take(h, DRAW_LEFT, rate, i + e, nullptr, 0, u, v);
-                sum += u + v;
-            }
+            double r[8];
+            left8<T>(a, h, DRAW_LEFT, rate, i, hi, nullptr, 0, r);
+            sum += sum8(r);
         }
         sum = block_sum(sum, b.d);
         if (tid == 0) w.left[((size_t)sr.row0 + child) * sh.ndraw + chunk] = sum;
@@ -1301,7 +1308,7 @@ __global__ __launch_bounds__(kVerThreads) void verify_left_kernel(ps_verify_tree
 }
 
 template <typename T>
-__global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
+__global__ __launch_bounds__(kVerThreads) __attribute__((amdgpu_waves_per_eu(1, 4))) void verify_draw_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
     __shared__ Walk walk;
     __shared__ BlockBuf b;
     __shared__ int path[PS_TREE_MAX], refused[PS_TREE_MAX], n, nref, all, last;
@@ -1378,14 +1385,9 @@ __global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree
         double sum = 0;
 #pragma unroll 1
         for (uint32_t i = lo + tid * 8; i < hi; i += kVerThreads * 8) {
-            Left8<T> l;
-            l.fill(a, h, h.kind, i, hi);
-#pragma unroll
-            for (uint32_t e = 0; e < 8; e += 2) {
-                double u, v;
-                l.take(h, h.kind, rate, i + e, refused, nref, u, v);
-                sum += u + v;
-            }
+            double v[8];
+            left8<T>(a, h, h.kind, rate, i, hi, refused, nref, v);
+            sum += sum8(v);
         }
         r.z = block_sum(sum, b.d);
     }
@@ -1393,7 +1395,7 @@ __global__ __launch_bounds__(kVerThreads) void verify_draw_kernel(ps_verify_tree
 }
 
 template <typename T>
-__global__ __launch_bounds__(kVerThreads) void verify_pick_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
+__global__ __launch_bounds__(kVerThreads) __attribute__((amdgpu_waves_per_eu(1, 2))) void verify_pick_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
     __shared__ double runs[4];
     __shared__ int refused[PS_TREE_MAX], pick[2];
     const uint32_t s = blockIdx.x;
@@ -1451,23 +1453,15 @@ __global__ __launch_bounds__(kVerThreads) void verify_pick_kernel(ps_verify_tree
     const uint32_t lo = chunk * chunk_len, hi = min(a.vocab, lo + chunk_len);
     double base = before;
     int last_some = -1;
-    Left8<T> none;
-    none.p.fill(nullptr, 0, 0);
-    none.q.fill(nullptr, 0, 0);
     for (uint32_t i0 = lo; i0 < hi; i0 += kVerThreads * 8) {
         const uint32_t i = i0 + tid * 8;
-        Left8<T> all, l;
-        if (i < hi) all.fill(a, h, kind, i, hi);
-        else all = none;
-        l = all;
-        double sum = 0;
+        double v[8], sum = 0;
         int some = -1;
+        if (i < hi) {
+            left8<T>(a, h, kind, rate, i, hi, refused, nref, v);
+            sum = sum8(v);
 #pragma unroll
-        for (uint32_t e = 0; e < 8; e += 2) {
-            double x, y;
-            l.take(h, kind, rate, i + e, refused, nref, x, y);
-            sum += x + y;
-            some = y > 0 ? (int)(i + e + 1) : x > 0 ? (int)(i + e) : some;
+            for (int e = 0; e < 8; ++e) some = v[e] > 0 ? (int)(i + e) : some;
         }
         double upto = sum;
         for (int o = 1; o < 64; o <<= 1) {
@@ -1489,13 +1483,10 @@ __global__ __launch_bounds__(kVerThreads) void verify_pick_kernel(ps_verify_tree
             if (tid != pick[0]) return;
             int found = -1;
             double r = from;
-#pragma unroll 1
-            for (uint32_t e = 0; e < 8; e += 2) {
-                double x, y;
-                all.take(h, kind, rate, i + e, refused, nref, x, y);
-                if (found < 0 && x > 0 && r + x > goal) found = i + e;
-                if (found < 0 && y > 0 && r + (x + y) > goal) found = i + e + 1;
-                r += x + y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                r += v[e];
+                if (found < 0 && v[e] > 0 && r > goal) found = (int)(i + e);
             }
             a.next_token[s] = found >= 0 ? found : some;
             return;
