@@ -1539,8 +1539,9 @@ hipError_t launch_verify(const ps_verify_tree_args &a, const VerifyShape &sh, co
 
 // ------------------------------------------------------------------------------------ kept rows
 // A wave per plane of a sequence, run of columns by run: kKeep pieces of 16 bytes a lane hold all rows of a run, and are all read before
-// one is written, so rows may move onto rows that others are read from.  Rows that stay where they are are not touched.
-constexpr uint32_t kKeep = 4;
+// one is written, so rows may move onto rows that others are read from.  Rows that stay where they are are not touched.  Bound by the
+// chain count, path, row, store of few waves: so two pieces a lane (46 registers, eight waves a SIMD; 48 sequences of 256 planes 9.5 us), and
+// four (98, four waves; 13.3 us) only for paths that may be longer than 128.
 struct BatchPlanes {
     __device__ __forceinline__ char *operator()(const ps_cache_keep_args &a, uint32_t s, uint32_t plane) const {
         return static_cast<char *>(a.cache) + s * a.seq_stride + plane * a.plane_stride;
@@ -1555,7 +1556,7 @@ struct StackPlanes {       // home[plane / 2]: K rows, then V rows
     }
     __device__ __forceinline__ int64_t context(const ps_cache_keep_args &, uint32_t) const { return ctx; }
 };
-template <class S>
+template <class S, uint32_t kKeep>
 __global__ __launch_bounds__(256) void cache_keep_kernel(ps_cache_keep_args a, S where) {
     const uint32_t lane = threadIdx.x & 63, plane = blockIdx.x * 4 + (threadIdx.x >> 6), s = blockIdx.y;
     if (plane >= a.n_planes) return;
@@ -1585,6 +1586,15 @@ __global__ __launch_bounds__(256) void cache_keep_kernel(ps_cache_keep_args a, S
             if (ok[u]) *reinterpret_cast<u4_t *>(base + (ctx + i) * a.row_stride + col * 16) = v[u];
         }
     }
+}
+
+template <class S>
+hipError_t launch_keep(const ps_cache_keep_args &a, const S &where, hipStream_t st) {
+    const dim3 grid((a.n_planes + 3) / 4, a.n_seq);
+    static_assert(64 * 4 >= PS_TREE_MAX, "a run of one column holds every row of a path");
+    if (a.max_tree <= 128) hipLaunchKernelGGL((cache_keep_kernel<S, 2>), grid, dim3(256), 0, st, a, where);
+    else hipLaunchKernelGGL((cache_keep_kernel<S, 4>), grid, dim3(256), 0, st, a, where);
+    return hipGetLastError();
 }
 
 __global__ __launch_bounds__(PS_TREE_MAX) void tree_tables_kernel(int32_t *first, int32_t *parent, StackTreeNodes tree, uint32_t n) {
@@ -1703,8 +1713,7 @@ hipError_t launch_stack_keep(const uint64_t *home, uint32_t n_homes, uint32_t ca
     ps_cache_keep_args a{};
     a.n_seq = 1; a.n_planes = 2 * n_homes; a.capacity = cap; a.row_bytes = 256; a.max_tree = width; a.row_stride = 256;
     a.path = path; a.count = count;
-    hipLaunchKernelGGL(cache_keep_kernel<StackPlanes>, dim3((a.n_planes + 3) / 4), dim3(256), 0, st, a, StackPlanes{home, ctx});
-    return hipGetLastError();
+    return launch_keep(a, StackPlanes{home, ctx}, st);
 }
 }  // namespace ps
 
@@ -1823,8 +1832,7 @@ int32_t ps_cache_keep(const ps_cache_keep_args *a, void *stream) {
     PS_WANT(aligned(a->cache, 16) && a->seq_stride % 16 == 0 && a->plane_stride % 16 == 0 && a->row_stride % 16 == 0, "the cache and its strides must be multiples of 16 bytes");
     PS_WANT(a->row_stride >= a->row_bytes || a->capacity == 1, "rows of %u bytes lie %llu bytes apart", a->row_bytes, (unsigned long long)a->row_stride);
     PS_WANT(aligned(a->path, 4) && aligned(a->count, 4) && aligned(a->context, 4), "path, count and context must be aligned to 4 bytes");
-    hipLaunchKernelGGL(cache_keep_kernel<BatchPlanes>, dim3((a->n_planes + 3) / 4, a->n_seq), dim3(256), 0, static_cast<hipStream_t>(stream), *a, BatchPlanes{});
-    PS_TRY(hipGetLastError());
+    PS_TRY(launch_keep(*a, BatchPlanes{}, static_cast<hipStream_t>(stream)));
     return PS_OK;
 }
 
