@@ -927,7 +927,7 @@ hipError_t launch_trees(const ps_tree_attention_args &a, const TreeDeal &d, floa
 // Exponentials and sums are in 64 bits: with fp32's 2^-24 a border of the running sum moves by as much as a hundred thousandth of
 // the vocabulary's entries weigh.  A 64-bit multiply-add costs this machine what a 32-bit one does; an exponential here is about
 // 17 of them, which in a large batch takes longer than the row's bytes do.  No result depends on the order of workgroups.
-constexpr uint32_t kVerThreads = 256, kMaxChunks = 32;
+constexpr uint32_t kVerThreads = 256, kPickThreads = 512, kMaxChunks = 32;
 struct RowPart { double z; float m; int best; };                 // one chunk of a row: sum of exp((x - m) k), m about its maximum (greedy: m its maximum, at `best`)
 struct DrawHead { double c, ip, iq; float m, mq; int row, kind, nref, pad; };   // what is left behind the last node, for the pick
 enum { DRAW_NONE = 0, DRAW_BEST = 1, DRAW_LEAF = 2, DRAW_LEFT = 3, DRAW_GIVEN = 4 };
@@ -1395,8 +1395,8 @@ __global__ __launch_bounds__(kVerThreads) __attribute__((amdgpu_waves_per_eu(1, 
 }
 
 template <typename T>
-__global__ __launch_bounds__(kVerThreads) __attribute__((amdgpu_waves_per_eu(1, 2))) void verify_pick_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
-    __shared__ double runs[4];
+__global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(1, 2))) void verify_pick_kernel(ps_verify_tree_args a, VerifyShape sh, VerifyWork w) {
+    __shared__ double runs[kPickThreads / 64];
     __shared__ int refused[PS_TREE_MAX], pick[2];
     const uint32_t s = blockIdx.x;
     const int tid = threadIdx.x, half = tid & 31;
@@ -1411,7 +1411,7 @@ __global__ __launch_bounds__(kVerThreads) __attribute__((amdgpu_waves_per_eu(1, 
     const float temp = a.temperature ? a.temperature[s] : 1.f, u = a.u_sample[s];
     const bool greedy = !(temp > 0.f);
     const double rate = greedy ? 0.0 : rate_of(temp);
-    refused[tid] = tid < h.nref ? mine_refused : -1;
+    if (tid < (int)PS_TREE_MAX) refused[tid] = tid < h.nref ? mine_refused : -1;
     __syncthreads();
     const int nref = h.nref;
     int kind = h.kind;
@@ -1449,11 +1449,11 @@ __global__ __launch_bounds__(kVerThreads) __attribute__((amdgpu_waves_per_eu(1, 
     const int chunk = passes ? __ffs(passes) - 1 : 31 - __clz(some_left);
     const double prior_run = __shfl_up(run, 1, 32);
     const double before = chunk ? __shfl(prior_run, chunk, 32) : 0.0;
-    // in it, threads take vectors of 8 entries in turn, 2048 entries at a time
+    // in it, threads take vectors of 8 entries in turn, 4096 entries at a time
     const uint32_t lo = chunk * chunk_len, hi = min(a.vocab, lo + chunk_len);
     double base = before;
     int last_some = -1;
-    for (uint32_t i0 = lo; i0 < hi; i0 += kVerThreads * 8) {
+    for (uint32_t i0 = lo; i0 < hi; i0 += kPickThreads * 8) {
         const uint32_t i = i0 + tid * 8;
         double v[8], sum = 0;
         int some = -1;
@@ -1492,7 +1492,7 @@ __global__ __launch_bounds__(kVerThreads) __attribute__((amdgpu_waves_per_eu(1, 
             return;
         }
         last_some = max(last_some, pick[1]);
-        base = ((base + runs[0]) + runs[1]) + runs[2] + runs[3];
+        for (uint32_t j = 0; j < kPickThreads / 64; ++j) base += runs[j];
     }
     if (tid == 0) a.next_token[s] = last_some;      // the goal lies within the last sum's rounding
 }
@@ -1533,7 +1533,7 @@ hipError_t launch_verify(const ps_verify_tree_args &a, const VerifyShape &sh, co
                 hipLaunchKernelGGL(verify_left_kernel<T>, dim3(sh.ndraw, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w, k);
     }
     hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(sh.ndraw, a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
-    hipLaunchKernelGGL(verify_pick_kernel<T>, dim3(a.n_seq), dim3(kVerThreads), 0, st, a, sh, w);
+    hipLaunchKernelGGL(verify_pick_kernel<T>, dim3(a.n_seq), dim3(kPickThreads), 0, st, a, sh, w);
     return hipGetLastError();
 }
 
