@@ -37,8 +37,9 @@ __device__ __forceinline__ uint32_t byte_of(const TreeBytes &t, uint32_t i) { re
 template <typename T> __device__ __forceinline__ float to_f(T v) { return (float)v; }
 
 // ------------------------------------------------------------------------------------ norms and rotation
-// Bound by memory: every element is read and written once.  The angle's product and its fraction of a turn are worked out in 64
-// bits, sine and cosine of the fraction in 32.
+// Bound by memory: every element is read and written once (16384 tokens of 32 + 8 heads of 128, 336 MB: 75 us = 4.5 TB/s, where a copy
+// runs at 4.9; one token 4.4 us, a launch's own time).  The angle's product and its fraction of a turn are worked out in 64 bits,
+// sine and cosine of the fraction in 32.
 struct Turn { float c, s; };
 __device__ __forceinline__ Turn turn_of(double pos, float freq) {
     const double turns = pos * (double)freq * 0.15915494309189535;        // 1 / (2 pi)
@@ -209,6 +210,8 @@ hipError_t launch_rope(const ps_qk_norm_rope_args &a, hipStream_t st) {
 //   by LDS transpose reads of the wave's own stage; and the weights' sum by one more product, with ones.
 // The next tile's K and V are requested as soon as the scores have used this one's K and its V lies in LDS.  They go through
 // registers: in front of a transpose read the compiler waits for every load into LDS, the next tile's too.
+// This is the kernel for up to 32 rows of a kv head, bound by the cache's bytes: 24 sequences of 2 tokens over 8192 positions (32 / 8
+// heads) 147 us = 5.5 TB/s, one of 2 over 131072 (32 / 4) 70 us = 3.8, of one over 32768 35 us; few positions take a launch's and a merge's time, about 8 and 4 us.
 typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef f16_t f16x8_t __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x8_t __attribute__((ext_vector_type(8)));
@@ -821,7 +824,7 @@ __global__ __launch_bounds__(256, 2) void tree_rows_kernel(ps_tree_attention_arg
     }
 }
 
-// A wave per (token, query head) merges the records of its sequence's splits, in their order: value sums, then maximum (in
+// The splits' records: 4 to 5 us, a launch and two dependent loads.  A wave per (token, query head) merges the records of its sequence's splits, in their order: value sums, then maximum (in
 // powers of two) and weight sum.
 template <typename T, int D, class S>
 __global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args a, S where, uint32_t nsplit, uint32_t unit, const float *part) {
@@ -925,8 +928,11 @@ hipError_t launch_trees(const ps_tree_attention_args &a, const TreeDeal &d, floa
 //  verify_draw_kernel   every workgroup works out the same walk; chunk sums of what is left to draw from behind its last node
 //  verify_pick_kernel   the chunk that the random number falls into, and the index in it
 // Exponentials and sums are in 64 bits: with fp32's 2^-24 a border of the running sum moves by as much as a hundred thousandth of
-// the vocabulary's entries weigh.  A 64-bit multiply-add costs this machine what a 32-bit one does; an exponential here is about
-// 17 of them, which in a large batch takes longer than the row's bytes do.  No result depends on the order of workgroups.
+// the vocabulary's entries weigh.  A 64-bit multiply-add takes this machine 6.1 clocks of a wave, a 32-bit one 4.3; an exponential
+// here is about 17 of them, which in a large batch takes longer than the row's bytes do.  No result depends on the order of workgroups.
+// 32 trees of up to 32 nodes, two drafts a node, 128256 entries, drafts' logits: 96 + 22 + 19 + 9 us (205 MB: 42 us as bytes, about 75 as
+// operations); 16 trees of given drafts 20 + 12 + 9 us; a chain of 4 drafts over 32000 5 + 9 + 8: chains of latencies (a step's loads, a few hundred
+// clocks for each reduction and exponential), no longer bound by anything that more workgroups would share.
 constexpr uint32_t kVerThreads = 256, kPickThreads = 512, kMaxChunks = 32;
 struct RowPart { double z; float m; int best; };                 // one chunk of a row: sum of exp((x - m) k), m about its maximum (greedy: m its maximum, at `best`)
 struct DrawHead { double c, ip, iq; float m, mq; int row, kind, nref, pad; };   // what is left behind the last node, for the pick
@@ -1127,14 +1133,13 @@ __global__ __launch_bounds__(kVerThreads) void verify_rows_kernel(ps_verify_tree
     __syncthreads();
     const uint32_t count = listed(parent[tid] != 0, list, cnt);
     const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
-    for (uint32_t j = blockIdx.y; j < count; j += gridDim.y) {
-        const size_t row = (size_t)sr.row0 + list[j];
-#pragma unroll 1
-        for (uint32_t which = 0; which < (a.draft_logits && !greedy ? 2u : 1u); ++which) {
-            const T *x = which ? static_cast<const T *>(a.draft_logits) + row * a.draft_row : static_cast<const T *>(a.target_logits) + row * a.target_row;
-            const RowPart p = chunk_part(x, lo, hi, k, greedy, b);
-            if (tid == 0) w.parts[(row * 2 + which) * sh.nchunk + chunk] = p;
-        }
+    const uint32_t both = a.draft_logits && !greedy ? 2 : 1;       // target and draft rows are tasks of their own
+    for (uint32_t j = blockIdx.y; j < count * both; j += gridDim.y) {
+        const size_t row = (size_t)sr.row0 + list[j / both];
+        const bool which = j % both;
+        const T *x = which ? static_cast<const T *>(a.draft_logits) + row * a.draft_row : static_cast<const T *>(a.target_logits) + row * a.target_row;
+        const RowPart p = chunk_part(x, lo, hi, k, greedy, b);
+        if (tid == 0) w.parts[(row * 2 + which) * sh.nchunk + chunk] = p;
     }
 }
 
@@ -1507,10 +1512,10 @@ VerifyShape verify_shape(const ps_verify_tree_args &a) {
         *len = (uint32_t)((std::max<uint64_t>(4096, (a.vocab + chunks - 1) / chunks) + 2047) / 2048 * 2048);
         *n = (a.vocab + *len - 1) / *len;
     };
-    const uint64_t seqs = std::max(1u, a.n_seq), nodes = std::max(1u, a.max_tree / 2);
+    const uint64_t seqs = std::max(1u, a.n_seq), both = a.draft_logits ? 2 : 1, nodes = std::max(1u, a.max_tree / 2) * both;
     cut((2048 + seqs * nodes - 1) / (seqs * nodes), &sh.chunk, &sh.nchunk);
     cut((1024 + seqs - 1) / seqs, &sh.dchunk, &sh.ndraw);
-    sh.loop = (uint32_t)std::min<uint64_t>(std::max(1u, a.max_tree - 1), std::max<uint64_t>(1, 4096 / (sh.nchunk * seqs)));
+    sh.loop = (uint32_t)std::min<uint64_t>(std::max(1u, a.max_tree - 1) * both, std::max<uint64_t>(1, 4096 / (sh.nchunk * seqs)));
     return sh;
 }
 uint64_t verify_work(const ps_verify_tree_args &a, const VerifyShape &sh, uint8_t *base, VerifyWork *w) {
