@@ -12,8 +12,9 @@
  * Around that core: the token-tier table with PickTier, the KV cache as a shard
  * class with decode attention, the output head as the lowest priority class,
  * the two plans that run unpinned low-priority shards on the CPU ("Plan Two",
- * "Plan Three") with HeuristicSplit choosing among the three, and the profile
- * database the time estimates can be drawn from.  Plan One is what every entry
+ * "Plan Three") with HeuristicSplit choosing among the three, the profile
+ * database the time estimates can be drawn from, and the operators of a step
+ * that answers several drafted tokens at once (at the end of this file).  Plan One is what every entry
  * point does unless a plan kind is asked for; nothing falls back to the CPU.
  *
  * Conventions
@@ -711,8 +712,9 @@ int32_t ps_stack_set_rotation(ps_stack *st, const ps_rotation *rotation);
 /* ps_stack_set_tree: the rows of the following ps_stack_forward calls are a tree of n tokens instead of a chunk: parents (host,
  * copied) as ps_tree_attention has them, parents[i] in -1 .. i - 1 (PS_E_ARG otherwise).  n <= the plan's token count and
  * <= PS_TREE_MAX; x_in, x_out are [n][hidden], router logits [n_layers][n][n_experts], logits of every token [n][vocab].
- * n = 0: chunks again; ps_stack_set_tier does the same.  The last forward's rows are verified and kept before the next tree is set.  ps_stack_forward_chunked returns PS_E_STATE meanwhile.  All n rows are appended
- * to the cache, node i at position context + i; ps_stack_keep_path puts the accepted ones in place. */
+ * All n rows are appended to the cache, node i at position context + i; ps_stack_keep_path puts the accepted ones in place.
+ * n = 0: chunks again; ps_stack_set_tier does the same.  ps_stack_forward_chunked returns PS_E_STATE while a tree is set.  The
+ * last forward's rows are verified and kept before the next tree is set (PS_E_STATE afterwards). */
 int32_t ps_stack_set_tree(ps_stack *st, const int32_t *parents, uint32_t n);
 /* ps_stack_verify_tree: ps_verify_tree over the logits of the last forward (ps_stack_set_logits_out with every token; with one
  * token: that token's row alone, i.e. the draw of the next token), the tree that ps_stack_set_tree set or, without one, the

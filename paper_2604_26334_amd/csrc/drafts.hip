@@ -1,6 +1,5 @@
 // Operators of a step that answers several drafted tokens at once: norms of queries and keys with the position rotation,
 // attention of a tree of tokens over a cache, verification of the drafts, and the accepted rows of the cache.
-#include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
