@@ -583,8 +583,8 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float mw = om[w * RB + row];
-            if (mw == -INFINITY && mx != -INFINITY) continue;            // (a wave that saw nothing of this row)
-            const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mw - mx) * c2);
+            // a wave that saw nothing of this row holds zeros and weighs nothing; one whose scores are no numbers holds none, and says so
+            const float f = mw == -INFINITY ? (mx == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f((mw - mx) * c2);
             l = fmaf(f, ol[w * RB + row], l);
             const f4_t v = *reinterpret_cast<const f4_t *>(ob + (w * RB + row) * OP + d0);
 #pragma unroll
@@ -856,8 +856,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args 
         mx = m8;
 #pragma unroll
         for (uint32_t u = 0; u < 8; ++u) {
-            const bool in = z0 + u < n && (mv[u] != -INFINITY || m8 == -INFINITY);     // left out, not weighed with zero: a sum may be infinite
-            const float w = mv[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mv[u] - ms);
+            const bool in = z0 + u < n;          // (a record past the last is the last again)
+            const float w = mv[u] == -INFINITY ? (m8 == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(mv[u] - ms);       // as the waves above
             l = in ? fmaf(w, lv[u], l) : l;
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = in ? fmaf(w, ov[u][e], o[e]) : o[e];

@@ -181,7 +181,7 @@ def _check_attention(a, out, first, parent, trees, ctxs, ty, d, scale):
         ref = D.tree_attention(q, kn, vn, kc, vc, c, parent[r], scale)
         v_max = max(np.abs(vn).max(), np.abs(vc).max() if c else 0)
         k_max = max(np.abs(kn).max(), np.abs(kc).max() if c else 0)
-        size = np.abs(q).sum(-1).max() * k_max * scale * 4
+        size = np.abs(q).sum(-1).max() * k_max * abs(scale) * 4
         tol = _attention_tolerance(ref, v_max, size * (d + 8) / d + 8, ty)
         off = np.abs(_np(out[r]) - ref) / tol
         assert off.max() <= 1, (s, t, c, off.max())
@@ -242,6 +242,28 @@ def test_hidden_tokens_may_hold_anything(ty):
             assert _same_bits(out[[0, 1, 3, 5]], clean[[0, 1, 3, 5]]), (bad, key)
             if not math.isfinite(bad) and not key:
                 assert not bool(torch.isfinite(out[[2, 4]]).any()), bad
+
+
+@pytest.mark.parametrize("t,hq", [(3, 2), (24, 4), (9, 16)])
+def test_keys_that_are_no_numbers_reach_every_row_that_sees_them(t, hq):
+    """A run of cached keys without a number, as long as a whole tile, step or split: no row may come out finite."""
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    for lo, hi in ((0, 32), (32, 64), (64, 192), (0, 700), (640, 700)):
+        a, first, _ = _attention_case("f16", 128, hq, 2, [t], [700], 740, "tree", 3)
+        a["k_cache"][0, 1, lo:hi] = float("nan")
+        out = B.tree_attention(**a, max_context=700, max_tree=t)
+        fine = torch.isfinite(out).all(-1)
+        assert bool(fine[:, :hq // 2].all()) and not bool(fine[:, hq // 2:].any()), (lo, hi)
+
+
+@pytest.mark.parametrize("t,hq", [(3, 2), (24, 4)])
+@pytest.mark.parametrize("scale", [-0.09, 0.0, 1.3])
+def test_tree_attention_with_any_scale(t, hq, scale):
+    from paper_2604_26334_amd import binding as B
+    a, first, parent = _attention_case("bf16", 128, hq, 2, [t, t], [333, 40], 400, "tree", 6)
+    out = B.tree_attention(**a, max_context=333, max_tree=t, scale=scale)
+    _check_attention(a, out, first, parent, [t, t], [333, 40], "bf16", 128, scale)
 
 
 def test_tree_attention_of_padded_batches_and_bounded_values():
