@@ -942,25 +942,28 @@ struct VerifyWork { RowPart *parts; double *left; RowPart *recs; DrawHead *heads
 // no number: -inf (the larger of the two that is one); +inf: the largest finite number
 __device__ __forceinline__ float sane(float v) { return fminf(fmaxf(v, -INFINITY), kFloatMax); }
 
-// exp((x - m) / T) with k = log2(e) / T, for N values in step (one after the other they are a chain of 17 operations each, which few
-// waves cannot hide): 2^t, t = n + f, |f| <= 1/2, and the polynomial of degree 8 whose largest relative error on that range is least (8e-13;
-// its ten extrema found by exchange; the exponential series takes two terms more for this).  t below 1000; -inf gives 0, where m is
-// finite.  (x k - m k in one operation would lose everything where m is the largest finite number)
+// exp((x - m) / T) with k = log2(e) / T, for N values in step (one after the other they are a chain of 15 operations each, which few
+// waves cannot hide): 2^t, t = n + f, |f| <= 1/2, and the polynomial of degree 7 whose largest relative error on that range is least (4e-11
+// where fp32 has 6e-8 beside the same exponent's; its nine extrema found by exchange; degree 8, 8e-13, takes 4 us more of 90).  n is
+// what remains of t beside 1.5 2^52, and then its low word.  t below 1000; -inf gives 0, where m is finite.  (x k - m k in one operation
+// would lose everything where m is the largest finite number)
 template <int N>
 __device__ __forceinline__ void weights(const float (&x)[N], float m, double k, double (&w)[N]) {
-    constexpr double c[9] = {1.317587152556586e-06, 1.53097370386769e-05, 0.000154038516881703, 0.0013333452064018458, 0.009618128542944679,
-                             0.05550410939339462, 0.24022650698879996, 0.6931471805465148, 0.9999999999997624};
+    constexpr double c[8] = {1.520192159459773e-05, 0.00015469291141683518, 0.001333392256353862, 0.00961802725366847, 0.0555041035344798,
+                             0.24022651198157585, 0.693147180728447, 0.9999999999616819};
+    constexpr double kWhole = 6755399441055744.0;
+    const double least = -1100.0 / k;
     double f[N];
     int n[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-        const double t = fmax(((double)x[e] - (double)m) * k, -1100.0), r = rint(t);
-        f[e] = t - r;
-        n[e] = (int)r;
+        const double d = fmax((double)x[e] - (double)m, least), t = fma(d, k, kWhole);
+        f[e] = fma(d, k, kWhole - t);
+        n[e] = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
         w[e] = c[0];
     }
 #pragma unroll
-    for (int j = 1; j < 9; ++j)
+    for (int j = 1; j < 8; ++j)
 #pragma unroll
         for (int e = 0; e < N; ++e) w[e] = fma(w[e], f[e], c[j]);
 #pragma unroll
@@ -1079,14 +1082,23 @@ __device__ __forceinline__ RowPart chunk_part(const T *x, uint32_t lo, uint32_t 
     Running r{-INFINITY, 0.0, 0x7FFFFFFF};
     const float slack = greedy ? 0.f : (float)fmin(800.0 / k, 1e38);
     const uint32_t step = kVerThreads * 8;
-    Oct<T> next;
     uint32_t i = lo + threadIdx.x * 8;
-    if (i < hi) next.fill(x, i, hi);
+    if (i + 8 <= hi) {
+        Oct<T> next;
+        next.fill(x, i);
+        bool more;
 #pragma unroll 1
-    for (; i < hi; i += step) {
-        Oct<T> o = next;
-        if (i + step + 8 <= hi) next.fill(x, i + step);
-        else if (i + step < hi) next.fill(x, i + step, hi);
+        do {
+            Oct<T> o = next;
+            more = i + step + 8 <= hi;
+            next.fill(x, more ? i + step : i);       // (no branch around a load: behind one the next wait is for everything)
+            take8(r, o, i, k, slack, greedy);
+            i += step;
+        } while (more);
+    }
+    if (i < hi) {
+        Oct<T> o;
+        o.fill(x, i, hi);
         take8(r, o, i, k, slack, greedy);
     }
     RowPart p{0.0, block_max(r.m, b.f), 0x7FFFFFFF};
