@@ -816,6 +816,15 @@ def _same(name, t, shape, dtype, device):
             name, dtype, list(shape), device, t.dtype, list(t.shape), t.device))
 
 
+def _like(name, out, t):
+    """The given output, which must be as t, or a new contiguous one."""
+    if out is None:
+        import torch
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    _same(name, out, t.shape, t.dtype, t.device)
+    return out
+
+
 def _rows(name, t):
     """Strides of a tensor whose last dimension lies together (a dimension of one element may have any stride)."""
     st = t.stride()
@@ -837,7 +846,7 @@ def _launch(device, call, *args):
     import torch
     if device.type != "cuda":
         raise PshardError(PS_E_ARG, "tensors on a GPU are taken, not on %s" % device)
-    stream = torch.cuda.current_stream(device).cuda_stream
+    stream = torch._C._cuda_getCurrentRawStream(device.index)      # (torch.cuda.current_stream makes an object of it: 1.9 us of a call's 11)
     if torch.cuda.current_device() == device.index:
         rc = call(*args, stream)
     else:
@@ -869,10 +878,8 @@ def qk_norm_rope(q, k, positions, inv_freq, q_gain=None, k_gain=None, eps=1e-6, 
     hk, dev, dt = k.shape[1], q.device, q.dtype
     ty = _type_of(q)
     _same("k", k, (n, hk, d), dt, dev)
-    q_out = torch.empty((n, hq, d), dtype=dt, device=dev) if q_out is None else q_out
-    k_out = torch.empty((n, hk, d), dtype=dt, device=dev) if k_out is None else k_out
-    _same("q_out", q_out, (n, hq, d), dt, dev)
-    _same("k_out", k_out, (n, hk, d), dt, dev)
+    q_out = _like("q_out", q_out, q)
+    k_out = _like("k_out", k_out, k)
     _want((positions is None) == (inv_freq is None), "positions and inv_freq come together")
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
     sq, sk, so, sp = _rows("q", q), _rows("k", k), _rows("q_out", q_out), _rows("k_out", k_out)
@@ -902,8 +909,7 @@ def tree_attention(q, k_new, v_new, k_cache, v_cache, first, context, parent, ma
     _same("v_new", v_new, (n, hk, d), dt, dev)
     _same("k_cache", k_cache, (b, hk, cap, d), dt, dev)
     _same("v_cache", v_cache, (b, hk, cap, d), dt, dev)
-    out = torch.empty((n, hq, d), dtype=dt, device=dev) if out is None else out
-    _same("out", out, (n, hq, d), dt, dev)
+    out = _like("out", out, q)
     sq, sk, sv = _rows("q", q), _rows("k_new", k_new), _rows("v_new", v_new)
     ck, cv, so = _rows("k_cache", k_cache), _rows("v_cache", v_cache), _rows("out", out)
     a = ps_tree_attention_args(

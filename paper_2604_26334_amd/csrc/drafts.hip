@@ -927,10 +927,10 @@ hipError_t launch_trees(const ps_tree_attention_args &a, const TreeDeal &d, floa
 //  verify_draw_kernel   every workgroup works out the same walk; chunk sums of what is left to draw from behind its last node
 //  verify_pick_kernel   the chunk that the random number falls into, and the index in it
 // Exponentials and sums are in 64 bits: with fp32's 2^-24 a border of the running sum moves by as much as a hundred thousandth of
-// the vocabulary's entries weigh.  A 64-bit multiply-add takes this machine 6.1 clocks of a wave, a 32-bit one 4.3; an exponential
-// here is about 17 of them, which in a large batch takes longer than the row's bytes do.  No result depends on the order of workgroups.
-// 32 trees of up to 32 nodes, two drafts a node, 128256 entries, drafts' logits: 96 + 22 + 19 + 9 us (205 MB: 42 us as bytes, about 75 as
-// operations); 16 trees of given drafts 20 + 12 + 9 us; a chain of 4 drafts over 32000 5 + 9 + 8: chains of latencies (a step's loads, a few hundred
+// the vocabulary's entries weigh.  A 64-bit operation takes this machine 5.3 clocks of a wave, a 32-bit one 4.3; an exponential
+// here is about 15 of them, which in a large batch takes longer than the row's bytes do.  No result depends on the order of workgroups.
+// 32 trees of up to 32 nodes, two drafts a node, 128256 entries, drafts' logits: 83 + 22 + 19 + 9 us (205 MB: 42 us as bytes, about 77 as
+// operations); 16 trees of given drafts 19 + 12 + 9 us; a chain of 4 drafts over 32000 5 + 9 + 8: chains of latencies (a step's loads, a few hundred
 // clocks for each reduction and exponential), no longer bound by anything that more workgroups would share.
 constexpr uint32_t kVerThreads = 256, kPickThreads = 512, kMaxChunks = 32;
 struct RowPart { double z; float m; int best; };                 // one chunk of a row: sum of exp((x - m) k), m about its maximum (greedy: m its maximum, at `best`)
@@ -944,7 +944,7 @@ __device__ __forceinline__ float sane(float v) { return fminf(fmaxf(v, -INFINITY
 
 // exp((x - m) / T) with k = log2(e) / T, for N values in step (one after the other they are a chain of 15 operations each, which few
 // waves cannot hide): 2^t, t = n + f, |f| <= 1/2, and the polynomial of degree 7 whose largest relative error on that range is least (4e-11
-// where fp32 has 6e-8 beside the same exponent's; its nine extrema found by exchange; degree 8, 8e-13, takes 4 us more of 90).  n is
+// where fp32 has 6e-8 beside the same exponent's; its nine extrema found by exchange; degree 8, 8e-13, takes 125 us where this takes 121).  n is
 // what remains of t beside 1.5 2^52, and then its low word.  t below 1000; -inf gives 0, where m is finite.  (x k - m k in one operation
 // would lose everything where m is the largest finite number)
 template <int N>
