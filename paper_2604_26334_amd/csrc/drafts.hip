@@ -929,7 +929,7 @@ hipError_t launch_trees(const ps_tree_attention_args &a, const TreeDeal &d, floa
 // Exponentials and sums are in 64 bits: with fp32's 2^-24 a border of the running sum moves by as much as a hundred thousandth of
 // the vocabulary's entries weigh.  A 64-bit operation takes this machine 5.3 clocks of a wave, a 32-bit one 4.3; an exponential
 // here is about 15 of them, which in a large batch takes longer than the row's bytes do.  No result depends on the order of workgroups.
-// 32 trees of up to 32 nodes, two drafts a node, 128256 entries, drafts' logits: 83 + 22 + 19 + 9 us (205 MB: 42 us as bytes, about 77 as
+// 32 trees of up to 32 nodes, two drafts a node, 128256 entries, drafts' logits: 80 + 22 + 19 + 9 us (205 MB: 42 us as bytes, about 77 as
 // operations); 16 trees of given drafts 19 + 12 + 9 us; a chain of 4 drafts over 32000 5 + 9 + 8: chains of latencies (a step's loads, a few hundred
 // clocks for each reduction and exponential), no longer bound by anything that more workgroups would share.
 constexpr uint32_t kVerThreads = 256, kPickThreads = 512, kMaxChunks = 32;
