@@ -711,7 +711,8 @@ typedef struct ps_rotation {
 int32_t ps_stack_set_rotation(ps_stack *st, const ps_rotation *rotation);
 /* ps_stack_set_tree: the rows of the following ps_stack_forward calls are a tree of n tokens instead of a chunk: parents (host,
  * copied) as ps_tree_attention has them, parents[i] in -1 .. i - 1 (PS_E_ARG otherwise).  n <= the plan's token count and
- * <= PS_TREE_MAX; x_in, x_out are [n][hidden], router logits [n_layers][n][n_experts], logits of every token [n][vocab].
+ * <= PS_TREE_MAX; x_in, x_out are [n][hidden], router logits [n_layers][n][n_experts], logits of every token [n][vocab]; the one
+ * token that ps_stack_set_logits_out may name is one of these n (PS_E_STATE from the forward otherwise, nothing enqueued).
  * All n rows are appended to the cache, node i at position context + i; ps_stack_keep_path puts the accepted ones in place.
  * n = 0: chunks again; ps_stack_set_tier does the same.  ps_stack_forward_chunked returns PS_E_STATE while a tree is set.  The
  * last forward's rows are verified and kept before the next tree is set (PS_E_STATE afterwards). */

@@ -1749,6 +1749,10 @@ int32_t ps_stack_forward(ps_stack *st, const void *x_in, void *x_out, const floa
     if (rc) return rc;
     const ps_plan &p = st->plan;
     const uint32_t n = st->tree.n ? st->tree.n : p.M;
+    if (st->head_rows == 1 && st->head_row0 >= n) {      // (x_out ends with row n - 1)
+        ps::set_error("logits of token %u are asked from a forward of %u rows", st->head_row0, n);
+        return PS_E_STATE;
+    }
     st->step_rows = 0;
     const int32_t rcf = forward_impl(st, x_in, x_out, router_logits, router_logits_dev, (uint64_t)n * p.g.m.n_experts, n);
     if (rcf == PS_OK) { st->step_rows = n; st->step_ctx = st->ctx; }
