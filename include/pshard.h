@@ -719,9 +719,10 @@ int32_t ps_stack_set_rotation(ps_stack *st, const ps_rotation *rotation);
 int32_t ps_stack_set_tree(ps_stack *st, const int32_t *parents, uint32_t n);
 /* ps_stack_verify_tree: ps_verify_tree over the logits of the last forward (ps_stack_set_logits_out with every token; with one
  * token: that token's row alone, i.e. the draw of the next token), the tree that ps_stack_set_tree set or, without one, the
- * chain of the forward's tokens.  Device pointers: token int32 [n], draft_logits fp16 [n][vocab] or NULL, u_accept fp32 [n],
- * u_sample, temperature (NULL: 1) fp32 [1]; path int32 [n], count, next_token int32 [1].  On the compute stream, asynchronous.
- * PS_E_STATE before a forward with logits. */
+ * chain of the forward's tokens.  The buffer is the one that forward wrote, whatever ps_stack_set_logits_out has set since.
+ * Device pointers: token int32 [n], draft_logits fp16 [n][vocab] or NULL, u_accept fp32 [n], u_sample, temperature (NULL: 1)
+ * fp32 [1]; path int32 [n], count, next_token int32 [1].  On the compute stream, asynchronous.
+ * PS_E_STATE where the last forward wrote no logits, or there was none. */
 typedef struct ps_stack_verify_args {
     const int32_t *token;
     const void *draft_logits;

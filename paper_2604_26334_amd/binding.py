@@ -536,7 +536,7 @@ class Stack:
         self.plan = plan
         s = plan.summary()
         self.M = s.n_tokens
-        self.tree_rows = self.logits_rows = 0
+        self.tree_rows = self.logits_rows = self.step_tokens = 0
         self.H = plan.cfg["hidden"]
         self.arena = torch.empty(int(s.budget_bytes), dtype=torch.uint8, device=self.device)
         self.device_index = self.arena.device.index
@@ -626,7 +626,7 @@ class Stack:
                                      _table("next_token", next_token, 1, i32, dev), int(max_children), 0)
             need = C.c_uint64()
             _check(lib().ps_stack_verify_workspace(self.h, C.byref(a), C.byref(need)))
-            _want(n == (1 if self.logits_rows == 1 else self.tree_rows or self.M), "one token per row of logits (got %d)" % n)
+            _want(n == self.step_tokens, "one token per row of the last forward's logits (%d, got %d)" % (self.step_tokens, n))
             at, size, _held = _workspace(need.value, workspace, dev)
             _check(lib().ps_stack_verify_tree(self.h, C.byref(a), at, size))
         return path, count, next_token
@@ -671,6 +671,7 @@ class Stack:
         else:
             with self.torch.cuda.device(self.device):
                 _check(lib().ps_stack_forward(self.h, x_in.data_ptr(), x_out.data_ptr(), _ptr(lg), ld))
+        self.step_tokens = 1 if self.logits_rows == 1 else shape[0]      # (rows of logits to verify)
 
     def forward_noalloc(self, x_in, x_out):
         """ps_stack_forward_noalloc: the same pass with the workspace in the library's static device array."""
@@ -679,6 +680,7 @@ class Stack:
         assert tuple(x_in.shape) == (self.M, self.H) and tuple(x_out.shape) == (self.M, self.H)
         with self.torch.cuda.device(self.device):
             _check(lib().ps_stack_forward_noalloc(self.h, x_in.data_ptr(), x_out.data_ptr()))
+        self.step_tokens = 1 if self.logits_rows == 1 else self.M
 
     def synchronize(self):
         with self.torch.cuda.device(self.device):

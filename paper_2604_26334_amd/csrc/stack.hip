@@ -95,6 +95,8 @@ struct ps_stack {
     ps::StackRotation rotation{};
     ps::StackTreeNodes tree{};                // n > 0: the rows of a forward are a tree
     uint32_t step_rows = 0, step_ctx = 0;     // rows and context of the last ps_stack_forward (0: none since its rows were kept, or the tier changed)
+    const __half *step_logits = nullptr;      // the logits it wrote (null: none): those of every row, or of one token alone
+    bool step_one_token = false;
     bool profiling = false;
     bool own_rinv_launch = false;             // decode mode 2: RMS factors always from rinv_kernel
     const void *rinv_of = nullptr;            // rows whose RMS factors the last residual epilogue or combine left in the workspace
@@ -1592,12 +1594,12 @@ int32_t ps_stack_set_tree(ps_stack *st, const int32_t *parents, uint32_t n) {
 static int32_t stack_verify_call(const ps_stack *st, const ps_stack_verify_args *v, ps_verify_tree_args *a, uint64_t *tables, uint64_t *bytes) {
     if (!st || !v) { ps::set_error("NULL argument"); return PS_E_ARG; }
     const ps_plan &p = st->plan;
-    if (!st->head_rows || !st->logits || !st->step_rows) { ps::set_error("verification needs the logits of a forward (ps_stack_set_logits_out, ps_stack_forward)"); return PS_E_STATE; }
-    const uint32_t n = st->head_rows == 1 ? 1 : st->step_rows;
+    if (!st->step_rows || !st->step_logits) { ps::set_error("verification needs the logits of a forward (ps_stack_set_logits_out, ps_stack_forward)"); return PS_E_STATE; }
+    const uint32_t n = st->step_one_token ? 1 : st->step_rows;
     if (n > PS_TREE_MAX) { ps::set_error("trees of up to %u tokens (the forward had %u)", PS_TREE_MAX, n); return PS_E_ARG; }
     *a = ps_verify_tree_args{};
     a->type = PS_TYPE_F16; a->n_seq = 1; a->n_tokens = n; a->vocab = p.g.m.vocab; a->max_tree = n; a->max_children = v->max_children;
-    a->target_logits = st->logits; a->draft_logits = v->draft_logits;
+    a->target_logits = st->step_logits; a->draft_logits = v->draft_logits;
     a->target_row = a->draft_row = p.g.m.vocab;
     a->path_seq = n;
     a->token = v->token; a->u_accept = v->u_accept; a->u_sample = v->u_sample; a->temperature = v->temperature;
@@ -1624,7 +1626,7 @@ int32_t ps_stack_verify_tree(ps_stack *st, const ps_stack_verify_args *args, voi
         ps::set_error("a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need); return PS_E_ARG;
     }
     int32_t *first = static_cast<int32_t *>(workspace), *parent = first + 2;
-    PS_HIP(ps::launch_tree_tables(first, parent, a.n_tokens, st->head_rows == 1 ? ps::StackTreeNodes{} : st->tree, st->compute));
+    PS_HIP(ps::launch_tree_tables(first, parent, a.n_tokens, st->step_one_token ? ps::StackTreeNodes{} : st->tree, st->compute));
     a.first = first;
     a.parent = parent;
     return ps_verify_tree(&a, static_cast<uint8_t *>(workspace) + tables, workspace_bytes - tables, st->compute);
@@ -1743,6 +1745,14 @@ static int32_t forward_checks(ps_stack *st, const void *x_in, void *x_out) {
     return PS_OK;
 }
 
+// What a forward of n rows did, for the verification and the kept rows that follow it (settings may change in between)
+static void note_step(ps_stack *st, uint32_t n) {
+    st->step_rows = n;
+    st->step_ctx = st->ctx;
+    st->step_logits = st->head_rows ? st->logits : nullptr;
+    st->step_one_token = st->head_rows == 1;
+}
+
 int32_t ps_stack_forward(ps_stack *st, const void *x_in, void *x_out, const float *router_logits,
                          const float *router_logits_dev) {
     const int32_t rc = forward_checks(st, x_in, x_out);
@@ -1755,7 +1765,7 @@ int32_t ps_stack_forward(ps_stack *st, const void *x_in, void *x_out, const floa
     }
     st->step_rows = 0;
     const int32_t rcf = forward_impl(st, x_in, x_out, router_logits, router_logits_dev, (uint64_t)n * p.g.m.n_experts, n);
-    if (rcf == PS_OK) { st->step_rows = n; st->step_ctx = st->ctx; }
+    if (rcf == PS_OK) note_step(st, n);
     return rcf;
 }
 
@@ -1777,7 +1787,9 @@ int32_t ps_stack_forward_noalloc(ps_stack *st, const void *x_in, void *x_out) {
     const bool graph = st->use_graph;
     st->use_graph = false;
     st->ws_base = st->static_ws;
+    st->step_rows = 0;
     const int32_t rc = forward_impl(st, x_in, x_out, nullptr, nullptr, 0, p.M);
+    if (rc == PS_OK) note_step(st, p.M);
     st->ws_base = st->arena + p.ws_off;
     st->use_graph = graph;
     return rc;

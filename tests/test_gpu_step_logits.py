@@ -1,7 +1,12 @@
-"""Which logits a stack's forward writes: of rows that lie in it."""
+"""Which logits a stack's forward writes and which a verification judges: rows that lie in the forward, buffers that are large enough,
+and what the last forward did rather than what is set for the next."""
+import ctypes as C
+
+import numpy as np
 import pytest
 
 import synth_inputs as S
+from oracle import drafts as D
 from oracle import oracle as O
 from tests import harness as Hn
 from tests import test_gpu_draft_step as T
@@ -51,3 +56,101 @@ def test_one_tokens_logits_are_of_a_row_of_the_tree():
     assert Hn.rel_err(one.cpu().numpy()[None], O.output_head(out[PLAN - 1:], cfg, head, mirror=True)) <= 5e-3
     st.close()
 
+
+def _draft(st, n, seed):
+    import torch
+    rng = np.random.default_rng(seed)
+    token = rng.integers(0, V, size=n)
+    return (torch.tensor(token, dtype=torch.int32, device=st.device), torch.tensor(rng.random(n) * 0.2, dtype=torch.float32, device=st.device),
+            torch.tensor(rng.random(1), dtype=torch.float32, device=st.device))
+
+
+def _check(got, logits, token, parents, u, us):
+    path, count, nxt = (t.cpu().tolist() for t in got)
+    want, w_next = D.verify_tree(logits.double().cpu().numpy(), token.tolist(), parents, u.tolist(), float(us[0]))
+    assert path == want + [-1] * (len(parents) - len(want)) and count == [len(want)] and nxt == [w_next]
+
+
+def test_verification_needs_a_forward_that_wrote_logits():
+    import torch
+    from paper_2604_26334_amd import binding as B
+    cfg, st, _ = _head_stack()
+    n = len(PARENTS)
+    st.set_tree(PARENTS)
+    x = S.activations(52, 0, n, cfg["hidden"])
+    token, u, us = _draft(st, n, 1)
+    T._forward(st, x)                                                       # the head was off
+    logits = torch.zeros(PLAN, V, dtype=torch.float16, device=st.device)
+    st.set_logits_out(logits, 0, PLAN)
+    _refused(B.PS_E_STATE, st.verify_tree, token, u, us)
+    one = torch.zeros(V, dtype=torch.float16, device=st.device)
+    st.set_logits_out(one, 0, 1)
+    _refused(B.PS_E_STATE, st.verify_tree, token[:1].contiguous(), u[:1].contiguous(), us)
+    a = B.ps_stack_verify_args(*[1 << 30] * 8, 2, 0)
+    need = C.c_uint64()
+    assert B.lib().ps_stack_verify_workspace(st.h, C.byref(a), C.byref(need)) == B.PS_E_STATE
+    # a prompt in chunks is no tree's step, whatever it wrote
+    st.set_tree()
+    st.set_logits_out(logits, 0, PLAN)
+    T._forward(st, S.activations(52, 1, PLAN, cfg["hidden"]))
+    st.set_context(CTX)
+    xin, xout = T._tensors(st, S.activations(52, 2, 11, cfg["hidden"]))
+    B.chunked_forward(st, xin, xout)
+    st.synchronize()
+    token, u, us = _draft(st, PLAN, 2)
+    _refused(B.PS_E_STATE, st.verify_tree, token, u, us)
+    st.close()
+
+
+@pytest.mark.parametrize("then", ["other buffer", "one token", "off"])
+def test_verification_judges_what_the_last_forward_wrote(then):
+    """The next step's logits may be set before this one's are judged."""
+    import torch
+    from paper_2604_26334_amd import binding as B
+    cfg, st, _ = _head_stack()
+    n = len(PARENTS)
+    st.set_tree(PARENTS)
+    x = S.activations(53, 0, n, cfg["hidden"])
+    token, u, us = _draft(st, n, 3)
+    logits = torch.zeros(PLAN, V, dtype=torch.float16, device=st.device)
+    st.set_logits_out(logits, 0, PLAN)
+    T._forward(st, x)
+    token[1] = int(logits[0].float().argmax())
+    other = torch.zeros(PLAN, V, dtype=torch.float16, device=st.device)
+    other[:, 3] = 60.0                                                      # where it is judged instead, token 3 follows everything
+    torch.cuda.synchronize()
+    if then == "other buffer":
+        st.set_logits_out(other, 0, PLAN)
+    elif then == "one token":
+        st.set_logits_out(other[0].contiguous(), 2, 1)
+    else:
+        st.set_logits_out(None, 0, 0)
+    us.fill_(0.0)                                                           # the first token that has any weight: 0 in these logits
+    torch.cuda.synchronize()
+    got = st.verify_tree(token, u, us)
+    st.synchronize()
+    _check(got, logits[:n], token, PARENTS, u, us)
+    _refused(B.PS_E_ARG, st.verify_tree, token[:1].contiguous(), u[:1].contiguous(), us)      # one number per row of that forward
+    st.keep_path(got[0], got[1])
+    st.close()
+
+
+def test_one_tokens_logits_are_judged_alone_whatever_is_set_next():
+    import torch
+    from paper_2604_26334_amd import binding as B
+    cfg, st, _ = _head_stack()
+    x = S.activations(54, 0, PLAN, cfg["hidden"])
+    one = torch.zeros(V, dtype=torch.float16, device=st.device)
+    st.set_logits_out(one, 4, 1)
+    T._forward(st, x)
+    rows = torch.zeros(PLAN, V, dtype=torch.float16, device=st.device)
+    st.set_logits_out(rows, 0, PLAN)
+    token, u, us = _draft(st, PLAN, 4)
+    torch.cuda.synchronize()
+    _refused(B.PS_E_ARG, st.verify_tree, token, u, us)
+    t1, u1 = token[:1].contiguous(), u[:1].contiguous()
+    torch.cuda.synchronize()
+    got = st.verify_tree(t1, u1, us)
+    st.synchronize()
+    _check(got, one[None], t1, [-1], u1, us)
+    st.close()
