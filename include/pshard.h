@@ -471,7 +471,8 @@ int32_t ps_stack_set_context(ps_stack *st, uint32_t context);
  * logits = W_out * RMSNorm(x_out row), fp32 accumulation, stored fp16.  logits_dev: device memory,
  * caller-owned, 16-byte aligned, must stay valid for every forward until changed, and must not
  * overlap the arena, x_in or x_out.  PS_E_STATE if the model has no head, PS_E_ARG for any other
- * rows / first_token. */
+ * rows / first_token.  The setting outlives ps_stack_set_tier: a forward of more rows than the buffer
+ * was set for, or without row first_token, returns PS_E_STATE. */
 int32_t ps_stack_set_logits_out(ps_stack *st, void *logits_dev, uint32_t first_token, uint32_t rows);
 /* The CPU back-end's matrix kernel on its own (host pointers only; for tests and for measuring
  * the CPU rate): `packed` is the image ps_pack_matrix (pshard_test.h) makes of a [rows][K] matrix; x fp16 [n_tokens][K];

@@ -1745,6 +1745,19 @@ static int32_t forward_checks(ps_stack *st, const void *x_in, void *x_out) {
     return PS_OK;
 }
 
+// The setting of ps_stack_set_logits_out against a forward of n rows: it may have been made for a plan of other rows
+static int32_t head_checks(const ps_stack *st, uint32_t n) {
+    if (st->head_rows == 1 && st->head_row0 >= n) {      // (x_out ends with row n - 1)
+        ps::set_error("logits of token %u are asked from a forward of %u rows", st->head_row0, n);
+        return PS_E_STATE;
+    }
+    if (st->head_rows > 1 && n > st->head_rows) {
+        ps::set_error("logits of a forward of %u rows do not fit the buffer of %u rows that was set", n, st->head_rows);
+        return PS_E_STATE;
+    }
+    return PS_OK;
+}
+
 // What a forward of n rows did, for the verification and the kept rows that follow it (settings may change in between)
 static void note_step(ps_stack *st, uint32_t n) {
     st->step_rows = n;
@@ -1759,10 +1772,7 @@ int32_t ps_stack_forward(ps_stack *st, const void *x_in, void *x_out, const floa
     if (rc) return rc;
     const ps_plan &p = st->plan;
     const uint32_t n = st->tree.n ? st->tree.n : p.M;
-    if (st->head_rows == 1 && st->head_row0 >= n) {      // (x_out ends with row n - 1)
-        ps::set_error("logits of token %u are asked from a forward of %u rows", st->head_row0, n);
-        return PS_E_STATE;
-    }
+    if (const int32_t rch = head_checks(st, n)) return rch;
     st->step_rows = 0;
     const int32_t rcf = forward_impl(st, x_in, x_out, router_logits, router_logits_dev, (uint64_t)n * p.g.m.n_experts, n);
     if (rcf == PS_OK) note_step(st, n);
@@ -1785,6 +1795,7 @@ int32_t ps_stack_forward_noalloc(ps_stack *st, const void *x_in, void *x_out) {
     // every kernel of this forward takes its workspace pointers from ws_base: the static array's
     // address on this device.  Launch per shard (a graph would have to be instantiated).
     const bool graph = st->use_graph;
+    if (const int32_t rch = head_checks(st, p.M)) return rch;
     st->use_graph = false;
     st->ws_base = st->static_ws;
     st->step_rows = 0;

@@ -154,3 +154,51 @@ def test_one_tokens_logits_are_judged_alone_whatever_is_set_next():
     st.synchronize()
     _check(got, one[None], t1, [-1], u1, us)
     st.close()
+
+
+def test_logits_set_in_one_tier_fit_the_forwards_of_another():
+    """A buffer set for fewer rows than the new tier's forward has, or a token that it does not have, is refused before anything is enqueued."""
+    import torch
+    from paper_2604_26334_amd import binding as B
+    cfg = dict(Hn.small_dense_cfg(1), vocab=V)
+    W, head = Hn.WeightCache(cfg, 55), S.head_matrix(55, cfg)
+    table = B.TierTable(cfg, 1 << 28)
+    tiers = {e.tier_tokens: e.tier for e in table.entries() if e.feasible}
+    st = B.Stack(table)
+    for kind, expert, N, K in S.matrix_shapes(cfg):
+        st.load_matrix(0, kind, expert, *W(0, kind, expert))
+    st.load_matrix(1, S.MAT_OUT, None, *head)
+    few, many = 16, 64
+    x = {n: S.activations(55, n, n, cfg["hidden"]) for n in (1, few, many)}
+    buf = torch.full((many + 1, V), 7.0, dtype=torch.float16, device=st.device)
+
+    def refused(n):
+        xin, xout = T._tensors(st, x[n])
+        torch.cuda.synchronize()
+        for call in (st.forward, st.forward_noalloc):
+            _refused(B.PS_E_STATE, call, xin, xout)
+        st.synchronize()
+        assert bool((xout == 0).all()) and bool((buf == 7).all())
+
+    def right(n, rows):
+        out = T._forward(st, x[n]).cpu().numpy()
+        got = buf[:len(rows)].cpu().numpy()
+        assert Hn.rel_err(got, O.output_head(out[rows], cfg, head, mirror=True)) <= 5e-3
+        assert bool((buf[len(rows):] == 7).all())
+        buf.fill_(7.0)
+        torch.cuda.synchronize()
+    st.set_tier(tiers[few])
+    st.set_logits_out(buf[:few], 0, few)
+    st.set_tier(tiers[many])
+    refused(many)
+    st.set_tier(tiers[few])
+    right(few, list(range(few)))
+    st.set_logits_out(buf[0], few - 1, 1)
+    st.set_tier(tiers[1])
+    refused(1)
+    st.set_tier(tiers[many])
+    right(many, [few - 1])
+    st.set_logits_out(buf[:many], 0, many)
+    st.set_tier(tiers[few])                       # (a larger buffer than the forward needs)
+    right(few, list(range(few)))
+    st.close()
