@@ -387,8 +387,16 @@ __device__ __forceinline__ bool made_finite(u4_t &v) {
     return odd;
 }
 
-// Scores of a tile (S, hidden positions -inf) to weights P relative to the running maximum, which a row raises only where its
-// weights would pass 2^8: each row by its own scores alone, so its result does not depend on its neighbours
+// Weights in the tensors' type are held as 2^kLift times exp(score - running maximum), and a row's maximum is raised only where one would
+// pass 2^(kLift + kSlack).  fp16 ends at 2^-24 below and 2^16 above: lifted by 2^10 its steps end at 2^-34 of the maximum, and the roundings of 2^17 keys
+// there are 2^-18 of it together (without the lift, 4000 keys 18 nats behind one whose value is zero vanished, where they are the whole result).
+// A larger lift leaves less slack and more rows to raise: 64 tokens over 131072 positions 185 us with 7 and 8, 186 with 10 and 5.9, 189 with 12 and 3.
+template <typename T> struct WeightRange;
+template <> struct WeightRange<f16_t> { static constexpr float kLift = 10.f, kSlack = 5.9f; };
+template <> struct WeightRange<bf16_t> { static constexpr float kLift = 0.f, kSlack = 8.f; };
+
+// Scores of a tile (S, hidden positions -inf) to weights P relative to the running maximum: each row by its own scores alone, so
+// its result does not depend on its neighbours
 template <typename T, int NT, int DT>
 __device__ __forceinline__ void weigh(const f4_t (&S)[NT][2], float (&m_run)[NT], f4_t (&L)[NT], f4_t (&O)[NT][DT], typename Mfma<T>::v8 (&P)[NT], float c2, float slack) {
 #pragma unroll
@@ -407,7 +415,7 @@ __device__ __forceinline__ void weigh(const f4_t (&S)[NT][2], float (&m_run)[NT]
         // time of 64 tokens over 131072 positions, nothing where the cache's bytes bound)
         const float ms = m_run[t] == -INFINITY ? 0.f : m_run[t];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) P[t][e] = (T)__builtin_amdgcn_exp2f((S[t][e >> 2][e & 3] - ms) * c2);
+        for (int e = 0; e < 8; ++e) P[t][e] = (T)__builtin_amdgcn_exp2f(fmaf(S[t][e >> 2][e & 3] - ms, c2, WeightRange<T>::kLift));
     }
 }
 
@@ -474,7 +482,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(ps_tree_attentio
     const float scale_abs = fabsf(a.scale);
     const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
     const float c2 = fmaxf(scale_abs * 1.4426950408889634f, 1e-30f);     // weights are 2^(c2 (s - m))
-    const float slack = 8.f / c2;      // a row is rescaled only where its weights would pass 2^8
+    const float slack = WeightRange<T>::kSlack / c2;
     uint32_t tok[NT];
     v8 q[NT][KK];
 #pragma unroll
@@ -686,7 +694,7 @@ __global__ __launch_bounds__(256, 2) void tree_rows_kernel(ps_tree_attention_arg
     request(lo);
     const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
     const float c2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
-    const float slack = 8.f / c2;
+    const float slack = WeightRange<T>::kSlack / c2;
     const uint32_t mine0 = row0 + wave * (NT * 16);      // the wave's rows
     const bool rows = mine0 < R;
     uint32_t tok[NT], head[NT];

@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+from oracle import drafts as D
 from tests import test_gpu_drafts as T
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +41,41 @@ def test_scores_of_any_size(ty, size, d, hq, hk, trees, ctxs):
                     continue
                 assert np.array_equal(out[first[s] + i, h], v[best[1]]), (s, i, h)
     assert left * 10 <= seen
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("d,t", [(64, 1), (128, 2), (64, 20), (128, 40), (64, 40)])
+@pytest.mark.parametrize("spot", ["first", "middle", "own"])
+def test_small_weights_add_up(ty, d, t, spot):
+    """One key `gap` nats ahead, whose value is zero, and 4000 alike with values about 100: what comes out is these alone.  512 heads, so
+    that a head's positions are not split.  The tolerance: a half step of the result, half a step of every weight and of
+    their sum, weights held to 2^-35 of the largest where the type's half step ends (half of fp16's least step 2^-24 under a largest weight of 2^10 or
+    more), scores and their exponentials in fp32 (a score of up to 20, 29 in powers of two: 2^-19 of a weight; 2^-17 allowed)."""
+    import torch
+    from paper_2604_26334_amd import binding as B
+    heads, n, dt = 512, 4000, T._dt(ty)
+    g = T._gen(7)
+    at = {"first": 0, "middle": n // 2 + 5, "own": None}[spot]
+    scale = 2.0 ** -3
+    for gap in (10.0, 14.0, 16.0, 18.0, 20.0):
+        q = torch.zeros(t, heads, d, dtype=dt, device=T.DEV)
+        q[..., 0] = 16.0
+        kc = torch.zeros(1, 1, n, d, dtype=dt, device=T.DEV)
+        vc = (100 + 10 * torch.rand(1, 1, n, d, generator=g, device=T.DEV)).to(dt)
+        kn = torch.zeros(t, 1, d, dtype=dt, device=T.DEV)
+        vn = (100 + 10 * torch.rand(t, 1, d, generator=g, device=T.DEV)).to(dt)
+        if at is None:
+            kn[0, 0, 0] = gap / 2                                     # every node comes behind node 0
+            vn[0] = 0
+        else:
+            kc[0, 0, at, 0] = gap / 2
+            vc[0, 0, at] = 0
+        parent = [-1] + [0] * (t - 1)
+        out = B.tree_attention(q, kn.expand(t, heads, d), vn.expand(t, heads, d), kc.expand(1, heads, n, d), vc.expand(1, heads, n, d),
+                               T._ints([0, t]), T._ints([n]), T._ints(parent), max_context=n, max_tree=t, scale=scale)
+        ref = D.tree_attention(T._np(q[:, :1]), T._np(kn), T._np(vn), T._np(kc[0]), T._np(vc[0]), n, parent, scale)
+        hs = T._half_step(ty)
+        least = 2.0 ** -35 if ty == "f16" else 2.0 ** -100
+        tol = np.abs(ref) * (3 * hs + 2.0 ** -17) + 2 * n * least * 110
+        off = np.abs(T._np(out) - ref) / tol
+        assert off.max() <= 1, (gap, off.max())
