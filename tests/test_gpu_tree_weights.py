@@ -79,3 +79,25 @@ def test_small_weights_add_up(ty, d, t, spot):
         tol = np.abs(ref) * (3 * hs + 2.0 ** -17) + 2 * n * least * 110
         off = np.abs(T._np(out) - ref) / tol
         assert off.max() <= 1, (gap, off.max())
+
+
+@pytest.mark.parametrize("t", [2, 20, 40])
+def test_large_values_do_not_overflow(t):
+    """bf16 values of 2^117 to 2^118 behind keys that rise by 5.2 nats after the first 128: 900 weights of at most 1 times these add up to less
+    than 2^128, within fp32 (weights of 2^7.5 would not).  All values alike in a dimension: the result is that value, to the rounding of the result (half a
+    step) and of a weight sum against the weighted sum, both of the same rounded weights in fp32 (900 x 2^-24)."""
+    import torch
+    from paper_2604_26334_amd import binding as B
+    heads, n, d, dt = 512, 900, 128, torch.bfloat16
+    q = torch.zeros(t, heads, d, dtype=dt, device=T.DEV)
+    q[..., 0] = 16.0
+    row = ((1 + torch.rand(d, generator=T._gen(3), device=T.DEV)) * 2.0 ** 117).to(dt)
+    kc, kn = torch.zeros(1, 1, n, d, dtype=dt, device=T.DEV), torch.zeros(t, 1, d, dtype=dt, device=T.DEV)
+    kc[:, :, 128:, 0] = 2.6
+    kn[..., 0] = 2.6
+    vc, vn = row.expand(1, heads, n, d), row.expand(t, heads, d)
+    vc, vn = vc[:, :1].contiguous().expand(1, heads, n, d), vn[:, :1].contiguous().expand(t, heads, d)
+    out = B.tree_attention(q, kn.expand(t, heads, d), vn, kc.expand(1, heads, n, d), vc, T._ints([0, t]), T._ints([n]), T._ints([-1] * t),
+                           max_context=n, max_tree=t, scale=2.0 ** -3)
+    ref = T._np(row)
+    assert (np.abs(T._np(out) - ref) <= ref * (2.0 ** -8 + 900 * 2.0 ** -23)).all()
