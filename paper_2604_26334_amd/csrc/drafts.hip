@@ -152,49 +152,51 @@ __global__ __launch_bounds__(256) void qk_norm_rope_wide_kernel(ps_qk_norm_rope_
 template <typename T>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(ps_qk_norm_rope_args a) {
     const uint32_t lane = threadIdx.x & 63, heads = a.n_q_heads + a.n_k_heads;
-    const uint64_t item = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (item >= (uint64_t)a.n_tokens * heads) return;
-    const uint32_t t = (uint32_t)(item / heads), hh = (uint32_t)(item % heads);
-    const bool isq = hh < a.n_q_heads;
-    const uint32_t h = isq ? hh : hh - a.n_q_heads;
-    const T *x = isq ? static_cast<const T *>(a.q) + t * a.q_token + h * a.q_head : static_cast<const T *>(a.k) + t * a.k_token + h * a.k_head;
-    T *y = isq ? static_cast<T *>(a.q_out) + t * a.q_out_token + h * a.q_out_head : static_cast<T *>(a.k_out) + t * a.k_out_token + h * a.k_out_head;
-    const T *gain = static_cast<const T *>(isq ? a.q_gain : a.k_gain);
-    float rinv = 1.f;
-    if (a.norm) {
-        float ss = 0.f;
-        for (uint32_t d = lane; d < a.head_dim; d += 64) { const float v = to_f(x[d]); ss = fmaf(v, v, ss); }
-        for (int o = 32; o; o >>= 1) ss += __shfl_xor(ss, o, 64);
-        rinv = 1.0f / sqrtf(ss / (float)a.head_dim + a.eps);
+    const uint64_t items = (uint64_t)a.n_tokens * heads;
+    for (uint64_t item = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (uint64_t)gridDim.x * 4) {
+        const uint32_t t = (uint32_t)(item / heads), hh = (uint32_t)(item % heads);
+        const bool isq = hh < a.n_q_heads;
+        const uint32_t h = isq ? hh : hh - a.n_q_heads;
+        const T *x = isq ? static_cast<const T *>(a.q) + t * a.q_token + h * a.q_head : static_cast<const T *>(a.k) + t * a.k_token + h * a.k_head;
+        T *y = isq ? static_cast<T *>(a.q_out) + t * a.q_out_token + h * a.q_out_head : static_cast<T *>(a.k_out) + t * a.k_out_token + h * a.k_out_head;
+        const T *gain = static_cast<const T *>(isq ? a.q_gain : a.k_gain);
+        float rinv = 1.f;
+        if (a.norm) {
+            float ss = 0.f;
+            for (uint32_t d = lane; d < a.head_dim; d += 64) { const float v = to_f(x[d]); ss = fmaf(v, v, ss); }
+            for (int o = 32; o; o >>= 1) ss += __shfl_xor(ss, o, 64);
+            rinv = 1.0f / sqrtf(ss / (float)a.head_dim + a.eps);
+        }
+        const uint32_t half = a.rot_dim / 2;
+        const double pos = a.rot_dim ? (double)a.positions[t] : 0.0;
+        for (uint32_t i = lane; i < half; i += 64) {
+            const uint32_t da = a.pairs ? 2 * i : i, db = a.pairs ? 2 * i + 1 : i + half;
+            const float ga = a.norm && gain ? to_f(gain[da]) : 1.f, gb = a.norm && gain ? to_f(gain[db]) : 1.f;
+            const float va = to_f(x[da]) * rinv * ga, vb = to_f(x[db]) * rinv * gb;
+            const Turn w = turn_of(pos, a.inv_freq[i]);
+            y[da] = (T)(va * w.c - vb * w.s);
+            y[db] = (T)(vb * w.c + va * w.s);
+        }
+        for (uint32_t d = a.rot_dim + lane; d < a.head_dim; d += 64)
+            y[d] = (T)(to_f(x[d]) * rinv * (a.norm && gain ? to_f(gain[d]) : 1.f));
     }
-    const uint32_t half = a.rot_dim / 2;
-    const double pos = a.rot_dim ? (double)a.positions[t] : 0.0;
-    for (uint32_t i = lane; i < half; i += 64) {
-        const uint32_t da = a.pairs ? 2 * i : i, db = a.pairs ? 2 * i + 1 : i + half;
-        const float ga = a.norm && gain ? to_f(gain[da]) : 1.f, gb = a.norm && gain ? to_f(gain[db]) : 1.f;
-        const float va = to_f(x[da]) * rinv * ga, vb = to_f(x[db]) * rinv * gb;
-        const Turn w = turn_of(pos, a.inv_freq[i]);
-        y[da] = (T)(va * w.c - vb * w.s);
-        y[db] = (T)(vb * w.c + va * w.s);
-    }
-    for (uint32_t d = a.rot_dim + lane; d < a.head_dim; d += 64)
-        y[d] = (T)(to_f(x[d]) * rinv * (a.norm && gain ? to_f(gain[d]) : 1.f));
 }
 
+constexpr uint64_t kMostGroups = (1u << 24) - 1;       // of 256 threads: a launch holds less than 2^32 (waves take more items in turn)
 template <typename T, class P>
 hipError_t launch_rope_wide(const ps_qk_norm_rope_args &a, const P &position, hipStream_t st) {
     uint32_t L = 1;
     while (L * 16 < a.head_dim) L *= 2;
     // a wave to a token, and below 4096 tokens (four waves a SIMD) its heads shared out as far as that takes
     const uint32_t rounds = ((a.n_q_heads + a.n_k_heads) * L + 63) / 64, splits = (uint32_t)std::min<uint64_t>(rounds, (4095ull + a.n_tokens) / a.n_tokens);
-    hipLaunchKernelGGL((qk_norm_rope_wide_kernel<T, P>), dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * splits + 3) / 4, 1u << 24)), dim3(256), P::kLds, st, a,
+    hipLaunchKernelGGL((qk_norm_rope_wide_kernel<T, P>), dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * splits + 3) / 4, kMostGroups)), dim3(256), P::kLds, st, a,
                        position, L, splits);
     return hipGetLastError();
 }
 template <typename T>
 hipError_t launch_rope(const ps_qk_norm_rope_args &a, hipStream_t st) {
     if (a.head_dim % 16 == 0 && a.rot_dim % 16 == 0) return launch_rope_wide<T>(a, GivenPositions{a.positions}, st);
-    hipLaunchKernelGGL(qk_norm_rope_kernel<T>, dim3((uint32_t)(((uint64_t)a.n_tokens * (a.n_q_heads + a.n_k_heads) + 3) / 4)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(qk_norm_rope_kernel<T>, dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * (a.n_q_heads + a.n_k_heads) + 3) / 4, kMostGroups)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
