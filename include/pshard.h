@@ -624,7 +624,9 @@ int32_t ps_qk_norm_rope(const ps_qk_norm_rope_args *args, void *stream);
  *  type F16 or BF16; head_dim 64 or 128; max_tree <= PS_TREE_MAX.  q, out [n_tokens][n_q_heads][head_dim]; k_new,
  *  v_new [n_tokens][n_kv_heads][head_dim]; k_cache, v_cache [n_seq][n_kv_heads][capacity][head_dim], all with the
  *  strides below.  Every address and stride in bytes is a multiple of 16 (PS_E_ARG otherwise), and 64 rows of the
- *  cache or of new tokens span less than 2 GiB.  max_context: a bound on context[], <= capacity; work is dealt out by it.
+ *  cache or of new tokens span less than 2 GiB.  Sequences times kv heads times their blocks of query rows (16, 32 or, for more
+ *  rows, 128 of a kv head) are less than 2^24 (PS_E_ARG: one launch).  max_context: a bound on context[], <= capacity; work is
+ *  dealt out by it.
  *  append = 1: the tokens' K and V rows are also written to the cache, row context[s] + t (max_context + max_tree
  *  <= capacity); each sequence's cache must then be its own.  out may not overlap any input.
  * Scores, softmax and sums in fp32; the weights of the value product are rounded to `type`, and the weights' sum is

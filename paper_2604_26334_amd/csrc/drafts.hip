@@ -21,6 +21,7 @@ typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u2_t __attribute__((ext_vector_type(2)));
 
 constexpr float kFloatMax = 3.402823466e38f;
+constexpr uint64_t kMostGroups = (1u << 24) - 1;       // of 256 threads: a launch holds less than 2^32
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
@@ -182,11 +183,11 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(ps_qk_norm_rope_args 
     }
 }
 
-constexpr uint64_t kMostGroups = (1u << 24) - 1;       // of 256 threads: a launch holds less than 2^32 (waves take more items in turn)
 template <typename T, class P>
 hipError_t launch_rope_wide(const ps_qk_norm_rope_args &a, const P &position, hipStream_t st) {
     uint32_t L = 1;
     while (L * 16 < a.head_dim) L *= 2;
+    // (where a launch ends, waves take more items in turn)
     // a wave to a token, and below 4096 tokens (four waves a SIMD) its heads shared out as far as that takes
     const uint32_t rounds = ((a.n_q_heads + a.n_k_heads) * L + 63) / 64, splits = (uint32_t)std::min<uint64_t>(rounds, (4095ull + a.n_tokens) / a.n_tokens);
     hipLaunchKernelGGL((qk_norm_rope_wide_kernel<T, P>), dim3((uint32_t)std::min<uint64_t>(((uint64_t)a.n_tokens * splits + 3) / 4, kMostGroups)), dim3(256), P::kLds, st, a,
@@ -1807,7 +1808,7 @@ int32_t ps_tree_attention(const ps_tree_attention_args *a, void *workspace, uint
     for (const int32_t *p : {a->first, a->context, a->parent}) PS_WANT(aligned(p, 4), "first, context and parent must be aligned to 4 bytes");
     PS_WANT(workspace_bytes >= need && (need == 0 || (workspace && aligned(workspace, kAlign))), "a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need);
     const TreeDeal d = tree_deal(*a);
-    PS_WANT((uint64_t)a->n_seq * a->n_kv_heads * d.nsplit * d.blocks < 1ull << 28, "too many sequences and heads for one call");
+    PS_WANT(((uint64_t)a->n_seq * a->n_kv_heads * d.nsplit + 7) / 8 * 8 * d.blocks <= kMostGroups, "too many sequences and heads for one call");
     hipStream_t st = static_cast<hipStream_t>(stream);
     float *part = static_cast<float *>(workspace);
     if (a->type == PS_TYPE_F16) PS_TRY(a->head_dim == 64 ? (launch_trees<f16_t, 64>(*a, d, part, st)) : (launch_trees<f16_t, 128>(*a, d, part, st)));
