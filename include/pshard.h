@@ -686,7 +686,7 @@ int32_t ps_verify_tree(const ps_verify_tree_args *args, void *workspace, uint64_
  * given, the same node twice too; an entry outside 0 .. max_tree - 1, or a row outside 0 .. capacity - 1, is left
  * out (its place keeps what it holds).  cache: n_planes planes of `capacity` rows of row_bytes bytes for each
  * sequence (every layer's and kv head's K and V are planes), strides in BYTES; everything a multiple of 16, row_bytes
- * 16 .. 4096, max_tree <= PS_TREE_MAX.  Rows that are not moved to are left as they were. */
+ * 16 .. 4096, max_tree <= PS_TREE_MAX, n_planes <= 2^26 - 4.  Rows that are not moved to are left as they were. */
 typedef struct ps_cache_keep_args {
     uint32_t n_seq, n_planes, capacity, row_bytes, max_tree, reserved;
     void *cache;

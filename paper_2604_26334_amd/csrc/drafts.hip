@@ -1856,7 +1856,7 @@ int32_t ps_cache_keep(const ps_cache_keep_args *a, void *stream) {
     PS_WANT(a, "NULL argument");
     PS_WANT(a->max_tree <= PS_TREE_MAX, "paths of up to %u entries (got %u)", PS_TREE_MAX, a->max_tree);
     PS_WANT(a->row_bytes >= 16 && a->row_bytes <= 4096 && a->row_bytes % 16 == 0, "row_bytes must be a multiple of 16, up to 4096 (got %u)", a->row_bytes);
-    PS_WANT(a->n_seq <= 65535 && a->n_planes <= 0x7FFFFFFF && a->capacity <= 0x7FFFFFFF, "too many sequences, planes or rows");
+    PS_WANT(a->n_seq <= 65535 && ((uint64_t)a->n_planes + 3) / 4 <= kMostGroups && a->capacity <= 0x7FFFFFFF, "too many sequences, planes or rows");
     if (a->n_seq == 0 || a->n_planes == 0 || a->max_tree == 0 || a->capacity == 0) return PS_OK;
     PS_WANT(a->cache && a->path && a->count && a->context, "NULL argument");
     PS_WANT(aligned(a->cache, 16) && a->seq_stride % 16 == 0 && a->plane_stride % 16 == 0 && a->row_stride % 16 == 0, "the cache and its strides must be multiples of 16 bytes");

@@ -15,3 +15,9 @@ def test_tree_attention_beyond_a_launch(kw):
     n = C.c_uint64()
     assert B.lib().ps_tree_attention_workspace(C.byref(a), C.byref(n)) == 0
     T._refused(B.lib().ps_tree_attention(C.byref(a), T.PTR, 1 << 60, None))
+
+
+@pytest.mark.parametrize("planes", [(1 << 26) - 3, 1 << 26, (1 << 31) - 1, (1 << 32) - 1])
+def test_kept_rows_of_more_planes_than_a_launch_holds(planes):
+    """Four planes to a workgroup of 256 threads."""
+    T._refused(B.lib().ps_cache_keep(C.byref(T._keep(n_planes=planes)), None))
