@@ -1724,6 +1724,7 @@ static int32_t forward_impl(ps_stack *st, const void *x_in, void *x_out, const f
     }
     rc = run_schedule(st, sc, static_cast<const __half *>(x_in), static_cast<__half *>(x_out));
     st->upload = ps::UploadArgs{};      // (issued with the schedule's first kernels, or given up with it)
+    if (rc == PS_OK && st->kv_copied) { PS_HIP(hipEventRecord(st->ev_step, st->compute)); st->step_pending = true; }
     // the buffer is free again once the uploads (compute stream) and the gathers (copy stream) are done
     if (has_copies(sc)) {
         PS_HIP(hipStreamWaitEvent(st->compute, st->ev_ready[0], 0));
