@@ -454,9 +454,10 @@ int32_t ps_stack_load_matrix(ps_stack *st, uint32_t layer, uint32_t mat, uint32_
  * forward attends over; that forward appends its tokens' K and V rows at positions context,
  * context + 1, ... of every head's home (context + tokens <= kv_context), so consecutive decode
  * steps pass context, context + 1, ... (ps_stack_forward_chunked advances the context by itself).
- * Attention (no positional encoding): the token at position p attends over positions 0 .. p -- the
- * cached ones and, in a chunk of several new tokens, the chunk's earlier tokens and itself: scores
- * q.K_j / sqrt(head_dim), softmax, weighted sum of V; query head h uses kv head h / (n_q / n_kv).
+ * Attention (no positional encoding but what ps_stack_set_rotation sets): the token at position p
+ * attends over positions 0 .. p -- the cached ones and, in a chunk of several new tokens, the chunk's
+ * earlier tokens and itself: scores q.K_j / sqrt(head_dim), softmax, weighted sum of V; query head h
+ * uses kv head h / (n_q / n_kv).
  * A streamed cache shard crosses PCIe with its `context` valid rows only. */
 int32_t ps_stack_load_kv(ps_stack *st, uint32_t layer, uint32_t kv_head, const uint16_t *k_rows,
                          const uint16_t *v_rows, uint32_t n_pos);
@@ -600,8 +601,9 @@ void ps_stack_destroy(ps_stack *st);
  *  [n_k_heads][head_dim] with the strides below (dimensions lie together); n_q_heads or n_k_heads may be 0.
  *  head_dim 1 .. 512, rot_dim even, 0 .. head_dim (0: no rotation, inv_freq and positions are not read).
  *  q_gain, k_gain [head_dim] or NULL (gain 1).  q_out may be q and k_out k, with the same strides (in place);
- *  otherwise outputs may not overlap inputs or each other.  Alignment of an element is enough; rows whose
- *  addresses and strides are multiples of 16 bytes are faster. */
+ *  otherwise outputs may not overlap inputs or each other.  Alignment of an element is enough.  Where head_dim and rot_dim are
+ *  multiples of 16 a lane takes 16 dimensions at once; other heads (80 with 40 rotated) go value by value, which is right
+ *  and slower. */
 typedef struct ps_qk_norm_rope_args {
     uint32_t type, n_tokens, n_q_heads, n_k_heads, head_dim, rot_dim, pairs, norm;
     float eps;
@@ -630,7 +632,7 @@ int32_t ps_qk_norm_rope(const ps_qk_norm_rope_args *args, void *stream);
  *  append = 1: the tokens' K and V rows are also written to the cache, row context[s] + t (max_context + max_tree
  *  <= capacity); each sequence's cache must then be its own.  out may not overlap any input.
  * Scores, softmax and sums in fp32; the weights of the value product are rounded to `type`, and the weights' sum is
- * taken of the rounded ones.  ps_tree_attention_workspace: the workspace bytes of these arguments (a function of
+ * taken of the rounded ones (fp16: in steps of at least 2^-34 of the largest, so that many small ones keep their share).  ps_tree_attention_workspace: the workspace bytes of these arguments (a function of
  * the sizes, not of pointers or device values); 256-byte aligned. */
 typedef struct ps_tree_attention_args {
     uint32_t type, n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim;
@@ -664,8 +666,10 @@ int32_t ps_tree_attention(const ps_tree_attention_args *args, void *workspace, u
  * lie in [0, 1).  A logit that is no number counts as -inf, +inf as the largest finite number; a row of -inf alone
  * accepts nothing and its token is -1.  A token outside the vocabulary has probability 0.
  * At most max_children children of a node are tried (1 .. 256; with draft_logits each costs a launch); parents of nodes other than 0
- * that count as none are never reached.  Sums and exponentials are in 64 bits: a border of the running sum lies among
- * a hundred thousand others, and the same inputs give the same tokens whatever the launch.
+ * that count as none are never reached.  Sums are in 64 bits and exponentials right to 4e-11 of each (fp32: 6e-8): a border of the
+ * running sum lies among a hundred thousand others.  A call repeated gives the same tokens; under other sizes (n_seq, max_tree,
+ * draft_logits there or not) the sums are taken in other chunks, and a random number within some 1e-10 of a border may fall
+ * on its other side.
  *  type F16, BF16 or F32 of the logits; rows [n_tokens][vocab] with the strides below, dimensions together;
  *  vocab 1 .. 2^24, alignment of an element is enough.
  *  path [n_seq][max_tree] (path_seq elements apart): the accepted nodes, node 0 first, then -1; count [n_seq]: how
@@ -717,6 +721,10 @@ int32_t ps_stack_set_rotation(ps_stack *st, const ps_rotation *rotation);
  * <= PS_TREE_MAX; x_in, x_out are [n][hidden], router logits [n_layers][n][n_experts], logits of every token [n][vocab]; the one
  * token that ps_stack_set_logits_out may name is one of these n (PS_E_STATE from the forward otherwise, nothing enqueued).
  * All n rows are appended to the cache, node i at position context + i; ps_stack_keep_path puts the accepted ones in place.
+ * A row's bits depend on the number of rows in its tree (the positions' splits go by it), not on where shards lie.  Plans of 256
+ * tokens and more hold no records of splits: a tree's attention there walks the whole context in one workgroup per kv head and
+ * 128 rows (24 rows over 65536 positions, 32 / 8 heads: 1.8 ms a layer in a 512-token plan, 0.1 ms in a 32-token one), so small
+ * trees belong in a tier below 256 tokens.
  * n = 0: chunks again; ps_stack_set_tier does the same.  ps_stack_forward_chunked returns PS_E_STATE while a tree is set.  The
  * last forward's rows are verified and kept before the next tree is set (PS_E_STATE afterwards). */
 int32_t ps_stack_set_tree(ps_stack *st, const int32_t *parents, uint32_t n);

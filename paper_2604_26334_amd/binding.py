@@ -898,9 +898,9 @@ def qk_norm_rope(q, k, positions, inv_freq, q_gain=None, k_gain=None, eps=1e-6, 
 def tree_attention(q, k_new, v_new, k_cache, v_cache, first, context, parent, max_context, max_tree, scale=None, append=False, out=None,
                    workspace=None):
     """ps_tree_attention.  q [tokens, q heads, dim], k_new / v_new [tokens, kv heads, dim], k_cache / v_cache [sequences, kv heads,
-    capacity, dim] of one type (last dimension contiguous, other strides free); first int32 [sequences + 1], context int32
-    [sequences], parent int32 [tokens].  max_context, max_tree: bounds on context and on the tokens of a sequence.  Returns out
-    [tokens, q heads, dim]: the given tensor, or a new one (whose rows of no sequence hold anything)."""
+    capacity, dim] of one type (last dimension contiguous; addresses and other strides multiples of 16 bytes); first int32
+    [sequences + 1], context int32 [sequences], parent int32 [tokens].  max_context, max_tree: bounds on context and on the tokens of a
+    sequence.  Returns out [tokens, q heads, dim]: the given tensor, or a new one (whose rows of no sequence hold anything)."""
     import torch
     _want(q.dim() == 3 and k_new.dim() == 3 and k_cache.dim() == 4, "q, k_new are [tokens, heads, dim], the caches [sequences, heads, capacity, dim]")
     n, hq, d = q.shape
@@ -959,8 +959,8 @@ def verify_tree(target_logits, token, parent, first, u_accept, u_sample, draft_l
 
 
 def cache_keep(cache, path, count, context):
-    """ps_cache_keep, in place.  cache [sequences, planes, capacity, dim] of any type (rows contiguous, other strides free); path int32
-    [sequences, max_tree], count, context int32 [sequences], as verify_tree and tree_attention have them.  Returns cache."""
+    """ps_cache_keep, in place.  cache [sequences, planes, capacity, dim] of any type (rows contiguous, their size, address and other strides
+    multiples of 16 bytes); path int32 [sequences, max_tree], count, context int32 [sequences], as verify_tree and tree_attention have them.  Returns cache."""
     import torch
     _want(cache.dim() == 4 and path.dim() == 2, "cache is [sequences, planes, capacity, dim], path [sequences, max_tree]")
     b, planes, cap, d = cache.shape

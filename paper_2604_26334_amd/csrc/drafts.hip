@@ -886,6 +886,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(ps_tree_attention_args 
 // sums between its two kinds of them in every tile).  Positions: as many splits as bring the launch to the workgroups the chip holds
 // at once (two per CU, by registers), none of less than four units of 32 or two of 64; for several sequences, whose lengths differ, twice as many
 // (16 sequences of 17 tokens, lengths of 600 to 8190, 57 -> 48 us, 32 of 8 tokens 87 -> 82; eight of one length 62 -> 70).
+// The kernels then give each split ceil(units / splits), so fewer may have work: 24 tokens over 4096 positions are 65 steps in up to 32 splits, and
+// 22 of them take 3 each (176 workgroups; 80 more return at once).
 TreeDeal tree_deal(const ps_tree_attention_args &a) {
     TreeDeal d;
     const uint32_t rows = std::max(1u, a.max_tree) * (a.n_q_heads / a.n_kv_heads);
@@ -940,7 +942,7 @@ hipError_t launch_trees(const ps_tree_attention_args &a, const TreeDeal &d, floa
 //                       children are refused and that the walk may still reach
 //  verify_draw_kernel   every workgroup works out the same walk; chunk sums of what is left to draw from behind its last node
 //  verify_pick_kernel   the chunk that the random number falls into, and the index in it
-// Exponentials and sums are in 64 bits: with fp32's 2^-24 a border of the running sum moves by as much as a hundred thousandth of
+// Sums are in 64 bits, exponentials to 4e-11 of each: with fp32's 2^-24 a border of the running sum moves by as much as a hundred thousandth of
 // the vocabulary's entries weigh.  A 64-bit operation takes this machine 5.3 clocks of a wave, a 32-bit one 4.3; an exponential
 // here is about 15 of them, which in a large batch takes longer than the row's bytes do.  No result depends on the order of workgroups.
 // 32 trees of up to 32 nodes, two drafts a node, 128256 entries, drafts' logits: 80 + 22 + 19 + 9 us (205 MB: 42 us as bytes, about 77 as
@@ -1711,6 +1713,7 @@ static ps_tree_attention_args stack_tree_call(const StackTreeArgs &s, uint32_t n
     a.out_head = 128;
     return a;
 }
+// (part_bytes: the plan's room for records.  Plans of kAttnOnePassTokens tokens and more have none, and their trees no splits)
 uint32_t stack_tree_splits(uint32_t n_q, uint32_t n_kv, uint32_t ctx, uint32_t n_tokens, uint64_t part_bytes) {
     ps_tree_attention_args a{};
     a.n_seq = 1; a.max_tree = n_tokens; a.n_q_heads = n_q; a.n_kv_heads = n_kv; a.max_context = ctx;
