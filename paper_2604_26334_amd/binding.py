@@ -610,7 +610,8 @@ class Stack:
     def verify_tree(self, token, u_accept, u_sample, draft_logits=None, temperature=None, max_children=PS_TREE_MAX, path=None, count=None,
                     next_token=None, workspace=None):
         """ps_stack_verify_tree over the last forward's logits, on self.compute: token int32, u_accept float32 [rows], u_sample, temperature
-        float32 [1] (CUDA tensors, ready on self.compute), draft_logits float16 [rows, vocab].  Returns (path [rows], count [1], next_token [1])."""
+        float32 [1] (CUDA tensors, ready on self.compute), draft_logits float16 [rows, vocab].  max_children: the most that a node has, or
+        that are tried (with draft_logits each up to the tree's size costs a launch).  Returns (path [rows], count [1], next_token [1])."""
         torch, dev, n, i32 = self.torch, self.arena.device, token.numel(), self.torch.int32
         with torch.cuda.device(dev), torch.cuda.stream(self.compute):
             path = torch.empty(n, dtype=i32, device=dev) if path is None else path
@@ -930,7 +931,8 @@ def tree_attention(q, k_new, v_new, k_cache, v_cache, first, context, parent, ma
 def verify_tree(target_logits, token, parent, first, u_accept, u_sample, draft_logits=None, temperature=None, max_tree=PS_TREE_MAX,
                 max_children=PS_TREE_MAX, path=None, count=None, next_token=None, workspace=None):
     """ps_verify_tree.  target_logits (and draft_logits) [tokens, vocab] of one type; token, parent int32 [tokens]; first int32
-    [sequences + 1]; u_accept float32 [tokens], u_sample float32 [sequences], temperature float32 [sequences] or None.  Returns
+    [sequences + 1]; u_accept float32 [tokens], u_sample float32 [sequences], temperature float32 [sequences] or None.  max_tree, max_children:
+    bounds on a sequence's tokens and a node's children (with draft_logits each child up to them costs a launch).  Returns
     (path int32 [sequences, max_tree], count int32 [sequences], next_token int32 [sequences])."""
     import torch
     _want(target_logits.dim() == 2, "logits are [tokens, vocab]")
