@@ -749,6 +749,120 @@ int32_t ps_stack_verify_tree(ps_stack *st, const ps_stack_verify_args *args, voi
  * forward (PS_E_STATE otherwise). */
 int32_t ps_stack_keep_path(ps_stack *st, const int32_t *path, const int32_t *count);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators of a step that answers a BATCH OF REQUESTS over one paged cache.  The cache is a pool of pages of `page`
+ * positions each (a power of two, 16 .. 1024); position i of a sequence is row i % page of the page that entry i / page of the
+ * sequence's row of a table names.  Sequences that begin with the same text form a group and share the pages of that
+ * prefix: a token's positions are its group's prefix and, behind it, the sequence's own.  A step: ps_page_tables gives
+ * the new tokens their places, ps_page_append writes their keys and values there (every layer), ps_page_attention
+ * answers them (every layer), ps_sample draws each sequence's next token.
+ *
+ * As with the operators above: device pointers of the stream's device, which must be the current one, asynchronous, no
+ * allocation, no memory written but outputs and workspace, capturable (kernel nodes only); calls that may overlap in time need
+ * workspaces of their own.  Sequence s owns rows first[s] .. first[s + 1] - 1 of the token arrays, rows from first[n_seq] on are
+ * neither read nor written.  Device values are bounded by the kernels: first is clamped to 0 .. n_tokens, lengths to
+ * 0 .. their bound; a page number outside 0 .. n_pages - 1 names nothing (its positions are seen by no token and take
+ * no rows). */
+
+/* Places of a step's new tokens.  Sequence s holds cached[s] positions and gets new_tokens[s] more:
+ *   first[s] = sum of new_tokens in front of s (first[n_seq]: all of them), length[s] = cached[s] + new_tokens[s],
+ *   position[t] = offset[s] + cached[s] + i for token t = first[s] + i (offset NULL: 0; a prefix's length makes it the position
+ *   behind the prefix), slot[t] = table[s][j / page] * page + j % page with j = cached[s] + i.
+ * Entries ceil(cached[s] / page) .. ceil(length[s] / page) - 1 of the table's row are written: pages taken from free_pages
+ * in the order of the sequences and their positions, from free_pages[free_at[0]] on; taken[0]: how many they need.  Where the
+ * list has no more (or names no page) the entry is -1 and its tokens' slots are -1, as are those of tokens behind the
+ * table's width; taken counts what was needed, so free_at[0] + taken[0] > n_free says that the list was short.  The other entries
+ * are not written.  Negative lengths count as 0, lengths end at 2^30; tokens beyond n_tokens are left out (first ends at n_tokens).
+ * A call repeated on the same lengths gives the same results, the table's among them.
+ *  n_seq <= 8192, n_tokens <= 2^30, n_pages * page <= 2^31; table [n_seq][width], rows table_seq elements apart.  No output may overlap
+ *  an input or another output. */
+typedef struct ps_page_tables_args {
+    uint32_t n_seq, n_tokens, page, width, n_pages, n_free;
+    const int32_t *cached, *new_tokens; /* [n_seq] */
+    const int32_t *offset;              /* [n_seq] or NULL */
+    const int32_t *free_pages;          /* [n_free] */
+    const int32_t *free_at;             /* [1], or NULL: 0 */
+    int32_t *table;
+    uint64_t table_seq;
+    int32_t *first, *length;   /* [n_seq + 1], [n_seq] */
+    int32_t *position, *slot;  /* [n_tokens] each; position may be NULL */
+    int32_t *taken;            /* [1] */
+} ps_page_tables_args;
+int32_t ps_page_tables(const ps_page_tables_args *args, void *stream);
+
+/* Rows of new tokens to their places: k[t][h] -> row slot[t] % page of head h of page slot[t] / page of k_pages, v likewise; a slot
+ * outside 0 .. n_pages * page - 1 is left out.  Two tokens of one call must not have the same slot (the row then holds pieces of
+ * either).  Rows of row_bytes bytes of any type; strides in BYTES; everything a multiple of 16, row_bytes 16 .. 4096.  Inputs and
+ * pages must not overlap. */
+typedef struct ps_page_append_args {
+    uint32_t n_tokens, n_heads, row_bytes, page, n_pages, reserved;
+    const void *k, *v;
+    void *k_pages, *v_pages;
+    uint64_t k_token, k_head, v_token, v_head;
+    uint64_t k_page, k_page_head, k_page_row, v_page, v_page_head, v_page_row;
+    const int32_t *slot; /* [n_tokens] */
+} ps_page_append_args;
+int32_t ps_page_append(const ps_page_append_args *args, void *stream);
+
+/* Attention of a batch over the paged cache, causal inside a sequence's new tokens, which lie in the cache already: token i of the n of
+ * sequence s sees the positions of its group's prefix and own positions 0 .. length[s] - n + i:
+ *   out[t][h] = sum_j w_j v_j,  w = softmax(scale q[t][h] . k_j),  kv head h / (n_q_heads / n_kv_heads)
+ * A token that sees no position (length 0, or less than n of them, and no prefix; pages that name nothing), and one whose
+ * weights are all zero, gets zeros.  A key or value that is infinite or no number reaches only the tokens that see it.
+ *  group_first [n_prefix + 1]: sequences group_first[p] .. group_first[p + 1] - 1 stand behind prefix p (ascending, so a group's
+ *  sequences follow one another; sequences of no group have no prefix); prefix_length [n_prefix], prefix_table [n_prefix]
+ *  [prefix_width]; n_prefix may be 0 (all three NULL).  length [n_seq] counts own positions, the new tokens' among them; table
+ *  [n_seq][width].  A group's prefix is read once for all of its tokens where sequences have few of them (up to 32 rows of a kv
+ *  head each), and once for each 128 rows where they have more.
+ *  type F16 or BF16; head_dim 64 or 128; page a power of two, 16 .. 1024.  q, out [n_tokens][n_q_heads][head_dim], pages
+ *  [n_pages][n_kv_heads][page][head_dim], all with the strides below (any order of pages, heads and rows); every address and
+ *  stride in bytes a multiple of 16, 16 rows of a page span less than 2 GiB.  max_length <= width * page, max_prefix <= prefix_width * page
+ *  and max_tokens: bounds on length, prefix_length and a sequence's tokens (what lies beyond is left out: tokens beyond max_tokens
+ *  are not written); work is dealt out by them.  n_prefix <= 4096, n_seq <= 65535; out may not overlap any input.
+ * Scores, softmax and sums in fp32; the weights of the value product are rounded to `type`, and their sum is taken of the rounded
+ * ones (fp16: in steps of at least 2^-34 of the largest).  A call repeated gives the same bits; under other bounds or batches sums are
+ * taken in other runs.  ps_page_attention_workspace: bytes for these arguments (a function of sizes alone); 256-byte aligned. */
+typedef struct ps_page_attention_args {
+    uint32_t type, n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, page, n_pages;
+    uint32_t width, n_prefix, prefix_width, max_length, max_prefix, max_tokens;
+    float scale;
+    uint32_t reserved;
+    const void *q, *k_pages, *v_pages;
+    void *out;
+    uint64_t q_token, q_head, k_page, k_head, k_row, v_page, v_head, v_row, out_token, out_head;
+    uint64_t table_seq, prefix_seq; /* elements between two rows of the tables */
+    const int32_t *first;           /* [n_seq + 1] */
+    const int32_t *length;          /* [n_seq] */
+    const int32_t *table, *group_first, *prefix_length, *prefix_table;
+} ps_page_attention_args;
+int32_t ps_page_attention_workspace(const ps_page_attention_args *args, uint64_t *bytes);
+int32_t ps_page_attention(const ps_page_attention_args *args, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Next tokens from given random numbers.  A row's entries in order: larger logits first, the lower index first among equals;
+ * w_i = exp((x_i - max) / T), C(r) = the sum of the first r weights in that order.  Kept are the first n entries:
+ *   n = min(n_k, n_p, n_m), at least 1:  n_k = top_k (0 or less: all), n_p = the least r with C(r) >= top_p C(n_k) (1 or more: all),
+ *   n_m = how many weights are at least min_p (0 or less: all); and entries of -inf are never kept
+ * and the token is the first entry of the order with C(r) > u C(n): every kept entry is drawn with its share of the kept
+ * weights.  T = temperature[row] (NULL: 1); T <= 0 or not a number: the first entry of the order.  top_k, top_p and min_p may be NULL
+ * (all kept); top_p or min_p that is no number keeps all.  u in [0, 1).  A logit that is no number counts as -inf, +inf as the largest
+ * finite number; a row of -inf alone gives token -1, of none kept.
+ * Weights are right to 4e-11 of each and added as whole numbers of 2^-(62 - log2 vocab) (2^-45 at 131072 entries) in 64 bits, so
+ * sums do not depend on their order: a row's result is the same in any batch, stride or type that holds its values.
+ *  type F16, BF16 or F32; rows [n_rows][vocab], logits_row elements apart, alignment of an element is enough; vocab 1 .. 2^24;
+ *  n_rows <= 65535.  token, kept [n_rows]; kept (n of each row) may be NULL. */
+typedef struct ps_sample_args {
+    uint32_t type, n_rows, vocab, reserved;
+    const void *logits;
+    uint64_t logits_row;
+    const float *u;           /* [n_rows] */
+    const float *temperature; /* [n_rows] or NULL */
+    const int32_t *top_k;     /* [n_rows] or NULL */
+    const float *top_p, *min_p;
+    int32_t *token, *kept;
+} ps_sample_args;
+int32_t ps_sample_workspace(const ps_sample_args *args, uint64_t *bytes);
+int32_t ps_sample(const ps_sample_args *args, void *workspace, uint64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -126,6 +126,33 @@ class ps_cache_keep_args(C.Structure):
                [(n, C.c_void_p) for n in ("path", "count", "context")]
 
 
+class ps_page_tables_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("n_seq", "n_tokens", "page", "width", "n_pages", "n_free")] + \
+               [(n, C.c_void_p) for n in ("cached", "new_tokens", "offset", "free_pages", "free_at", "table")] + [("table_seq", C.c_uint64)] + \
+               [(n, C.c_void_p) for n in ("first", "length", "position", "slot", "taken")]
+
+
+class ps_page_append_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("n_tokens", "n_heads", "row_bytes", "page", "n_pages", "reserved")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "k_pages", "v_pages")] + \
+               [(n, C.c_uint64) for n in ("k_token", "k_head", "v_token", "v_head", "k_page", "k_page_head", "k_page_row", "v_page",
+                                          "v_page_head", "v_page_row")] + [("slot", C.c_void_p)]
+
+
+class ps_page_attention_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "n_seq", "n_tokens", "n_q_heads", "n_kv_heads", "head_dim", "page", "n_pages", "width",
+                                          "n_prefix", "prefix_width", "max_length", "max_prefix", "max_tokens")] + \
+               [("scale", C.c_float), ("reserved", C.c_uint32)] + [(n, C.c_void_p) for n in ("q", "k_pages", "v_pages", "out")] + \
+               [(n, C.c_uint64) for n in ("q_token", "q_head", "k_page", "k_head", "k_row", "v_page", "v_head", "v_row", "out_token", "out_head",
+                                          "table_seq", "prefix_seq")] + \
+               [(n, C.c_void_p) for n in ("first", "length", "table", "group_first", "prefix_length", "prefix_table")]
+
+
+class ps_sample_args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "n_rows", "vocab", "reserved")] + [("logits", C.c_void_p), ("logits_row", C.c_uint64)] + \
+               [(n, C.c_void_p) for n in ("u", "temperature", "top_k", "top_p", "min_p", "token", "kept")]
+
+
 class ps_rotation(C.Structure):
     _fields_ = [(n, C.c_uint32) for n in ("rot_dim", "pairs", "norm", "reserved")] + [(n, C.c_void_p) for n in ("inv_freq", "q_gain", "k_gain")]
 
@@ -146,7 +173,8 @@ EXPORTS = ["ps_stack_set_rotation", "ps_stack_set_tree", "ps_stack_verify_worksp
            "ps_stack_set_logits_out", "ps_cpu_matmul", "ps_plan_create_kind", "ps_stack_set_cpu_threads",
            "ps_tier_table_create_kind", "ps_tier_table_create_db", "ps_profile_db_create", "ps_profile_db_destroy", "ps_profile_db_add",
            "ps_profile_db_count", "ps_profile_db_get", "ps_profile_db_estimate", "ps_profile_db_save",
-           "ps_profile_db_load", "ps_profile_db_measure", "ps_plan_create_db"]
+           "ps_profile_db_load", "ps_profile_db_measure", "ps_plan_create_db", "ps_page_tables", "ps_page_append", "ps_page_attention_workspace",
+           "ps_page_attention", "ps_sample_workspace", "ps_sample"]
 
 _lib = None
 
@@ -226,6 +254,12 @@ def lib():
             "ps_verify_tree_workspace": [C.POINTER(ps_verify_tree_args), C.POINTER(u64)],
             "ps_verify_tree": [C.POINTER(ps_verify_tree_args), vp, u64, vp],
             "ps_cache_keep": [C.POINTER(ps_cache_keep_args), vp],
+            "ps_page_tables": [C.POINTER(ps_page_tables_args), vp],
+            "ps_page_append": [C.POINTER(ps_page_append_args), vp],
+            "ps_page_attention_workspace": [C.POINTER(ps_page_attention_args), C.POINTER(u64)],
+            "ps_page_attention": [C.POINTER(ps_page_attention_args), vp, u64, vp],
+            "ps_sample_workspace": [C.POINTER(ps_sample_args), C.POINTER(u64)],
+            "ps_sample": [C.POINTER(ps_sample_args), vp, u64, vp],
             "ps_stack_set_rotation": [vp, C.POINTER(ps_rotation)],
             "ps_stack_set_tree": [vp, vp, u32],
             "ps_stack_verify_workspace": [vp, C.POINTER(ps_stack_verify_args), C.POINTER(u64)],
@@ -792,7 +826,8 @@ def load_synthetic(stacks, cfg, seed, threads=8, lookahead=12, progress=None):
 
 
 # ---------------------------------------------------------------- operators on device tensors
-# Thin forms of ps_qk_norm_rope, ps_tree_attention, ps_verify_tree and ps_cache_keep: torch CUDA tensors in, launched on the
+# Thin forms of ps_qk_norm_rope, ps_tree_attention, ps_verify_tree, ps_cache_keep, ps_page_tables, ps_page_append, ps_page_attention and
+# ps_sample: torch CUDA tensors in, launched on the
 # current stream of their device; outputs (and workspaces, unless given) come from torch's allocator on that stream.
 
 _TYPE = {}
@@ -973,3 +1008,109 @@ def cache_keep(cache, path, count, context):
                            path.data_ptr(), _table("count", count, b, torch.int32, dev), _table("context", context, b, torch.int32, dev))
     _launch(dev, lib().ps_cache_keep, C.byref(a))
     return cache
+
+
+def page_tables(cached, new_tokens, table, free_pages, free_at, page, n_pages, n_tokens, offset=None, first=None, length=None, position=None,
+                slot=None, taken=None):
+    """ps_page_tables.  cached, new_tokens (and offset) int32 [sequences]; table int32 [sequences, width], extended in place; free_pages int32
+    [free], free_at int32 [1] or None (0); page: positions of a page, n_pages: pages of the pool, n_tokens: room for tokens (at least the sum of
+    new_tokens; the rest is left as it is).  Returns (first [sequences + 1], length [sequences], position [n_tokens], slot [n_tokens], taken [1]):
+    new int32 tensors, or the given ones."""
+    import torch
+    _want(cached.dim() == 1 and table.dim() == 2 and free_pages.dim() == 1, "cached is [sequences], table [sequences, width], free_pages [free]")
+    b, dev, i32, n = cached.shape[0], cached.device, torch.int32, int(n_tokens)
+    _want(n >= 0, "n_tokens must not be negative")
+    _same("table", table, (b, table.shape[1]), i32, dev)
+    first = torch.empty(b + 1, dtype=i32, device=dev) if first is None else first
+    length = torch.empty(b, dtype=i32, device=dev) if length is None else length
+    position = torch.empty(n, dtype=i32, device=dev) if position is None else position
+    slot = torch.empty(n, dtype=i32, device=dev) if slot is None else slot
+    taken = torch.empty(1, dtype=i32, device=dev) if taken is None else taken
+    a = ps_page_tables_args(
+        b, n, int(page), table.shape[1], int(n_pages), free_pages.shape[0], _table("cached", cached, b, i32, dev),
+        _table("new_tokens", new_tokens, b, i32, dev), None if offset is None else _table("offset", offset, b, i32, dev),
+        _table("free_pages", free_pages, free_pages.shape[0], i32, dev), None if free_at is None else _table("free_at", free_at, 1, i32, dev),
+        table.data_ptr(), _rows("table", table)[0], _table("first", first, b + 1, i32, dev), _table("length", length, b, i32, dev),
+        _table("position", position, n, i32, dev), _table("slot", slot, n, i32, dev), _table("taken", taken, 1, i32, dev))
+    _launch(dev, lib().ps_page_tables, C.byref(a))
+    return first, length, position, slot, taken
+
+
+def page_append(k, v, k_pages, v_pages, slot):
+    """ps_page_append, in place.  k, v [tokens, heads, dim], k_pages, v_pages [pages, heads, page, dim] of one type (rows contiguous, their size,
+    addresses and other strides multiples of 16 bytes); slot int32 [tokens], as page_tables gives it.  Returns (k_pages, v_pages)."""
+    import torch
+    _want(k.dim() == 3 and k_pages.dim() == 4, "k is [tokens, heads, dim], pages [pages, heads, page, dim]")
+    n, h, d = k.shape
+    dev, dt, e = k.device, k.dtype, k.element_size()
+    pages, page = k_pages.shape[0], k_pages.shape[2]
+    _same("v", v, (n, h, d), dt, dev)
+    _same("k_pages", k_pages, (pages, h, page, d), dt, dev)
+    _same("v_pages", v_pages, (pages, h, page, d), dt, dev)
+    sk, sv, ck, cv = _rows("k", k), _rows("v", v), _rows("k_pages", k_pages), _rows("v_pages", v_pages)
+    a = ps_page_append_args(n, h, d * e, page, pages, 0, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                            sk[0] * e, sk[1] * e, sv[0] * e, sv[1] * e, ck[0] * e, ck[1] * e, ck[2] * e, cv[0] * e, cv[1] * e, cv[2] * e,
+                            _table("slot", slot, n, torch.int32, dev))
+    _launch(dev, lib().ps_page_append, C.byref(a))
+    return k_pages, v_pages
+
+
+def page_attention(q, k_pages, v_pages, first, length, table, max_length, max_tokens, group_first=None, prefix_length=None, prefix_table=None,
+                   max_prefix=0, scale=None, out=None, workspace=None):
+    """ps_page_attention.  q [tokens, q heads, dim], k_pages, v_pages [pages, kv heads, page, dim] of one type (last dimension contiguous;
+    addresses and other strides multiples of 16 bytes); first int32 [sequences + 1], length int32 [sequences], table int32 [sequences, width];
+    group_first int32 [prefixes + 1], prefix_length int32 [prefixes], prefix_table int32 [prefixes, width], or all three None.  max_length,
+    max_prefix, max_tokens: bounds on length, prefix_length and the tokens of a sequence.  Returns out [tokens, q heads, dim]: the given
+    tensor, or a new one (whose rows of no sequence hold anything)."""
+    import torch
+    _want(q.dim() == 3 and k_pages.dim() == 4 and table.dim() == 2, "q is [tokens, heads, dim], pages [pages, heads, page, dim], table [sequences, width]")
+    n, hq, d = q.shape
+    dev, dt, i32 = q.device, q.dtype, torch.int32
+    ty = _type_of(q)
+    pages, hk, page = k_pages.shape[0], k_pages.shape[1], k_pages.shape[2]
+    b, width = table.shape
+    _same("k_pages", k_pages, (pages, hk, page, d), dt, dev)
+    _same("v_pages", v_pages, (pages, hk, page, d), dt, dev)
+    _same("table", table, (b, width), i32, dev)
+    _want((group_first is None) == (prefix_length is None) == (prefix_table is None), "group_first, prefix_length and prefix_table come together")
+    p = pw = ps = 0
+    if group_first is not None:
+        _want(prefix_table.dim() == 2, "prefix_table is [prefixes, width]")
+        p, pw = prefix_table.shape
+        _same("prefix_table", prefix_table, (p, pw), i32, dev)
+        ps = _rows("prefix_table", prefix_table)[0]
+    out = _like("out", out, q)
+    sq, so, ck, cv = _rows("q", q), _rows("out", out), _rows("k_pages", k_pages), _rows("v_pages", v_pages)
+    a = ps_page_attention_args(
+        ty, b, n, hq, hk, d, page, pages, width, p, pw, int(max_length), int(max_prefix), int(max_tokens), d ** -0.5 if scale is None else scale, 0,
+        q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(), sq[0], sq[1], ck[0], ck[1], ck[2], cv[0], cv[1], cv[2], so[0], so[1],
+        _rows("table", table)[0], ps, _table("first", first, b + 1, i32, dev), _table("length", length, b, i32, dev), table.data_ptr(),
+        None if not p else _table("group_first", group_first, p + 1, i32, dev), None if not p else _table("prefix_length", prefix_length, p, i32, dev),
+        None if not p else prefix_table.data_ptr())
+    need = C.c_uint64()
+    _check(lib().ps_page_attention_workspace(C.byref(a), C.byref(need)))
+    at, size, _held = _workspace(need.value, workspace, dev)
+    _launch(dev, lib().ps_page_attention, C.byref(a), at, size)
+    return out
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, kept=None, workspace=None):
+    """ps_sample.  logits [rows, vocab] (float16, bfloat16 or float32; last dimension contiguous); u float32 [rows]; temperature, top_p, min_p
+    float32 [rows] and top_k int32 [rows], or None.  Returns (token int32 [rows], kept int32 [rows]): new tensors, or the given ones."""
+    import torch
+    _want(logits.dim() == 2, "logits are [rows, vocab]")
+    n, v = logits.shape
+    dev, i32, f32 = logits.device, torch.int32, torch.float32
+    ty = _type_of(logits)
+    token = torch.empty(n, dtype=i32, device=dev) if token is None else token
+    kept = torch.empty(n, dtype=i32, device=dev) if kept is None else kept
+    a = ps_sample_args(
+        ty, n, v, 0, logits.data_ptr(), _rows("logits", logits)[0], _table("u", u, n, f32, dev),
+        None if temperature is None else _table("temperature", temperature, n, f32, dev), None if top_k is None else _table("top_k", top_k, n, i32, dev),
+        None if top_p is None else _table("top_p", top_p, n, f32, dev), None if min_p is None else _table("min_p", min_p, n, f32, dev),
+        _table("token", token, n, i32, dev), _table("kept", kept, n, i32, dev))
+    need = C.c_uint64()
+    _check(lib().ps_sample_workspace(C.byref(a), C.byref(need)))
+    at, size, _held = _workspace(need.value, workspace, dev)
+    _launch(dev, lib().ps_sample, C.byref(a), at, size)
+    return token, kept
