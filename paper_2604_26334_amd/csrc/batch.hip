@@ -110,61 +110,590 @@ __global__ __launch_bounds__(256) void page_append_kernel(ps_page_append_args a,
 }
 
 // ------------------------------------------------------------------------------------ attention
-// a wave per (token, query head): 64 positions at a time, a lane's whole dot product each, then the values' dimensions by lane
-template <typename T, int D>
-__global__ __launch_bounds__(256) void page_attention_kernel(ps_page_attention_args a, uint32_t shift) {
-    constexpr int E = D / 64;
-    const uint32_t lane = threadIdx.x & 63, hb = (a.n_q_heads + 3) / 4;
-    const uint32_t h = blockIdx.x % hb * 4 + (threadIdx.x >> 6), i = blockIdx.x / hb % a.max_tokens, s = blockIdx.x / hb / a.max_tokens;
-    const int row0 = clampi(a.first[s], 0, (int)a.n_tokens), n = clampi(a.first[s + 1], 0, (int)a.n_tokens) - row0;
-    if (h >= a.n_q_heads || (int)i >= n) return;
-    const int length = clampi(a.length[s], 0, (int)a.max_length);
-    int group = -1;
-    for (uint32_t p0 = 0; p0 < a.n_prefix && group < 0; p0 += 64) {
-        const uint32_t p = p0 + lane;
-        const uint64_t in = __ballot(p < a.n_prefix && a.group_first[p] <= (int)s && (int)s < a.group_first[p + 1]);
-        if (in) group = (int)p0 + __ffsll((unsigned long long)in) - 1;
+// Score rows are (token, query head of the kv group) pairs.  Two forms of a task, a workgroup of four waves each:
+//  rows_few   up to NT x 16 rows over a run of positions: the waves take tiles of 32 positions in turn, each with a running maximum,
+//             weight sum and value sums of its own, and meet in LDS at the end.  Bound by the cache's bytes.
+//  rows_many  128 rows, 32 a wave, over a run of steps of 64 positions, whose K and V rows all four waves read from LDS (two stages, one
+//             barrier a step, rows requested two steps ahead).  Bound by matrix products and exponentials.
+// Products:
+//  scores, transposed: S^T = K Q^T, A = 16 positions x 32 dims of K, B = 16 rows of queries: lane (row i, c) then holds four positions of
+//   row i, 4 c .. 4 c + 3 of each half tile of 16;
+//  weights x values, transposed: O^T = V^T P^T, B = the weights exactly as the score accumulators hold them, A = 16 dims x 32 positions of V
+//   by LDS transpose reads of rows 4 c .. 4 c + 3 of each half; and the weights' sum by one more product, with ones.
+// Half a tile never crosses a page (pages are multiples of 16 positions): its rows come through a buffer whose range ends with the sequence or
+// is empty where the table names no page, so nothing else is ever read and hidden values are zeros.  A wave keeps the
+// next 64 entries of its table in a register, one a lane.
+// Sequences of few tokens (up to 32 rows of a kv head): a group's prefix is walked once for all of its rows (rows_many, or rows_few where the
+// whole group has few), and each sequence's own positions by rows_few; both in one launch, alternating, so that a CU holds products and
+// loads at the same time, and a merge of their records.  More tokens: blocks of 128 rows walk prefix and own positions one after the other.
+constexpr uint32_t kTile = 32, kStep = 64;
+constexpr uint32_t kFewRows = 32;
+
+// 16-byte piece u of a staged row lies in slot u ^ swizzle, so that the rows that are read together lie in different banks: V rows 0 .. 7 (in
+// pairs of pieces), K rows 0 .. 15
+template <int D> __device__ __forceinline__ uint32_t v_slot(uint32_t row) { return D == 128 ? (row & 7u) << 1 : (row >> 1 & 3u) << 1; }
+template <int D> __device__ __forceinline__ uint32_t k_slot(uint32_t row) { return D == 128 ? row & 15u : row >> 1 & 7u; }
+
+struct PageDeal {
+    uint32_t shared;             // 1: prefixes for all their tokens at once; 0: blocks of 128 rows of a sequence
+    uint32_t nt;                 // rows of a sequence, in 16 (shared)
+    uint32_t blocks;             // of 128 rows: of all groups at most (shared), of a sequence
+    uint32_t psplit, plen;       // runs of a prefix, positions of a run (shared)
+    uint32_t osplit, olen;       // runs of own positions (shared), or of a sequence's steps
+    uint32_t direct;             // no records: the result itself
+};
+template <int D, int NT> constexpr uint32_t few_lds() { return std::max<uint32_t>(4 * kTile * D * 2, 4 * NT * 16 * (D + 4) * 4 + 4 * NT * 16 * 2 * 4) + 16; }
+template <int D> constexpr uint32_t many_lds() { return 2 * 2 * kStep * D * 2 + 16; }
+
+struct RowSet { int token0; uint32_t rows, group; };             // rows of consecutive tokens, `group` query heads each
+struct Span {                                                    // positions that one table names
+    const int32_t *table;
+    int entries, len;                                            // entries of the table, positions
+};
+
+// page numbers of a table, 64 at a time, one a lane; -1: none
+struct PageWindow {
+    int number, base;
+    __device__ __forceinline__ void fill(const Span &s, int entry, uint32_t n_pages) {
+        base = entry;
+        const int at = entry + (int)(threadIdx.x & 63);
+        number = at < s.entries ? s.table[at] : -1;
+        if (number < 0 || number >= (int)n_pages) number = -1;
     }
-    const uint32_t hk = h / (a.n_q_heads / a.n_kv_heads);
-    const size_t token = (size_t)row0 + i;
-    const T *q = static_cast<const T *>(a.q) + token * a.q_token + h * a.q_head;
-    float m = -INFINITY, l = 0.f, o[E] = {};
-    for (int part = 0; part < 2; ++part) {
-        if (part == 0 && group < 0) continue;
-        const int limit = part ? max(0, length - n + (int)i + 1) : clampi(a.prefix_length[group], 0, (int)a.max_prefix);
-        const int32_t *table = part ? a.table + s * a.table_seq : a.prefix_table + group * a.prefix_seq;
-        for (int p0 = 0; p0 < limit; p0 += 64) {
-            const int pos = p0 + (int)lane;
-            const int number = pos < limit ? table[pos >> shift] : -1;
-            const bool seen = number >= 0 && number < (int)a.n_pages;
-            float z = -INFINITY;
-            if (seen) {
-                const T *k = static_cast<const T *>(a.k_pages) + number * a.k_page + hk * a.k_head + (uint64_t)(pos & ((1 << shift) - 1)) * a.k_row;
-                float dot = 0.f;
-                for (int d = 0; d < D; ++d) dot = fmaf(to_f(q[d]), to_f(k[d]), dot);
-                z = dot * a.scale;
+    __device__ __forceinline__ int operator()(int entry) const { return __builtin_amdgcn_readlane(number, entry - base); }
+};
+
+// Sixteen positions from P on (one half tile) of one kv head as a buffer: empty where no page is named or the positions have ended
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_rows(const char *pages, uint64_t page_b, uint32_t row_b, int number, int P, uint32_t mask, int n, uint32_t bytes) {
+    const uint64_t at = (uint64_t)max(number, 0) * page_b + (uint64_t)((uint32_t)P & mask) * row_b;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pages + at), 0, number >= 0 && n > 0 ? (int)((uint32_t)(min(n, 16) - 1) * row_b + bytes) : 0, 0x00020000);
+}
+__device__ __forceinline__ u4_t piece_of(__amdgpu_buffer_rsrc_t rows, uint32_t offset) { return __builtin_bit_cast(u4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 0, 0)); }
+
+// Values that are infinite or no number and that a row sees: what the products had zeros for (positions from .. to - 1 of a span)
+template <typename T, int N>
+__device__ __forceinline__ void add_wild(const ps_page_attention_args &a, const Span &s, uint32_t shift, uint32_t hk, int from, int to, uint32_t d0, float (&o)[N]) {
+    for (int j = from; j < to; ++j) {
+        const int number = s.table[j >> shift];
+        if (number < 0 || number >= (int)a.n_pages) continue;
+        const T *v = static_cast<const T *>(a.v_pages) + (uint64_t)number * a.v_page + hk * a.v_head + (uint64_t)((uint32_t)j & ((1u << shift) - 1)) * a.v_row + d0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float x = to_f(v[e]);
+            if (!(fabsf(x) < INFINITY)) o[e] += x;
+        }
+    }
+}
+
+// Rows of `set` (up to NT x 16) over positions lo .. hi - 1 of a span (lo a multiple of 32).  Row rho sees positions below limit0 + rho / group.
+template <typename T, int D, int NT>
+__device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const RowSet &set, const Span &span, uint32_t shift, uint32_t hk, int lo, int hi, int limit0,
+                                         uint32_t records, uint32_t z, float *part, unsigned char *lds) {
+    using M = Mfma<T>;
+    using v8 = typename M::v8;
+    constexpr int KK = D / 32, DT = D / 16, RB = NT * 16, OP = D + 4;
+    constexpr uint32_t kStage = kTile * D * 2, kRowPieces = D / 8, kVLoads = kStage / 1024;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t i = lane & 15, c = lane >> 4, R = set.rows, G = set.group, mask = (1u << shift) - 1;
+    int *const wild = reinterpret_cast<int *>(lds + few_lds<D, NT>() - 16);      // some value of the last tiles is infinite or no number
+    const uint32_t krow_b = (uint32_t)a.k_row * 2, vrow_b = (uint32_t)a.v_row * 2;
+    const char *const kc = static_cast<const char *>(a.k_pages) + hk * a.k_head * 2, *const vc = static_cast<const char *>(a.v_pages) + hk * a.v_head * 2;
+    unsigned char *const stage = lds + wave * kStage;
+    const uint32_t vrow = lane / kRowPieces;
+    u4_t kreg[2][KK], vreg[kVLoads];
+    PageWindow window{-1, 0};
+    uint32_t gone = 0;                         // halves of the requested tile that no page holds
+    int P0 = lo + (int)wave * (int)kTile;
+    auto request = [&](int P) {
+        gone = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int number = window(min(P + h * 16, hi - 1) >> shift);
+            if (number < 0) gone |= 1u << h;
+            const __amdgpu_buffer_rsrc_t kb = half_rows(kc, a.k_page * 2, krow_b, number, P + h * 16, mask, hi - P - h * 16, D * 2);
+            const __amdgpu_buffer_rsrc_t vb = half_rows(vc, a.v_page * 2, vrow_b, number, P + h * 16, mask, hi - P - h * 16, D * 2);
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) kreg[h][kk] = piece_of(kb, i * krow_b + c * 16 + kk * 64);
+#pragma unroll
+            for (uint32_t u = h * kVLoads / 2; u < (h + 1) * kVLoads / 2; ++u) {
+                const uint32_t row = u * (64 / kRowPieces) + vrow;
+                vreg[u] = piece_of(vb, (row & 15) * vrow_b + ((lane % kRowPieces) ^ v_slot<D>(row)) * 16);
             }
-            float top = z;
-            for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-            top = fmaxf(top, m);
-            const float base = top == -INFINITY ? 0.f : top, resc = expf(m - base), w = expf(z - base);
-            m = top;
-            l *= resc;
-            float sum = w;
-            for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x, 64);
-            l += sum;
-            for (int e = 0; e < E; ++e) o[e] *= resc;
-            for (int j = 0; j < 64; ++j) {
-                if (!__shfl((int)seen, j, 64)) continue;
-                const float wj = __shfl(w, j, 64);
-                const int nj = __shfl(number, j, 64), pj = p0 + j;
-                const T *v = static_cast<const T *>(a.v_pages) + nj * a.v_page + hk * a.v_head + (uint64_t)(pj & ((1 << shift) - 1)) * a.v_row;
-                for (int e = 0; e < E; ++e) o[e] = fmaf(wj, to_f(v[lane * E + e]), o[e]);
+        }
+    };
+    auto move_window = [&](int P) {
+        if (((P + 31) >> shift) - window.base >= 64) window.fill(span, P >> shift, a.n_pages);
+    };
+    if (P0 < hi) {
+        window.fill(span, P0 >> shift, a.n_pages);
+        request(P0);
+    }
+    if (tid == 0) *wild = 0;
+    __syncthreads();
+
+    // the rows of queries; a negative scale turns their signs
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+    const float c2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);     // weights are 2^(c2 (s - m))
+    const float slack = WeightRange<T>::kSlack / c2;
+    int limit[NT];
+    v8 q[NT][KK];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const uint32_t rho = min(t * 16 + i, R - 1), tok = rho / G;
+        limit[t] = limit0 + (int)tok;
+        const T *qr = static_cast<const T *>(a.q) + ((size_t)set.token0 + tok) * a.q_token + (size_t)(hk * G + rho % G) * a.q_head + c * 8;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) q[t][kk] = __builtin_bit_cast(v8, *reinterpret_cast<const u4_t *>(qr + kk * 32) ^ u4_t{sign, sign, sign, sign});
+    }
+    float m_run[NT];
+    f4_t O[NT][DT], L[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m_run[t] = -INFINITY;
+        L[t] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) O[t][dt] = f4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    v8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (T)1.f;
+    uint32_t vread[DT];
+    {
+        const uint32_t row = 4 * c + (i >> 2);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vread[dt] = row * (D * 2) + (((2 * dt + ((i & 3) >> 1)) ^ v_slot<D>(row)) << 4) + (i & 1) * 8;
+    }
+    const int wild0 = max(limit0, 0) & ~(int)(kTile - 1);        // from here on not every row sees every position
+    for (; P0 < hi; P0 += 4 * (int)kTile) {
+        const uint32_t missing = gone;
+        f4_t S[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) S[t][h] = M::mul(__builtin_bit_cast(v8, kreg[h][kk]), q[t][kk], S[t][h]);
+        if (P0 >= wild0) {
+            bool odd = false;
+#pragma unroll
+            for (uint32_t u = 0; u < kVLoads; ++u) odd |= made_finite<T>(vreg[u]);
+            if (odd) *wild = 1;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kVLoads; ++u) *reinterpret_cast<u4_t *>(stage + u * 1024 + lane * 16) = vreg[u];
+        if (P0 + 4 * (int)kTile < hi) {
+            move_window(P0 + 4 * (int)kTile);
+            request(P0 + 4 * (int)kTile);
+        }
+        if (missing || P0 + (int)kTile > min(hi, limit0)) {
+            asm volatile("");
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int last = min(hi, limit[t]) - P0 - 4 * (int)c;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < last && !(missing >> (e >> 2) & 1) ? S[t][e >> 2][e & 3] : -INFINITY;
+            }
+        }
+        v8 P[NT];
+        weigh<T>(S, m_run, L, O, P, c2, slack);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const v8 vr = __builtin_bit_cast(v8, transposed(stage + vread[dt], 16 * D * 2));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) O[t][dt] = M::mul(vr, P[t], O[t][dt]);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) L[t] = M::mul(ones, P[t], L[t]);
+    }
+    // the four waves meet
+    __syncthreads();
+    float *ob = reinterpret_cast<float *>(lds), *om = ob + 4 * RB * OP, *ol = om + 4 * RB;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const uint32_t row = t * 16 + i;
+        float *dst = ob + (wave * RB + row) * OP + 4 * c;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4_t *>(dst + 16 * dt) = O[t][dt];
+        if (c == 0) { om[wave * RB + row] = m_run[t]; ol[wave * RB + row] = L[t][0]; }
+    }
+    __syncthreads();
+    constexpr uint32_t kPerRow = D / 4;
+    for (uint32_t u = tid; u < RB * kPerRow; u += 256) {
+        const uint32_t rho = u / kPerRow, d0 = u % kPerRow * 4;
+        if (rho >= R) break;
+        float mx = om[rho];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) mx = fmaxf(mx, om[w * RB + rho]);
+        float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float mw = om[w * RB + rho];
+            // a wave that saw nothing of this row holds zeros and weighs nothing; one whose scores are no numbers holds none, and says so
+            const float f = mw == -INFINITY ? (mx == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f((mw - mx) * c2);
+            l = fmaf(f, ol[w * RB + rho], l);
+            const f4_t v = *reinterpret_cast<const f4_t *>(ob + (w * RB + rho) * OP + d0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[e], o[e]);
+        }
+        const uint32_t tok = rho / G, h = hk * G + rho % G;
+        if (*wild) add_wild<T>(a, span, shift, hk, max(lo, wild0), min(hi, limit0 + (int)tok), d0, o);
+        const size_t token = (size_t)set.token0 + tok;
+        if (records) {
+            float *dst = part + ((token * a.n_q_heads + h) * records + z) * OP;
+            *reinterpret_cast<f4_t *>(dst + d0) = f4_t{o[0], o[1], o[2], o[3]};
+            if (d0 == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(mx * c2, l);
+        } else {
+            T r[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = (T)(l == 0.f ? 0.f : o[e] / l);
+            *reinterpret_cast<u2_t *>(static_cast<T *>(a.out) + token * a.out_token + h * a.out_head + d0) = *reinterpret_cast<const u2_t *>(r);
+        }
+    }
+}
+
+// Rows row0 .. row0 + 127 of `set` over steps lo .. hi - 1: those of `prefix` (which every row sees), then those of `own` (row rho sees
+// positions below limit0 + rho / group).
+template <typename T, int D>
+__device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const RowSet &set, uint32_t row0, const Span &prefix, const Span &own, uint32_t shift, uint32_t hk,
+                                          int lo, int hi, int limit0, uint32_t records, uint32_t z, float *part, unsigned char *lds) {
+    using M = Mfma<T>;
+    using v8 = typename M::v8;
+    constexpr int KK = D / 32, DT = D / 16, NT = 2, OP = D + 4;
+    constexpr uint32_t kHalf = kStep * D * 2, kRowPieces = D / 8, kLoads = kStep * kRowPieces / 256;     // a step's K (or V) rows; pieces a thread moves of them
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t i = lane & 15, c = lane >> 4, R = set.rows, G = set.group, mask = (1u << shift) - 1;
+    int *const wild = reinterpret_cast<int *>(lds + many_lds<D>() - 16);
+    const uint32_t krow_b = (uint32_t)a.k_row * 2, vrow_b = (uint32_t)a.v_row * 2;
+    const char *const kc = static_cast<const char *>(a.k_pages) + hk * a.k_head * 2, *const vc = static_cast<const char *>(a.v_pages) + hk * a.v_head * 2;
+    const int np = (prefix.len + (int)kStep - 1) / (int)kStep;
+    const uint32_t mine0 = row0 + wave * (NT * 16);      // the wave's rows
+    const bool rows = mine0 < R;
+    // own positions: every row of the block sees those below `least`, none sees `own_end` and beyond, no row of the wave `wave_end`
+    const int least = limit0 + (int)(row0 / G), own_end = min(own.len, limit0 + (int)(min(row0 + 127, R - 1) / G));
+    const int wave_least = limit0 + (int)(min(mine0, R - 1) / G), wave_end = limit0 + (int)(min(mine0 + 31, R - 1) / G);
+    const int wild0 = max(least, 0) & ~(int)(kStep - 1);
+
+    u4_t kreg[kLoads], vreg[kLoads];
+    PageWindow window{-1, 1 << 30};
+    int held = -1;                                       // which table the window is of
+    uint32_t gone = 0;                                   // halves of the requested step that no page holds
+    auto request = [&](int step) {
+        const bool mine = step >= np;
+        const Span &s = mine ? own : prefix;
+        const int P = (mine ? step - np : step) * (int)kStep, end = mine ? own_end : prefix.len;
+        if (held != (int)mine || ((P + 63) >> shift) - window.base >= 64) {
+            window.fill(s, P >> shift, a.n_pages);
+            held = mine;
+        }
+        int number[4];
+        gone = 0;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            number[h] = window(min(P + h * 16, end - 1) >> shift);
+            if (number[h] < 0) gone |= 1u << h;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kLoads; ++u) {
+            const uint32_t row = (u * 256 + tid) / kRowPieces, slot = tid % kRowPieces;
+            const int h = D == 128 ? (int)u : (int)(2 * u + (wave >> 1));          // (uniform)
+            const int n = D == 128 ? number[u] : wave >> 1 ? number[2 * u + 1] : number[2 * u];
+            const __amdgpu_buffer_rsrc_t kb = half_rows(kc, a.k_page * 2, krow_b, n, P + h * 16, mask, end - P - h * 16, D * 2);
+            const __amdgpu_buffer_rsrc_t vb = half_rows(vc, a.v_page * 2, vrow_b, n, P + h * 16, mask, end - P - h * 16, D * 2);
+            kreg[u] = piece_of(kb, (row & 15) * krow_b + (slot ^ k_slot<D>(row)) * 16);
+            vreg[u] = piece_of(vb, (row & 15) * vrow_b + (slot ^ v_slot<D>(row)) * 16);
+        }
+    };
+    auto store = [&](int step, uint32_t buf) {
+        if (step >= np && (step - np) * (int)kStep >= wild0) {
+            bool odd = false;
+#pragma unroll
+            for (uint32_t u = 0; u < kLoads; ++u) odd |= made_finite<T>(vreg[u]);
+            if (odd) *wild = 1;
+        }
+        unsigned char *to = lds + buf * 2 * kHalf;
+#pragma unroll
+        for (uint32_t u = 0; u < kLoads; ++u) {
+            *reinterpret_cast<u4_t *>(to + (u * 256 + tid) * 16) = kreg[u];
+            *reinterpret_cast<u4_t *>(to + kHalf + (u * 256 + tid) * 16) = vreg[u];
+        }
+    };
+    if (lo < hi) request(lo);
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+    const float c2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
+    const float slack = WeightRange<T>::kSlack / c2;
+    uint32_t tok[NT], head[NT];
+    v8 q[NT][KK];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const uint32_t rho = min(mine0 + t * 16 + i, R - 1);
+        tok[t] = rho / G;
+        head[t] = hk * G + rho % G;
+        const T *qr = static_cast<const T *>(a.q) + ((size_t)set.token0 + tok[t]) * a.q_token + (size_t)head[t] * a.q_head + c * 8;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) q[t][kk] = __builtin_bit_cast(v8, *reinterpret_cast<const u4_t *>(qr + kk * 32) ^ u4_t{sign, sign, sign, sign});
+    }
+    float m_run[NT];
+    f4_t O[NT][DT], L[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m_run[t] = -INFINITY;
+        L[t] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) O[t][dt] = f4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    v8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (T)1.f;
+    // LDS byte offsets of this lane's operand pieces in a stage's first tile (half a tile or a tile further the swizzles are the same)
+    uint32_t kread[KK], vread[DT];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) kread[kk] = i * (D * 2) + (((4 * kk + c) ^ k_slot<D>(i)) << 4);
+    {
+        const uint32_t row = 4 * c + (i >> 2);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vread[dt] = kHalf + row * (D * 2) + (((2 * dt + ((i & 3) >> 1)) ^ v_slot<D>(row)) << 4) + (i & 1) * 8;
+    }
+    auto meet = [] {      // everyone's LDS accesses are done (loads from memory stay on their way)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if (tid == 0) *wild = 0;
+    meet();
+    uint32_t missing = gone, next = 0;
+    if (lo < hi) {
+        store(lo, 0);
+        if (lo + 1 < hi) request(lo + 1);
+        meet();
+    }
+    for (int step = lo; step < hi; ++step) {
+        const bool mine = step >= np;
+        const int P0 = (mine ? step - np : step) * (int)kStep, end = mine ? own_end : prefix.len;
+        const unsigned char *st = lds + ((step - lo) & 1) * 2 * kHalf;
+        if (rows) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int T0 = P0 + h * (int)kTile;
+                if (T0 >= end || (mine && T0 >= wave_end)) break;            // (uniform)
+                const unsigned char *tile = st + h * kTile * D * 2;
+                f4_t S[NT][2];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk) {
+                        const v8 kr = __builtin_bit_cast(v8, *reinterpret_cast<const u4_t *>(tile + kread[kk] + g * 16 * D * 2));
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) S[t][g] = M::mul(kr, q[t][kk], S[t][g]);
+                    }
+                const uint32_t miss = missing >> (2 * h) & 3;
+                if (miss || T0 + (int)kTile > end || (mine && T0 + (int)kTile > wave_least)) {
+                    asm volatile("");
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const int last = (mine ? min(end, limit0 + (int)tok[t]) : end) - T0 - 4 * (int)c;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < last && !(miss >> (e >> 2) & 1) ? S[t][e >> 2][e & 3] : -INFINITY;
+                    }
+                }
+                v8 P[NT];
+                weigh<T>(S, m_run, L, O, P, c2, slack);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    const v8 vr = __builtin_bit_cast(v8, transposed(tile + vread[dt], 16 * D * 2));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) O[t][dt] = M::mul(vr, P[t], O[t][dt]);
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) L[t] = M::mul(ones, P[t], L[t]);
+            }
+        }
+        if (step + 1 < hi) {
+            next = gone;
+            store(step + 1, (step + 1 - lo) & 1);
+            if (step + 2 < hi) request(step + 2);
+        }
+        meet();
+        missing = next;
+    }
+    if (!rows) return;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (mine0 + t * 16 + i >= R) continue;
+        const size_t token = (size_t)set.token0 + tok[t];
+        if (*wild) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                float o[4] = {O[t][dt][0], O[t][dt][1], O[t][dt][2], O[t][dt][3]};
+                add_wild<T>(a, own, shift, hk, max(wild0, (lo - np) * (int)kStep), min(min(own_end, (hi - np) * (int)kStep), limit0 + (int)tok[t]), 16 * dt + 4 * c, o);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[t][dt][e] = o[e];
+            }
+        }
+        if (records) {
+            float *dst = part + ((token * a.n_q_heads + head[t]) * records + z) * OP;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4_t *>(dst + 16 * dt + 4 * c) = O[t][dt];
+            if (c == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(m_run[t] * c2, L[t][0]);
+        } else {
+            T *dst = static_cast<T *>(a.out) + token * a.out_token + (size_t)head[t] * a.out_head + 4 * c;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                T r[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = (T)(L[t][0] == 0.f ? 0.f : O[t][dt][e] / L[t][0]);
+                *reinterpret_cast<u2_t *>(dst + 16 * dt) = *reinterpret_cast<const u2_t *>(r);
             }
         }
     }
-    T *out = static_cast<T *>(a.out) + token * a.out_token + h * a.out_head;
-    for (int e = 0; e < E; ++e) out[lane * E + e] = (T)(l == 0.f ? 0.f : o[e] / l);
+}
+
+// tokens of a sequence: first row, how many there are, how many of them count
+struct SeqTokens { int row0, n, answered; };
+__device__ __forceinline__ SeqTokens tokens_of(const ps_page_attention_args &a, uint32_t s) {
+    const int lo = clampi(a.first[s], 0, (int)a.n_tokens), hi = clampi(a.first[s + 1], 0, (int)a.n_tokens), n = max(0, hi - lo);
+    return {lo, n, min(n, (int)min(a.max_tokens, 0x7FFFFFFFu))};
+}
+__device__ __forceinline__ int length_of(const ps_page_attention_args &a, uint32_t s) { return clampi(a.length[s], 0, (int)a.max_length); }
+__device__ __forceinline__ int prefix_length_of(const ps_page_attention_args &a, int p) { return clampi(a.prefix_length[p], 0, (int)a.max_prefix); }
+// the prefix that a sequence stands behind, -1: none; by a whole wave
+__device__ __forceinline__ int prefix_of(const ps_page_attention_args &a, uint32_t s) {
+    for (uint32_t p0 = 0; p0 < a.n_prefix; p0 += 64) {
+        const uint32_t p = p0 + (threadIdx.x & 63);
+        const uint64_t in = __ballot(p < a.n_prefix && a.group_first[min(p, a.n_prefix - 1)] <= (int)s && (int)s < a.group_first[min(p, a.n_prefix - 1) + 1]);
+        if (in) return __builtin_amdgcn_readfirstlane((int)p0 + __ffsll((unsigned long long)in) - 1);
+    }
+    return -1;
+}
+// the `flat`-th block of 128 rows of all groups' tokens; rows 0: there is none
+struct GroupBlock { RowSet set; uint32_t prefix, block; };
+__device__ __forceinline__ GroupBlock group_block(const ps_page_attention_args &a, uint32_t flat) {
+    const uint32_t G = a.n_q_heads / a.n_kv_heads, lane = threadIdx.x & 63;
+    uint32_t base = 0;
+    for (uint32_t p0 = 0; p0 < a.n_prefix; p0 += 64) {
+        const uint32_t p = p0 + lane;
+        int t0 = 0, n = 0;
+        if (p < a.n_prefix) {
+            t0 = clampi(a.first[clampi(a.group_first[p], 0, (int)a.n_seq)], 0, (int)a.n_tokens);
+            n = max(0, clampi(a.first[clampi(a.group_first[p + 1], 0, (int)a.n_seq)], 0, (int)a.n_tokens) - t0);
+        }
+        const uint32_t mine = (uint32_t)(((uint64_t)n * G + 127) / 128);
+        uint32_t upto = mine;
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t x = __shfl_up(upto, o, 64);
+            if ((int)lane >= o) upto += x;
+        }
+        const uint64_t past = __ballot(base + upto > flat);
+        if (past) {
+            const int at = __ffsll((unsigned long long)past) - 1;
+            const uint32_t before = base + __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at);
+            return {{__builtin_amdgcn_readlane(t0, at), (uint32_t)__builtin_amdgcn_readlane(n, at) * G, G}, p0 + at, flat - before};
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return {{0, 0, G}, 0, 0};
+}
+
+extern __shared__ u4_t page_lds[];
+
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, uint32_t prefix8, uint32_t own8, float *part) {
+    unsigned char *const lds = reinterpret_cast<unsigned char *>(page_lds);
+    const uint32_t records = d.direct ? 0 : d.psplit + d.osplit;
+    // runs of eight workgroups (one on each XCD): prefixes and own positions in turn, as their numbers are to each other
+    const uint32_t run = blockIdx.x / 8, all = prefix8 + own8;
+    const uint32_t before = (uint32_t)((uint64_t)run * prefix8 / all), upto = (uint32_t)((uint64_t)(run + 1) * prefix8 / all);
+    if (upto > before) {
+        // blocks of the same positions follow one another on one XCD, whose L2 they share
+        const uint32_t unit = before / d.blocks * 8 + blockIdx.x % 8;
+        if (unit >= a.n_kv_heads * d.psplit) return;
+        const GroupBlock g = group_block(a, before % d.blocks);
+        if (g.set.rows == 0) return;
+        const uint32_t z = unit % d.psplit, hk = unit / d.psplit;
+        const int len = prefix_length_of(a, g.prefix), lo = (int)min((uint64_t)z * d.plen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.plen, (uint64_t)len);
+        if (lo >= hi) return;
+        const Span span{a.prefix_table + g.prefix * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), len};
+        if (g.set.rows <= NT * 16) rows_few<T, D, NT>(a, g.set, span, shift, hk, lo, hi, len, records, z, part, lds);
+        else rows_many<T, D>(a, g.set, g.block * 128, Span{span.table, span.entries, hi}, Span{nullptr, 0, 0}, shift, hk, lo / (int)kStep, (hi + (int)kStep - 1) / (int)kStep, 0, records, z, part, lds);
+    } else {
+        const uint32_t unit = (run - before) * 8 + blockIdx.x % 8, z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads;
+        if (s >= a.n_seq) return;
+        const SeqTokens t = tokens_of(a, s);
+        const int len = length_of(a, s), lo = (int)min((uint64_t)z * d.olen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)len);
+        if (t.answered == 0 || (lo >= hi && records)) return;
+        const uint32_t G = a.n_q_heads / a.n_kv_heads;
+        rows_few<T, D, NT>(a, RowSet{t.row0, t.answered * G, G}, Span{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), len}, shift, hk, lo, hi, len - t.n + 1, records, d.psplit + z, part, lds);
+    }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void page_rows_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, float *part) {
+    unsigned char *const lds = reinterpret_cast<unsigned char *>(page_lds);
+    const uint32_t units = a.n_seq * a.n_kv_heads * d.osplit;
+    const uint32_t unit = blockIdx.x / 8 / d.blocks * 8 + blockIdx.x % 8, block = blockIdx.x / 8 % d.blocks;
+    if (unit >= units) return;
+    const uint32_t z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads, G = a.n_q_heads / a.n_kv_heads;
+    const SeqTokens t = tokens_of(a, s);
+    if (block * 128 >= t.answered * G) return;
+    const int p = prefix_of(a, s);
+    const Span prefix = p < 0 ? Span{nullptr, 0, 0} : Span{a.prefix_table + p * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), prefix_length_of(a, p)};
+    const Span own{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), length_of(a, s)};
+    const RowSet set{t.row0, t.answered * G, G};
+    const int np = (prefix.len + (int)kStep - 1) / (int)kStep, limit0 = own.len - t.n + 1;
+    const int last = min(own.len, limit0 + (int)(min(block * 128 + 127, set.rows - 1) / G));
+    const int steps = np + (max(last, 0) + (int)kStep - 1) / (int)kStep;
+    const int lo = (int)min((uint64_t)z * d.olen, (uint64_t)steps), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)steps);
+    // (a run that none of the block's rows sees leaves records of nothing)
+    rows_many<T, D>(a, set, block * 128, prefix, own, shift, hk, lo, hi, limit0, d.direct ? 0 : d.osplit, z, part, lds);
+}
+
+// A wave per (token, query head) puts the records of its prefix's and of its sequence's runs together, in their order: value sums, then maximum
+// (in powers of two) and weight sum.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args a, PageDeal d, const float *part) {
+    constexpr int E = D / 64, OP = D + 4;
+    const uint32_t lane = threadIdx.x & 63, hb = (a.n_q_heads + 3) / 4, h = blockIdx.x % hb * 4 + (threadIdx.x >> 6), i = blockIdx.x / hb % a.max_tokens, s = blockIdx.x / hb / a.max_tokens;
+    const SeqTokens t = tokens_of(a, s);
+    if (h >= a.n_q_heads || (int)i >= t.answered) return;
+    const int p = prefix_of(a, s), plen = p < 0 ? 0 : prefix_length_of(a, p), len = length_of(a, s);
+    const uint32_t np = d.shared && plen ? (plen + d.plen - 1) / d.plen : 0;
+    const uint32_t positions = d.shared ? len : (plen + kStep - 1) / kStep + (len + kStep - 1) / kStep;
+    const uint32_t n = np + (positions + d.olen - 1) / d.olen;
+    const size_t token = (size_t)t.row0 + i;
+    const float *r0 = part + (token * a.n_q_heads + h) * (d.psplit + d.osplit) * OP;
+    float mx = -INFINITY, l = 0.f, o[E] = {};
+    for (uint32_t z0 = 0; z0 < n; z0 += 8) {
+        float mv[8], lv[8], ov[8][E], m8 = mx;
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) {
+            const uint32_t z = min(z0 + u, n - 1);
+            const float *r = r0 + (size_t)(z < np ? z : d.psplit + z - np) * OP;
+            mv[u] = r[D];
+            lv[u] = r[D + 1];
+#pragma unroll
+            for (int e = 0; e < E; ++e) ov[u][e] = r[lane * E + e];
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) m8 = fmaxf(m8, mv[u]);
+        const float ms = m8 == -INFINITY ? 0.f : m8, resc = __builtin_amdgcn_exp2f(mx - ms);
+        l *= resc;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= resc;
+        mx = m8;
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) {
+            const bool in = z0 + u < n;          // (a record past the last is the last again)
+            const float w = mv[u] == -INFINITY ? (m8 == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(mv[u] - ms);       // as the waves above
+            l = in ? fmaf(w, lv[u], l) : l;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = in ? fmaf(w, ov[u][e], o[e]) : o[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) static_cast<T *>(a.out)[token * a.out_token + h * a.out_head + lane * E + e] = (T)(l == 0.f ? 0.f : o[e] / l);
 }
 
 // ------------------------------------------------------------------------------------ sampling
@@ -315,6 +844,7 @@ int32_t check_page_attention(const ps_page_attention_args *a) {
             "%u query heads over %u kv heads: a multiple of the kv heads, at most 1024", a->n_q_heads, a->n_kv_heads);
     PS_WANT(power_of_two(a->page) && a->page >= 16 && a->page <= kMostPage, "pages of a power of two positions, 16 .. %u (got %u)", kMostPage, a->page);
     PS_WANT(a->n_seq <= kMostSeqs && a->n_tokens <= 0x7FFFFFFF && a->n_pages <= 0x7FFFFFFF, "%u sequences, %u tokens, %u pages: too many", a->n_seq, a->n_tokens, a->n_pages);
+    PS_WANT((uint64_t)a->n_tokens * a->n_q_heads <= 0x7FFFFFFFull, "%u tokens of %u heads are too many for one call", a->n_tokens, a->n_q_heads);
     PS_WANT(a->n_prefix <= kMostPrefixes, "up to %u prefixes (got %u)", kMostPrefixes, a->n_prefix);
     PS_WANT(a->max_length <= (uint32_t)kMostPositions && a->max_length <= (uint64_t)a->width * a->page, "lengths of up to %u in tables of %u pages of %u", a->max_length, a->width, a->page);
     PS_WANT(!a->n_prefix || (a->max_prefix <= (uint32_t)kMostPositions && a->max_prefix <= (uint64_t)a->prefix_width * a->page), "prefixes of up to %u in tables of %u pages of %u", a->max_prefix,
@@ -322,11 +852,82 @@ int32_t check_page_attention(const ps_page_attention_args *a) {
     return PS_OK;
 }
 
+// How the work is dealt out: see the comments at the kernels.  Runs bring the launch to about the workgroups that the chip holds at once (two per CU).
+PageDeal page_deal(const ps_page_attention_args &a) {
+    PageDeal d{};
+    const uint32_t G = a.n_q_heads / a.n_kv_heads;
+    const uint64_t tokens = std::min(a.max_tokens, a.n_tokens), rows = tokens * G;
+    const bool prefixes = a.n_prefix && a.max_prefix;
+    d.shared = rows <= kFewRows;
+    auto cut = [](uint64_t units, uint64_t want, uint64_t whole, uint64_t least, uint64_t multiple, uint32_t *n, uint32_t *len) {
+        const uint64_t most = std::max<uint64_t>(1, whole / least), runs = std::min(std::max<uint64_t>(1, want / std::max<uint64_t>(1, units)), most);
+        *len = (uint32_t)std::max<uint64_t>(multiple, ((whole + runs - 1) / runs + multiple - 1) / multiple * multiple);
+        *n = (uint32_t)std::max<uint64_t>(1, (whole + *len - 1) / *len);
+    };
+    if (d.shared) {
+        d.nt = rows <= 16 ? 1 : 2;
+        d.blocks = prefixes ? (uint32_t)((uint64_t)a.n_tokens * G / 128 + std::min(a.n_prefix, a.n_seq)) : 0;
+        if (prefixes) cut((uint64_t)d.blocks * a.n_kv_heads, 512, a.max_prefix, 256, kStep, &d.psplit, &d.plen);
+        cut((uint64_t)a.n_seq * a.n_kv_heads, 1024, a.max_length, 128, 4 * kTile, &d.osplit, &d.olen);
+        d.direct = d.psplit == 0 && d.osplit == 1;
+    } else {
+        d.blocks = (uint32_t)((rows + 127) / 128);
+        const uint64_t steps = (prefixes ? (a.max_prefix + kStep - 1) / kStep : 0) + (a.max_length + kStep - 1) / kStep;
+        cut((uint64_t)a.n_seq * a.n_kv_heads * d.blocks, 512, steps, 2, 1, &d.osplit, &d.olen);
+        d.direct = d.osplit == 1;
+    }
+    return d;
+}
+uint64_t page_workspace(const ps_page_attention_args &a, const PageDeal &d) {
+    return d.direct ? 0 : align_up((uint64_t)a.n_tokens * a.n_q_heads * (d.psplit + d.osplit) * (a.head_dim + 4) * 4, kAlign);
+}
+// workgroups of a call's launches, 0: more than a launch holds
+uint64_t page_groups(const ps_page_attention_args &a, const PageDeal &d, uint64_t *prefix8, uint64_t *own8) {
+    *prefix8 = d.shared ? ((uint64_t)a.n_kv_heads * d.psplit + 7) / 8 * d.blocks : 0;
+    *own8 = ((uint64_t)a.n_seq * a.n_kv_heads * d.osplit + 7) / 8 * (d.shared ? 1 : d.blocks);
+    const uint64_t groups = (*prefix8 + *own8) * 8, merge = (uint64_t)a.n_seq * std::min(a.max_tokens, a.n_tokens) * ((a.n_q_heads + 3) / 4);
+    return groups > kMostGroups || (!d.direct && merge > kMostGroups) ? 0 : groups;
+}
+
+// a kernel that takes more LDS than a launch gets by itself: announced once per device
+template <class K>
+hipError_t take_lds(K kernel, uint32_t lds, std::atomic<uint64_t> &done) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess || (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1))) return e;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e == hipSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+    return e;
+}
+template <typename T, int D, int NT>
+hipError_t launch_shared(const ps_page_attention_args &a, const PageDeal &d, uint32_t prefix8, uint32_t own8, float *part, hipStream_t st) {
+    static std::atomic<uint64_t> done;
+    constexpr uint32_t lds = std::max(few_lds<D, NT>(), many_lds<D>());
+    const hipError_t e = take_lds(&page_shared_kernel<T, D, NT>, lds, done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((page_shared_kernel<T, D, NT>), dim3((prefix8 + own8) * 8), dim3(256), lds, st, a, d, log2_of(a.page), prefix8, own8, part);
+    return hipGetLastError();
+}
 template <typename T, int D>
-hipError_t launch_page_attention(const ps_page_attention_args &a, hipStream_t st) {
-    const uint64_t groups = (uint64_t)a.n_seq * a.max_tokens * ((a.n_q_heads + 3) / 4);
-    if (groups > kMostGroups) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((page_attention_kernel<T, D>), dim3((uint32_t)groups), dim3(256), 0, st, a, log2_of(a.page));
+hipError_t launch_rows(const ps_page_attention_args &a, const PageDeal &d, uint32_t own8, float *part, hipStream_t st) {
+    static std::atomic<uint64_t> done;
+    const hipError_t e = take_lds(&page_rows_kernel<T, D>, many_lds<D>(), done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((page_rows_kernel<T, D>), dim3(own8 * 8), dim3(256), many_lds<D>(), st, a, d, log2_of(a.page), part);
+    return hipGetLastError();
+}
+template <typename T, int D>
+hipError_t launch_page_attention(const ps_page_attention_args &call, float *part, hipStream_t st) {
+    ps_page_attention_args a = call;
+    a.max_tokens = std::min(a.max_tokens, a.n_tokens);
+    const PageDeal d = page_deal(a);
+    uint64_t prefix8, own8;
+    page_groups(a, d, &prefix8, &own8);
+    const hipError_t e = !d.shared ? launch_rows<T, D>(a, d, (uint32_t)own8, part, st)
+                         : d.nt == 1 ? launch_shared<T, D, 1>(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st)
+                                     : launch_shared<T, D, 2>(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st);
+    if (e != hipSuccess || d.direct) return e;
+    hipLaunchKernelGGL((page_merge_kernel<T, D>), dim3(a.n_seq * a.max_tokens * ((a.n_q_heads + 3) / 4)), dim3(256), 0, st, a, d, part);
     return hipGetLastError();
 }
 template <typename T>
@@ -392,7 +993,7 @@ int32_t ps_page_attention_workspace(const ps_page_attention_args *a, uint64_t *b
     PS_WANT(bytes, "NULL argument");
     const int32_t rc = check_page_attention(a);
     if (rc) return rc;
-    *bytes = 0;
+    *bytes = page_workspace(*a, page_deal(*a));
     return PS_OK;
 }
 
@@ -411,9 +1012,12 @@ int32_t ps_page_attention(const ps_page_attention_args *a, void *workspace, uint
     for (uint64_t n : {a->k_row, a->v_row}) PS_WANT(n <= (1ull << 30) / 16, "16 rows of a page must span less than 2 GiB (stride of %llu elements)", (unsigned long long)n);
     for (const int32_t *p : {a->first, a->length, a->table, a->group_first, a->prefix_length, a->prefix_table}) PS_WANT(aligned(p, 4), "tables must be aligned to 4 bytes");
     PS_WANT(workspace_bytes >= need && (need == 0 || (workspace && aligned(workspace, kAlign))), "a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need);
+    uint64_t prefix8, own8;
+    PS_WANT(page_groups(*a, page_deal(*a), &prefix8, &own8), "too many sequences, tokens and heads for one call");
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a->type == PS_TYPE_F16) PS_TRY(a->head_dim == 64 ? (launch_page_attention<f16_t, 64>(*a, st)) : (launch_page_attention<f16_t, 128>(*a, st)));
-    else PS_TRY(a->head_dim == 64 ? (launch_page_attention<bf16_t, 64>(*a, st)) : (launch_page_attention<bf16_t, 128>(*a, st)));
+    float *part = static_cast<float *>(workspace);
+    if (a->type == PS_TYPE_F16) PS_TRY(a->head_dim == 64 ? (launch_page_attention<f16_t, 64>(*a, part, st)) : (launch_page_attention<f16_t, 128>(*a, part, st)));
+    else PS_TRY(a->head_dim == 64 ? (launch_page_attention<bf16_t, 64>(*a, part, st)) : (launch_page_attention<bf16_t, 128>(*a, part, st)));
     return PS_OK;
 }
 
