@@ -697,140 +697,575 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
 }
 
 // ------------------------------------------------------------------------------------ sampling
-// Sums are whole numbers, so a run of the order is known by its count and its sum whatever order it was added in.  A border
-// of the order (the first entry at which count or sum pass a goal) is found digit by digit of the logits' bits.
-constexpr uint32_t kSampleThreads = 1024;
+// Launches, in order:
+//  sample_rows_kernel   a row's chunks: largest logit and where; clears the row's bins
+//  sample_bins_kernel   entries by how far they lie behind the row's largest logit, in bins of 40 / 2047 nats (the last one: all from 40 nats on):
+//                       counts, and sums of weights relative to the bin's front as whole numbers of 2^-35, so that their order does not matter
+//  sample_pick_kernel   a workgroup per row: running counts and sums over the bins say in which bins the borders lie (of top-k, top-p, min-p, and the
+//                       drawn entry).  The entries of these bins are picked out of the row (most often a few hundred), put in order, and
+//                       searched; where they are more than a list holds, each border is found by the digits of the logits' bits instead.
+// The sum of the first entries of the order is that of whole bins (64 bits, always added alike) and of a part of one, whose whole numbers are exact.
+constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 1024, kList = 1024, kMostChunk = 8192;
+constexpr double kBinsPerNat = 2047.0 / 40.0;
 
-// bits that order as the values do: larger for larger logits
+struct RowTop { float m; int at; };
+struct SampleShape { uint32_t chunk, nchunk; };
+struct SampleWork { RowTop *tops; unsigned long long *sums; uint32_t *counts; };       // [row][chunk], [row][bin], [row][bin]
+
+// bits that order as the values do, and back: larger for larger logits
 __device__ __forceinline__ uint32_t order_of(float v) {
     const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f);        // (-0 is 0)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-struct SampleRow { double k, unit; float m; uint32_t vocab; };
-__device__ __forceinline__ uint64_t whole(double w, const SampleRow &r) { return (uint64_t)rint(w * r.unit); }
+__device__ __forceinline__ float value_of(uint32_t key) { return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-struct Border { uint32_t key, before, equal; uint64_t sum, each; };      // entries in front of those equal to the border's, their sum; a weight of these
-struct SampleLds { uint32_t cnt[256]; unsigned long long sum[256]; uint32_t digit, before; unsigned long long total; uint32_t wave[16]; float top[16]; };
-
-template <typename T, class Cond>
-__device__ Border find_border(const T *x, const SampleRow &r, SampleLds &s, Cond passes) {
-    Border b{0, 0, 0, 0, 0};
-    uint32_t mask = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        __syncthreads();
-        if (threadIdx.x < 256) { s.cnt[threadIdx.x] = 0; s.sum[threadIdx.x] = 0; }
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < r.vocab; i += kSampleThreads) {
-            const float v = sane(to_f(x[i]));
-            const uint32_t key = order_of(v);
-            if (v == -INFINITY || (key & mask) != b.key) continue;
-            atomicAdd(&s.cnt[key >> shift & 255], 1u);
-            atomicAdd(&s.sum[key >> shift & 255], (unsigned long long)whole(weight(v, r.m, r.k), r));
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            uint32_t c = b.before;
-            unsigned long long t = b.sum;
-            int d = 255;
-            while (d > 0 && !(s.cnt[d] && passes(c + s.cnt[d], (uint64_t)(t + s.sum[d])))) { c += s.cnt[d]; t += s.sum[d]; --d; }
-            s.digit = d; s.before = c; s.total = t;
-        }
-        __syncthreads();
-        b.key |= s.digit << shift;
-        b.before = s.before;
-        b.sum = s.total;
-        mask |= 255u << shift;
-        if (shift == 0) { b.equal = s.cnt[s.digit]; b.each = b.equal ? s.sum[s.digit] / b.equal : 0; }
-    }
-    __syncthreads();
-    return b;
+// How far an entry lies behind the largest one, in bins; and its weight, relative to its bin's front, in whole numbers of 2^-35: exp(-g / 51.175) for a
+// place g of a bin, as a polynomial of degree 4 around the bin's middle (off by 7.5e-13 of it, the rounding by 1.5e-11); in the last bin, which
+// weighs e^-40 together, by the 32-bit exponential.
+struct BinScale {
+    double rate;
+    float m, coarse;
+    __device__ __forceinline__ double place(float v) const { return ((double)m - (double)v) * rate; }
+    __device__ __forceinline__ float about(float v) const { return fminf((m - v) * coarse, 2047.f); }     // a place to within 0.01
+};
+__device__ __forceinline__ BinScale bin_scale(float m, float temp) {
+    const double rate = kBinsPerNat / (double)fminf(temp, 1e30f);
+    return {rate, m, (float)fmin(rate, 1e30)};
 }
-// how many of the entries equal to a border's it takes for the sum to pass: 1 .. equal
-template <class Cond>
-__device__ __forceinline__ uint32_t within(const Border &b, Cond passes) {
-    uint32_t lo = 1, hi = max(1u, b.equal);
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (passes(b.before + mid, b.sum + mid * b.each)) hi = mid;
-        else lo = mid + 1;
-    }
-    return lo;
+__device__ __forceinline__ int bin_of(double y) { return y < 2047.0 ? (int)y : 2047; }
+__device__ __forceinline__ unsigned long long whole_of(double y, int b) {
+    if (b == 2047) return (unsigned long long)(__builtin_amdgcn_exp2f(-(float)fmin((y - 2047.0) * 0.028191402850785804, 1000.0)) * 34359738368.f);
+    const double h = y - (double)b - 0.5;
+    double w = 206.71118141261828;
+    w = fma(w, h, -42313.77914196292);
+    w = fma(w, h, 6496222.942769858);
+    w = fma(w, h, -664888418.192495);
+    w = fma(w, h, 34025664801.00093);
+    return __builtin_bit_cast(uint64_t, w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSampleThreads) void sample_kernel(ps_sample_args a, double unit) {
-    __shared__ SampleLds s;
-    const uint32_t row = blockIdx.x, tid = threadIdx.x;
+__global__ __launch_bounds__(kRowThreads) void sample_rows_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
+    __shared__ float top[kRowThreads / 64];
+    __shared__ int where[kRowThreads / 64];
+    const uint32_t tid = threadIdx.x, row = blockIdx.y, chunk = blockIdx.x;
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_row;
-    float top = -INFINITY;
-    for (uint32_t i = tid; i < a.vocab; i += kSampleThreads) top = fmaxf(top, sane(to_f(x[i])));
-    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    if ((tid & 63) == 0) s.top[tid >> 6] = top;
-    __syncthreads();
-    for (int w = 0; w < 16; ++w) top = fmaxf(top, s.top[w]);
-    if (top == -INFINITY) {
-        if (tid == 0) { a.token[row] = -1; if (a.kept) a.kept[row] = 0; }
-        return;
+    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    RowTop r{-INFINITY, 0x7FFFFFFF};
+#pragma unroll 2
+    for (uint32_t i = lo + tid * 8; i < hi; i += kRowThreads * 8) {
+        Oct<T> o;
+        o.fill(x, i, hi);
+        float v[8], mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            o.take(v[e], v[e + 1]);
+            mx = fmaxf(mx, fmaxf(v[e], v[e + 1]));
+        }
+        if (mx > r.m) {
+            r.m = mx;
+#pragma unroll
+            for (int e = 7; e >= 0; --e) r.at = v[e] == mx ? (int)(i + e) : r.at;
+        }
     }
+    const uint32_t per = (kBins + sh.nchunk - 1) / sh.nchunk;
+    for (uint32_t b = chunk * per + tid; b < min(kBins, (chunk + 1) * per); b += kRowThreads) {
+        w.sums[(size_t)row * kBins + b] = 0;
+        w.counts[(size_t)row * kBins + b] = 0;
+    }
+    float m = r.m;
+    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    int at = r.m == m ? r.at : 0x7FFFFFFF;
+    for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
+    if ((tid & 63) == 0) { top[tid >> 6] = m; where[tid >> 6] = at; }
+    __syncthreads();
+    if (tid == 0) {
+        RowTop t{top[0], where[0]};
+        for (uint32_t i = 1; i < kRowThreads / 64; ++i) {
+            if (top[i] > t.m) t = {top[i], where[i]};
+            else if (top[i] == t.m) t.at = min(t.at, where[i]);
+        }
+        w.tops[(size_t)row * sh.nchunk + chunk] = t;
+    }
+}
+// the largest logit of a row and its lowest index; every thread of the workgroup calls it
+template <uint32_t kThreads>
+__device__ __forceinline__ RowTop row_top(const RowTop *tops, uint32_t n, float *fbuf, int *ibuf) {
+    const uint32_t tid = threadIdx.x;
+    RowTop t{-INFINITY, 0x7FFFFFFF};
+    for (uint32_t i = tid; i < n; i += kThreads) {
+        const RowTop o = tops[i];
+        if (o.m > t.m) t = o;
+        else if (o.m == t.m) t.at = min(t.at, o.at);
+    }
+    for (int o = 32; o; o >>= 1) {
+        const float m = __shfl_xor(t.m, o, 64);
+        const int at = __shfl_xor(t.at, o, 64);
+        if (m > t.m) t = {m, at};
+        else if (m == t.m) t.at = min(t.at, at);
+    }
+    if (n <= 64) {             // (the first wave has them all)
+        if (tid == 0) { fbuf[0] = t.m; ibuf[0] = t.at; }
+        __syncthreads();
+        return {fbuf[0], ibuf[0]};
+    }
+    if ((tid & 63) == 0) { fbuf[tid >> 6] = t.m; ibuf[tid >> 6] = t.at; }
+    __syncthreads();
+    for (uint32_t i = 0; i < kThreads / 64; ++i) {
+        if (fbuf[i] > t.m) t = {fbuf[i], ibuf[i]};
+        else if (fbuf[i] == t.m) t.at = min(t.at, ibuf[i]);
+    }
+    return t;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void sample_bins_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
+    __shared__ unsigned long long bins[kBins];             // sum of weights, and from bit 49 on how many (a chunk has 2^13 at most)
+    __shared__ float fbuf[kRowThreads / 64];
+    __shared__ int ibuf[kRowThreads / 64];
+    const uint32_t tid = threadIdx.x, row = blockIdx.y, chunk = blockIdx.x;
     const float temp = a.temperature ? a.temperature[row] : 1.f;
-    const bool greedy = !(temp > 0.f);
-    const SampleRow r{greedy ? 0.0 : rate_of(temp), unit, top, a.vocab};
-    uint32_t kept = 1, skip = 0, key = order_of(top);        // the token: entry number `skip` of those with this key
-    if (!greedy) {
-        auto all = [](uint32_t, uint64_t) { return false; };
-        const Border last = find_border<T>(x, r, s, all);      // the least of all kept entries
-        kept = last.before + last.equal;
-        uint64_t sum = last.sum + last.equal * last.each;
-        if (a.top_k && a.top_k[row] > 0 && (uint32_t)a.top_k[row] < kept) {
-            const uint32_t most = a.top_k[row];
-            auto cond = [=](uint32_t c, uint64_t) { return c >= most; };
-            const Border b = find_border<T>(x, r, s, cond);
-            kept = most;
-            sum = b.sum + (most - b.before) * b.each;
+    if (!(temp > 0.f)) return;
+    for (uint32_t b = tid; b < kBins; b += kRowThreads) bins[b] = 0;
+    const float m = row_top<kRowThreads>(w.tops + (size_t)row * sh.nchunk, sh.nchunk, fbuf, ibuf).m;
+    if (m == -INFINITY) return;
+    __syncthreads();
+    const BinScale s = bin_scale(m, temp);
+    const T *x = static_cast<const T *>(a.logits) + row * a.logits_row;
+    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    for (uint32_t i = lo + tid * 8; i < hi; i += kRowThreads * 8) {
+        Oct<T> o;
+        o.fill(x, i, hi);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            float v[2];
+            o.take(v[0], v[1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (v[j] == -INFINITY) continue;
+                const double y = s.place(v[j]);
+                const int b = bin_of(y);
+                atomicAdd(&bins[b], whole_of(y, b) + (1ull << 49));
+            }
         }
-        uint32_t n = kept;
-        uint64_t total = sum;
-        if (a.top_p && a.top_p[row] < 1.f) {
-            const double goal = (double)a.top_p[row] * (double)sum;
-            auto cond = [=](uint32_t, uint64_t t) { return (double)t >= goal; };
-            const Border b = find_border<T>(x, r, s, cond);
-            const uint32_t j = within(b, cond);
-            if (b.before + j < n) { n = b.before + j; total = b.sum + j * b.each; }
+    }
+    __syncthreads();
+    for (uint32_t b = tid; b < kBins; b += kRowThreads) {
+        const unsigned long long v = bins[b];
+        if (v) {
+            atomicAdd(&w.sums[(size_t)row * kBins + b], v & ((1ull << 49) - 1));
+            atomicAdd(&w.counts[(size_t)row * kBins + b], (uint32_t)(v >> 49));
         }
-        if (a.min_p && a.min_p[row] > 0.f) {
-            const double least = a.min_p[row];
-            if (tid == 0) { s.before = 0; s.total = 0; }
+    }
+}
+
+struct PickLds {
+    double sum[kBins + 1];                 // of all entries in front of a bin, and of all
+    uint32_t count[kBins + 1];             // likewise
+    uint16_t start[kBins];                 // where a bin's entries begin in the list
+    uint32_t marked[kBins / 32];
+    union {
+        struct { unsigned long long raw[kList], sorted[kList]; } list;       // (inverted order, index): ascending as the order
+        struct { unsigned long long sum[256]; uint32_t count[256]; } digits;
+    };
+    unsigned long long part[kList + 1];    // running sums of the list's weights
+    double dbuf[kPickThreads / 64];
+    unsigned long long lbuf[kPickThreads / 64];
+    uint32_t ubuf[kPickThreads / 64];
+    float fbuf[kPickThreads / 64];
+    int ibuf[kPickThreads / 64], found[6], lo, hi;
+    uint32_t n;
+    struct { uint32_t key, before, equal; unsigned long long sum, each; } digit;
+};
+// a part of one bin: its first `count` entries, whose weights are `sum`; by digits: the last one is number `skip` of those with `key`
+struct InBin { uint32_t count, key, skip; unsigned long long sum; };
+
+template <typename T>
+struct Picker {
+    const T *x;
+    uint32_t vocab, tid;
+    BinScale s;
+    PickLds &l;
+
+    __device__ __forceinline__ double sum_at(int b, unsigned long long part) const { return l.sum[b] + exp(-(double)b / kBinsPerNat) * (double)part; }
+
+    // the first bin that has entries and at whose end `passes` is true, or the last one with entries; into l.found[slot], which holds that
+    template <class Passes>
+    __device__ __forceinline__ void look(int slot, Passes passes) {
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+            const uint32_t b = tid + j * kPickThreads;
+            const uint64_t yes = __ballot(l.count[b + 1] > l.count[b] && passes(b));
+            if (yes && (tid & 63) == 0) atomicMin(&l.found[slot], (int)(b + __ffsll((unsigned long long)yes) - 1));
+        }
+    }
+    // every entry of the row in a bin for which want(bin) is true: take(value, index, place, bin)
+    template <class Want, class Take>
+    __device__ __forceinline__ void each(int lo, int hi, Want want, Take take) {
+        const float from = (float)lo - 2.f, to = hi >= 2045 ? INFINITY : (float)hi + 3.f;
+        for (uint32_t i = tid * 8; i < vocab; i += kPickThreads * 8) {
+            Oct<T> o;
+            o.fill(x, i, vocab);
+            float v[8];
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) o.take(v[e], v[e + 1]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = s.about(v[e]);
+                any |= y >= from && y <= to;
+            }
+            if (!any) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float about = s.about(v[e]);
+                if (!(about >= from && about <= to) || v[e] == -INFINITY) continue;
+                const double y = s.place(v[e]);
+                const int b = bin_of(y);
+                if (want(b)) take(v[e], i + e, y, b);
+            }
+        }
+    }
+
+    // by the list: the first entry of bin b at which passes(entries of the bin up to it, their sum), or its last
+    template <class Passes>
+    __device__ __forceinline__ InBin listed(int b, Passes passes) const {
+        const uint32_t at = l.start[b];
+        const unsigned long long base = l.part[at];
+        uint32_t lo = 1, hi = l.count[b + 1] - l.count[b];
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (passes(mid, l.part[at + mid] - base)) hi = mid;
+            else lo = mid + 1;
+        }
+        return {lo, 0, 0, l.part[at + lo] - base};
+    }
+    // the same by the digits of the entries' bits, from the highest on
+    template <class Passes>
+    __device__ InBin by_digits(int b, Passes passes) {
+        uint32_t key = 0, mask = 0, before = 0;
+        unsigned long long sum = 0;
+        for (int shift = 24; shift >= 0; shift -= 8) {
             __syncthreads();
-            for (uint32_t i = tid; i < a.vocab; i += kSampleThreads) {
-                const float v = sane(to_f(x[i]));
-                if (v == -INFINITY) continue;
-                const double w = weight(v, top, r.k);
-                if ((v == top ? 1.0 : w) >= least) { atomicAdd(&s.before, 1u); atomicAdd(&s.total, (unsigned long long)whole(w, r)); }
+            if (tid < 256) { l.digits.count[tid] = 0; l.digits.sum[tid] = 0; }
+            __syncthreads();
+            each(b, b, [=](int in) { return in == b; }, [&](float v, uint32_t, double y, int in) {
+                const uint32_t k = order_of(v);
+                if ((k & mask) != key) return;
+                atomicAdd(&l.digits.count[k >> shift & 255], 1u);
+                atomicAdd(&l.digits.sum[k >> shift & 255], whole_of(y, in));
+            });
+            __syncthreads();
+            if (tid < 64) {             // lane 0 has the four highest digits
+                uint32_t c[4], upto_c = 0;
+                unsigned long long t[4], upto_t = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    c[j] = l.digits.count[255 - (4 * tid + j)];
+                    t[j] = l.digits.sum[255 - (4 * tid + j)];
+                    upto_c += c[j];
+                    upto_t += t[j];
+                }
+                for (int o = 1; o < 64; o <<= 1) {
+                    const uint32_t xc = __shfl_up(upto_c, o, 64);
+                    const unsigned long long xt = __shfl_up(upto_t, o, 64);
+                    if ((int)tid >= o) { upto_c += xc; upto_t += xt; }
+                }
+                uint32_t from_c = before + upto_c;
+                unsigned long long from_t = sum + upto_t;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { from_c -= c[j]; from_t -= t[j]; }
+                int first = -1, last = -1;
+                uint32_t first_c = 0, last_c = 0;
+                unsigned long long first_t = 0, last_t = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (c[j]) {
+                        last = j; last_c = from_c; last_t = from_t;
+                        if (first < 0 && passes(from_c + c[j], from_t + t[j])) { first = j; first_c = from_c; first_t = from_t; }
+                    }
+                    from_c += c[j];
+                    from_t += t[j];
+                }
+                const uint64_t yes = __ballot(first >= 0), some = __ballot(last >= 0);
+                const int lane = yes ? __ffsll((unsigned long long)yes) - 1 : 63 - __clzll((long long)some);
+                if ((int)tid == lane) {
+                    const int j = yes ? first : last;
+                    l.digit.key = 255 - (4 * tid + j);
+                    l.digit.before = yes ? first_c : last_c;
+                    l.digit.sum = yes ? first_t : last_t;
+                    l.digit.equal = c[j];
+                    l.digit.each = t[j] / c[j];
+                }
             }
             __syncthreads();
-            if (s.before == 0) { n = 1; total = whole(weight(top, top, r.k), r); }
-            else if (s.before < n) { n = s.before; total = s.total; }
+            key |= l.digit.key << shift;
+            mask |= 255u << shift;
+            before = l.digit.before;
+            sum = l.digit.sum;
         }
-        kept = n;
-        const double goal = (double)a.u[row] * (double)total;
-        auto cond = [=](uint32_t c, uint64_t t) { return (double)t > goal || c >= n; };
-        const Border b = find_border<T>(x, r, s, cond);
-        key = b.key;
-        skip = within(b, cond) - 1;
+        const uint32_t equal = l.digit.equal;
+        const unsigned long long weight = l.digit.each;
+        uint32_t lo = 1, hi = equal;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (passes(before + mid, sum + mid * weight)) hi = mid;
+            else lo = mid + 1;
+        }
+        return {before + lo, key, lo - 1, sum + lo * weight};
     }
+};
+
+template <typename T>
+__global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
+    __shared__ PickLds l;
+    const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const RowTop top = row_top<kPickThreads>(w.tops + (size_t)row * sh.nchunk, sh.nchunk, l.fbuf, l.ibuf);
+    const float temp = a.temperature ? a.temperature[row] : 1.f;
+    if (top.m == -INFINITY || !(temp > 0.f)) {
+        if (tid == 0) {
+            a.token[row] = top.m == -INFINITY ? -1 : top.at;
+            if (a.kept) a.kept[row] = top.m == -INFINITY ? 0 : 1;
+        }
+        return;
+    }
+    Picker<T> p{static_cast<const T *>(a.logits) + row * a.logits_row, a.vocab, tid, bin_scale(top.m, temp), l};
+    const double u = fmax(fmin((double)a.u[row], 1.0 - 0x1p-24), 0.0);
+    // running counts and sums in front of the bins, two bins a thread, always added alike
+    {
+        const uint32_t b = tid * 2;
+        const uint2 c = *reinterpret_cast<const uint2 *>(w.counts + (size_t)row * kBins + b);
+        const unsigned long long s0 = w.sums[(size_t)row * kBins + b], s1 = w.sums[(size_t)row * kBins + b + 1];
+        const double v0 = exp(-(double)b / kBinsPerNat) * (double)s0, v1 = exp(-(double)(b + 1) / kBinsPerNat) * (double)s1;
+        uint32_t upto = c.x + c.y;
+        double sum = v0 + v1;
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t xc = __shfl_up(upto, o, 64);
+            const double xs = __shfl_up(sum, o, 64);
+            if ((int)lane >= o) { upto += xc; sum = xs + sum; }
+        }
+        const uint32_t prior_c = __shfl_up(upto, 1, 64);
+        const double prior_s = __shfl_up(sum, 1, 64);
+        if (lane == 63) { l.ubuf[wave] = upto; l.dbuf[wave] = sum; }
+        if (tid < 6) l.found[tid] = 0x7FFFFFFF;
+        if (tid < kBins / 32) l.marked[tid] = 0;
+        if (tid == 0) { l.lo = 0x7FFFFFFF; l.hi = -1; l.n = 0; }
+        __syncthreads();
+        uint32_t from_c = 0;
+        double from_s = 0;
+        for (uint32_t i = 0; i < wave; ++i) { from_c += l.ubuf[i]; from_s += l.dbuf[i]; }
+        if (lane) { from_c += prior_c; from_s += prior_s; }
+        l.count[b] = from_c;
+        l.sum[b] = from_s;
+        l.count[b + 1] = from_c + c.x;
+        l.sum[b + 1] = from_s + v0;
+        if (tid == kPickThreads - 1) { l.count[kBins] = from_c + c.x + c.y; l.sum[kBins] = from_s + v0 + v1; }
+        const uint64_t some = __ballot(c.x + c.y > 0);
+        if (some && lane == 0) l.ibuf[wave] = (int)(wave * 64 + 63 - __clzll((long long)some));
+        else if (lane == 0) l.ibuf[wave] = -1;
+    }
+    __syncthreads();
+    const uint32_t all = l.count[kBins];
+    const bool by_k = a.top_k && a.top_k[row] > 0 && (uint32_t)a.top_k[row] < all, by_p = a.top_p && a.top_p[row] < 1.f, by_m = a.min_p && a.min_p[row] > 0.f;
+    const uint32_t most = by_k ? (uint32_t)a.top_k[row] : all;
+    const double share = by_p ? (double)a.top_p[row] : 1.0;
+    const double reach = by_m ? -log((double)a.min_p[row]) * kBinsPerNat : 0.0;        // weights of at least min_p lie up to this place
+    // the bins that the borders may lie in.  Ends of what C(n) may be: low, high.
+    int last = -1;
+    for (uint32_t i = 0; i < kPickThreads / 64; ++i) last = max(last, l.ibuf[i]);
+    last = l.count[2 * last + 2] > l.count[2 * last + 1] ? 2 * last + 1 : 2 * last;     // the last bin with entries
+    auto found = [&](int slot) { return min(l.found[slot], last); };
+    int bk = last;
+    double low = l.sum[kBins], high = low;
+    if (by_k) {
+        p.look(0, [&](uint32_t b) { return l.count[b + 1] >= most; });
+        __syncthreads();
+        bk = found(0);
+        low = l.sum[bk];
+        high = l.sum[bk + 1];
+    }
+    int p0 = -1, p1 = -1, bm = -1;
+    if (by_p) {
+        const double g0 = share * low, g1 = share * high;
+        p.look(1, [&](uint32_t b) { return l.sum[b + 1] >= g0; });
+        p.look(2, [&](uint32_t b) { return l.sum[b + 1] >= g1; });
+        __syncthreads();
+        p0 = found(1);
+        p1 = max(p0, found(2));
+        low = fmin(low, l.sum[p0]);
+        high = fmin(high, l.sum[p1 + 1]);
+    }
+    if (by_m) {
+        bm = reach < 0.0 ? 0 : bin_of(reach);
+        low = fmin(low, l.sum[bm]);
+        high = fmin(high, l.sum[bm + 1]);
+    }
+    int d0, d1;
+    {
+        const double g0 = u * low, g1 = u * high;
+        p.look(3, [&](uint32_t b) { return l.sum[b + 1] > g0; });
+        p.look(4, [&](uint32_t b) { return l.sum[b + 1] > g1; });
+        __syncthreads();
+        d0 = found(3);
+        d1 = max(d0, found(4));
+    }
+    auto marked = [&](int b) { return (by_k && b == bk) || (b >= p0 && b <= p1) || b == bm || (b >= d0 && b <= d1); };
+    {       // where the bins' entries begin in the list
+        const uint32_t b = tid * 2;
+        const bool m0 = marked(b), m1 = marked(b + 1);
+        const uint32_t c0 = m0 ? l.count[b + 1] - l.count[b] : 0, c1 = m1 ? l.count[b + 2] - l.count[b + 1] : 0;
+        uint32_t upto = c0 + c1;
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t xc = __shfl_up(upto, o, 64);
+            if ((int)lane >= o) upto += xc;
+        }
+        if (lane == 63) l.ubuf[wave] = upto;
+        __syncthreads();
+        uint32_t from = upto - c0 - c1;
+        for (uint32_t i = 0; i < wave; ++i) from += l.ubuf[i];
+        l.start[b] = (uint16_t)min(from, kList);
+        l.start[b + 1] = (uint16_t)min(from + c0, kList);
+        if (m0 | m1) {
+            atomicOr(&l.marked[b / 32], (m0 ? 1u : 0u) << b % 32 | (m1 ? 2u : 0u) << b % 32);
+            atomicMin(&l.lo, (int)(m0 ? b : b + 1));
+            atomicMax(&l.hi, (int)(m1 ? b + 1 : b));
+        }
+        if (tid == kPickThreads - 1) l.n = from + c0 + c1;
+    }
+    __syncthreads();
+    const uint32_t n = l.n;
+    const bool listed = n <= kList;
+    if (listed) {
+        __syncthreads();
+        if (tid == 0) l.n = 0;
+        __syncthreads();
+        p.each(l.lo, l.hi, [&](int b) { return l.marked[b / 32] >> b % 32 & 1; }, [&](float v, uint32_t i, double, int) {
+            const uint32_t at = atomicAdd(&l.n, 1u);
+            if (at < kList) l.list.raw[at] = (unsigned long long)~order_of(v) << 32 | i;
+        });
+        __syncthreads();
+        // each entry's place: how many come before it, counted by as many threads as there are for one
+        uint32_t g = 64;
+        while (g > 1 && n * g > kPickThreads) g /= 2;
+        const uint32_t e = tid / g;
+        if (e < n) {
+            const unsigned long long mine = l.list.raw[e];
+            uint32_t before = 0;
+            for (uint32_t j = tid % g; j < n; j += g) before += l.list.raw[j] < mine;
+            for (uint32_t o = g / 2; o; o >>= 1) before += __shfl_xor(before, o, 64);
+            if (tid % g == 0) l.list.sorted[before] = mine;
+        }
+        __syncthreads();
+        unsigned long long weight = 0;
+        if (tid < n) {
+            const double y = p.s.place(value_of(~(uint32_t)(l.list.sorted[tid] >> 32)));
+            weight = whole_of(y, bin_of(y));
+        }
+        unsigned long long upto = weight;
+        for (int o = 1; o < 64; o <<= 1) {
+            const unsigned long long t = __shfl_up(upto, o, 64);
+            if ((int)lane >= o) upto += t;
+        }
+        if (lane == 63) l.lbuf[wave] = upto;
+        __syncthreads();
+        for (uint32_t i = 0; i < wave; ++i) upto += l.lbuf[i];
+        l.part[tid + 1] = upto;
+        if (tid == 0) l.part[0] = 0;
+        __syncthreads();
+    }
+    auto border = [&](int b, auto passes) { return listed ? p.listed(b, passes) : p.by_digits(b, passes); };
+    auto look_again = [&](int lo, int hi, auto passes) {          // the bin of a goal that is known by now; between the two that were marked
+        __syncthreads();
+        if (tid == 0) l.found[5] = 0x7FFFFFFF;
+        __syncthreads();
+        p.look(5, passes);
+        __syncthreads();
+        return min(max(found(5), lo), hi);
+    };
+    uint32_t kept = all;
+    double sum = l.sum[kBins];
+    if (by_k) {
+        const uint32_t want = most - l.count[bk];
+        const InBin in = border(bk, [=](uint32_t c, unsigned long long) { return c >= want; });
+        kept = most;
+        sum = p.sum_at(bk, in.sum);
+    }
+    if (by_p) {
+        const double goal = share * sum;
+        const int b = p0 == p1 ? p0 : look_again(p0, p1, [&](uint32_t j) { return l.sum[j + 1] >= goal; });
+        const double base = l.sum[b], front = exp(-(double)b / kBinsPerNat);
+        const InBin in = border(b, [=](uint32_t, unsigned long long t) { return base + front * (double)t >= goal; });
+        if (l.count[b] + in.count < kept) { kept = l.count[b] + in.count; sum = p.sum_at(b, in.sum); }
+    }
+    if (by_m) {
+        uint32_t c = 0;
+        unsigned long long t = 0;
+        if (reach >= 0.0) {
+            if (listed) {
+                const uint32_t at = l.start[bm];
+                uint32_t hi = l.count[bm + 1] - l.count[bm];
+                while (c < hi) {                 // how many of the bin's lie up to `reach`
+                    const uint32_t mid = (c + hi + 1) / 2;
+                    if (p.s.place(value_of(~(uint32_t)(l.list.sorted[at + mid - 1] >> 32))) <= reach) c = mid;
+                    else hi = mid - 1;
+                }
+                t = l.part[at + c] - l.part[at];
+            } else {
+                __syncthreads();
+                if (tid == 0) { l.digit.before = 0; l.digit.sum = 0; }
+                __syncthreads();
+                const int in = bm;
+                p.each(in, in, [=](int b) { return b == in; }, [&](float, uint32_t, double y, int b) {
+                    if (y <= reach) { atomicAdd(&l.digit.before, 1u); atomicAdd(&l.digit.sum, whole_of(y, b)); }
+                });
+                __syncthreads();
+                c = l.digit.before;
+                t = l.digit.sum;
+            }
+            c += l.count[bm];
+        }
+        if (c == 0) { kept = 1; sum = 34359738368.0; }
+        else if (c < kept) { kept = c; sum = p.sum_at(bm, t); }
+    }
+    const double goal = u * sum;
+    const int b = d0 == d1 ? d0 : look_again(d0, d1, [&](uint32_t j) { return l.sum[j + 1] > goal; });
+    const double base = l.sum[b], front = exp(-(double)b / kBinsPerNat);
+    const uint32_t end = kept, ahead = l.count[b];
+    const InBin in = border(b, [=](uint32_t c, unsigned long long t) { return base + front * (double)t > goal || ahead + c >= end; });
     if (a.kept && tid == 0) a.kept[row] = (int)kept;
-    for (uint32_t i0 = 0, seen = 0; i0 < a.vocab; i0 += kSampleThreads) {
+    if (listed) {
+        if (tid == 0) a.token[row] = (int)(uint32_t)l.list.sorted[l.start[b] + in.count - 1];
+        return;
+    }
+    for (uint32_t i0 = 0, seen = 0; i0 < a.vocab; i0 += kPickThreads) {          // number `skip` of the entries with that key
         const uint32_t i = i0 + tid;
-        const bool is = i < a.vocab && order_of(sane(to_f(x[i]))) == key;
+        const bool is = i < a.vocab && order_of(sane(to_f(p.x[i]))) == in.key;
         const uint64_t same = __ballot(is);
         __syncthreads();
-        if ((tid & 63) == 0) s.wave[tid >> 6] = __popcll(same);
+        if (lane == 0) l.ubuf[wave] = __popcll(same);
         __syncthreads();
-        uint32_t at = seen + __popcll(same & ((1ull << (tid & 63)) - 1));
-        for (uint32_t w = 0; w < 16; ++w) { at += w < tid >> 6 ? s.wave[w] : 0; seen += s.wave[w]; }
-        if (is && at == skip) a.token[row] = (int)i;
-        if (seen > skip) return;
+        uint32_t at = seen + __popcll(same & ((1ull << lane) - 1));
+        for (uint32_t v = 0; v < kPickThreads / 64; ++v) { at += v < wave ? l.ubuf[v] : 0; seen += l.ubuf[v]; }
+        if (is && at == in.skip) a.token[row] = (int)i;
+        if (seen > in.skip) return;
     }
+}
+
+// Chunks are multiples of 2048 entries, up to 8192 (what a bin's count has room for): as few as keep about 1024 workgroups.
+SampleShape sample_shape(const ps_sample_args &a) {
+    SampleShape sh;
+    const uint64_t rows = std::max(1u, a.n_rows), chunks = std::max<uint64_t>(1, 1024 / rows);
+    sh.chunk = (uint32_t)std::min<uint64_t>(kMostChunk, ((a.vocab + chunks - 1) / chunks + 2047) / 2048 * 2048);
+    sh.nchunk = (a.vocab + sh.chunk - 1) / sh.chunk;
+    return sh;
+}
+uint64_t sample_work(const ps_sample_args &a, const SampleShape &sh, uint8_t *base, SampleWork *w) {
+    uint64_t off = 0;
+    auto take = [&](uint64_t bytes) { uint8_t *p = base ? base + off : nullptr; off = align_up(off + bytes, kAlign); return p; };
+    w->tops = reinterpret_cast<RowTop *>(take((uint64_t)a.n_rows * sh.nchunk * sizeof(RowTop)));
+    w->sums = reinterpret_cast<unsigned long long *>(take((uint64_t)a.n_rows * kBins * 8));
+    w->counts = reinterpret_cast<uint32_t *>(take((uint64_t)a.n_rows * kBins * 4));
+    return off;
 }
 
 bool power_of_two(uint32_t v) { return v && (v & (v - 1)) == 0; }
@@ -931,9 +1366,10 @@ hipError_t launch_page_attention(const ps_page_attention_args &call, float *part
     return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_sample(const ps_sample_args &a, hipStream_t st) {
-    const uint32_t bits = a.vocab > 1 ? log2_of(a.vocab - 1) + 1 : 0;
-    hipLaunchKernelGGL(sample_kernel<T>, dim3(a.n_rows), dim3(kSampleThreads), 0, st, a, std::ldexp(1.0, 62 - (int)bits));
+hipError_t launch_sample(const ps_sample_args &a, const SampleShape &sh, const SampleWork &w, hipStream_t st) {
+    hipLaunchKernelGGL(sample_rows_kernel<T>, dim3(sh.nchunk, a.n_rows), dim3(kRowThreads), 0, st, a, sh, w);
+    hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(sh.nchunk, a.n_rows), dim3(kRowThreads), 0, st, a, sh, w);
+    hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
     return hipGetLastError();
 }
 
@@ -1026,7 +1462,8 @@ int32_t ps_sample_workspace(const ps_sample_args *a, uint64_t *bytes) {
     PS_WANT(a->type <= PS_TYPE_F32, "unknown type %u", a->type);
     PS_WANT(a->vocab >= 1 && a->vocab <= 1u << 24, "vocab 1 .. 2^24 (got %u)", a->vocab);
     PS_WANT(a->n_rows <= 65535, "up to 65535 rows (got %u)", a->n_rows);
-    *bytes = 0;
+    SampleWork w;
+    *bytes = sample_work(*a, sample_shape(*a), nullptr, &w);
     return PS_OK;
 }
 
@@ -1041,9 +1478,13 @@ int32_t ps_sample(const ps_sample_args *a, void *workspace, uint64_t workspace_b
         PS_WANT(aligned(p, 4), "settings, random numbers and outputs must be aligned to 4 bytes");
     PS_WANT(workspace_bytes >= need && (need == 0 || (workspace && aligned(workspace, kAlign))), "a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a->type == PS_TYPE_F16) PS_TRY(launch_sample<f16_t>(*a, st));
-    else if (a->type == PS_TYPE_BF16) PS_TRY(launch_sample<bf16_t>(*a, st));
-    else PS_TRY(launch_sample<float>(*a, st));
+    const SampleShape sh = sample_shape(*a);
+    PS_WANT((uint64_t)sh.nchunk * a->n_rows <= kMostGroups, "%u rows of %u entries are too many for one call", a->n_rows, a->vocab);
+    SampleWork w;
+    sample_work(*a, sh, static_cast<uint8_t *>(workspace), &w);
+    if (a->type == PS_TYPE_F16) PS_TRY(launch_sample<f16_t>(*a, sh, w, st));
+    else if (a->type == PS_TYPE_BF16) PS_TRY(launch_sample<bf16_t>(*a, sh, w, st));
+    else PS_TRY(launch_sample<float>(*a, sh, w, st));
     return PS_OK;
 }
 

@@ -330,7 +330,7 @@ def test_attention_far_into_a_large_pool():
 # ------------------------------------------------------------------ sampling
 
 def _check_sample(logits, u, token, kept, temperature=None, top_k=None, top_p=None, min_p=None):
-    """The oracle's sums are right to V 2^-53, the kernel's to 4e-11 of each weight and V 2^-(63 - log2 V): a border that lies closer to its
+    """The oracle's sums are right to V 2^-53 (2^-29 at 2^24 entries), the kernel's to 2e-11 of each weight: a border that lies closer to its
     goal than 1e-10 of the sum (2^-28 where a vocabulary passes 2^17) may be passed one entry earlier or later."""
     for i, x in enumerate(_np(logits)):
         s = dict(temperature=1.0 if temperature is None else float(temperature[i]), top_k=0 if top_k is None else int(top_k[i]),
