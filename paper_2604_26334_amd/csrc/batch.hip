@@ -699,18 +699,25 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
 // ------------------------------------------------------------------------------------ sampling
 // Launches, in order:
 //  sample_rows_kernel   a row's chunks: largest logit and where; clears the row's bins
-//  sample_bins_kernel   entries by how far they lie behind the row's largest logit, in bins of 40 / 2047 nats (the last one: all from 40 nats on):
+//  sample_bins_kernel   entries by how far they lie behind the row's largest logit, in bins of 24 / 2047 nats (the last one: all from 24 nats on):
 //                       counts, and sums of weights relative to the bin's front as whole numbers of 2^-35, so that their order does not matter
-//  sample_pick_kernel   a workgroup per row: running counts and sums over the bins say in which bins the borders lie (of top-k, top-p, min-p, and the
-//                       drawn entry).  The entries of these bins are picked out of the row (most often a few hundred), put in order, and
-//                       searched; where they are more than a list holds, each border is found by the digits of the logits' bits instead.
+//  sample_find_kernel   running counts and sums over the bins say in which bins the borders lie (of top-k, top-p, min-p, and the drawn
+//                       entry); the entries of these bins, most often a few hundred, are picked out of the row
+//  sample_pick_kernel   a workgroup per row puts them in order and searches them.  Where they are more than a list holds, each border is found by
+//                       the digits of the logits' bits instead, in passes over the row.
 // The sum of the first entries of the order is that of whole bins (64 bits, always added alike) and of a part of one, whose whole numbers are exact.
-constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 1024, kList = 1024, kMostChunk = 8192;
-constexpr double kBinsPerNat = 2047.0 / 40.0;
+constexpr uint32_t kBins = 2048, kRowThreads = 1024, kPickThreads = 512, kList = 2048, kChunk = 8192;
+constexpr double kBinsPerNat = 2047.0 / 24.0;
 
 struct RowTop { float m; int at; };
-struct SampleShape { uint32_t chunk, nchunk; };
-struct SampleWork { RowTop *tops; unsigned long long *sums; uint32_t *counts; };       // [row][chunk], [row][bin], [row][bin]
+struct SampleShape { uint32_t nchunk, find, nfind; };       // chunks of a row: of kChunk entries for the first two launches, of `find` for the third
+struct SampleWork {
+    RowTop *tops;                  // [row][chunk]
+    unsigned long long *sums;      // [row][bin]
+    uint32_t *counts;              // [row][bin]
+    uint32_t *listed;              // [row]
+    unsigned long long *list;      // [row][kList]: inverted order, index
+};
 
 // bits that order as the values do, and back: larger for larger logits
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -719,9 +726,9 @@ __device__ __forceinline__ uint32_t order_of(float v) {
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-// How far an entry lies behind the largest one, in bins; and its weight, relative to its bin's front, in whole numbers of 2^-35: exp(-g / 51.175) for a
-// place g of a bin, as a polynomial of degree 4 around the bin's middle (off by 7.5e-13 of it, the rounding by 1.5e-11); in the last bin, which
-// weighs e^-40 together, by the 32-bit exponential.
+// How far an entry lies behind the largest one, in bins; and its weight, relative to its bin's front, in whole numbers of 2^-35: exp(-g / 85.3) for a
+// place g of a bin, as a polynomial of degree 4 around the bin's middle (off by 6e-14 of it, the rounding by 1.5e-11).  In the last bin
+// by the exponential itself, as far as that leaves a whole number.
 struct BinScale {
     double rate;
     float m, coarse;
@@ -734,13 +741,13 @@ __device__ __forceinline__ BinScale bin_scale(float m, float temp) {
 }
 __device__ __forceinline__ int bin_of(double y) { return y < 2047.0 ? (int)y : 2047; }
 __device__ __forceinline__ unsigned long long whole_of(double y, int b) {
-    if (b == 2047) return (unsigned long long)(__builtin_amdgcn_exp2f(-(float)fmin((y - 2047.0) * 0.028191402850785804, 1000.0)) * 34359738368.f);
+    if (b == 2047) return y < 2047.0 + 26.0 * kBinsPerNat ? (unsigned long long)rint(exp((2047.0 - y) / kBinsPerNat) * 34359738368.0) : 0ull;
     const double h = y - (double)b - 0.5;
-    double w = 206.71118141261828;
-    w = fma(w, h, -42313.77914196292);
-    w = fma(w, h, 6496222.942769858);
-    w = fma(w, h, -664888418.192495);
-    w = fma(w, h, 34025664801.00093);
+    double w = 26.894672820306212;
+    w = fma(w, h, -9175.56587719447);
+    w = fma(w, h, 2347797.918827135);
+    w = fma(w, h, -400495194.98659545);
+    w = fma(w, h, 34158902672.398373);
     return __builtin_bit_cast(uint64_t, w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
 }
 
@@ -750,29 +757,28 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows_kernel(ps_sample_args
     __shared__ int where[kRowThreads / 64];
     const uint32_t tid = threadIdx.x, row = blockIdx.y, chunk = blockIdx.x;
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_row;
-    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
+    const uint32_t lo = chunk * kChunk, hi = min(a.vocab, lo + kChunk);
     RowTop r{-INFINITY, 0x7FFFFFFF};
-#pragma unroll 2
-    for (uint32_t i = lo + tid * 8; i < hi; i += kRowThreads * 8) {
+    const uint32_t i = lo + tid * 8;
+    if (i < hi) {
         Oct<T> o;
         o.fill(x, i, hi);
-        float v[8], mx = -INFINITY;
+        float v[8];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             o.take(v[e], v[e + 1]);
-            mx = fmaxf(mx, fmaxf(v[e], v[e + 1]));
+            r.m = fmaxf(r.m, fmaxf(v[e], v[e + 1]));
         }
-        if (mx > r.m) {
-            r.m = mx;
+        if (r.m > -INFINITY)
 #pragma unroll
-            for (int e = 7; e >= 0; --e) r.at = v[e] == mx ? (int)(i + e) : r.at;
-        }
+            for (int e = 7; e >= 0; --e) r.at = v[e] == r.m ? (int)(i + e) : r.at;
     }
     const uint32_t per = (kBins + sh.nchunk - 1) / sh.nchunk;
     for (uint32_t b = chunk * per + tid; b < min(kBins, (chunk + 1) * per); b += kRowThreads) {
         w.sums[(size_t)row * kBins + b] = 0;
         w.counts[(size_t)row * kBins + b] = 0;
     }
+    if (chunk == 0 && tid == 0) w.listed[row] = 0;
     float m = r.m;
     for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     int at = r.m == m ? r.at : 0x7FFFFFFF;
@@ -832,8 +838,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_bins_kernel(ps_sample_args
     __syncthreads();
     const BinScale s = bin_scale(m, temp);
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_row;
-    const uint32_t lo = chunk * sh.chunk, hi = min(a.vocab, lo + sh.chunk);
-    for (uint32_t i = lo + tid * 8; i < hi; i += kRowThreads * 8) {
+    const uint32_t lo = chunk * kChunk, hi = min(a.vocab, lo + kChunk);
+    const uint32_t i = lo + tid * 8;
+    if (i < hi) {
         Oct<T> o;
         o.fill(x, i, hi);
 #pragma unroll
@@ -859,22 +866,222 @@ __global__ __launch_bounds__(kRowThreads) void sample_bins_kernel(ps_sample_args
     }
 }
 
-struct PickLds {
+// What the borders of a row are found by, and the bins that they may lie in: up to four runs of bins, apart and ascending
+struct Wanted { uint32_t most; bool by_k, by_p, by_m; double share, reach, u; int bk, p0, p1, bm, d0, d1; };
+struct Runs {
+    int lo[4], hi[4];
+    uint32_t before[5];          // entries of the runs in front
+    __device__ __forceinline__ bool has(int b) const { return (b >= lo[0] && b <= hi[0]) || (b >= lo[1] && b <= hi[1]) || (b >= lo[2] && b <= hi[2]) || (b >= lo[3] && b <= hi[3]); }
+};
+struct BinLds {
     double sum[kBins + 1];                 // of all entries in front of a bin, and of all
     uint32_t count[kBins + 1];             // likewise
-    uint16_t start[kBins];                 // where a bin's entries begin in the list
-    uint32_t marked[kBins / 32];
-    union {
-        struct { unsigned long long raw[kList], sorted[kList]; } list;       // (inverted order, index): ascending as the order
-        struct { unsigned long long sum[256]; uint32_t count[256]; } digits;
-    };
-    unsigned long long part[kList + 1];    // running sums of the list's weights
     double dbuf[kPickThreads / 64];
-    unsigned long long lbuf[kPickThreads / 64];
     uint32_t ubuf[kPickThreads / 64];
     float fbuf[kPickThreads / 64];
-    int ibuf[kPickThreads / 64], found[6], lo, hi;
-    uint32_t n;
+    int ibuf[kPickThreads / 64], found[6];
+};
+
+// the first bin that has entries and at whose end `passes` is true, into l.found[slot] where it comes before what that holds
+template <class Passes>
+__device__ __forceinline__ void look(BinLds &l, int slot, Passes passes) {
+#pragma unroll
+    for (uint32_t j = 0; j < kBins / kPickThreads; ++j) {
+        const uint32_t b = threadIdx.x + j * kPickThreads;
+        const uint64_t yes = __ballot(l.count[b + 1] > l.count[b] && passes(b));
+        if (yes) {
+            if ((threadIdx.x & 63) == 0) atomicMin(&l.found[slot], (int)(b + __ffsll((unsigned long long)yes) - 1));
+            return;
+        }
+    }
+}
+
+// Running counts and sums of a row's bins, and where its borders may lie.  By every workgroup that needs it, always added alike.
+__device__ __forceinline__ Wanted analyse(const ps_sample_args &a, const SampleWork &w, uint32_t row, BinLds &l) {
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = tid * 4;
+    static_assert(kBins == 4 * kPickThreads, "four bins a thread");
+    Wanted q{};
+    {
+        const uint4 c = *reinterpret_cast<const uint4 *>(w.counts + (size_t)row * kBins + b);
+        const ulonglong2 s0 = *reinterpret_cast<const ulonglong2 *>(w.sums + (size_t)row * kBins + b), s1 = *reinterpret_cast<const ulonglong2 *>(w.sums + (size_t)row * kBins + b + 2);
+        const double front = exp(-(double)b / kBinsPerNat);
+        // (a bin's front is 0.988 of the one before)
+        const double v0 = front * (double)s0.x, v1 = front * 0.9883439889852305 * (double)s0.y, v2 = front * 0.9768238405632375 * (double)s1.x, v3 = front * 0.9654379711181429 * (double)s1.y;
+        const uint32_t c1 = c.x + c.y, c2 = c1 + c.z, c3 = c2 + c.w;
+        const double t1 = v0 + v1, t2 = t1 + v2, t3 = t2 + v3;
+        uint32_t upto = c3;
+        double sum = t3;
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t xc = __shfl_up(upto, o, 64);
+            const double xs = __shfl_up(sum, o, 64);
+            if ((int)lane >= o) { upto += xc; sum = xs + sum; }
+        }
+        const uint32_t prior_c = __shfl_up(upto, 1, 64);
+        const double prior_s = __shfl_up(sum, 1, 64);
+        const uint64_t some = __ballot(c3 > 0);
+        if (lane == 63) { l.ubuf[wave] = upto; l.dbuf[wave] = sum; }
+        const int mine = c.w ? 3 : c.z ? 2 : c.y ? 1 : 0, at = some ? 63 - __clzll((long long)some) : 0;
+        const int last = (int)(wave * 64 + at) * 4 + __shfl(mine, at, 64);
+        if (lane == 0) l.ibuf[wave] = some ? last : -1;
+        if (tid < 6) l.found[tid] = 0x7FFFFFFF;
+        __syncthreads();
+        uint32_t from_c = 0;
+        double from_s = 0;
+        for (uint32_t i = 0; i < wave; ++i) { from_c += l.ubuf[i]; from_s += l.dbuf[i]; }
+        if (lane) { from_c += prior_c; from_s += prior_s; }
+        l.count[b] = from_c;
+        l.count[b + 1] = from_c + c.x;
+        l.count[b + 2] = from_c + c1;
+        l.count[b + 3] = from_c + c2;
+        l.sum[b] = from_s;
+        l.sum[b + 1] = from_s + v0;
+        l.sum[b + 2] = from_s + t1;
+        l.sum[b + 3] = from_s + t2;
+        if (tid == kPickThreads - 1) { l.count[kBins] = from_c + c3; l.sum[kBins] = from_s + t3; }
+    }
+    __syncthreads();
+    int last = -1;                              // the last bin with entries
+    for (uint32_t i = 0; i < kPickThreads / 64; ++i) last = max(last, l.ibuf[i]);
+    const uint32_t all = l.count[kBins];
+    q.by_k = a.top_k && a.top_k[row] > 0 && (uint32_t)a.top_k[row] < all;
+    q.by_p = a.top_p && a.top_p[row] < 1.f;
+    q.by_m = a.min_p && a.min_p[row] > 0.f;
+    q.most = q.by_k ? (uint32_t)a.top_k[row] : all;
+    q.share = q.by_p ? (double)a.top_p[row] : 1.0;
+    q.reach = q.by_m ? -log((double)a.min_p[row]) * kBinsPerNat : 0.0;        // weights of at least min_p lie up to this place
+    q.u = fmax(fmin((double)a.u[row], 1.0 - 0x1p-24), 0.0);
+    auto found = [&](int slot) { return min(l.found[slot], last); };
+    double low = l.sum[kBins], high = low;      // what C(n) may be
+    q.bk = q.p0 = q.p1 = q.bm = -1;
+    if (q.by_k) {
+        look(l, 0, [&](uint32_t j) { return l.count[j + 1] >= q.most; });
+        __syncthreads();
+        q.bk = found(0);
+        low = l.sum[q.bk];
+        high = l.sum[q.bk + 1];
+    }
+    if (q.by_p) {
+        const double g0 = q.share * low, g1 = q.share * high;
+        look(l, 1, [&](uint32_t j) { return l.sum[j + 1] >= g0; });
+        look(l, 2, [&](uint32_t j) { return l.sum[j + 1] >= g1; });
+        __syncthreads();
+        q.p0 = found(1);
+        q.p1 = max(q.p0, found(2));
+        low = fmin(low, l.sum[q.p0]);
+        high = fmin(high, l.sum[q.p1 + 1]);
+    }
+    if (q.by_m) {
+        q.bm = q.reach < 0.0 ? 0 : bin_of(q.reach);
+        low = fmin(low, l.sum[q.bm]);
+        high = fmin(high, l.sum[q.bm + 1]);
+    }
+    const double g0 = q.u * low, g1 = q.u * high;
+    look(l, 3, [&](uint32_t j) { return l.sum[j + 1] > g0; });
+    look(l, 4, [&](uint32_t j) { return l.sum[j + 1] > g1; });
+    __syncthreads();
+    q.d0 = found(3);
+    q.d1 = max(q.d0, found(4));
+    return q;
+}
+__device__ __forceinline__ Runs runs_of(const Wanted &q, const BinLds &l) {
+    Runs r{{q.by_k ? q.bk : (int)kBins, q.by_p ? q.p0 : (int)kBins, q.by_m ? q.bm : (int)kBins, q.d0}, {q.by_k ? q.bk : -1, q.by_p ? q.p1 : -1, q.by_m ? q.bm : -1, q.d1}, {}};
+    auto order = [&](int i, int j) {
+        if (r.lo[j] < r.lo[i]) {
+            const int lo = r.lo[i], hi = r.hi[i];
+            r.lo[i] = r.lo[j]; r.hi[i] = r.hi[j];
+            r.lo[j] = lo; r.hi[j] = hi;
+        }
+    };
+    order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2);
+    int end = -1;
+    r.before[0] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.lo[i] = max(r.lo[i], end + 1);
+        const bool some = r.lo[i] <= r.hi[i];
+        r.before[i + 1] = r.before[i] + (some ? l.count[r.hi[i] + 1] - l.count[r.lo[i]] : 0);
+        end = max(end, r.hi[i]);
+    }
+    return r;
+}
+// where a bin's entries begin in the list
+__device__ __forceinline__ uint32_t start_of(const Runs &r, const BinLds &l, int b) {
+    uint32_t at = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at = b >= r.lo[i] && b <= r.hi[i] ? r.before[i] + l.count[b] - l.count[r.lo[i]] : at;
+    return at;
+}
+
+// every entry lo .. hi - 1 of a row (by `kThreads` threads) in a bin for which want(bin) is true: take(value, index, place, bin)
+template <typename T, uint32_t kThreads, class Want, class Take>
+__device__ __forceinline__ void each_in(const T *x, uint32_t lo, uint32_t hi, const BinScale &s, int b0, int b1, Want want, Take take) {
+    const float from = (float)b0 - 2.f, to = b1 >= 2045 ? INFINITY : (float)b1 + 3.f;
+    for (uint32_t i = lo + threadIdx.x * 8; i < hi; i += kThreads * 8) {
+        Oct<T> o;
+        o.fill(x, i, hi);
+        float v[8];
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) o.take(v[e], v[e + 1]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = s.about(v[e]);
+            any |= y >= from && y <= to;
+        }
+        if (!any) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float about = s.about(v[e]);
+            if (!(about >= from && about <= to) || v[e] == -INFINITY) continue;
+            const double y = s.place(v[e]);
+            const int b = bin_of(y);
+            if (want(b)) take(v[e], i + e, y, b);
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kPickThreads) void sample_find_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
+    __shared__ BinLds l;
+    __shared__ unsigned long long mine[kList];
+    __shared__ uint32_t n, at;
+    const uint32_t tid = threadIdx.x, row = blockIdx.y;
+    const float temp = a.temperature ? a.temperature[row] : 1.f;
+    if (!(temp > 0.f)) return;
+    const float m = row_top<kPickThreads>(w.tops + (size_t)row * sh.nchunk, sh.nchunk, l.fbuf, l.ibuf).m;
+    if (m == -INFINITY) return;
+    if (tid == 0) n = 0;
+    __syncthreads();
+    const Wanted q = analyse(a, w, row, l);
+    const Runs r = runs_of(q, l);
+    if (r.before[4] > kList) return;
+    const uint32_t lo = blockIdx.x * sh.find, hi = min(a.vocab, lo + sh.find);
+    int b0 = kBins, b1 = -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (r.lo[i] <= r.hi[i]) { b0 = min(b0, r.lo[i]); b1 = max(b1, r.hi[i]); }
+    each_in<T, kPickThreads>(static_cast<const T *>(a.logits) + row * a.logits_row, lo, hi, bin_scale(m, temp), b0, b1, [&](int b) { return r.has(b); }, [&](float v, uint32_t i, double, int) {
+        const uint32_t slot = atomicAdd(&n, 1u);
+        if (slot < kList) mine[slot] = (unsigned long long)~order_of(v) << 32 | i;
+    });
+    __syncthreads();
+    const uint32_t count = min(n, kList);
+    if (tid == 0 && count) at = atomicAdd(&w.listed[row], count);
+    __syncthreads();
+    for (uint32_t i = tid; i < count; i += kPickThreads)
+        if (at + i < kList) w.list[(size_t)row * kList + at + i] = mine[i];
+}
+
+struct PickLds {
+    BinLds bins;
+    union {
+        unsigned long long raw[kList];
+        unsigned long long part[kList + 1];    // running sums of the list's weights
+        struct { unsigned long long sum[256]; uint32_t count[256]; } digits;
+    };
+    unsigned long long sorted[kList];
+    uint32_t filled[4];
+    unsigned long long lbuf[kPickThreads / 64];
     struct { uint32_t key, before, equal; unsigned long long sum, each; } digit;
 };
 // a part of one bin: its first `count` entries, whose weights are `sum`; by digits: the last one is number `skip` of those with `key`
@@ -885,54 +1092,17 @@ struct Picker {
     const T *x;
     uint32_t vocab, tid;
     BinScale s;
+    Runs runs;
     PickLds &l;
 
-    __device__ __forceinline__ double sum_at(int b, unsigned long long part) const { return l.sum[b] + exp(-(double)b / kBinsPerNat) * (double)part; }
-
-    // the first bin that has entries and at whose end `passes` is true, or the last one with entries; into l.found[slot], which holds that
-    template <class Passes>
-    __device__ __forceinline__ void look(int slot, Passes passes) {
-#pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) {
-            const uint32_t b = tid + j * kPickThreads;
-            const uint64_t yes = __ballot(l.count[b + 1] > l.count[b] && passes(b));
-            if (yes && (tid & 63) == 0) atomicMin(&l.found[slot], (int)(b + __ffsll((unsigned long long)yes) - 1));
-        }
-    }
-    // every entry of the row in a bin for which want(bin) is true: take(value, index, place, bin)
-    template <class Want, class Take>
-    __device__ __forceinline__ void each(int lo, int hi, Want want, Take take) {
-        const float from = (float)lo - 2.f, to = hi >= 2045 ? INFINITY : (float)hi + 3.f;
-        for (uint32_t i = tid * 8; i < vocab; i += kPickThreads * 8) {
-            Oct<T> o;
-            o.fill(x, i, vocab);
-            float v[8];
-            bool any = false;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) o.take(v[e], v[e + 1]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float y = s.about(v[e]);
-                any |= y >= from && y <= to;
-            }
-            if (!any) continue;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float about = s.about(v[e]);
-                if (!(about >= from && about <= to) || v[e] == -INFINITY) continue;
-                const double y = s.place(v[e]);
-                const int b = bin_of(y);
-                if (want(b)) take(v[e], i + e, y, b);
-            }
-        }
-    }
+    __device__ __forceinline__ double sum_at(int b, unsigned long long part) const { return l.bins.sum[b] + exp(-(double)b / kBinsPerNat) * (double)part; }
 
     // by the list: the first entry of bin b at which passes(entries of the bin up to it, their sum), or its last
     template <class Passes>
     __device__ __forceinline__ InBin listed(int b, Passes passes) const {
-        const uint32_t at = l.start[b];
+        const uint32_t at = start_of(runs, l.bins, b);
         const unsigned long long base = l.part[at];
-        uint32_t lo = 1, hi = l.count[b + 1] - l.count[b];
+        uint32_t lo = 1, hi = l.bins.count[b + 1] - l.bins.count[b];
         while (lo < hi) {
             const uint32_t mid = (lo + hi) / 2;
             if (passes(mid, l.part[at + mid] - base)) hi = mid;
@@ -949,7 +1119,7 @@ struct Picker {
             __syncthreads();
             if (tid < 256) { l.digits.count[tid] = 0; l.digits.sum[tid] = 0; }
             __syncthreads();
-            each(b, b, [=](int in) { return in == b; }, [&](float v, uint32_t, double y, int in) {
+            each_in<T, kPickThreads>(x, 0, vocab, s, b, b, [=](int in) { return in == b; }, [&](float v, uint32_t, double y, int in) {
                 const uint32_t k = order_of(v);
                 if ((k & mask) != key) return;
                 atomicAdd(&l.digits.count[k >> shift & 255], 1u);
@@ -1018,7 +1188,8 @@ struct Picker {
 
 template <typename T>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
-    __shared__ PickLds l;
+    __shared__ PickLds lds;
+    BinLds &l = lds.bins;
     const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const RowTop top = row_top<kPickThreads>(w.tops + (size_t)row * sh.nchunk, sh.nchunk, l.fbuf, l.ibuf);
     const float temp = a.temperature ? a.temperature[row] : 1.f;
@@ -1029,212 +1200,126 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
         }
         return;
     }
-    Picker<T> p{static_cast<const T *>(a.logits) + row * a.logits_row, a.vocab, tid, bin_scale(top.m, temp), l};
-    const double u = fmax(fmin((double)a.u[row], 1.0 - 0x1p-24), 0.0);
-    // running counts and sums in front of the bins, two bins a thread, always added alike
-    {
-        const uint32_t b = tid * 2;
-        const uint2 c = *reinterpret_cast<const uint2 *>(w.counts + (size_t)row * kBins + b);
-        const unsigned long long s0 = w.sums[(size_t)row * kBins + b], s1 = w.sums[(size_t)row * kBins + b + 1];
-        const double v0 = exp(-(double)b / kBinsPerNat) * (double)s0, v1 = exp(-(double)(b + 1) / kBinsPerNat) * (double)s1;
-        uint32_t upto = c.x + c.y;
-        double sum = v0 + v1;
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t xc = __shfl_up(upto, o, 64);
-            const double xs = __shfl_up(sum, o, 64);
-            if ((int)lane >= o) { upto += xc; sum = xs + sum; }
-        }
-        const uint32_t prior_c = __shfl_up(upto, 1, 64);
-        const double prior_s = __shfl_up(sum, 1, 64);
-        if (lane == 63) { l.ubuf[wave] = upto; l.dbuf[wave] = sum; }
-        if (tid < 6) l.found[tid] = 0x7FFFFFFF;
-        if (tid < kBins / 32) l.marked[tid] = 0;
-        if (tid == 0) { l.lo = 0x7FFFFFFF; l.hi = -1; l.n = 0; }
-        __syncthreads();
-        uint32_t from_c = 0;
-        double from_s = 0;
-        for (uint32_t i = 0; i < wave; ++i) { from_c += l.ubuf[i]; from_s += l.dbuf[i]; }
-        if (lane) { from_c += prior_c; from_s += prior_s; }
-        l.count[b] = from_c;
-        l.sum[b] = from_s;
-        l.count[b + 1] = from_c + c.x;
-        l.sum[b + 1] = from_s + v0;
-        if (tid == kPickThreads - 1) { l.count[kBins] = from_c + c.x + c.y; l.sum[kBins] = from_s + v0 + v1; }
-        const uint64_t some = __ballot(c.x + c.y > 0);
-        if (some && lane == 0) l.ibuf[wave] = (int)(wave * 64 + 63 - __clzll((long long)some));
-        else if (lane == 0) l.ibuf[wave] = -1;
-    }
     __syncthreads();
-    const uint32_t all = l.count[kBins];
-    const bool by_k = a.top_k && a.top_k[row] > 0 && (uint32_t)a.top_k[row] < all, by_p = a.top_p && a.top_p[row] < 1.f, by_m = a.min_p && a.min_p[row] > 0.f;
-    const uint32_t most = by_k ? (uint32_t)a.top_k[row] : all;
-    const double share = by_p ? (double)a.top_p[row] : 1.0;
-    const double reach = by_m ? -log((double)a.min_p[row]) * kBinsPerNat : 0.0;        // weights of at least min_p lie up to this place
-    // the bins that the borders may lie in.  Ends of what C(n) may be: low, high.
-    int last = -1;
-    for (uint32_t i = 0; i < kPickThreads / 64; ++i) last = max(last, l.ibuf[i]);
-    last = l.count[2 * last + 2] > l.count[2 * last + 1] ? 2 * last + 1 : 2 * last;     // the last bin with entries
-    auto found = [&](int slot) { return min(l.found[slot], last); };
-    int bk = last;
-    double low = l.sum[kBins], high = low;
-    if (by_k) {
-        p.look(0, [&](uint32_t b) { return l.count[b + 1] >= most; });
-        __syncthreads();
-        bk = found(0);
-        low = l.sum[bk];
-        high = l.sum[bk + 1];
-    }
-    int p0 = -1, p1 = -1, bm = -1;
-    if (by_p) {
-        const double g0 = share * low, g1 = share * high;
-        p.look(1, [&](uint32_t b) { return l.sum[b + 1] >= g0; });
-        p.look(2, [&](uint32_t b) { return l.sum[b + 1] >= g1; });
-        __syncthreads();
-        p0 = found(1);
-        p1 = max(p0, found(2));
-        low = fmin(low, l.sum[p0]);
-        high = fmin(high, l.sum[p1 + 1]);
-    }
-    if (by_m) {
-        bm = reach < 0.0 ? 0 : bin_of(reach);
-        low = fmin(low, l.sum[bm]);
-        high = fmin(high, l.sum[bm + 1]);
-    }
-    int d0, d1;
-    {
-        const double g0 = u * low, g1 = u * high;
-        p.look(3, [&](uint32_t b) { return l.sum[b + 1] > g0; });
-        p.look(4, [&](uint32_t b) { return l.sum[b + 1] > g1; });
-        __syncthreads();
-        d0 = found(3);
-        d1 = max(d0, found(4));
-    }
-    auto marked = [&](int b) { return (by_k && b == bk) || (b >= p0 && b <= p1) || b == bm || (b >= d0 && b <= d1); };
-    {       // where the bins' entries begin in the list
-        const uint32_t b = tid * 2;
-        const bool m0 = marked(b), m1 = marked(b + 1);
-        const uint32_t c0 = m0 ? l.count[b + 1] - l.count[b] : 0, c1 = m1 ? l.count[b + 2] - l.count[b + 1] : 0;
-        uint32_t upto = c0 + c1;
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t xc = __shfl_up(upto, o, 64);
-            if ((int)lane >= o) upto += xc;
-        }
-        if (lane == 63) l.ubuf[wave] = upto;
-        __syncthreads();
-        uint32_t from = upto - c0 - c1;
-        for (uint32_t i = 0; i < wave; ++i) from += l.ubuf[i];
-        l.start[b] = (uint16_t)min(from, kList);
-        l.start[b + 1] = (uint16_t)min(from + c0, kList);
-        if (m0 | m1) {
-            atomicOr(&l.marked[b / 32], (m0 ? 1u : 0u) << b % 32 | (m1 ? 2u : 0u) << b % 32);
-            atomicMin(&l.lo, (int)(m0 ? b : b + 1));
-            atomicMax(&l.hi, (int)(m1 ? b + 1 : b));
-        }
-        if (tid == kPickThreads - 1) l.n = from + c0 + c1;
-    }
-    __syncthreads();
-    const uint32_t n = l.n;
+    const Wanted q = analyse(a, w, row, l);
+    Picker<T> p{static_cast<const T *>(a.logits) + row * a.logits_row, a.vocab, tid, bin_scale(top.m, temp), runs_of(q, l), lds};
+    const uint32_t n = p.runs.before[4];
     const bool listed = n <= kList;
     if (listed) {
+        // the entries of each run of bins together; then an entry's place in its run: how many come before it, counted by as many threads as there
+        // are for one
+        if (tid < 4) lds.filled[tid] = 0;
         __syncthreads();
-        if (tid == 0) l.n = 0;
+        for (uint32_t i = tid; i < n; i += kPickThreads) {
+            const unsigned long long e = w.list[(size_t)row * kList + i];
+            const int b = bin_of(p.s.place(value_of(~(uint32_t)(e >> 32))));
+            uint32_t k = 0, base = 0;
+#pragma unroll
+            for (uint32_t j = 1; j < 4; ++j)
+                if (b >= p.runs.lo[j] && b <= p.runs.hi[j]) { k = j; base = p.runs.before[j]; }
+            lds.raw[base + atomicAdd(&lds.filled[k], 1u)] = e;
+        }
         __syncthreads();
-        p.each(l.lo, l.hi, [&](int b) { return l.marked[b / 32] >> b % 32 & 1; }, [&](float v, uint32_t i, double, int) {
-            const uint32_t at = atomicAdd(&l.n, 1u);
-            if (at < kList) l.list.raw[at] = (unsigned long long)~order_of(v) << 32 | i;
-        });
-        __syncthreads();
-        // each entry's place: how many come before it, counted by as many threads as there are for one
         uint32_t g = 64;
         while (g > 1 && n * g > kPickThreads) g /= 2;
-        const uint32_t e = tid / g;
-        if (e < n) {
-            const unsigned long long mine = l.list.raw[e];
+        for (uint32_t e = tid / g; e < n; e += kPickThreads / g) {
+            const unsigned long long mine = lds.raw[e];
+            uint32_t k0 = 0, k1 = n;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (e >= p.runs.before[j] && e < p.runs.before[j + 1]) { k0 = p.runs.before[j]; k1 = p.runs.before[j + 1]; }
             uint32_t before = 0;
-            for (uint32_t j = tid % g; j < n; j += g) before += l.list.raw[j] < mine;
+            for (uint32_t j = k0 + tid % g; j < k1; j += g) before += lds.raw[j] < mine;
             for (uint32_t o = g / 2; o; o >>= 1) before += __shfl_xor(before, o, 64);
-            if (tid % g == 0) l.list.sorted[before] = mine;
+            if (tid % g == 0) lds.sorted[k0 + before] = mine;
         }
         __syncthreads();
-        unsigned long long weight = 0;
-        if (tid < n) {
-            const double y = p.s.place(value_of(~(uint32_t)(l.list.sorted[tid] >> 32)));
-            weight = whole_of(y, bin_of(y));
+        constexpr int kEach = kList / kPickThreads;
+        unsigned long long weight[kEach], upto = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (tid * kEach + j < n) {
+                const double y = p.s.place(value_of(~(uint32_t)(lds.sorted[tid * kEach + j] >> 32)));
+                upto += whole_of(y, bin_of(y));
+            }
+            weight[j] = upto;
         }
-        unsigned long long upto = weight;
+        const unsigned long long mine = upto;
         for (int o = 1; o < 64; o <<= 1) {
             const unsigned long long t = __shfl_up(upto, o, 64);
             if ((int)lane >= o) upto += t;
         }
-        if (lane == 63) l.lbuf[wave] = upto;
+        if (lane == 63) lds.lbuf[wave] = upto;
         __syncthreads();
-        for (uint32_t i = 0; i < wave; ++i) upto += l.lbuf[i];
-        l.part[tid + 1] = upto;
-        if (tid == 0) l.part[0] = 0;
+        upto -= mine;
+        for (uint32_t i = 0; i < wave; ++i) upto += lds.lbuf[i];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) lds.part[tid * kEach + j + 1] = upto + weight[j];
+        if (tid == 0) lds.part[0] = 0;
         __syncthreads();
     }
     auto border = [&](int b, auto passes) { return listed ? p.listed(b, passes) : p.by_digits(b, passes); };
-    auto look_again = [&](int lo, int hi, auto passes) {          // the bin of a goal that is known by now; between the two that were marked
+    auto look_again = [&](int lo, int hi, auto passes) {          // the bin of a goal that is known by now; between the two that it may lie in
         __syncthreads();
         if (tid == 0) l.found[5] = 0x7FFFFFFF;
         __syncthreads();
-        p.look(5, passes);
+        look(l, 5, passes);
         __syncthreads();
-        return min(max(found(5), lo), hi);
+        return min(max(l.found[5], lo), hi);
     };
-    uint32_t kept = all;
+    uint32_t kept = l.count[kBins];
     double sum = l.sum[kBins];
-    if (by_k) {
-        const uint32_t want = most - l.count[bk];
-        const InBin in = border(bk, [=](uint32_t c, unsigned long long) { return c >= want; });
-        kept = most;
-        sum = p.sum_at(bk, in.sum);
+    if (q.by_k) {
+        const uint32_t want = q.most - l.count[q.bk];
+        const InBin in = border(q.bk, [=](uint32_t c, unsigned long long) { return c >= want; });
+        kept = q.most;
+        sum = p.sum_at(q.bk, in.sum);
     }
-    if (by_p) {
-        const double goal = share * sum;
-        const int b = p0 == p1 ? p0 : look_again(p0, p1, [&](uint32_t j) { return l.sum[j + 1] >= goal; });
+    if (q.by_p) {
+        const double goal = q.share * sum;
+        const int b = q.p0 == q.p1 ? q.p0 : look_again(q.p0, q.p1, [&](uint32_t j) { return l.sum[j + 1] >= goal; });
         const double base = l.sum[b], front = exp(-(double)b / kBinsPerNat);
         const InBin in = border(b, [=](uint32_t, unsigned long long t) { return base + front * (double)t >= goal; });
         if (l.count[b] + in.count < kept) { kept = l.count[b] + in.count; sum = p.sum_at(b, in.sum); }
     }
-    if (by_m) {
+    if (q.by_m) {
         uint32_t c = 0;
         unsigned long long t = 0;
-        if (reach >= 0.0) {
+        if (q.reach >= 0.0) {
             if (listed) {
-                const uint32_t at = l.start[bm];
-                uint32_t hi = l.count[bm + 1] - l.count[bm];
-                while (c < hi) {                 // how many of the bin's lie up to `reach`
+                const uint32_t at = start_of(p.runs, l, q.bm);
+                uint32_t hi = l.count[q.bm + 1] - l.count[q.bm];
+                while (c < hi) {                 // how many of the bin's lie up to `q.reach`
                     const uint32_t mid = (c + hi + 1) / 2;
-                    if (p.s.place(value_of(~(uint32_t)(l.list.sorted[at + mid - 1] >> 32))) <= reach) c = mid;
+                    if (p.s.place(value_of(~(uint32_t)(lds.sorted[at + mid - 1] >> 32))) <= q.reach) c = mid;
                     else hi = mid - 1;
                 }
-                t = l.part[at + c] - l.part[at];
+                t = lds.part[at + c] - lds.part[at];
             } else {
                 __syncthreads();
-                if (tid == 0) { l.digit.before = 0; l.digit.sum = 0; }
+                if (tid == 0) { lds.digit.before = 0; lds.digit.sum = 0; }
                 __syncthreads();
-                const int in = bm;
-                p.each(in, in, [=](int b) { return b == in; }, [&](float, uint32_t, double y, int b) {
-                    if (y <= reach) { atomicAdd(&l.digit.before, 1u); atomicAdd(&l.digit.sum, whole_of(y, b)); }
+                const int in = q.bm;
+                each_in<T, kPickThreads>(p.x, 0, a.vocab, p.s, in, in, [=](int b) { return b == in; }, [&](float, uint32_t, double y, int b) {
+                    if (y <= q.reach) { atomicAdd(&lds.digit.before, 1u); atomicAdd(&lds.digit.sum, whole_of(y, b)); }
                 });
                 __syncthreads();
-                c = l.digit.before;
-                t = l.digit.sum;
+                c = lds.digit.before;
+                t = lds.digit.sum;
             }
-            c += l.count[bm];
+            c += l.count[q.bm];
         }
         if (c == 0) { kept = 1; sum = 34359738368.0; }
-        else if (c < kept) { kept = c; sum = p.sum_at(bm, t); }
+        else if (c < kept) { kept = c; sum = p.sum_at(q.bm, t); }
     }
-    const double goal = u * sum;
-    const int b = d0 == d1 ? d0 : look_again(d0, d1, [&](uint32_t j) { return l.sum[j + 1] > goal; });
+    const double goal = q.u * sum;
+    const int b = q.d0 == q.d1 ? q.d0 : look_again(q.d0, q.d1, [&](uint32_t j) { return l.sum[j + 1] > goal; });
     const double base = l.sum[b], front = exp(-(double)b / kBinsPerNat);
     const uint32_t end = kept, ahead = l.count[b];
     const InBin in = border(b, [=](uint32_t c, unsigned long long t) { return base + front * (double)t > goal || ahead + c >= end; });
     if (a.kept && tid == 0) a.kept[row] = (int)kept;
     if (listed) {
-        if (tid == 0) a.token[row] = (int)(uint32_t)l.list.sorted[l.start[b] + in.count - 1];
+        if (tid == 0) a.token[row] = (int)(uint32_t)lds.sorted[start_of(p.runs, l, b) + in.count - 1];
         return;
     }
     for (uint32_t i0 = 0, seen = 0; i0 < a.vocab; i0 += kPickThreads) {          // number `skip` of the entries with that key
@@ -1251,12 +1336,15 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     }
 }
 
-// Chunks are multiples of 2048 entries, up to 8192 (what a bin's count has room for): as few as keep about 1024 workgroups.
+// Chunks of the first two launches are one round of a workgroup (and what a bin's count has room for); of the third as few as keep about 512
+// workgroups, each of which works the bins out for itself.
 SampleShape sample_shape(const ps_sample_args &a) {
     SampleShape sh;
-    const uint64_t rows = std::max(1u, a.n_rows), chunks = std::max<uint64_t>(1, 1024 / rows);
-    sh.chunk = (uint32_t)std::min<uint64_t>(kMostChunk, ((a.vocab + chunks - 1) / chunks + 2047) / 2048 * 2048);
-    sh.nchunk = (a.vocab + sh.chunk - 1) / sh.chunk;
+    const uint64_t rows = std::max(1u, a.n_rows), finds = std::max<uint64_t>(1, 512 / rows);
+    static_assert(kChunk == kRowThreads * 8 && kChunk <= 1u << 13, "eight entries a thread; 14 bits count them");
+    sh.nchunk = (a.vocab + kChunk - 1) / kChunk;
+    sh.find = (uint32_t)(((a.vocab + finds - 1) / finds + 4095) / 4096 * 4096);
+    sh.nfind = (a.vocab + sh.find - 1) / sh.find;
     return sh;
 }
 uint64_t sample_work(const ps_sample_args &a, const SampleShape &sh, uint8_t *base, SampleWork *w) {
@@ -1265,6 +1353,8 @@ uint64_t sample_work(const ps_sample_args &a, const SampleShape &sh, uint8_t *ba
     w->tops = reinterpret_cast<RowTop *>(take((uint64_t)a.n_rows * sh.nchunk * sizeof(RowTop)));
     w->sums = reinterpret_cast<unsigned long long *>(take((uint64_t)a.n_rows * kBins * 8));
     w->counts = reinterpret_cast<uint32_t *>(take((uint64_t)a.n_rows * kBins * 4));
+    w->listed = reinterpret_cast<uint32_t *>(take((uint64_t)a.n_rows * 4));
+    w->list = reinterpret_cast<unsigned long long *>(take((uint64_t)a.n_rows * kList * 8));
     return off;
 }
 
@@ -1369,6 +1459,7 @@ template <typename T>
 hipError_t launch_sample(const ps_sample_args &a, const SampleShape &sh, const SampleWork &w, hipStream_t st) {
     hipLaunchKernelGGL(sample_rows_kernel<T>, dim3(sh.nchunk, a.n_rows), dim3(kRowThreads), 0, st, a, sh, w);
     hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(sh.nchunk, a.n_rows), dim3(kRowThreads), 0, st, a, sh, w);
+    hipLaunchKernelGGL(sample_find_kernel<T>, dim3(sh.nfind, a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
     hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
     return hipGetLastError();
 }
