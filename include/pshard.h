@@ -816,7 +816,7 @@ int32_t ps_page_append(const ps_page_append_args *args, void *stream);
  *  head each), and once for each 128 rows where they have more.
  *  type F16 or BF16; head_dim 64 or 128; page a power of two, 16 .. 1024.  q, out [n_tokens][n_q_heads][head_dim], pages
  *  [n_pages][n_kv_heads][page][head_dim], all with the strides below (any order of pages, heads and rows); every address and
- *  stride in bytes a multiple of 16, 16 rows of a page span less than 2 GiB.  max_length <= width * page, max_prefix <= prefix_width * page
+ *  stride in bytes a multiple of 16, a page's rows span less than 4 GiB, pages lie less than 64 GiB apart.  max_length <= width * page, max_prefix <= prefix_width * page
  *  and max_tokens: bounds on length, prefix_length and a sequence's tokens (what lies beyond is left out: tokens beyond max_tokens
  *  are not written); work is dealt out by them.  n_prefix <= 4096, n_seq <= 65535; out may not overlap any input.
  * Scores, softmax and sums in fp32; the weights of the value product are rounded to `type`, and their sum is taken of the rounded

@@ -120,9 +120,9 @@ __global__ __launch_bounds__(256) void page_append_kernel(ps_page_append_args a,
 //   row i, 4 c .. 4 c + 3 of each half tile of 16;
 //  weights x values, transposed: O^T = V^T P^T, B = the weights exactly as the score accumulators hold them, A = 16 dims x 32 positions of V
 //   by LDS transpose reads of rows 4 c .. 4 c + 3 of each half; and the weights' sum by one more product, with ones.
-// Half a tile never crosses a page (pages are multiples of 16 positions): its rows come through a buffer whose range ends with the sequence or
-// is empty where the table names no page, so nothing else is ever read and hidden values are zeros.  A wave keeps the
-// next 64 entries of its table in a register, one a lane.
+// Half a tile never crosses a page (pages are multiples of 16 positions), so it has one address, and all of its rows lie in the pool: they are
+// read even where the sequence ends among them (page 0 where the table names none), their scores are then hidden and their values taken as zeros.
+// A wave keeps the next 64 entries of its table in a register, one a lane.
 // Sequences of few tokens (up to 32 rows of a kv head): a group's prefix is walked once for all of its rows (rows_many, or rows_few where the
 // whole group has few), and each sequence's own positions by rows_few; both in one launch, alternating, so that a CU holds products and
 // loads at the same time, and a merge of their records.  More tokens: blocks of 128 rows walk prefix and own positions one after the other.
@@ -163,12 +163,17 @@ struct PageWindow {
     __device__ __forceinline__ int operator()(int entry) const { return __builtin_amdgcn_readlane(number, entry - base); }
 };
 
-// Sixteen positions from P on (one half tile) of one kv head as a buffer: empty where no page is named or the positions have ended
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_rows(const char *pages, uint64_t page_b, uint32_t row_b, int number, int P, uint32_t mask, int n, uint32_t bytes) {
-    const uint64_t at = (uint64_t)max(number, 0) * page_b + (uint64_t)((uint32_t)P & mask) * row_b;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(pages + at), 0, number >= 0 && n > 0 ? (int)((uint32_t)(min(n, 16) - 1) * row_b + bytes) : 0, 0x00020000);
-}
-__device__ __forceinline__ u4_t piece_of(__amdgpu_buffer_rsrc_t rows, uint32_t offset) { return __builtin_bit_cast(u4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 0, 0)); }
+// Where the positions from P on of one kv head lie, as far as the page goes (strides between pages are less than 2^32 pieces of 16 bytes, a
+// page's rows span less than 2^32 bytes)
+struct PageRows {
+    const char *k, *v;
+    __device__ __forceinline__ PageRows(const ps_page_attention_args &a, const char *kc, const char *vc, int number, int P, uint32_t mask) {
+        const uint32_t page = (uint32_t)max(number, 0), row = (uint32_t)P & mask;
+        k = kc + ((uint64_t)page * (uint32_t)(a.k_page / 8) << 4) + row * (uint32_t)(a.k_row * 2);
+        v = vc + ((uint64_t)page * (uint32_t)(a.v_page / 8) << 4) + row * (uint32_t)(a.v_row * 2);
+    }
+};
+__device__ __forceinline__ u4_t piece_of(const char *rows, uint32_t offset) { return *reinterpret_cast<const u4_t *>(rows + offset); }
 
 // Values that are infinite or no number and that a row sees: what the products had zeros for (positions from .. to - 1 of a span)
 template <typename T, int N>
@@ -210,14 +215,13 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
         for (int h = 0; h < 2; ++h) {
             const int number = window(min(P + h * 16, hi - 1) >> shift);
             if (number < 0) gone |= 1u << h;
-            const __amdgpu_buffer_rsrc_t kb = half_rows(kc, a.k_page * 2, krow_b, number, P + h * 16, mask, hi - P - h * 16, D * 2);
-            const __amdgpu_buffer_rsrc_t vb = half_rows(vc, a.v_page * 2, vrow_b, number, P + h * 16, mask, hi - P - h * 16, D * 2);
+            const PageRows rows(a, kc, vc, number, P + h * 16, mask);
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) kreg[h][kk] = piece_of(kb, i * krow_b + c * 16 + kk * 64);
+            for (int kk = 0; kk < KK; ++kk) kreg[h][kk] = piece_of(rows.k, i * krow_b + c * 16 + kk * 64);
 #pragma unroll
             for (uint32_t u = h * kVLoads / 2; u < (h + 1) * kVLoads / 2; ++u) {
                 const uint32_t row = u * (64 / kRowPieces) + vrow;
-                vreg[u] = piece_of(vb, (row & 15) * vrow_b + ((lane % kRowPieces) ^ v_slot<D>(row)) * 16);
+                vreg[u] = piece_of(rows.v, (row & 15) * vrow_b + ((lane % kRowPieces) ^ v_slot<D>(row)) * 16);
             }
         }
     };
@@ -275,6 +279,14 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
             for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) S[t][h] = M::mul(__builtin_bit_cast(v8, kreg[h][kk]), q[t][kk], S[t][h]);
+        if (missing || P0 + (int)kTile > hi) {
+            asm volatile("");
+#pragma unroll
+            for (uint32_t u = 0; u < kVLoads; ++u) {
+                const uint32_t row = u * (64 / kRowPieces) + vrow;
+                vreg[u] = P0 + (int)row < hi && !(missing >> (2 * u / kVLoads) & 1) ? vreg[u] : u4_t{0, 0, 0, 0};
+            }
+        }
         if (P0 >= wild0) {
             bool odd = false;
 #pragma unroll
@@ -354,8 +366,9 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
 }
 
 // Rows row0 .. row0 + 127 of `set` over steps lo .. hi - 1: those of `prefix` (which every row sees), then those of `own` (row rho sees
-// positions below limit0 + rho / group).
-template <typename T, int D>
+// positions below limit0 + rho / group).  kOwn false: a prefix alone (what that leaves out frees scalar registers: 64 sequences over a prefix
+// of 32761, 109 -> 62 us).
+template <typename T, int D, bool kOwn>
 __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const RowSet &set, uint32_t row0, const Span &prefix, const Span &own, uint32_t shift, uint32_t hk,
                                           int lo, int hi, int limit0, uint32_t records, uint32_t z, float *part, unsigned char *lds) {
     using M = Mfma<T>;
@@ -375,20 +388,34 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
     const int wave_least = limit0 + (int)(min(mine0, R - 1) / G), wave_end = limit0 + (int)(min(mine0 + 31, R - 1) / G);
     const int wild0 = max(least, 0) & ~(int)(kStep - 1);
 
+    // a thread's piece of its first row of a step (further ones: a multiple of 16 rows on, with the same swizzle)
+    const uint32_t kpiece = tid / kRowPieces * krow_b + ((tid % kRowPieces) ^ k_slot<D>(tid / kRowPieces)) * 16;
+    const uint32_t vpiece = tid / kRowPieces * vrow_b + ((tid % kRowPieces) ^ v_slot<D>(tid / kRowPieces)) * 16;
     u4_t kreg[kLoads], vreg[kLoads];
     PageWindow window{-1, 1 << 30};
     int held = -1;                                       // which table the window is of
     uint32_t gone = 0;                                   // halves of the requested step that no page holds
     auto request = [&](int step) {
-        const bool mine = step >= np;
+        const bool mine = kOwn && step >= np;
         const Span &s = mine ? own : prefix;
         const int P = (mine ? step - np : step) * (int)kStep, end = mine ? own_end : prefix.len;
         if (held != (int)mine || ((P + 63) >> shift) - window.base >= 64) {
             window.fill(s, P >> shift, a.n_pages);
             held = mine;
         }
-        int number[4];
         gone = 0;
+        if (shift >= 6) {               // a page holds the whole step
+            const int number = window(P >> shift);
+            if (number < 0) gone = 15;
+            const PageRows at(a, kc, vc, number, P, mask);
+#pragma unroll
+            for (uint32_t u = 0; u < kLoads; ++u) {
+                kreg[u] = piece_of(at.k + u * (256 / kRowPieces) * krow_b, kpiece);
+                vreg[u] = piece_of(at.v + u * (256 / kRowPieces) * vrow_b, vpiece);
+            }
+            return;
+        }
+        int number[4];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
             number[h] = window(min(P + h * 16, end - 1) >> shift);
@@ -396,17 +423,27 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
         }
 #pragma unroll
         for (uint32_t u = 0; u < kLoads; ++u) {
-            const uint32_t row = (u * 256 + tid) / kRowPieces, slot = tid % kRowPieces;
             const int h = D == 128 ? (int)u : (int)(2 * u + (wave >> 1));          // (uniform)
             const int n = D == 128 ? number[u] : wave >> 1 ? number[2 * u + 1] : number[2 * u];
-            const __amdgpu_buffer_rsrc_t kb = half_rows(kc, a.k_page * 2, krow_b, n, P + h * 16, mask, end - P - h * 16, D * 2);
-            const __amdgpu_buffer_rsrc_t vb = half_rows(vc, a.v_page * 2, vrow_b, n, P + h * 16, mask, end - P - h * 16, D * 2);
-            kreg[u] = piece_of(kb, (row & 15) * krow_b + (slot ^ k_slot<D>(row)) * 16);
-            vreg[u] = piece_of(vb, (row & 15) * vrow_b + (slot ^ v_slot<D>(row)) * 16);
+            // (where rows are counted through two halves, the upper one's count from 16)
+            const PageRows at(a, kc, vc, n, P + h * 16, mask);
+            const uint32_t back = D == 128 ? 0u : (wave >> 1) * 16;
+            kreg[u] = piece_of(at.k - back * krow_b, kpiece);
+            vreg[u] = piece_of(at.v - back * vrow_b, vpiece);
         }
     };
     auto store = [&](int step, uint32_t buf) {
-        if (step >= np && (step - np) * (int)kStep >= wild0) {
+        const bool mine = kOwn && step >= np;
+        const int P = (mine ? step - np : step) * (int)kStep, end = mine ? own_end : prefix.len;
+        if (gone || P + (int)kStep > end) {
+            asm volatile("");
+#pragma unroll
+            for (uint32_t u = 0; u < kLoads; ++u) {
+                const uint32_t row = (u * 256 + tid) / kRowPieces;
+                vreg[u] = P + (int)row < end && !(gone >> (row >> 4) & 1) ? vreg[u] : u4_t{0, 0, 0, 0};
+            }
+        }
+        if (mine && P >= wild0) {
             bool odd = false;
 #pragma unroll
             for (uint32_t u = 0; u < kLoads; ++u) odd |= made_finite<T>(vreg[u]);
@@ -419,7 +456,6 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
             *reinterpret_cast<u4_t *>(to + kHalf + (u * 256 + tid) * 16) = vreg[u];
         }
     };
-    if (lo < hi) request(lo);
     const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
     const float c2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
     const float slack = WeightRange<T>::kSlack / c2;
@@ -460,25 +496,23 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    if (tid == 0) *wild = 0;
+    if (kOwn && tid == 0) *wild = 0;
     meet();
-    uint32_t missing = gone, next = 0;
-    if (lo < hi) {
-        store(lo, 0);
-        if (lo + 1 < hi) request(lo + 1);
-        meet();
-    }
-    for (int step = lo; step < hi; ++step) {
-        const bool mine = step >= np;
+    uint32_t missing = 0, next = 0;
+    // a step's rows are requested two rounds before it and written one before (one place each in the code: scalar registers are short)
+    if (lo < hi)
+    for (int step = lo - 2; step < hi; ++step) {
+        const bool mine = kOwn && step >= np;
         const int P0 = (mine ? step - np : step) * (int)kStep, end = mine ? own_end : prefix.len;
         const unsigned char *st = lds + ((step - lo) & 1) * 2 * kHalf;
-        if (rows) {
+        if (rows && step >= lo) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int T0 = P0 + h * (int)kTile;
                 if (T0 >= end || (mine && T0 >= wave_end)) break;            // (uniform)
                 const unsigned char *tile = st + h * kTile * D * 2;
                 f4_t S[NT][2];
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -489,6 +523,7 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
 #pragma unroll
                         for (int t = 0; t < NT; ++t) S[t][g] = M::mul(kr, q[t][kk], S[t][g]);
                     }
+                __builtin_amdgcn_s_setprio(0);
                 const uint32_t miss = missing >> (2 * h) & 3;
                 if (miss || T0 + (int)kTile > end || (mine && T0 + (int)kTile > wave_least)) {
                     asm volatile("");
@@ -501,6 +536,7 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
                 }
                 v8 P[NT];
                 weigh<T>(S, m_run, L, O, P, c2, slack);
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
                     const v8 vr = __builtin_bit_cast(v8, transposed(tile + vread[dt], 16 * D * 2));
@@ -509,13 +545,14 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
                 }
 #pragma unroll
                 for (int t = 0; t < NT; ++t) L[t] = M::mul(ones, P[t], L[t]);
+                __builtin_amdgcn_s_setprio(0);
             }
         }
-        if (step + 1 < hi) {
+        if (step + 1 >= lo && step + 1 < hi) {
             next = gone;
             store(step + 1, (step + 1 - lo) & 1);
-            if (step + 2 < hi) request(step + 2);
         }
+        if (step + 2 < hi) request(step + 2);
         meet();
         missing = next;
     }
@@ -524,7 +561,7 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
     for (int t = 0; t < NT; ++t) {
         if (mine0 + t * 16 + i >= R) continue;
         const size_t token = (size_t)set.token0 + tok[t];
-        if (*wild) {
+        if (kOwn && *wild) {
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 float o[4] = {O[t][dt][0], O[t][dt][1], O[t][dt][2], O[t][dt][3]};
@@ -568,6 +605,16 @@ __device__ __forceinline__ int prefix_of(const ps_page_attention_args &a, uint32
     }
     return -1;
 }
+// the length of the prefix that a sequence stands behind; by a whole wave
+__device__ __forceinline__ int prefix_length_behind(const ps_page_attention_args &a, uint32_t s) {
+    for (uint32_t p0 = 0; p0 < a.n_prefix; p0 += 64) {
+        const uint32_t p = p0 + (threadIdx.x & 63), at = min(p, a.n_prefix - 1);
+        const int len = prefix_length_of(a, at), lo = a.group_first[at], hi = a.group_first[at + 1];
+        const uint64_t in = __ballot(p < a.n_prefix && lo <= (int)s && (int)s < hi);
+        if (in) return __builtin_amdgcn_readlane(len, __ffsll((unsigned long long)in) - 1);
+    }
+    return 0;
+}
 // the `flat`-th block of 128 rows of all groups' tokens; rows 0: there is none
 struct GroupBlock { RowSet set; uint32_t prefix, block; };
 __device__ __forceinline__ GroupBlock group_block(const ps_page_attention_args &a, uint32_t flat) {
@@ -600,26 +647,25 @@ __device__ __forceinline__ GroupBlock group_block(const ps_page_attention_args &
 extern __shared__ u4_t page_lds[];
 
 template <typename T, int D, int NT>
-__global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, uint32_t prefix8, uint32_t own8, float *part) {
+__global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, uint32_t prefix8, float *part) {
     unsigned char *const lds = reinterpret_cast<unsigned char *>(page_lds);
     const uint32_t records = d.direct ? 0 : d.psplit + d.osplit;
-    // runs of eight workgroups (one on each XCD): prefixes and own positions in turn, as their numbers are to each other
-    const uint32_t run = blockIdx.x / 8, all = prefix8 + own8;
-    const uint32_t before = (uint32_t)((uint64_t)run * prefix8 / all), upto = (uint32_t)((uint64_t)(run + 1) * prefix8 / all);
-    if (upto > before) {
+    // the prefixes' workgroups first, in runs of eight (one on each XCD)
+    const uint32_t run = blockIdx.x / 8;
+    if (run < prefix8) {
         // blocks of the same positions follow one another on one XCD, whose L2 they share
-        const uint32_t unit = before / d.blocks * 8 + blockIdx.x % 8;
+        const uint32_t unit = run / d.blocks * 8 + blockIdx.x % 8;
         if (unit >= a.n_kv_heads * d.psplit) return;
-        const GroupBlock g = group_block(a, before % d.blocks);
+        const GroupBlock g = group_block(a, run % d.blocks);
         if (g.set.rows == 0) return;
         const uint32_t z = unit % d.psplit, hk = unit / d.psplit;
         const int len = prefix_length_of(a, g.prefix), lo = (int)min((uint64_t)z * d.plen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.plen, (uint64_t)len);
         if (lo >= hi) return;
         const Span span{a.prefix_table + g.prefix * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), len};
         if (g.set.rows <= NT * 16) rows_few<T, D, NT>(a, g.set, span, shift, hk, lo, hi, len, records, z, part, lds);
-        else rows_many<T, D>(a, g.set, g.block * 128, Span{span.table, span.entries, hi}, Span{nullptr, 0, 0}, shift, hk, lo / (int)kStep, (hi + (int)kStep - 1) / (int)kStep, 0, records, z, part, lds);
+        else rows_many<T, D, false>(a, g.set, g.block * 128, Span{span.table, span.entries, hi}, Span{nullptr, 0, 0}, shift, hk, lo / (int)kStep, (hi + (int)kStep - 1) / (int)kStep, 0, records, z, part, lds);
     } else {
-        const uint32_t unit = (run - before) * 8 + blockIdx.x % 8, z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads;
+        const uint32_t unit = (run - prefix8) * 8 + blockIdx.x % 8, z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads;
         if (s >= a.n_seq) return;
         const SeqTokens t = tokens_of(a, s);
         const int len = length_of(a, s), lo = (int)min((uint64_t)z * d.olen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)len);
@@ -647,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void page_rows_kernel(ps_page_attention_arg
     const int steps = np + (max(last, 0) + (int)kStep - 1) / (int)kStep;
     const int lo = (int)min((uint64_t)z * d.olen, (uint64_t)steps), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)steps);
     // (a run that none of the block's rows sees leaves records of nothing)
-    rows_many<T, D>(a, set, block * 128, prefix, own, shift, hk, lo, hi, limit0, d.direct ? 0 : d.osplit, z, part, lds);
+    rows_many<T, D, true>(a, set, block * 128, prefix, own, shift, hk, lo, hi, limit0, d.direct ? 0 : d.osplit, z, part, lds);
 }
 
 // A wave per (token, query head) puts the records of its prefix's and of its sequence's runs together, in their order: value sums, then maximum
@@ -656,9 +702,10 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args a, PageDeal d, const float *part) {
     constexpr int E = D / 64, OP = D + 4;
     const uint32_t lane = threadIdx.x & 63, hb = (a.n_q_heads + 3) / 4, h = blockIdx.x % hb * 4 + (threadIdx.x >> 6), i = blockIdx.x / hb % a.max_tokens, s = blockIdx.x / hb / a.max_tokens;
+    // (all of these are asked for before one is waited for)
     const SeqTokens t = tokens_of(a, s);
+    const int len = length_of(a, s), plen = prefix_length_behind(a, s);
     if (h >= a.n_q_heads || (int)i >= t.answered) return;
-    const int p = prefix_of(a, s), plen = p < 0 ? 0 : prefix_length_of(a, p), len = length_of(a, s);
     const uint32_t np = d.shared && plen ? (plen + d.plen - 1) / d.plen : 0;
     const uint32_t positions = d.shared ? len : (plen + kStep - 1) / kStep + (len + kStep - 1) / kStep;
     const uint32_t n = np + (positions + d.olen - 1) / d.olen;
@@ -706,11 +753,11 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
 //  sample_pick_kernel   a workgroup per row puts them in order and searches them.  Where they are more than a list holds, each border is found by
 //                       the digits of the logits' bits instead, in passes over the row.
 // The sum of the first entries of the order is that of whole bins (64 bits, always added alike) and of a part of one, whose whole numbers are exact.
-constexpr uint32_t kBins = 2048, kRowThreads = 1024, kPickThreads = 512, kList = 2048, kChunk = 8192;
+constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 512, kList = 2048, kRound = kPickThreads * 8;
 constexpr double kBinsPerNat = 2047.0 / 24.0;
 
 struct RowTop { float m; int at; };
-struct SampleShape { uint32_t nchunk, find, nfind; };       // chunks of a row: of kChunk entries for the first two launches, of `find` for the third
+struct SampleShape { uint32_t top, ntop, bins, nbins, find, nfind; };       // chunks of a row for the first three launches: entries, how many
 struct SampleWork {
     RowTop *tops;                  // [row][chunk]
     unsigned long long *sums;      // [row][bin]
@@ -757,23 +804,25 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows_kernel(ps_sample_args
     __shared__ int where[kRowThreads / 64];
     const uint32_t tid = threadIdx.x, row = blockIdx.y, chunk = blockIdx.x;
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_row;
-    const uint32_t lo = chunk * kChunk, hi = min(a.vocab, lo + kChunk);
+    const uint32_t lo = chunk * sh.top, hi = min(a.vocab, lo + sh.top);
     RowTop r{-INFINITY, 0x7FFFFFFF};
-    const uint32_t i = lo + tid * 8;
-    if (i < hi) {
+#pragma unroll 2
+    for (uint32_t i = lo + tid * 8; i < hi; i += kRowThreads * 8) {
         Oct<T> o;
         o.fill(x, i, hi);
-        float v[8];
+        float v[8], mx = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             o.take(v[e], v[e + 1]);
-            r.m = fmaxf(r.m, fmaxf(v[e], v[e + 1]));
+            mx = fmaxf(mx, fmaxf(v[e], v[e + 1]));
         }
-        if (r.m > -INFINITY)
+        if (mx > r.m) {
+            r.m = mx;
 #pragma unroll
-            for (int e = 7; e >= 0; --e) r.at = v[e] == r.m ? (int)(i + e) : r.at;
+            for (int e = 7; e >= 0; --e) r.at = v[e] == mx ? (int)(i + e) : r.at;
+        }
     }
-    const uint32_t per = (kBins + sh.nchunk - 1) / sh.nchunk;
+    const uint32_t per = (kBins + sh.ntop - 1) / sh.ntop;
     for (uint32_t b = chunk * per + tid; b < min(kBins, (chunk + 1) * per); b += kRowThreads) {
         w.sums[(size_t)row * kBins + b] = 0;
         w.counts[(size_t)row * kBins + b] = 0;
@@ -791,7 +840,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows_kernel(ps_sample_args
             if (top[i] > t.m) t = {top[i], where[i]};
             else if (top[i] == t.m) t.at = min(t.at, where[i]);
         }
-        w.tops[(size_t)row * sh.nchunk + chunk] = t;
+        w.tops[(size_t)row * sh.ntop + chunk] = t;
     }
 }
 // the largest logit of a row and its lowest index; every thread of the workgroup calls it
@@ -825,45 +874,58 @@ __device__ __forceinline__ RowTop row_top(const RowTop *tops, uint32_t n, float 
 }
 
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void sample_bins_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
-    __shared__ unsigned long long bins[kBins];             // sum of weights, and from bit 49 on how many (a chunk has 2^13 at most)
-    __shared__ float fbuf[kRowThreads / 64];
-    __shared__ int ibuf[kRowThreads / 64];
+__global__ __launch_bounds__(kPickThreads) void sample_bins_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
+    __shared__ unsigned long long bins[kBins];             // sum of weights, and from bit 49 on how many: of 2^13 entries
+    __shared__ float fbuf[kPickThreads / 64];
+    __shared__ int ibuf[kPickThreads / 64];
     const uint32_t tid = threadIdx.x, row = blockIdx.y, chunk = blockIdx.x;
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (!(temp > 0.f)) return;
-    for (uint32_t b = tid; b < kBins; b += kRowThreads) bins[b] = 0;
-    const float m = row_top<kRowThreads>(w.tops + (size_t)row * sh.nchunk, sh.nchunk, fbuf, ibuf).m;
+    constexpr uint32_t kMine = kBins / kPickThreads;
+    for (uint32_t j = 0; j < kMine; ++j) bins[tid + j * kPickThreads] = 0;
+    const float m = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, fbuf, ibuf).m;
     if (m == -INFINITY) return;
     __syncthreads();
     const BinScale s = bin_scale(m, temp);
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_row;
-    const uint32_t lo = chunk * kChunk, hi = min(a.vocab, lo + kChunk);
-    const uint32_t i = lo + tid * 8;
-    if (i < hi) {
-        Oct<T> o;
-        o.fill(x, i, hi);
+    const uint32_t lo = chunk * sh.bins, hi = min(a.vocab, lo + sh.bins);
+    unsigned long long sum[kMine] = {};
+    uint32_t count[kMine] = {};
+    for (uint32_t i0 = lo; i0 < hi; i0 += 2 * kRound) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            float v[2];
-            o.take(v[0], v[1]);
+        for (uint32_t r = 0; r < 2; ++r) {
+            const uint32_t i = i0 + r * kRound + tid * 8;
+            if (i < hi) {
+                Oct<T> o;
+                o.fill(x, i, hi);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (v[j] == -INFINITY) continue;
-                const double y = s.place(v[j]);
-                const int b = bin_of(y);
-                atomicAdd(&bins[b], whole_of(y, b) + (1ull << 49));
+                for (int e = 0; e < 8; e += 2) {
+                    float v[2];
+                    o.take(v[0], v[1]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (v[j] == -INFINITY) continue;
+                        const double y = s.place(v[j]);
+                        const int b = bin_of(y);
+                        atomicAdd(&bins[b], whole_of(y, b) + (1ull << 49));
+                    }
+                }
             }
         }
-    }
-    __syncthreads();
-    for (uint32_t b = tid; b < kBins; b += kRowThreads) {
-        const unsigned long long v = bins[b];
-        if (v) {
-            atomicAdd(&w.sums[(size_t)row * kBins + b], v & ((1ull << 49) - 1));
-            atomicAdd(&w.counts[(size_t)row * kBins + b], (uint32_t)(v >> 49));
+        __syncthreads();
+        for (uint32_t j = 0; j < kMine; ++j) {             // a bin has room for two rounds
+            const unsigned long long v = bins[tid + j * kPickThreads];
+            bins[tid + j * kPickThreads] = 0;
+            sum[j] += v & ((1ull << 49) - 1);
+            count[j] += (uint32_t)(v >> 49);
         }
+        __syncthreads();
     }
+    for (uint32_t j = 0; j < kMine; ++j)
+        if (count[j]) {
+            atomicAdd(&w.sums[(size_t)row * kBins + tid + j * kPickThreads], sum[j]);
+            atomicAdd(&w.counts[(size_t)row * kBins + tid + j * kPickThreads], count[j]);
+        }
 }
 
 // What the borders of a row are found by, and the bins that they may lie in: up to four runs of bins, apart and ascending
@@ -1048,7 +1110,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_find_kernel(ps_sample_arg
     const uint32_t tid = threadIdx.x, row = blockIdx.y;
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (!(temp > 0.f)) return;
-    const float m = row_top<kPickThreads>(w.tops + (size_t)row * sh.nchunk, sh.nchunk, l.fbuf, l.ibuf).m;
+    const float m = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, l.fbuf, l.ibuf).m;
     if (m == -INFINITY) return;
     if (tid == 0) n = 0;
     __syncthreads();
@@ -1191,7 +1253,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     __shared__ PickLds lds;
     BinLds &l = lds.bins;
     const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const RowTop top = row_top<kPickThreads>(w.tops + (size_t)row * sh.nchunk, sh.nchunk, l.fbuf, l.ibuf);
+    const RowTop top = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, l.fbuf, l.ibuf);
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (top.m == -INFINITY || !(temp > 0.f)) {
         if (tid == 0) {
@@ -1336,21 +1398,26 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     }
 }
 
-// Chunks of the first two launches are one round of a workgroup (and what a bin's count has room for); of the third as few as keep about 512
-// workgroups, each of which works the bins out for itself.
+// Chunks: as many as make about 2048 workgroups of the first launch and 256 of the second; of the third as few as keep about 512, each
+// of which works the bins out for itself.
 SampleShape sample_shape(const ps_sample_args &a) {
     SampleShape sh;
-    const uint64_t rows = std::max(1u, a.n_rows), finds = std::max<uint64_t>(1, 512 / rows);
-    static_assert(kChunk == kRowThreads * 8 && kChunk <= 1u << 13, "eight entries a thread; 14 bits count them");
-    sh.nchunk = (a.vocab + kChunk - 1) / kChunk;
-    sh.find = (uint32_t)(((a.vocab + finds - 1) / finds + 4095) / 4096 * 4096);
-    sh.nfind = (a.vocab + sh.find - 1) / sh.find;
+    const uint64_t rows = std::max(1u, a.n_rows);
+    static_assert(2 * kRound <= 1u << 13, "two rounds in a bin: 14 bits count them");
+    auto cut = [&](uint64_t groups, uint32_t multiple, uint32_t *len, uint32_t *n) {
+        const uint64_t chunks = std::max<uint64_t>(1, groups / rows);
+        *len = (uint32_t)(((a.vocab + chunks - 1) / chunks + multiple - 1) / multiple * multiple);
+        *n = (a.vocab + *len - 1) / *len;
+    };
+    cut(2048, 2048, &sh.top, &sh.ntop);
+    cut(256, kRound / 2, &sh.bins, &sh.nbins);
+    cut(512, kRound, &sh.find, &sh.nfind);
     return sh;
 }
 uint64_t sample_work(const ps_sample_args &a, const SampleShape &sh, uint8_t *base, SampleWork *w) {
     uint64_t off = 0;
     auto take = [&](uint64_t bytes) { uint8_t *p = base ? base + off : nullptr; off = align_up(off + bytes, kAlign); return p; };
-    w->tops = reinterpret_cast<RowTop *>(take((uint64_t)a.n_rows * sh.nchunk * sizeof(RowTop)));
+    w->tops = reinterpret_cast<RowTop *>(take((uint64_t)a.n_rows * sh.ntop * sizeof(RowTop)));
     w->sums = reinterpret_cast<unsigned long long *>(take((uint64_t)a.n_rows * kBins * 8));
     w->counts = reinterpret_cast<uint32_t *>(take((uint64_t)a.n_rows * kBins * 4));
     w->listed = reinterpret_cast<uint32_t *>(take((uint64_t)a.n_rows * 4));
@@ -1377,7 +1444,10 @@ int32_t check_page_attention(const ps_page_attention_args *a) {
     return PS_OK;
 }
 
-// How the work is dealt out: see the comments at the kernels.  Runs bring the launch to about the workgroups that the chip holds at once (two per CU).
+// How the work is dealt out.  Runs bring the launch to about the workgroups that the chip holds at once (two per CU).  Shared prefixes beside own
+// positions: one workgroup per CU for the prefixes, which come first, so that the other place is the loads' (64 sequences, 32 / 8 heads, prefix
+// 32761: own lengths to 1000 in 105 us, to 4000 in 184; with two per CU 108 and 218); two where own positions are few (lengths of 1: 76 for 93).  Own positions of several
+// sequences, whose lengths differ: twice as many runs as places (48 of up to 8190, 16 / 8 heads of 64, 107 us for 115), where a run is not a whole sequence anyway.
 PageDeal page_deal(const ps_page_attention_args &a) {
     PageDeal d{};
     const uint32_t G = a.n_q_heads / a.n_kv_heads;
@@ -1391,9 +1461,12 @@ PageDeal page_deal(const ps_page_attention_args &a) {
     };
     if (d.shared) {
         d.nt = rows <= 16 ? 1 : 2;
-        d.blocks = prefixes ? (uint32_t)((uint64_t)a.n_tokens * G / 128 + std::min(a.n_prefix, a.n_seq)) : 0;
-        if (prefixes) cut((uint64_t)d.blocks * a.n_kv_heads, 512, a.max_prefix, 256, kStep, &d.psplit, &d.plen);
-        cut((uint64_t)a.n_seq * a.n_kv_heads, 1024, a.max_length, 128, 4 * kTile, &d.osplit, &d.olen);
+        d.blocks = prefixes ? (uint32_t)(((uint64_t)a.n_tokens * G + 127ull * a.n_prefix) / 128) : 0;
+        // about how long each part takes by itself, at 700 TFLOP/s and 5 TB/s
+        const double prefix_us = (double)a.n_tokens * a.n_q_heads * a.max_prefix * a.head_dim * 4 / 700e6, own_us = (double)a.n_seq * a.n_kv_heads * a.max_length * a.head_dim * 4 / 5e6;
+        if (prefixes) cut((uint64_t)d.blocks * a.n_kv_heads, own_us * 4 > prefix_us ? 256 : 512, a.max_prefix, 256, kStep, &d.psplit, &d.plen);
+        const uint64_t units = (uint64_t)a.n_seq * a.n_kv_heads;
+        cut(units, a.n_seq > 1 && units < 1024 ? 2048 : 1024, a.max_length, 128, 4 * kTile, &d.osplit, &d.olen);
         d.direct = d.psplit == 0 && d.osplit == 1;
     } else {
         d.blocks = (uint32_t)((rows + 127) / 128);
@@ -1430,7 +1503,7 @@ hipError_t launch_shared(const ps_page_attention_args &a, const PageDeal &d, uin
     constexpr uint32_t lds = std::max(few_lds<D, NT>(), many_lds<D>());
     const hipError_t e = take_lds(&page_shared_kernel<T, D, NT>, lds, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((page_shared_kernel<T, D, NT>), dim3((prefix8 + own8) * 8), dim3(256), lds, st, a, d, log2_of(a.page), prefix8, own8, part);
+    hipLaunchKernelGGL((page_shared_kernel<T, D, NT>), dim3((prefix8 + own8) * 8), dim3(256), lds, st, a, d, log2_of(a.page), prefix8, part);
     return hipGetLastError();
 }
 template <typename T, int D>
@@ -1446,6 +1519,7 @@ hipError_t launch_page_attention(const ps_page_attention_args &call, float *part
     ps_page_attention_args a = call;
     a.max_tokens = std::min(a.max_tokens, a.n_tokens);
     const PageDeal d = page_deal(a);
+    if (a.n_pages == 0) a.max_length = a.max_prefix = 0;         // (where there is a page, page 0 can be read)
     uint64_t prefix8, own8;
     page_groups(a, d, &prefix8, &own8);
     const hipError_t e = !d.shared ? launch_rows<T, D>(a, d, (uint32_t)own8, part, st)
@@ -1457,8 +1531,8 @@ hipError_t launch_page_attention(const ps_page_attention_args &call, float *part
 }
 template <typename T>
 hipError_t launch_sample(const ps_sample_args &a, const SampleShape &sh, const SampleWork &w, hipStream_t st) {
-    hipLaunchKernelGGL(sample_rows_kernel<T>, dim3(sh.nchunk, a.n_rows), dim3(kRowThreads), 0, st, a, sh, w);
-    hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(sh.nchunk, a.n_rows), dim3(kRowThreads), 0, st, a, sh, w);
+    hipLaunchKernelGGL(sample_rows_kernel<T>, dim3(sh.ntop, a.n_rows), dim3(kRowThreads), 0, st, a, sh, w);
+    hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(sh.nbins, a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
     hipLaunchKernelGGL(sample_find_kernel<T>, dim3(sh.nfind, a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
     hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
     return hipGetLastError();
@@ -1536,7 +1610,8 @@ int32_t ps_page_attention(const ps_page_attention_args *a, void *workspace, uint
     for (const void *p : {a->q, a->k_pages, a->v_pages, (const void *)a->out}) PS_WANT(aligned(p, 16), "q, the pages and out must be 16-byte aligned");
     for (uint64_t n : {a->q_token, a->q_head, a->k_page, a->k_head, a->k_row, a->v_page, a->v_head, a->v_row, a->out_token, a->out_head})
         PS_WANT(n % 8 == 0, "strides must be multiples of 16 bytes (got %llu elements)", (unsigned long long)n);
-    for (uint64_t n : {a->k_row, a->v_row}) PS_WANT(n <= (1ull << 30) / 16, "16 rows of a page must span less than 2 GiB (stride of %llu elements)", (unsigned long long)n);
+    for (uint64_t n : {a->k_row, a->v_row}) PS_WANT(n < (1ull << 31) / a->page, "a page's rows must span less than 4 GiB (stride of %llu elements)", (unsigned long long)n);
+    for (uint64_t n : {a->k_page, a->v_page}) PS_WANT(n < 1ull << 35, "pages must lie less than 64 GiB apart (stride of %llu elements)", (unsigned long long)n);
     for (const int32_t *p : {a->first, a->length, a->table, a->group_first, a->prefix_length, a->prefix_table}) PS_WANT(aligned(p, 4), "tables must be aligned to 4 bytes");
     PS_WANT(workspace_bytes >= need && (need == 0 || (workspace && aligned(workspace, kAlign))), "a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need);
     uint64_t prefix8, own8;
@@ -1570,7 +1645,7 @@ int32_t ps_sample(const ps_sample_args *a, void *workspace, uint64_t workspace_b
     PS_WANT(workspace_bytes >= need && (need == 0 || (workspace && aligned(workspace, kAlign))), "a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need);
     hipStream_t st = static_cast<hipStream_t>(stream);
     const SampleShape sh = sample_shape(*a);
-    PS_WANT((uint64_t)sh.nchunk * a->n_rows <= kMostGroups, "%u rows of %u entries are too many for one call", a->n_rows, a->vocab);
+    PS_WANT((uint64_t)std::max({sh.ntop, sh.nbins, sh.nfind}) * a->n_rows <= kMostGroups / 2, "%u rows of %u entries are too many for one call", a->n_rows, a->vocab);
     SampleWork w;
     sample_work(*a, sh, static_cast<uint8_t *>(workspace), &w);
     if (a->type == PS_TYPE_F16) PS_TRY(launch_sample<f16_t>(*a, sh, w, st));
