@@ -747,11 +747,11 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
 // Launches, in order:
 //  sample_rows_kernel   a row's chunks: largest logit and where; clears the row's bins
 //  sample_bins_kernel   entries by how far they lie behind the row's largest logit, in bins of 24 / 2047 nats (the last one: all from 24 nats on):
-//                       counts, and sums of weights relative to the bin's front as whole numbers of 2^-35, so that their order does not matter
+//                       counts, and sums of weights relative to the bin's middle as whole numbers of 2^-35, so that their order does not matter
 //  sample_find_kernel   running counts and sums over the bins say in which bins the borders lie (of top-k, top-p, min-p, and the drawn
 //                       entry); the entries of these bins, most often a few hundred, are picked out of the row
-//  sample_pick_kernel   a workgroup per row puts them in order and searches them.  Where they are more than a list holds, each border is found by
-//                       the digits of the logits' bits instead, in passes over the row.
+//  sample_pick_kernel   a workgroup per row finds the borders among them, digit by digit of the logits' bits.  Where they are more than a list holds, in
+//                       passes over the row instead.
 // The sum of the first entries of the order is that of whole bins (64 bits, always added alike) and of a part of one, whose whole numbers are exact.
 constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 512, kList = 2048, kRound = kPickThreads * 8;
 constexpr double kBinsPerNat = 2047.0 / 24.0;
@@ -763,7 +763,7 @@ struct SampleWork {
     unsigned long long *sums;      // [row][bin]
     uint32_t *counts;              // [row][bin]
     uint32_t *listed;              // [row]
-    unsigned long long *list;      // [row][kList]: inverted order, index
+    unsigned long long *list;      // [row][kList]
 };
 
 // bits that order as the values do, and back: larger for larger logits
@@ -771,31 +771,59 @@ __device__ __forceinline__ uint32_t order_of(float v) {
     const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f);        // (-0 is 0)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+// an entry of a list: inverted bits in front of the index (24 bits), so that it ascends as the order does
+__device__ __forceinline__ unsigned long long entry_of(float v, uint32_t i) { return (unsigned long long)~order_of(v) << 24 | i; }
 __device__ __forceinline__ float value_of(uint32_t key) { return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
+__device__ __forceinline__ float value_in(unsigned long long entry) { return value_of(~(uint32_t)(entry >> 24)); }
 
-// How far an entry lies behind the largest one, in bins; and its weight, relative to its bin's front, in whole numbers of 2^-35: exp(-g / 85.3) for a
-// place g of a bin, as a polynomial of degree 4 around the bin's middle (off by 6e-14 of it, the rounding by 1.5e-11).  In the last bin
-// by the exponential itself, as far as that leaves a whole number.
+// How far an entry lies behind the largest one, in bins: the nearest whole number and what remains, by adding 1.5 2^52 (a conversion takes as long as four
+// operations).  Its weight, relative to that of its bin's middle, in whole numbers of 2^-35: exp(-rest / 85.3) as a polynomial of degree 4 (off by
+// 6e-14 of it, the rounding by 1.5e-11).  In the last bin, which is all from 24 nats on, by the 32-bit exponential in steps of 2^-31: all of it weighs
+// at most e^-24 of the largest entry for each of its own.
+constexpr double kWhole = 6755399441055744.0;
+struct Place {
+    int n;
+    double rest;
+    __device__ __forceinline__ int bin() const { return min(n, (int)kBins - 1); }
+    __device__ __forceinline__ double value() const { return (double)n + rest; }
+};
 struct BinScale {
-    double rate;
-    float m, coarse;
-    __device__ __forceinline__ double place(float v) const { return ((double)m - (double)v) * rate; }
-    __device__ __forceinline__ float about(float v) const { return fminf((m - v) * coarse, 2047.f); }     // a place to within 0.01
+    double m, rate, least;
+    float top, coarse;
+    __device__ __forceinline__ Place place(float v) const {
+        const double d = fmax((double)v - m, least), t = fma(d, -rate, kWhole);
+        return {(int)(uint32_t)__builtin_bit_cast(uint64_t, t), fma(d, -rate, kWhole - t)};
+    }
+    __device__ __forceinline__ float about(float v) const { return fminf((top - v) * coarse, (float)kBins); }     // a place to within 0.01
 };
 __device__ __forceinline__ BinScale bin_scale(float m, float temp) {
     const double rate = kBinsPerNat / (double)fminf(temp, 1e30f);
-    return {rate, m, (float)fmin(rate, 1e30)};
+    return {(double)m, rate, -1e6 / rate, m, (float)fmin(rate, 1e30)};
 }
-__device__ __forceinline__ int bin_of(double y) { return y < 2047.0 ? (int)y : 2047; }
-__device__ __forceinline__ unsigned long long whole_of(double y, int b) {
-    if (b == 2047) return y < 2047.0 + 26.0 * kBinsPerNat ? (unsigned long long)rint(exp((2047.0 - y) / kBinsPerNat) * 34359738368.0) : 0ull;
-    const double h = y - (double)b - 0.5;
-    double w = 26.894672820306212;
-    w = fma(w, h, -9175.56587719447);
-    w = fma(w, h, 2347797.918827135);
-    w = fma(w, h, -400495194.98659545);
-    w = fma(w, h, 34158902672.398373);
-    return __builtin_bit_cast(uint64_t, w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+__device__ __forceinline__ unsigned long long whole_far(int n, double rest) {
+    const float back = (float)(n - ((int)kBins - 1)) + (float)rest;
+    return (unsigned long long)(uint32_t)(__builtin_amdgcn_exp2f(back * -0.01691484171047148f) * 2147483648.f) << 4;
+}
+// N in step: one after the other they are a chain of a dozen operations each
+template <int N>
+__device__ __forceinline__ void wholes_of(const double (&rest)[N], unsigned long long (&w)[N]) {
+    constexpr double c[5] = {27.052798810934387, -9229.51319433045, 2361601.688599304, -402849888.0468979, 34359738368.0};
+    double v[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = c[0];
+#pragma unroll
+    for (int j = 1; j < 5; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = fma(v[e], rest[e], c[j]);
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] = __builtin_bit_cast(uint64_t, v[e] + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+}
+__device__ __forceinline__ unsigned long long whole_of(const Place &y) {
+    if (y.n >= (int)kBins - 1) return whole_far(y.n, y.rest);
+    const double rest[1] = {y.rest};
+    unsigned long long w[1];
+    wholes_of(rest, w);
+    return w[0];
 }
 
 template <typename T>
@@ -891,24 +919,43 @@ __global__ __launch_bounds__(kPickThreads) void sample_bins_kernel(ps_sample_arg
     const uint32_t lo = chunk * sh.bins, hi = min(a.vocab, lo + sh.bins);
     unsigned long long sum[kMine] = {};
     uint32_t count[kMine] = {};
+    Oct<T> next;
+    next.fill(x, min(lo + tid * 8, a.vocab), hi);
     for (uint32_t i0 = lo; i0 < hi; i0 += 2 * kRound) {
 #pragma unroll
         for (uint32_t r = 0; r < 2; ++r) {
             const uint32_t i = i0 + r * kRound + tid * 8;
+            Oct<T> o = next;
+            if (i + kRound < hi) next.fill(x, i + kRound, hi);
             if (i < hi) {
-                Oct<T> o;
-                o.fill(x, i, hi);
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    float v[2];
-                    o.take(v[0], v[1]);
+                for (int half = 0; half < 2; ++half) {
+                    float v[4];
+                    double d[4], rest[4];
+                    int n[4], most = 0;
+                    unsigned long long whole[4];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        if (v[j] == -INFINITY) continue;
-                        const double y = s.place(v[j]);
-                        const int b = bin_of(y);
-                        atomicAdd(&bins[b], whole_of(y, b) + (1ull << 49));
+                    for (int e = 0; e < 4; e += 2) o.take(v[e], v[e + 1]);
+                    // (as BinScale::place has it)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) d[e] = fmax((double)v[e] - s.m, s.least);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const double t = fma(d[e], -s.rate, kWhole);
+                        n[e] = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+                        rest[e] = fma(d[e], -s.rate, kWhole - t);
+                        most = max(most, n[e]);
                     }
+                    wholes_of(rest, whole);
+                    if (most >= (int)kBins - 1)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            whole[e] = n[e] >= (int)kBins - 1 ? whole_far(n[e], rest[e]) : whole[e];
+                            n[e] = min(n[e], (int)kBins - 1);
+                        }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (v[e] != -INFINITY) atomicAdd(&bins[n[e]], whole[e] + (1ull << 49));
                 }
             }
         }
@@ -966,9 +1013,9 @@ __device__ __forceinline__ Wanted analyse(const ps_sample_args &a, const SampleW
     {
         const uint4 c = *reinterpret_cast<const uint4 *>(w.counts + (size_t)row * kBins + b);
         const ulonglong2 s0 = *reinterpret_cast<const ulonglong2 *>(w.sums + (size_t)row * kBins + b), s1 = *reinterpret_cast<const ulonglong2 *>(w.sums + (size_t)row * kBins + b + 2);
-        const double front = exp(-(double)b / kBinsPerNat);
-        // (a bin's front is 0.988 of the one before)
-        const double v0 = front * (double)s0.x, v1 = front * 0.9883439889852305 * (double)s0.y, v2 = front * 0.9768238405632375 * (double)s1.x, v3 = front * 0.9654379711181429 * (double)s1.y;
+        const double middle = exp(-(double)b / kBinsPerNat);
+        // (a bin's middle weighs 0.988 of the one before)
+        const double v0 = middle * (double)s0.x, v1 = middle * 0.9883439889852305 * (double)s0.y, v2 = middle * 0.9768238405632375 * (double)s1.x, v3 = middle * 0.9654379711181429 * (double)s1.y;
         const uint32_t c1 = c.x + c.y, c2 = c1 + c.z, c3 = c2 + c.w;
         const double t1 = v0 + v1, t2 = t1 + v2, t3 = t2 + v3;
         uint32_t upto = c3;
@@ -1033,7 +1080,7 @@ __device__ __forceinline__ Wanted analyse(const ps_sample_args &a, const SampleW
         high = fmin(high, l.sum[q.p1 + 1]);
     }
     if (q.by_m) {
-        q.bm = q.reach < 0.0 ? 0 : bin_of(q.reach);
+        q.bm = (int)rint(fmin(fmax(q.reach, 0.0), (double)(kBins - 1)));
         low = fmin(low, l.sum[q.bm]);
         high = fmin(high, l.sum[q.bm + 1]);
     }
@@ -1066,41 +1113,45 @@ __device__ __forceinline__ Runs runs_of(const Wanted &q, const BinLds &l) {
     }
     return r;
 }
-// where a bin's entries begin in the list
-__device__ __forceinline__ uint32_t start_of(const Runs &r, const BinLds &l, int b) {
-    uint32_t at = 0;
+// every entry lo .. hi - 1 of a row in one of the runs: take(value, index, place)
+template <typename T, class Take>
+__device__ __forceinline__ void each_in(const T *x, uint32_t lo, uint32_t hi, const BinScale &s, const Runs &r, Take take) {
+    float from[4], to[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) at = b >= r.lo[i] && b <= r.hi[i] ? r.before[i] + l.count[b] - l.count[r.lo[i]] : at;
-    return at;
-}
-
-// every entry lo .. hi - 1 of a row (by `kThreads` threads) in a bin for which want(bin) is true: take(value, index, place, bin)
-template <typename T, uint32_t kThreads, class Want, class Take>
-__device__ __forceinline__ void each_in(const T *x, uint32_t lo, uint32_t hi, const BinScale &s, int b0, int b1, Want want, Take take) {
-    const float from = (float)b0 - 2.f, to = b1 >= 2045 ? INFINITY : (float)b1 + 3.f;
-    for (uint32_t i = lo + threadIdx.x * 8; i < hi; i += kThreads * 8) {
-        Oct<T> o;
-        o.fill(x, i, hi);
-        float v[8];
-        bool any = false;
+    for (int j = 0; j < 4; ++j) {
+        const bool some = r.lo[j] <= r.hi[j];
+        from[j] = some ? (float)r.lo[j] - 1.f : INFINITY;
+        to[j] = !some ? -INFINITY : r.hi[j] == (int)kBins - 1 ? INFINITY : (float)r.hi[j] + 1.f;
+    }
+    constexpr uint32_t kStride = kPickThreads * 8;
+    uint32_t i = lo + threadIdx.x * 8;
+    if (i >= hi) return;
+    Oct<T> next;
+    next.fill(x, i, hi);
+    for (; i < hi; i += kStride) {
+        Oct<T> o = next;
+        if (i + kStride < hi) next.fill(x, i + kStride, hi);
+        float v[8], y[8];
+        bool in[8] = {};
 #pragma unroll
         for (int e = 0; e < 8; e += 2) o.take(v[e], v[e + 1]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = s.about(v[e]);
-            any |= y >= from && y <= to;
-        }
-        if (!any) continue;
+        for (int e = 0; e < 8; ++e) y[e] = s.about(v[e]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (r.lo[j] <= r.hi[j])         // (uniform)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) in[e] |= y[e] >= from[j] && y[e] <= to[j];
+        if (!(in[0] | in[1] | in[2] | in[3] | in[4] | in[5] | in[6] | in[7])) continue;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float about = s.about(v[e]);
-            if (!(about >= from && about <= to) || v[e] == -INFINITY) continue;
-            const double y = s.place(v[e]);
-            const int b = bin_of(y);
-            if (want(b)) take(v[e], i + e, y, b);
+            if (!in[e] || v[e] == -INFINITY) continue;
+            const Place p = s.place(v[e]);
+            if (r.has(p.bin())) take(v[e], i + e, p);
         }
     }
 }
+__device__ __forceinline__ Runs run_of(int b) { return {{b, (int)kBins, (int)kBins, (int)kBins}, {b, -1, -1, -1}, {}}; }
 
 template <typename T>
 __global__ __launch_bounds__(kPickThreads) void sample_find_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
@@ -1118,13 +1169,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_find_kernel(ps_sample_arg
     const Runs r = runs_of(q, l);
     if (r.before[4] > kList) return;
     const uint32_t lo = blockIdx.x * sh.find, hi = min(a.vocab, lo + sh.find);
-    int b0 = kBins, b1 = -1;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (r.lo[i] <= r.hi[i]) { b0 = min(b0, r.lo[i]); b1 = max(b1, r.hi[i]); }
-    each_in<T, kPickThreads>(static_cast<const T *>(a.logits) + row * a.logits_row, lo, hi, bin_scale(m, temp), b0, b1, [&](int b) { return r.has(b); }, [&](float v, uint32_t i, double, int) {
+    each_in(static_cast<const T *>(a.logits) + row * a.logits_row, lo, hi, bin_scale(m, temp), r, [&](float v, uint32_t i, const Place &) {
         const uint32_t slot = atomicAdd(&n, 1u);
-        if (slot < kList) mine[slot] = (unsigned long long)~order_of(v) << 32 | i;
+        if (slot < kList) mine[slot] = entry_of(v, i);
     });
     __syncthreads();
     const uint32_t count = min(n, kList);
@@ -1136,115 +1183,144 @@ __global__ __launch_bounds__(kPickThreads) void sample_find_kernel(ps_sample_arg
 
 struct PickLds {
     BinLds bins;
-    union {
-        unsigned long long raw[kList];
-        unsigned long long part[kList + 1];    // running sums of the list's weights
-        struct { unsigned long long sum[256]; uint32_t count[256]; } digits;
-    };
-    unsigned long long sorted[kList];
-    uint32_t filled[4];
-    unsigned long long lbuf[kPickThreads / 64];
-    struct { uint32_t key, before, equal; unsigned long long sum, each; } digit;
+    unsigned long long list[kList];
+    uint16_t bin[kList];
+    unsigned long long sum[256], both, any, spot_sum;
+    uint32_t count[256], digit, before, equal;
 };
-// a part of one bin: its first `count` entries, whose weights are `sum`; by digits: the last one is number `skip` of those with `key`
-struct InBin { uint32_t count, key, skip; unsigned long long sum; };
+// The first entries of a bin: how many, the sum of their weights, and the index of the last one
+struct Spot { uint32_t count; unsigned long long sum; int index; };
 
 template <typename T>
 struct Picker {
     const T *x;
-    uint32_t vocab, tid;
+    uint32_t vocab, n;           // n: entries in the list
+    bool listed;
     BinScale s;
-    Runs runs;
     PickLds &l;
 
     __device__ __forceinline__ double sum_at(int b, unsigned long long part) const { return l.bins.sum[b] + exp(-(double)b / kBinsPerNat) * (double)part; }
-
-    // by the list: the first entry of bin b at which passes(entries of the bin up to it, their sum), or its last
-    template <class Passes>
-    __device__ __forceinline__ InBin listed(int b, Passes passes) const {
-        const uint32_t at = start_of(runs, l.bins, b);
-        const unsigned long long base = l.part[at];
-        uint32_t lo = 1, hi = l.bins.count[b + 1] - l.bins.count[b];
-        while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (passes(mid, l.part[at + mid] - base)) hi = mid;
-            else lo = mid + 1;
+    // every entry of a bin: take(entry); from the list, or where there is none from the row
+    template <class Take>
+    __device__ __forceinline__ void entries(int b, Take take) const {
+        if (listed) {
+            for (uint32_t i = threadIdx.x; i < n; i += kPickThreads)
+                if (l.bin[i] == b) take(l.list[i]);
+        } else {
+            each_in(x, 0, vocab, s, run_of(b), [&](float v, uint32_t i, const Place &) { take(entry_of(v, i)); });
         }
-        return {lo, 0, 0, l.part[at + lo] - base};
     }
-    // the same by the digits of the entries' bits, from the highest on
+    __device__ __forceinline__ unsigned long long weight_of(unsigned long long e) const { return whole_of(s.place(value_in(e))); }
+    // Of the 256 digits that have been counted (l.count, l.sum), the first with entries at which passes(entries up to it, their sum) is true, or the last one with any;
+    // c0 and t0 come in front.  Leaves l.digit, l.equal (its entries), l.before and l.spot_sum (all in front of it).
     template <class Passes>
-    __device__ InBin by_digits(int b, Passes passes) {
-        uint32_t key = 0, mask = 0, before = 0;
+    __device__ __forceinline__ void first_digit(uint32_t c0, unsigned long long t0, Passes passes) {
+        const uint32_t tid = threadIdx.x;
+        if (tid >= 64) return;
+        uint32_t c[4], upto_c = 0;
+        unsigned long long t[4], upto_t = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            c[j] = l.count[4 * tid + j];
+            t[j] = l.sum[4 * tid + j];
+            upto_c += c[j];
+            upto_t += t[j];
+        }
+        uint32_t from_c = c0 - upto_c;
+        unsigned long long from_t = t0 - upto_t;
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t xc = __shfl_up(upto_c, o, 64);
+            const unsigned long long xt = __shfl_up(upto_t, o, 64);
+            if ((int)tid >= o) { upto_c += xc; upto_t += xt; }
+        }
+        from_c += upto_c;
+        from_t += upto_t;
+        int first = -1, last = -1;
+        uint32_t first_c = 0, last_c = 0, first_n = 0, last_n = 0;
+        unsigned long long first_t = 0, last_t = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (c[j]) {
+                last = j; last_c = from_c; last_t = from_t; last_n = c[j];
+                if (first < 0 && passes(from_c + c[j], from_t + t[j])) { first = j; first_c = from_c; first_t = from_t; first_n = c[j]; }
+            }
+            from_c += c[j];
+            from_t += t[j];
+        }
+        const uint64_t yes = __ballot(first >= 0), some = __ballot(last >= 0);
+        const int lane = yes ? __ffsll((unsigned long long)yes) - 1 : 63 - __clzll((long long)some);
+        if ((int)tid == lane) {
+            l.digit = 4 * tid + (yes ? first : last);
+            l.before = yes ? first_c : last_c;
+            l.spot_sum = yes ? first_t : last_t;
+            l.equal = yes ? first_n : last_n;
+        }
+    }
+    // The first entry of bin b (in the order) at which passes(entries of the bin up to it, their sum) is true, or its last: digit by digit of the entries' bits
+    // from the first one that is not common to all.  Equal logits weigh alike, so that the value's bits say where the sum passes, and the index's
+    // bits which entry it is (asked for by `which`).
+    template <class Passes>
+    __device__ Spot find(int b, bool which, Passes passes) {
+        const uint32_t tid = threadIdx.x;
+        __syncthreads();
+        if (tid == 0) { l.both = ~0ull; l.any = 0; }
+        __syncthreads();
+        {
+            unsigned long long both = ~0ull, any = 0;
+            entries(b, [&](unsigned long long e) { both &= e; any |= e; });
+            for (int o = 32; o; o >>= 1) { both &= __shfl_xor(both, o, 64); any |= __shfl_xor(any, o, 64); }
+            if ((tid & 63) == 0 && any) { atomicAnd(&l.both, both); atomicOr(&l.any, any); }
+        }
+        __syncthreads();
+        const unsigned long long differ = l.both ^ l.any;
+        int at = differ >> 24 ? 64 - __clzll((long long)differ) : 24;         // bits from here on are known
+        unsigned long long known = l.both >> at;
+        uint32_t before = 0, equal = l.bins.count[b + 1] - l.bins.count[b];
         unsigned long long sum = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
+        auto digits = [&](int bits, bool weigh, auto up_to) {
             __syncthreads();
-            if (tid < 256) { l.digits.count[tid] = 0; l.digits.sum[tid] = 0; }
+            if (tid < 256) { l.count[tid] = 0; l.sum[tid] = 0; }
             __syncthreads();
-            each_in<T, kPickThreads>(x, 0, vocab, s, b, b, [=](int in) { return in == b; }, [&](float v, uint32_t, double y, int in) {
-                const uint32_t k = order_of(v);
-                if ((k & mask) != key) return;
-                atomicAdd(&l.digits.count[k >> shift & 255], 1u);
-                atomicAdd(&l.digits.sum[k >> shift & 255], whole_of(y, in));
+            entries(b, [&](unsigned long long e) {
+                if (e >> at != known) return;
+                const uint32_t digit = (uint32_t)(e >> (at - bits)) & ((1u << bits) - 1);
+                atomicAdd(&l.count[digit], 1u);
+                if (weigh) atomicAdd(&l.sum[digit], weight_of(e));
             });
             __syncthreads();
-            if (tid < 64) {             // lane 0 has the four highest digits
-                uint32_t c[4], upto_c = 0;
-                unsigned long long t[4], upto_t = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    c[j] = l.digits.count[255 - (4 * tid + j)];
-                    t[j] = l.digits.sum[255 - (4 * tid + j)];
-                    upto_c += c[j];
-                    upto_t += t[j];
-                }
-                for (int o = 1; o < 64; o <<= 1) {
-                    const uint32_t xc = __shfl_up(upto_c, o, 64);
-                    const unsigned long long xt = __shfl_up(upto_t, o, 64);
-                    if ((int)tid >= o) { upto_c += xc; upto_t += xt; }
-                }
-                uint32_t from_c = before + upto_c;
-                unsigned long long from_t = sum + upto_t;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { from_c -= c[j]; from_t -= t[j]; }
-                int first = -1, last = -1;
-                uint32_t first_c = 0, last_c = 0;
-                unsigned long long first_t = 0, last_t = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (c[j]) {
-                        last = j; last_c = from_c; last_t = from_t;
-                        if (first < 0 && passes(from_c + c[j], from_t + t[j])) { first = j; first_c = from_c; first_t = from_t; }
-                    }
-                    from_c += c[j];
-                    from_t += t[j];
-                }
-                const uint64_t yes = __ballot(first >= 0), some = __ballot(last >= 0);
-                const int lane = yes ? __ffsll((unsigned long long)yes) - 1 : 63 - __clzll((long long)some);
-                if ((int)tid == lane) {
-                    const int j = yes ? first : last;
-                    l.digit.key = 255 - (4 * tid + j);
-                    l.digit.before = yes ? first_c : last_c;
-                    l.digit.sum = yes ? first_t : last_t;
-                    l.digit.equal = c[j];
-                    l.digit.each = t[j] / c[j];
-                }
-            }
+            first_digit(before, sum, up_to);
             __syncthreads();
-            key |= l.digit.key << shift;
-            mask |= 255u << shift;
-            before = l.digit.before;
-            sum = l.digit.sum;
-        }
-        const uint32_t equal = l.digit.equal;
-        const unsigned long long weight = l.digit.each;
+            at -= bits;
+            known = known << bits | l.digit;
+            before = l.before;
+            sum = l.spot_sum;
+            equal = l.equal;
+        };
+        while (at > 24) digits(min(8, at - 24), true, passes);
+        const unsigned long long each = weight_of(known << 24);
         uint32_t lo = 1, hi = equal;
         while (lo < hi) {
             const uint32_t mid = (lo + hi) / 2;
-            if (passes(before + mid, sum + mid * weight)) hi = mid;
+            if (passes(before + mid, sum + mid * each)) hi = mid;
             else lo = mid + 1;
         }
-        return {before + lo, key, lo - 1, sum + lo * weight};
+        Spot r{before + lo, sum + lo * each, 0};
+        if (which && equal == 1) {
+            __syncthreads();
+            entries(b, [&](unsigned long long e) {
+                if (e >> 24 == known) l.digit = (uint32_t)(e & 0xFFFFFF);
+            });
+            __syncthreads();
+            r.index = (int)l.digit;
+        } else if (which) {
+            const int bits = 32 - __clz((int)(vocab - 1 | 1));
+            known = known << (24 - bits);
+            at = bits;
+            const uint32_t want = r.count;
+            while (at > 0) digits(min(8, at), false, [=](uint32_t c, unsigned long long) { return c >= want; });
+            r.index = (int)(known & 0xFFFFFF);
+        }
+        return r;
     }
 };
 
@@ -1252,7 +1328,7 @@ template <typename T>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
     __shared__ PickLds lds;
     BinLds &l = lds.bins;
-    const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t row = blockIdx.x, tid = threadIdx.x;
     const RowTop top = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, l.fbuf, l.ibuf);
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (top.m == -INFINITY || !(temp > 0.f)) {
@@ -1264,63 +1340,14 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     }
     __syncthreads();
     const Wanted q = analyse(a, w, row, l);
-    Picker<T> p{static_cast<const T *>(a.logits) + row * a.logits_row, a.vocab, tid, bin_scale(top.m, temp), runs_of(q, l), lds};
-    const uint32_t n = p.runs.before[4];
-    const bool listed = n <= kList;
-    if (listed) {
-        // the entries of each run of bins together; then an entry's place in its run: how many come before it, counted by as many threads as there
-        // are for one
-        if (tid < 4) lds.filled[tid] = 0;
-        __syncthreads();
+    const uint32_t n = runs_of(q, l).before[4];
+    Picker<T> p{static_cast<const T *>(a.logits) + row * a.logits_row, a.vocab, n, n <= kList, bin_scale(top.m, temp), lds};
+    if (p.listed)
         for (uint32_t i = tid; i < n; i += kPickThreads) {
             const unsigned long long e = w.list[(size_t)row * kList + i];
-            const int b = bin_of(p.s.place(value_of(~(uint32_t)(e >> 32))));
-            uint32_t k = 0, base = 0;
-#pragma unroll
-            for (uint32_t j = 1; j < 4; ++j)
-                if (b >= p.runs.lo[j] && b <= p.runs.hi[j]) { k = j; base = p.runs.before[j]; }
-            lds.raw[base + atomicAdd(&lds.filled[k], 1u)] = e;
+            lds.list[i] = e;
+            lds.bin[i] = (uint16_t)p.s.place(value_in(e)).bin();
         }
-        __syncthreads();
-        uint32_t g = 64;
-        while (g > 1 && n * g > kPickThreads) g /= 2;
-        for (uint32_t e = tid / g; e < n; e += kPickThreads / g) {
-            const unsigned long long mine = lds.raw[e];
-            uint32_t k0 = 0, k1 = n;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (e >= p.runs.before[j] && e < p.runs.before[j + 1]) { k0 = p.runs.before[j]; k1 = p.runs.before[j + 1]; }
-            uint32_t before = 0;
-            for (uint32_t j = k0 + tid % g; j < k1; j += g) before += lds.raw[j] < mine;
-            for (uint32_t o = g / 2; o; o >>= 1) before += __shfl_xor(before, o, 64);
-            if (tid % g == 0) lds.sorted[k0 + before] = mine;
-        }
-        __syncthreads();
-        constexpr int kEach = kList / kPickThreads;
-        unsigned long long weight[kEach], upto = 0;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            if (tid * kEach + j < n) {
-                const double y = p.s.place(value_of(~(uint32_t)(lds.sorted[tid * kEach + j] >> 32)));
-                upto += whole_of(y, bin_of(y));
-            }
-            weight[j] = upto;
-        }
-        const unsigned long long mine = upto;
-        for (int o = 1; o < 64; o <<= 1) {
-            const unsigned long long t = __shfl_up(upto, o, 64);
-            if ((int)lane >= o) upto += t;
-        }
-        if (lane == 63) lds.lbuf[wave] = upto;
-        __syncthreads();
-        upto -= mine;
-        for (uint32_t i = 0; i < wave; ++i) upto += lds.lbuf[i];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) lds.part[tid * kEach + j + 1] = upto + weight[j];
-        if (tid == 0) lds.part[0] = 0;
-        __syncthreads();
-    }
-    auto border = [&](int b, auto passes) { return listed ? p.listed(b, passes) : p.by_digits(b, passes); };
     auto look_again = [&](int lo, int hi, auto passes) {          // the bin of a goal that is known by now; between the two that it may lie in
         __syncthreads();
         if (tid == 0) l.found[5] = 0x7FFFFFFF;
@@ -1333,72 +1360,43 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     double sum = l.sum[kBins];
     if (q.by_k) {
         const uint32_t want = q.most - l.count[q.bk];
-        const InBin in = border(q.bk, [=](uint32_t c, unsigned long long) { return c >= want; });
+        const Spot in = p.find(q.bk, false, [=](uint32_t c, unsigned long long) { return c >= want; });
         kept = q.most;
         sum = p.sum_at(q.bk, in.sum);
     }
     if (q.by_p) {
         const double goal = q.share * sum;
         const int b = q.p0 == q.p1 ? q.p0 : look_again(q.p0, q.p1, [&](uint32_t j) { return l.sum[j + 1] >= goal; });
-        const double base = l.sum[b], front = exp(-(double)b / kBinsPerNat);
-        const InBin in = border(b, [=](uint32_t, unsigned long long t) { return base + front * (double)t >= goal; });
+        const double base = l.sum[b], middle = exp(-(double)b / kBinsPerNat);
+        const Spot in = p.find(b, false, [=](uint32_t, unsigned long long t) { return base + middle * (double)t >= goal; });
         if (l.count[b] + in.count < kept) { kept = l.count[b] + in.count; sum = p.sum_at(b, in.sum); }
     }
     if (q.by_m) {
-        uint32_t c = 0;
-        unsigned long long t = 0;
-        if (q.reach >= 0.0) {
-            if (listed) {
-                const uint32_t at = start_of(p.runs, l, q.bm);
-                uint32_t hi = l.count[q.bm + 1] - l.count[q.bm];
-                while (c < hi) {                 // how many of the bin's lie up to `q.reach`
-                    const uint32_t mid = (c + hi + 1) / 2;
-                    if (p.s.place(value_of(~(uint32_t)(lds.sorted[at + mid - 1] >> 32))) <= q.reach) c = mid;
-                    else hi = mid - 1;
-                }
-                t = lds.part[at + c] - lds.part[at];
-            } else {
-                __syncthreads();
-                if (tid == 0) { lds.digit.before = 0; lds.digit.sum = 0; }
-                __syncthreads();
-                const int in = q.bm;
-                each_in<T, kPickThreads>(p.x, 0, a.vocab, p.s, in, in, [=](int b) { return b == in; }, [&](float, uint32_t, double y, int b) {
-                    if (y <= q.reach) { atomicAdd(&lds.digit.before, 1u); atomicAdd(&lds.digit.sum, whole_of(y, b)); }
-                });
-                __syncthreads();
-                c = lds.digit.before;
-                t = lds.digit.sum;
-            }
-            c += l.count[q.bm];
-        }
+        __syncthreads();
+        if (tid == 0) { lds.before = 0; lds.spot_sum = 0; }
+        __syncthreads();
+        if (q.reach >= 0.0)
+            p.entries(q.bm, [&](unsigned long long e) {
+                if (p.s.place(value_in(e)).value() <= q.reach) { atomicAdd(&lds.before, 1u); atomicAdd(&lds.spot_sum, p.weight_of(e)); }
+            });
+        __syncthreads();
+        const uint32_t c = q.reach >= 0.0 ? l.count[q.bm] + lds.before : 0;
         if (c == 0) { kept = 1; sum = 34359738368.0; }
-        else if (c < kept) { kept = c; sum = p.sum_at(q.bm, t); }
+        else if (c < kept) { kept = c; sum = p.sum_at(q.bm, lds.spot_sum); }
     }
     const double goal = q.u * sum;
     const int b = q.d0 == q.d1 ? q.d0 : look_again(q.d0, q.d1, [&](uint32_t j) { return l.sum[j + 1] > goal; });
-    const double base = l.sum[b], front = exp(-(double)b / kBinsPerNat);
+    const double base = l.sum[b], middle = exp(-(double)b / kBinsPerNat);
     const uint32_t end = kept, ahead = l.count[b];
-    const InBin in = border(b, [=](uint32_t c, unsigned long long t) { return base + front * (double)t > goal || ahead + c >= end; });
-    if (a.kept && tid == 0) a.kept[row] = (int)kept;
-    if (listed) {
-        if (tid == 0) a.token[row] = (int)(uint32_t)lds.sorted[start_of(p.runs, l, b) + in.count - 1];
-        return;
-    }
-    for (uint32_t i0 = 0, seen = 0; i0 < a.vocab; i0 += kPickThreads) {          // number `skip` of the entries with that key
-        const uint32_t i = i0 + tid;
-        const bool is = i < a.vocab && order_of(sane(to_f(p.x[i]))) == in.key;
-        const uint64_t same = __ballot(is);
-        __syncthreads();
-        if (lane == 0) l.ubuf[wave] = __popcll(same);
-        __syncthreads();
-        uint32_t at = seen + __popcll(same & ((1ull << lane) - 1));
-        for (uint32_t v = 0; v < kPickThreads / 64; ++v) { at += v < wave ? l.ubuf[v] : 0; seen += l.ubuf[v]; }
-        if (is && at == in.skip) a.token[row] = (int)i;
-        if (seen > in.skip) return;
+    const Spot in = p.find(b, true, [=](uint32_t c, unsigned long long t) { return base + middle * (double)t > goal || ahead + c >= end; });
+    if (tid == 0) {
+        a.token[row] = in.index;
+        if (a.kept) a.kept[row] = (int)kept;
     }
 }
 
-// Chunks: as many as make about 2048 workgroups of the first launch and 256 of the second; of the third as few as keep about 512, each
+// Chunks: as many as make about 2048 workgroups of the first launch and 1024 of the second, or 320 where rows are few
+// (each leaves about a thousand atomic additions: 16 rows of 128256, 17 us with 1024, 8 with 256); of the third as few as keep about 768, each
 // of which works the bins out for itself.
 SampleShape sample_shape(const ps_sample_args &a) {
     SampleShape sh;
@@ -1410,8 +1408,8 @@ SampleShape sample_shape(const ps_sample_args &a) {
         *n = (a.vocab + *len - 1) / *len;
     };
     cut(2048, 2048, &sh.top, &sh.ntop);
-    cut(256, kRound / 2, &sh.bins, &sh.nbins);
-    cut(512, kRound, &sh.find, &sh.nfind);
+    cut(rows < 128 ? 320 : 1024, kRound / 2, &sh.bins, &sh.nbins);
+    cut(768, kRound, &sh.find, &sh.nfind);
     return sh;
 }
 uint64_t sample_work(const ps_sample_args &a, const SampleShape &sh, uint8_t *base, SampleWork *w) {
