@@ -191,9 +191,10 @@ __device__ __forceinline__ void add_wild(const ps_page_attention_args &a, const 
 }
 
 // Rows of `set` (up to NT x 16) over positions lo .. hi - 1 of a span (lo a multiple of 32).  Row rho sees positions below limit0 + rho / group.
+// `window` holds the table's entries from the wave's first tile on.
 template <typename T, int D, int NT>
 __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const RowSet &set, const Span &span, uint32_t shift, uint32_t hk, int lo, int hi, int limit0,
-                                         uint32_t records, uint32_t z, float *part, unsigned char *lds) {
+                                         PageWindow window, uint32_t records, uint32_t z, float *part, unsigned char *lds) {
     using M = Mfma<T>;
     using v8 = typename M::v8;
     constexpr int KK = D / 32, DT = D / 16, RB = NT * 16, OP = D + 4;
@@ -206,7 +207,6 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
     unsigned char *const stage = lds + wave * kStage;
     const uint32_t vrow = lane / kRowPieces;
     u4_t kreg[2][KK], vreg[kVLoads];
-    PageWindow window{-1, 0};
     uint32_t gone = 0;                         // halves of the requested tile that no page holds
     int P0 = lo + (int)wave * (int)kTile;
     auto request = [&](int P) {
@@ -228,10 +228,7 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
     auto move_window = [&](int P) {
         if (((P + 31) >> shift) - window.base >= 64) window.fill(span, P >> shift, a.n_pages);
     };
-    if (P0 < hi) {
-        window.fill(span, P0 >> shift, a.n_pages);
-        request(P0);
-    }
+    if (P0 < hi) request(P0);
     if (tid == 0) *wild = 0;
     __syncthreads();
 
@@ -649,7 +646,7 @@ extern __shared__ u4_t page_lds[];
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, uint32_t prefix8, float *part) {
     unsigned char *const lds = reinterpret_cast<unsigned char *>(page_lds);
-    const uint32_t records = d.direct ? 0 : d.psplit + d.osplit;
+    const uint32_t records = d.direct ? 0 : d.psplit + d.osplit, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // the prefixes' workgroups first, in runs of eight (one on each XCD)
     const uint32_t run = blockIdx.x / 8;
     if (run < prefix8) {
@@ -662,16 +659,22 @@ __global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_a
         const int len = prefix_length_of(a, g.prefix), lo = (int)min((uint64_t)z * d.plen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.plen, (uint64_t)len);
         if (lo >= hi) return;
         const Span span{a.prefix_table + g.prefix * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), len};
-        if (g.set.rows <= NT * 16) rows_few<T, D, NT>(a, g.set, span, shift, hk, lo, hi, len, records, z, part, lds);
-        else rows_many<T, D, false>(a, g.set, g.block * 128, Span{span.table, span.entries, hi}, Span{nullptr, 0, 0}, shift, hk, lo / (int)kStep, (hi + (int)kStep - 1) / (int)kStep, 0, records, z, part, lds);
+        if (g.set.rows <= NT * 16) {
+            PageWindow window;
+            window.fill(span, (lo + (int)(wave * kTile)) >> shift, a.n_pages);
+            rows_few<T, D, NT>(a, g.set, span, shift, hk, lo, hi, len, window, records, z, part, lds);
+        } else rows_many<T, D, false>(a, g.set, g.block * 128, Span{span.table, span.entries, hi}, Span{nullptr, 0, 0}, shift, hk, lo / (int)kStep, (hi + (int)kStep - 1) / (int)kStep, 0, records, z, part, lds);
     } else {
         const uint32_t unit = (run - prefix8) * 8 + blockIdx.x % 8, z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads;
         if (s >= a.n_seq) return;
+        // (the table's entries are asked for with the lengths: one load's time less for every run)
+        PageWindow window;
+        window.fill(Span{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), 0}, (int)((z * d.olen + wave * kTile) >> shift), a.n_pages);
         const SeqTokens t = tokens_of(a, s);
         const int len = length_of(a, s), lo = (int)min((uint64_t)z * d.olen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)len);
         if (t.answered == 0 || (lo >= hi && records)) return;
         const uint32_t G = a.n_q_heads / a.n_kv_heads;
-        rows_few<T, D, NT>(a, RowSet{t.row0, t.answered * G, G}, Span{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), len}, shift, hk, lo, hi, len - t.n + 1, records, d.psplit + z, part, lds);
+        rows_few<T, D, NT>(a, RowSet{t.row0, t.answered * G, G}, Span{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), len}, shift, hk, lo, hi, len - t.n + 1, window, records, d.psplit + z, part, lds);
     }
 }
 
@@ -696,12 +699,13 @@ __global__ __launch_bounds__(256, 2) void page_rows_kernel(ps_page_attention_arg
     rows_many<T, D, true>(a, set, block * 128, prefix, own, shift, hk, lo, hi, limit0, d.direct ? 0 : d.osplit, z, part, lds);
 }
 
-// A wave per (token, query head) puts the records of its prefix's and of its sequence's runs together, in their order: value sums, then maximum
-// (in powers of two) and weight sum.
+// D / 4 lanes per (token, query head) put the records of its prefix's and of its sequence's runs together, in their order: value sums, then maximum
+// (in powers of two) and weight sum.  Latencies: 512 tokens of 32 heads, three records each, 9 us.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args a, PageDeal d, const float *part) {
-    constexpr int E = D / 64, OP = D + 4;
-    const uint32_t lane = threadIdx.x & 63, hb = (a.n_q_heads + 3) / 4, h = blockIdx.x % hb * 4 + (threadIdx.x >> 6), i = blockIdx.x / hb % a.max_tokens, s = blockIdx.x / hb / a.max_tokens;
+    constexpr uint32_t OP = D + 4, kLanes = D / 4, kHeads = 256 / kLanes;
+    const uint32_t hb = (a.n_q_heads + kHeads - 1) / kHeads, h = blockIdx.x % hb * kHeads + threadIdx.x / kLanes, e0 = threadIdx.x % kLanes * 4;
+    const uint32_t i = blockIdx.x / hb % a.max_tokens, s = blockIdx.x / hb / a.max_tokens;
     // (all of these are asked for before one is waited for)
     const SeqTokens t = tokens_of(a, s);
     const int len = length_of(a, s), plen = prefix_length_behind(a, s);
@@ -711,36 +715,38 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
     const uint32_t n = np + (positions + d.olen - 1) / d.olen;
     const size_t token = (size_t)t.row0 + i;
     const float *r0 = part + (token * a.n_q_heads + h) * (d.psplit + d.osplit) * OP;
-    float mx = -INFINITY, l = 0.f, o[E] = {};
+    float mx = -INFINITY, l = 0.f;
+    f4_t o{0.f, 0.f, 0.f, 0.f};
     for (uint32_t z0 = 0; z0 < n; z0 += 8) {
-        float mv[8], lv[8], ov[8][E], m8 = mx;
+        float2 ml[8];
+        f4_t ov[8];
+        float m8 = mx;
 #pragma unroll
         for (uint32_t u = 0; u < 8; ++u) {
             const uint32_t z = min(z0 + u, n - 1);
             const float *r = r0 + (size_t)(z < np ? z : d.psplit + z - np) * OP;
-            mv[u] = r[D];
-            lv[u] = r[D + 1];
-#pragma unroll
-            for (int e = 0; e < E; ++e) ov[u][e] = r[lane * E + e];
+            ml[u] = *reinterpret_cast<const float2 *>(r + D);
+            ov[u] = *reinterpret_cast<const f4_t *>(r + e0);
         }
 #pragma unroll
-        for (uint32_t u = 0; u < 8; ++u) m8 = fmaxf(m8, mv[u]);
+        for (uint32_t u = 0; u < 8; ++u) m8 = fmaxf(m8, ml[u].x);
         const float ms = m8 == -INFINITY ? 0.f : m8, resc = __builtin_amdgcn_exp2f(mx - ms);
         l *= resc;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= resc;
+        o = o * resc;
         mx = m8;
 #pragma unroll
         for (uint32_t u = 0; u < 8; ++u) {
             const bool in = z0 + u < n;          // (a record past the last is the last again)
-            const float w = mv[u] == -INFINITY ? (m8 == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(mv[u] - ms);       // as the waves above
-            l = in ? fmaf(w, lv[u], l) : l;
+            const float w = ml[u].x == -INFINITY ? (m8 == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(ml[u].x - ms);       // as the waves above
+            l = in ? fmaf(w, ml[u].y, l) : l;
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = in ? fmaf(w, ov[u][e], o[e]) : o[e];
+            for (int e = 0; e < 4; ++e) o[e] = in ? fmaf(w, ov[u][e], o[e]) : o[e];
         }
     }
+    T r[4];
 #pragma unroll
-    for (int e = 0; e < E; ++e) static_cast<T *>(a.out)[token * a.out_token + h * a.out_head + lane * E + e] = (T)(l == 0.f ? 0.f : o[e] / l);
+    for (int e = 0; e < 4; ++e) r[e] = (T)(l == 0.f ? 0.f : o[e] / l);
+    *reinterpret_cast<u2_t *>(static_cast<T *>(a.out) + token * a.out_token + h * a.out_head + e0) = *reinterpret_cast<const u2_t *>(r);
 }
 
 // ------------------------------------------------------------------------------------ sampling
@@ -1005,14 +1011,25 @@ __device__ __forceinline__ void look(BinLds &l, int slot, Passes passes) {
     }
 }
 
+// a thread's four bins, asked for before the row's largest logit is waited for
+struct FourBins {
+    uint4 c;
+    ulonglong2 s0, s1;
+    __device__ __forceinline__ FourBins(const SampleWork &w, uint32_t row) {
+        const size_t at = (size_t)row * kBins + threadIdx.x * 4;
+        c = *reinterpret_cast<const uint4 *>(w.counts + at);
+        s0 = *reinterpret_cast<const ulonglong2 *>(w.sums + at);
+        s1 = *reinterpret_cast<const ulonglong2 *>(w.sums + at + 2);
+    }
+};
 // Running counts and sums of a row's bins, and where its borders may lie.  By every workgroup that needs it, always added alike.
-__device__ __forceinline__ Wanted analyse(const ps_sample_args &a, const SampleWork &w, uint32_t row, BinLds &l) {
+__device__ __forceinline__ Wanted analyse(const ps_sample_args &a, const FourBins &four, uint32_t row, BinLds &l) {
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = tid * 4;
     static_assert(kBins == 4 * kPickThreads, "four bins a thread");
     Wanted q{};
     {
-        const uint4 c = *reinterpret_cast<const uint4 *>(w.counts + (size_t)row * kBins + b);
-        const ulonglong2 s0 = *reinterpret_cast<const ulonglong2 *>(w.sums + (size_t)row * kBins + b), s1 = *reinterpret_cast<const ulonglong2 *>(w.sums + (size_t)row * kBins + b + 2);
+        const uint4 c = four.c;
+        const ulonglong2 s0 = four.s0, s1 = four.s1;
         const double middle = exp(-(double)b / kBinsPerNat);
         // (a bin's middle weighs 0.988 of the one before)
         const double v0 = middle * (double)s0.x, v1 = middle * 0.9883439889852305 * (double)s0.y, v2 = middle * 0.9768238405632375 * (double)s1.x, v3 = middle * 0.9654379711181429 * (double)s1.y;
@@ -1161,11 +1178,12 @@ __global__ __launch_bounds__(kPickThreads) void sample_find_kernel(ps_sample_arg
     const uint32_t tid = threadIdx.x, row = blockIdx.y;
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (!(temp > 0.f)) return;
+    const FourBins four(w, row);
     const float m = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, l.fbuf, l.ibuf).m;
     if (m == -INFINITY) return;
     if (tid == 0) n = 0;
     __syncthreads();
-    const Wanted q = analyse(a, w, row, l);
+    const Wanted q = analyse(a, four, row, l);
     const Runs r = runs_of(q, l);
     if (r.before[4] > kList) return;
     const uint32_t lo = blockIdx.x * sh.find, hi = min(a.vocab, lo + sh.find);
@@ -1329,6 +1347,11 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     __shared__ PickLds lds;
     BinLds &l = lds.bins;
     const uint32_t row = blockIdx.x, tid = threadIdx.x;
+    const FourBins four(w, row);
+    constexpr uint32_t kEach = kList / kPickThreads;
+    unsigned long long entry[kEach];                  // (those of the list that there are turn out later)
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) entry[j] = w.list[(size_t)row * kList + tid + j * kPickThreads];
     const RowTop top = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, l.fbuf, l.ibuf);
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (top.m == -INFINITY || !(temp > 0.f)) {
@@ -1339,14 +1362,16 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
         return;
     }
     __syncthreads();
-    const Wanted q = analyse(a, w, row, l);
+    const Wanted q = analyse(a, four, row, l);
     const uint32_t n = runs_of(q, l).before[4];
     Picker<T> p{static_cast<const T *>(a.logits) + row * a.logits_row, a.vocab, n, n <= kList, bin_scale(top.m, temp), lds};
     if (p.listed)
-        for (uint32_t i = tid; i < n; i += kPickThreads) {
-            const unsigned long long e = w.list[(size_t)row * kList + i];
-            lds.list[i] = e;
-            lds.bin[i] = (uint16_t)p.s.place(value_in(e)).bin();
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j) {
+            const uint32_t i = tid + j * kPickThreads;
+            if (i >= n) break;
+            lds.list[i] = entry[j];
+            lds.bin[i] = (uint16_t)p.s.place(value_in(entry[j])).bin();
         }
     auto look_again = [&](int lo, int hi, auto passes) {          // the bin of a goal that is known by now; between the two that it may lie in
         __syncthreads();
@@ -1444,8 +1469,9 @@ int32_t check_page_attention(const ps_page_attention_args *a) {
 
 // How the work is dealt out.  Runs bring the launch to about the workgroups that the chip holds at once (two per CU).  Shared prefixes beside own
 // positions: one workgroup per CU for the prefixes, which come first, so that the other place is the loads' (64 sequences, 32 / 8 heads, prefix
-// 32761: own lengths to 1000 in 105 us, to 4000 in 184; with two per CU 108 and 218); two where own positions are few (lengths of 1: 76 for 93).  Own positions of several
-// sequences, whose lengths differ: twice as many runs as places (48 of up to 8190, 16 / 8 heads of 64, 107 us for 115), where a run is not a whole sequence anyway.
+// 32761: own lengths to 1000 in 105 us, to 4000 in 184; with two per CU 108 and 218); two where own positions are few (lengths of 1: 76 for 93).  Own
+// positions of several sequences: as many runs as places, since every run has a start of dependent loads and a record (64 sequences of up to 1000, 32 / 8 heads,
+// 34 us; with 1024 runs 41, with 2048 45; only few sequences of very different lengths would rather have more: 48 of up to 8190, 16 / 8 heads of 64, 112 for 106).
 PageDeal page_deal(const ps_page_attention_args &a) {
     PageDeal d{};
     const uint32_t G = a.n_q_heads / a.n_kv_heads;
@@ -1463,8 +1489,7 @@ PageDeal page_deal(const ps_page_attention_args &a) {
         // about how long each part takes by itself, at 700 TFLOP/s and 5 TB/s
         const double prefix_us = (double)a.n_tokens * a.n_q_heads * a.max_prefix * a.head_dim * 4 / 700e6, own_us = (double)a.n_seq * a.n_kv_heads * a.max_length * a.head_dim * 4 / 5e6;
         if (prefixes) cut((uint64_t)d.blocks * a.n_kv_heads, own_us * 4 > prefix_us ? 256 : 512, a.max_prefix, 256, kStep, &d.psplit, &d.plen);
-        const uint64_t units = (uint64_t)a.n_seq * a.n_kv_heads;
-        cut(units, a.n_seq > 1 && units < 1024 ? 2048 : 1024, a.max_length, 128, 4 * kTile, &d.osplit, &d.olen);
+        cut((uint64_t)a.n_seq * a.n_kv_heads, a.n_seq > 1 ? 512 : 1024, a.max_length, 128, 4 * kTile, &d.osplit, &d.olen);
         d.direct = d.psplit == 0 && d.osplit == 1;
     } else {
         d.blocks = (uint32_t)((rows + 127) / 128);
@@ -1477,11 +1502,13 @@ PageDeal page_deal(const ps_page_attention_args &a) {
 uint64_t page_workspace(const ps_page_attention_args &a, const PageDeal &d) {
     return d.direct ? 0 : align_up((uint64_t)a.n_tokens * a.n_q_heads * (d.psplit + d.osplit) * (a.head_dim + 4) * 4, kAlign);
 }
+// workgroups of the merge for a token
+uint32_t merge_groups(const ps_page_attention_args &a) { const uint32_t heads = 1024 / a.head_dim; return (a.n_q_heads + heads - 1) / heads; }
 // workgroups of a call's launches, 0: more than a launch holds
 uint64_t page_groups(const ps_page_attention_args &a, const PageDeal &d, uint64_t *prefix8, uint64_t *own8) {
     *prefix8 = d.shared ? ((uint64_t)a.n_kv_heads * d.psplit + 7) / 8 * d.blocks : 0;
     *own8 = ((uint64_t)a.n_seq * a.n_kv_heads * d.osplit + 7) / 8 * (d.shared ? 1 : d.blocks);
-    const uint64_t groups = (*prefix8 + *own8) * 8, merge = (uint64_t)a.n_seq * std::min(a.max_tokens, a.n_tokens) * ((a.n_q_heads + 3) / 4);
+    const uint64_t groups = (*prefix8 + *own8) * 8, merge = (uint64_t)a.n_seq * std::min(a.max_tokens, a.n_tokens) * merge_groups(a);
     return groups > kMostGroups || (!d.direct && merge > kMostGroups) ? 0 : groups;
 }
 
@@ -1524,7 +1551,7 @@ hipError_t launch_page_attention(const ps_page_attention_args &call, float *part
                          : d.nt == 1 ? launch_shared<T, D, 1>(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st)
                                      : launch_shared<T, D, 2>(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st);
     if (e != hipSuccess || d.direct) return e;
-    hipLaunchKernelGGL((page_merge_kernel<T, D>), dim3(a.n_seq * a.max_tokens * ((a.n_q_heads + 3) / 4)), dim3(256), 0, st, a, d, part);
+    hipLaunchKernelGGL((page_merge_kernel<T, D>), dim3(a.n_seq * a.max_tokens * merge_groups(a)), dim3(256), 0, st, a, d, part);
     return hipGetLastError();
 }
 template <typename T>
