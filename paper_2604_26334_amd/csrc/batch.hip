@@ -502,48 +502,63 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
         const bool mine = kOwn && step >= np;
         const int P0 = (mine ? step - np : step) * (int)kStep, end = mine ? own_end : prefix.len;
         const unsigned char *st = lds + ((step - lo) & 1) * 2 * kHalf;
-        if (rows && step >= lo) {
+        if (rows && step >= lo && !(mine && P0 >= wave_end)) {
+            f4_t S[NT][4];
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) S[t][g] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    const v8 kr = __builtin_bit_cast(v8, *reinterpret_cast<const u4_t *>(st + kread[kk] + g * 16 * D * 2));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) S[t][g] = M::mul(kr, q[t][kk], S[t][g]);
+                }
+            __builtin_amdgcn_s_setprio(0);
+            if (missing || P0 + (int)kStep > end || (mine && P0 + (int)kStep > wave_least)) {
+                asm volatile("");
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int last = (mine ? min(end, limit0 + (int)tok[t]) : end) - P0 - 4 * (int)c;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) S[t][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < last && !(missing >> (e >> 2) & 1) ? S[t][e >> 2][e & 3] : -INFINITY;
+                }
+            }
+            v8 P[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) mx = fmaxf(mx, fmaxf(fmaxf(S[t][g][0], S[t][g][1]), fmaxf(S[t][g][2], S[t][g][3])));
+                if (__any(mx > m_run[t] + slack)) {
+                    mx = row_max(mx);
+                    mx = mx > m_run[t] + slack ? mx : m_run[t];
+                    const float resc = m_run[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[t] - mx) * c2);
+                    m_run[t] = mx;
+                    L[t] = L[t] * resc;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) O[t][dt] = O[t][dt] * resc;
+                }
+                const float ms = m_run[t] == -INFINITY ? 0.f : m_run[t];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) P[t][e >> 3][e & 7] = (T)__builtin_amdgcn_exp2f(fmaf(S[t][e >> 2][e & 3] - ms, c2, WeightRange<T>::kLift));
+            }
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int T0 = P0 + h * (int)kTile;
-                if (T0 >= end || (mine && T0 >= wave_end)) break;            // (uniform)
-                const unsigned char *tile = st + h * kTile * D * 2;
-                f4_t S[NT][2];
-                __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = f4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int g = 0; g < 2; ++g)
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) {
-                        const v8 kr = __builtin_bit_cast(v8, *reinterpret_cast<const u4_t *>(tile + kread[kk] + g * 16 * D * 2));
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) S[t][g] = M::mul(kr, q[t][kk], S[t][g]);
-                    }
-                __builtin_amdgcn_s_setprio(0);
-                const uint32_t miss = missing >> (2 * h) & 3;
-                if (miss || T0 + (int)kTile > end || (mine && T0 + (int)kTile > wave_least)) {
-                    asm volatile("");
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const int last = (mine ? min(end, limit0 + (int)tok[t]) : end) - T0 - 4 * (int)c;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < last && !(miss >> (e >> 2) & 1) ? S[t][e >> 2][e & 3] : -INFINITY;
-                    }
-                }
-                v8 P[NT];
-                weigh<T>(S, m_run, L, O, P, c2, slack);
-                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    const v8 vr = __builtin_bit_cast(v8, transposed(tile + vread[dt], 16 * D * 2));
+                    const v8 vr = __builtin_bit_cast(v8, transposed(st + h * kTile * D * 2 + vread[dt], 16 * D * 2));
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) O[t][dt] = M::mul(vr, P[t], O[t][dt]);
+                    for (int t = 0; t < NT; ++t) O[t][dt] = M::mul(vr, P[t][h], O[t][dt]);
                 }
 #pragma unroll
-                for (int t = 0; t < NT; ++t) L[t] = M::mul(ones, P[t], L[t]);
-                __builtin_amdgcn_s_setprio(0);
+                for (int t = 0; t < NT; ++t) L[t] = M::mul(ones, P[t][h], L[t]);
             }
+            __builtin_amdgcn_s_setprio(0);
         }
         if (step + 1 >= lo && step + 1 < hi) {
             next = gone;
