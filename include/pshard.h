@@ -762,7 +762,7 @@ int32_t ps_stack_keep_path(ps_stack *st, const int32_t *path, const int32_t *cou
  * workspaces of their own.  Sequence s owns rows first[s] .. first[s + 1] - 1 of the token arrays, rows from first[n_seq] on are
  * neither read nor written.  Device values are bounded by the kernels: first is clamped to 0 .. n_tokens, lengths to
  * 0 .. their bound; a page number outside 0 .. n_pages - 1 names nothing (its positions are seen by no token and take
- * no rows). */
+ * no rows).  first and group_first ascend; tokens of those that do not may get anything. */
 
 /* Places of a step's new tokens.  Sequence s holds cached[s] positions and gets new_tokens[s] more:
  *   first[s] = sum of new_tokens in front of s (first[n_seq]: all of them), length[s] = cached[s] + new_tokens[s],
@@ -816,7 +816,7 @@ int32_t ps_page_append(const ps_page_append_args *args, void *stream);
  *  head each), and once for each 128 rows where they have more.
  *  type F16 or BF16; head_dim 64 or 128; page a power of two, 16 .. 1024.  q, out [n_tokens][n_q_heads][head_dim], pages
  *  [n_pages][n_kv_heads][page][head_dim], all with the strides below (any order of pages, heads and rows); every address and
- *  stride in bytes a multiple of 16, a page's rows span less than 4 GiB, pages lie less than 64 GiB apart.  max_length <= width * page, max_prefix <= prefix_width * page
+ *  stride in bytes a multiple of 16, a page's rows (and 32 rows) span less than 4 GiB, pages lie less than 64 GiB apart.  max_length <= width * page, max_prefix <= prefix_width * page
  *  and max_tokens: bounds on length, prefix_length and a sequence's tokens (what lies beyond is left out: tokens beyond max_tokens
  *  are not written); work is dealt out by them.  n_prefix <= 4096, n_seq <= 65535; out may not overlap any input.
  * Scores, softmax and sums in fp32; the weights of the value product are rounded to `type`, and their sum is taken of the rounded
@@ -849,7 +849,7 @@ int32_t ps_page_attention(const ps_page_attention_args *args, void *workspace, u
  * Weights are right to 2e-11 of each (those below e^-24 of the largest to 2^-31 of e^-24) and added as whole numbers, runs of them in 64 bits
  * and always alike, so a row's result is the same in any call, batch, stride or type that holds its values.
  *  type F16, BF16 or F32; rows [n_rows][vocab], logits_row elements apart, alignment of an element is enough; vocab 1 .. 2^24;
- *  n_rows <= 65535.  token, kept [n_rows]; kept (n of each row) may be NULL. */
+ *  n_rows <= 65535.  token, kept [n_rows]; kept (n of each row) may be NULL.  ps_sample_workspace: about 40 KB a row; 256-byte aligned. */
 typedef struct ps_sample_args {
     uint32_t type, n_rows, vocab, reserved;
     const void *logits;

@@ -164,7 +164,7 @@ struct PageWindow {
 };
 
 // Where the positions from P on of one kv head lie, as far as the page goes (strides between pages are less than 2^32 pieces of 16 bytes, a
-// page's rows span less than 2^32 bytes)
+// page's rows and 32 rows span less than 2^32 bytes)
 struct PageRows {
     const char *k, *v;
     __device__ __forceinline__ PageRows(const ps_page_attention_args &a, const char *kc, const char *vc, int number, int P, uint32_t mask) {
@@ -774,7 +774,7 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
 //  sample_pick_kernel   a workgroup per row finds the borders among them, digit by digit of the logits' bits.  Where they are more than a list holds, in
 //                       passes over the row instead.
 // The sum of the first entries of the order is that of whole bins (64 bits, always added alike) and of a part of one, whose whole numbers are exact.
-constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 512, kList = 2048, kRound = kPickThreads * 8;
+constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 512, kList = 2048, kRound = kPickThreads * 8, kShortRow = 32768;
 constexpr double kBinsPerNat = 2047.0 / 24.0;
 
 struct RowTop { float m; int at; };
@@ -1219,7 +1219,7 @@ struct PickLds {
     unsigned long long list[kList];
     uint16_t bin[kList];
     unsigned long long sum[256], both, any, spot_sum;
-    uint32_t count[256], digit, before, equal;
+    uint32_t count[256], digit, before, equal, n;
 };
 // The first entries of a bin: how many, the sum of their weights, and the index of the last one
 struct Spot { uint32_t count; unsigned long long sum; int index; };
@@ -1366,7 +1366,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     constexpr uint32_t kEach = kList / kPickThreads;
     unsigned long long entry[kEach];                  // (those of the list that there are turn out later)
 #pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) entry[j] = w.list[(size_t)row * kList + tid + j * kPickThreads];
+    for (uint32_t j = 0; j < kEach; ++j) entry[j] = sh.nfind ? w.list[(size_t)row * kList + tid + j * kPickThreads] : 0;
     const RowTop top = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, l.fbuf, l.ibuf);
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (top.m == -INFINITY || !(temp > 0.f)) {
@@ -1378,9 +1378,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     }
     __syncthreads();
     const Wanted q = analyse(a, four, row, l);
-    const uint32_t n = runs_of(q, l).before[4];
+    const Runs runs = runs_of(q, l);
+    const uint32_t n = runs.before[4];
     Picker<T> p{static_cast<const T *>(a.logits) + row * a.logits_row, a.vocab, n, n <= kList, bin_scale(top.m, temp), lds};
-    if (p.listed)
+    if (p.listed && sh.nfind) {
 #pragma unroll
         for (uint32_t j = 0; j < kEach; ++j) {
             const uint32_t i = tid + j * kPickThreads;
@@ -1388,6 +1389,16 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
             lds.list[i] = entry[j];
             lds.bin[i] = (uint16_t)p.s.place(value_in(entry[j])).bin();
         }
+    } else if (p.listed) {                            // (a short row: picked out here)
+        if (tid == 0) lds.n = 0;
+        __syncthreads();
+        each_in(p.x, 0, a.vocab, p.s, runs, [&](float v, uint32_t i, const Place &y) {
+            const uint32_t slot = atomicAdd(&lds.n, 1u);
+            if (slot >= kList) return;
+            lds.list[slot] = entry_of(v, i);
+            lds.bin[slot] = (uint16_t)y.bin();
+        });
+    }
     auto look_again = [&](int lo, int hi, auto passes) {          // the bin of a goal that is known by now; between the two that it may lie in
         __syncthreads();
         if (tid == 0) l.found[5] = 0x7FFFFFFF;
@@ -1449,7 +1460,8 @@ SampleShape sample_shape(const ps_sample_args &a) {
     };
     cut(2048, 2048, &sh.top, &sh.ntop);
     cut(rows < 128 ? 320 : 1024, kRound / 2, &sh.bins, &sh.nbins);
-    cut(768, kRound, &sh.find, &sh.nfind);
+    sh.find = sh.nfind = 0;
+    if (a.vocab > kShortRow) cut(768, kRound, &sh.find, &sh.nfind);
     return sh;
 }
 uint64_t sample_work(const ps_sample_args &a, const SampleShape &sh, uint8_t *base, SampleWork *w) {
@@ -1559,7 +1571,10 @@ hipError_t launch_page_attention(const ps_page_attention_args &call, float *part
     ps_page_attention_args a = call;
     a.max_tokens = std::min(a.max_tokens, a.n_tokens);
     const PageDeal d = page_deal(a);
-    if (a.n_pages == 0) a.max_length = a.max_prefix = 0;         // (where there is a page, page 0 can be read)
+    // (where there is a page, page 0 can be read; where there are no positions, tables may be NULL)
+    if (a.n_pages == 0) a.max_length = a.max_prefix = 0;
+    if (a.max_length == 0) a.width = 0;
+    if (a.max_prefix == 0) a.prefix_width = 0;
     uint64_t prefix8, own8;
     page_groups(a, d, &prefix8, &own8);
     const hipError_t e = !d.shared ? launch_rows<T, D>(a, d, (uint32_t)own8, part, st)
@@ -1573,7 +1588,7 @@ template <typename T>
 hipError_t launch_sample(const ps_sample_args &a, const SampleShape &sh, const SampleWork &w, hipStream_t st) {
     hipLaunchKernelGGL(sample_rows_kernel<T>, dim3(sh.ntop, a.n_rows), dim3(kRowThreads), 0, st, a, sh, w);
     hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(sh.nbins, a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
-    hipLaunchKernelGGL(sample_find_kernel<T>, dim3(sh.nfind, a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
+    if (sh.nfind) hipLaunchKernelGGL(sample_find_kernel<T>, dim3(sh.nfind, a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
     hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.n_rows), dim3(kPickThreads), 0, st, a, sh, w);
     return hipGetLastError();
 }
@@ -1650,7 +1665,7 @@ int32_t ps_page_attention(const ps_page_attention_args *a, void *workspace, uint
     for (const void *p : {a->q, a->k_pages, a->v_pages, (const void *)a->out}) PS_WANT(aligned(p, 16), "q, the pages and out must be 16-byte aligned");
     for (uint64_t n : {a->q_token, a->q_head, a->k_page, a->k_head, a->k_row, a->v_page, a->v_head, a->v_row, a->out_token, a->out_head})
         PS_WANT(n % 8 == 0, "strides must be multiples of 16 bytes (got %llu elements)", (unsigned long long)n);
-    for (uint64_t n : {a->k_row, a->v_row}) PS_WANT(n < (1ull << 31) / a->page, "a page's rows must span less than 4 GiB (stride of %llu elements)", (unsigned long long)n);
+    for (uint64_t n : {a->k_row, a->v_row}) PS_WANT(n < (1ull << 31) / std::max(32u, a->page), "a page's rows, and 32 rows, must span less than 4 GiB (stride of %llu elements)", (unsigned long long)n);
     for (uint64_t n : {a->k_page, a->v_page}) PS_WANT(n < 1ull << 35, "pages must lie less than 64 GiB apart (stride of %llu elements)", (unsigned long long)n);
     for (const int32_t *p : {a->first, a->length, a->table, a->group_first, a->prefix_length, a->prefix_table}) PS_WANT(aligned(p, 4), "tables must be aligned to 4 bytes");
     PS_WANT(workspace_bytes >= need && (need == 0 || (workspace && aligned(workspace, kAlign))), "a workspace of %llu bytes, 256-byte aligned, is needed", (unsigned long long)need);

@@ -67,7 +67,7 @@ def test_append_refuses(kw):
     dict(page=48), dict(page=2048), dict(n_seq=1 << 16), dict(n_tokens=1 << 31), dict(n_pages=1 << 31), dict(n_prefix=4097), dict(max_length=129),
     dict(max_prefix=321), dict(q=None), dict(out=None), dict(k_pages=None), dict(v_pages=None), dict(first=None), dict(length=None), dict(table=None),
     dict(group_first=None), dict(prefix_length=None), dict(prefix_table=None), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=PTR + 8),
-    dict(v_pages=PTR + 2), dict(q_token=516), dict(k_row=129), dict(v_page=4), dict(out_head=132), dict(k_row=1 << 27), dict(v_row=1 << 27), dict(k_page=1 << 35), dict(v_page=1 << 36),
+    dict(v_pages=PTR + 2), dict(q_token=516), dict(k_row=129), dict(v_page=4), dict(out_head=132), dict(k_row=1 << 26), dict(v_row=1 << 27), dict(page=1024, width=2, v_row=1 << 21), dict(k_page=1 << 35), dict(v_page=1 << 36),
     dict(first=PTR + 2), dict(prefix_table=PTR + 1)])
 def test_attention_refuses(kw):
     _refused(B.lib().ps_page_attention(C.byref(_attend(**kw)), PTR, 1 << 60, None))

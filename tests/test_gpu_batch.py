@@ -299,8 +299,37 @@ def test_attention_of_padded_batches_and_bounded_values():
     assert float(err) <= 32 * 2.0 ** -11 and bool((out[5:9] == 0).all())
     # offsets and groups: bounded; a sequence that ends before it starts has no token
     out.fill_(3.0)
-    B.page_attention(**dict(b, first=_ints([12, 2 ** 31 - 1, 7, -3]), group_first=_ints([-7, 2 ** 31 - 1])), out=out)
+    B.page_attention(**dict(b, first=_ints([12, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1]), group_first=_ints([-7, 2 ** 31 - 1])), out=out)
+    assert bool((out[:12] == 3).all()) and bool(torch.isfinite(out).all()) and not bool((out[12:] == 3).all())
+    out.fill_(3.0)
+    for n in ("group_first", "prefix_length", "prefix_table"):
+        b[n] = None
+    B.page_attention(**dict(b, first=_ints([12, 2 ** 31 - 1, 7, -3])), out=out)
     assert bool((out[:12] == 3).all()) and bool(torch.isfinite(out).all())
+
+
+def test_attention_without_positions_needs_no_tables():
+    """max_length 0, or a pool of no pages: zeros, whatever the tables are."""
+    import ctypes as C
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    q = torch.ones(3, 4, 64, dtype=torch.float16, device=DEV)
+    first, length, pages = _ints([0, 1, 3]), _ints([5, 7]), torch.full((2, 2, 16, 64), float("nan"), dtype=torch.float16, device=DEV)
+    gf, pl = _ints([0, 2]), _ints([20])
+    for kw in (dict(max_length=0, n_pages=2, k_pages=pages.data_ptr(), v_pages=pages.data_ptr()), dict(max_length=128, n_pages=0),
+               dict(max_length=0, n_pages=0, n_prefix=1, prefix_width=4, max_prefix=64, group_first=gf.data_ptr(), prefix_length=pl.data_ptr()),
+               dict(max_length=0, n_pages=2, k_pages=pages.data_ptr(), v_pages=pages.data_ptr(), n_prefix=1, prefix_width=4, max_prefix=0,
+                    group_first=gf.data_ptr(), prefix_length=pl.data_ptr())):
+        for tokens in (2, 40):
+            out = torch.full_like(q, 3.0)
+            a = B.ps_page_attention_args(type=0, n_seq=2, n_tokens=3, n_q_heads=4, n_kv_heads=2, head_dim=64, page=16, width=8, max_tokens=tokens, scale=0.1,
+                                         q=q.data_ptr(), out=out.data_ptr(), q_token=256, q_head=64, out_token=256, out_head=64, k_page=2048, k_head=1024, k_row=64,
+                                         v_page=2048, v_head=1024, v_row=64, table_seq=8, prefix_seq=4, first=first.data_ptr(), length=length.data_ptr(), **kw)
+            need = C.c_uint64()
+            assert B.lib().ps_page_attention_workspace(C.byref(a), C.byref(need)) == 0
+            work = torch.empty(need.value + 1, dtype=torch.uint8, device=DEV)
+            assert B.lib().ps_page_attention(C.byref(a), work.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == 0
+            assert bool((out == 0).all()), kw
 
 
 def test_attention_far_into_a_large_pool():
