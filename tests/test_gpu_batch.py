@@ -400,7 +400,7 @@ def _settings(rng, n, V, which):
 
 @pytest.mark.parametrize("ty", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("which", range(len(SETTINGS)))
-@pytest.mark.parametrize("n,V,spread", [(1, 1, 1.0), (3, 2, 1.0), (9, 7, 3.0), (24, 1000, 2.5), (40, 257, 0.0), (12, 32000, 2.5), (5, 32001, 0.1), (6, 128256, 2.5), (3, 128256, 40.0)])
+@pytest.mark.parametrize("n,V,spread", [(1, 1, 1.0), (3, 2, 1.0), (9, 7, 3.0), (24, 1000, 2.5), (40, 257, 0.0), (12, 32000, 2.5), (5, 32001, 0.1), (6, 128256, 2.5), (3, 128256, 40.0), (4, 128256, 0.0), (4, 70000, 0.01), (3, 32768, 1.0), (3, 32769, 1.0)])
 def test_sample(ty, which, n, V, spread):
     from paper_2604_26334_amd import binding as B
     torch, g = _t(), _gen(V + which)
@@ -437,6 +437,57 @@ def test_sample_draws_every_kept_entry_with_its_share():
         assert torch.equal(B.sample(x, u)[0].long(), torch.arange(V, device=DEV))
         token, kept = B.sample(x, torch.full((V,), 1 - 2.0 ** -24, device=DEV), top_p=torch.full((V,), 0.5, device=DEV))
         assert bool((kept == V // 2).all()) and bool((token == V // 2 - 1).all())
+
+
+def test_sample_random_numbers_out_of_range():
+    """Below 0 counts as 0, anything else that is not in [0, 1) as the largest number that is."""
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    for V in (300, 50000):
+        x = torch.randn(6, V, generator=_gen(V), device=DEV)
+        x[:] = x[0]
+        u = torch.tensor([0.0, -3.0, 1 - 2.0 ** -24, 1.0, float("inf"), float("nan")], device=DEV)
+        for s in (dict(), dict(top_k=_ints([20] * 6)), dict(top_p=torch.full((6,), 0.5, device=DEV))):
+            token, kept = B.sample(x, u, **s)
+            assert token.tolist() == [int(token[0])] * 2 + [int(token[2])] * 4 and len(set(kept.tolist())) == 1
+            _check_sample(x[:3], u.clamp(0, 1 - 2.0 ** -24)[:3], token[:3], kept[:3], **{k: v[:3] for k, v in s.items()})
+
+
+def test_calls_at_once_on_streams_of_their_own():
+    """Two batches on two streams, several times: each gives what it gives alone."""
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    work = []
+    for i, (toks, lens, groups, plens) in enumerate((([1] * 30, [60 * j + 1 for j in range(30)], (0, 30), [3000]), ([70, 3], [900, 500], (0, 2), [1000]))):
+        a, _, _ = _attend_case("f16", 128, 8, 2, 16, toks, lens, groups, plens, i)
+        x, u = (torch.randn(9, 90000, generator=_gen(i), device=DEV) * 2).half(), torch.rand(9, generator=_gen(i), device=DEV)
+        work.append((a, x, u, B.page_attention(**a), B.sample(x, u, top_p=torch.full((9,), 0.9, device=DEV))))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    got = []
+    for _ in range(4):
+        for st, (a, x, u, _, _) in zip(streams, work):
+            with torch.cuda.stream(st):
+                got.append((B.page_attention(**a), B.sample(x, u, top_p=torch.full((9,), 0.9, device=DEV))))
+    torch.cuda.synchronize()
+    for i, (out, (token, kept)) in enumerate(got):
+        want = work[i % 2]
+        assert _same_bits(out, want[3]) and torch.equal(token, want[4][0]) and torch.equal(kept, want[4][1]), i
+
+
+def test_attention_into_a_part_of_a_larger_tensor():
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    for toks, lens in (([1, 2, 1], [50, 300, 7]), ([50, 20], [70, 300])):
+        a, _, _ = _attend_case("bf16", 64, 8, 2, 32, toks, lens, (0, 2), [100], 2)
+        plain = B.page_attention(**a)
+        n = plain.shape[0]
+        big = torch.full((n, 3, 8, 72), 5.0, dtype=torch.bfloat16, device=DEV)
+        out = big[:, 1, :, :64]
+        B.page_attention(**a, out=out)
+        assert _same_bits(out, plain)
+        big[:, 1, :, :64] = 5.0
+        assert bool((big == 5).all())
 
 
 def test_sample_infinities_and_masks():
