@@ -1021,19 +1021,24 @@ def page_tables(cached, new_tokens, table, free_pages, free_at, page, n_pages, n
     b, dev, i32, n = cached.shape[0], cached.device, torch.int32, int(n_tokens)
     _want(n >= 0, "n_tokens must not be negative")
     _same("table", table, (b, table.shape[1]), i32, dev)
-    if first is None and length is None and position is None and slot is None and taken is None:      # (one allocation takes 1 us, a split of it 2)
-        first, length, position, slot, taken = torch.empty(2 * b + 2 * n + 2, dtype=i32, device=dev).split((b + 1, b, n, n, 1))
-    first = torch.empty(b + 1, dtype=i32, device=dev) if first is None else first
-    length = torch.empty(b, dtype=i32, device=dev) if length is None else length
-    position = torch.empty(n, dtype=i32, device=dev) if position is None else position
-    slot = torch.empty(n, dtype=i32, device=dev) if slot is None else slot
-    taken = torch.empty(1, dtype=i32, device=dev) if taken is None else taken
+    if first is None and length is None and position is None and slot is None and taken is None:      # (one allocation, and nothing to check: 3 us less)
+        buf = torch.empty(2 * b + 2 * n + 2, dtype=i32, device=dev)
+        first, length, position, slot, taken = buf.split((b + 1, b, n, n, 1))
+        at = buf.data_ptr()
+        out = (at, at + 4 * (b + 1), at + 4 * (2 * b + 1), at + 4 * (2 * b + 1 + n), at + 4 * (2 * b + 1 + 2 * n))
+    else:
+        first = torch.empty(b + 1, dtype=i32, device=dev) if first is None else first
+        length = torch.empty(b, dtype=i32, device=dev) if length is None else length
+        position = torch.empty(n, dtype=i32, device=dev) if position is None else position
+        slot = torch.empty(n, dtype=i32, device=dev) if slot is None else slot
+        taken = torch.empty(1, dtype=i32, device=dev) if taken is None else taken
+        out = (_table("first", first, b + 1, i32, dev), _table("length", length, b, i32, dev), _table("position", position, n, i32, dev),
+               _table("slot", slot, n, i32, dev), _table("taken", taken, 1, i32, dev))
     a = ps_page_tables_args(
         b, n, int(page), table.shape[1], int(n_pages), free_pages.shape[0], _table("cached", cached, b, i32, dev),
         _table("new_tokens", new_tokens, b, i32, dev), None if offset is None else _table("offset", offset, b, i32, dev),
         _table("free_pages", free_pages, free_pages.shape[0], i32, dev), None if free_at is None else _table("free_at", free_at, 1, i32, dev),
-        table.data_ptr(), _rows("table", table)[0], _table("first", first, b + 1, i32, dev), _table("length", length, b, i32, dev),
-        _table("position", position, n, i32, dev), _table("slot", slot, n, i32, dev), _table("taken", taken, 1, i32, dev))
+        table.data_ptr(), _rows("table", table)[0], *out)
     _launch(dev, lib().ps_page_tables, C.byref(a))
     return first, length, position, slot, taken
 
