@@ -131,7 +131,7 @@ __global__ __launch_bounds__(256) void page_append_kernel(ps_page_append_args a,
 // same time, and a merge of their records.  More tokens: blocks of 128 rows walk prefix and own positions one after the other.
 // Measured: own positions alone, 48 sequences of up to 8190 (16 / 8 heads of 64) 102 us = 5.3 TB/s; 64 sequences behind a prefix of 32761 (32 / 8
 // heads), own lengths up to 1000, 91 us: about 60 for the prefix's products and 34 for the own positions' bytes when each runs alone; prompts, 2 of 2048
-// tokens behind 16384 positions, 798 TFLOP/s, 8 of 512 behind 2048 205 us = 726: the matrix cores are busy 41 % of the time and the vector
+// tokens behind 16384 positions, 798 TFLOP/s, 8 of 512 behind 2048 198 us = 750: the matrix cores are busy 41 % of the time and the vector
 // instructions of the softmax, which share their issue port, 47 %.
 constexpr uint32_t kTile = 32, kStep = 64;
 constexpr uint32_t kFewRows = 32;
@@ -614,24 +614,19 @@ __device__ __forceinline__ SeqTokens tokens_of(const ps_page_attention_args &a, 
 }
 __device__ __forceinline__ int length_of(const ps_page_attention_args &a, uint32_t s) { return clampi(a.length[s], 0, (int)a.max_length); }
 __device__ __forceinline__ int prefix_length_of(const ps_page_attention_args &a, int p) { return clampi(a.prefix_length[p], 0, (int)a.max_prefix); }
-// the prefix that a sequence stands behind, -1: none; by a whole wave
-__device__ __forceinline__ int prefix_of(const ps_page_attention_args &a, uint32_t s) {
-    for (uint32_t p0 = 0; p0 < a.n_prefix; p0 += 64) {
-        const uint32_t p = p0 + (threadIdx.x & 63);
-        const uint64_t in = __ballot(p < a.n_prefix && a.group_first[min(p, a.n_prefix - 1)] <= (int)s && (int)s < a.group_first[min(p, a.n_prefix - 1) + 1]);
-        if (in) return __builtin_amdgcn_readfirstlane((int)p0 + __ffsll((unsigned long long)in) - 1);
-    }
-    return -1;
-}
-// the length of the prefix that a sequence stands behind; by a whole wave
-__device__ __forceinline__ int prefix_length_behind(const ps_page_attention_args &a, uint32_t s) {
+// the prefix that a sequence stands behind (-1: none) and its length; by a whole wave, all of it asked for at once
+struct Behind { int prefix, len; };
+__device__ __forceinline__ Behind prefix_behind(const ps_page_attention_args &a, uint32_t s) {
     for (uint32_t p0 = 0; p0 < a.n_prefix; p0 += 64) {
         const uint32_t p = p0 + (threadIdx.x & 63), at = min(p, a.n_prefix - 1);
         const int len = prefix_length_of(a, at), lo = a.group_first[at], hi = a.group_first[at + 1];
         const uint64_t in = __ballot(p < a.n_prefix && lo <= (int)s && (int)s < hi);
-        if (in) return __builtin_amdgcn_readlane(len, __ffsll((unsigned long long)in) - 1);
+        if (in) {
+            const int lane = __ffsll((unsigned long long)in) - 1;
+            return {(int)p0 + lane, __builtin_amdgcn_readlane(len, lane)};
+        }
     }
-    return 0;
+    return {-1, 0};
 }
 // the `flat`-th block of 128 rows of all groups' tokens; rows 0: there is none
 struct GroupBlock { RowSet set; uint32_t prefix, block; };
@@ -707,10 +702,10 @@ __global__ __launch_bounds__(256, 2) void page_rows_kernel(ps_page_attention_arg
     if (unit >= units) return;
     const uint32_t z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads, G = a.n_q_heads / a.n_kv_heads;
     const SeqTokens t = tokens_of(a, s);
-    if (block * 128 >= t.answered * G) return;
-    const int p = prefix_of(a, s);
-    const Span prefix = p < 0 ? Span{nullptr, 0, 0} : Span{a.prefix_table + p * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), prefix_length_of(a, p)};
     const Span own{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), length_of(a, s)};
+    const Behind p = prefix_behind(a, s);
+    if (block * 128 >= t.answered * G) return;
+    const Span prefix = p.prefix < 0 ? Span{nullptr, 0, 0} : Span{a.prefix_table + p.prefix * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), p.len};
     const RowSet set{t.row0, t.answered * G, G};
     const int np = (prefix.len + (int)kStep - 1) / (int)kStep, limit0 = own.len - t.n + 1;
     const int last = min(own.len, limit0 + (int)(min(block * 128 + 127, set.rows - 1) / G));
@@ -729,7 +724,7 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
     const uint32_t i = blockIdx.x / hb % a.max_tokens, s = blockIdx.x / hb / a.max_tokens;
     // (all of these are asked for before one is waited for)
     const SeqTokens t = tokens_of(a, s);
-    const int len = length_of(a, s), plen = prefix_length_behind(a, s);
+    const int len = length_of(a, s), plen = prefix_behind(a, s).len;
     if (h >= a.n_q_heads || (int)i >= t.answered) return;
     const uint32_t np = d.shared && plen ? (plen + d.plen - 1) / d.plen : 0;
     const uint32_t positions = d.shared ? len : (plen + kStep - 1) / kStep + (len + kStep - 1) / kStep;
@@ -780,19 +775,24 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
 //  sample_pick_kernel   a workgroup per row finds the borders among them, digit by digit of the logits' bits.  Where they are more than a list holds, in
 //                       passes over the row instead.
 // The sum of the first entries of the order is that of whole bins (64 bits, always added alike) and of a part of one, whose whole numbers are exact.
-// 256 rows of 128256 fp32 logits: 22 + 37 + 38 + 19 us, where each of the first three reads the 131 MB (27 us at a copy's rate); the second has a dozen
-// 64-bit operations and an addition in LDS for each entry beside.  16 rows 4 + 8 + 12 + 15 us, one of 32000 3 + 5 + 16: latencies.
-constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 512, kList = 2048, kRound = kPickThreads * 8, kShortRow = 32768;
+// 256 rows of 128256 fp32 logits: 22 + 37 + 39 + 16 us, where each of the first three reads the 131 MB (27 us at a copy's rate); the second has a dozen
+// 64-bit operations and an addition in LDS for each entry beside.  16 rows 4 + 8 + 13 + 12 us, one of 32000 3 + 5 + 16: latencies.
+constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 512, kBinsPad = kBins + 8, kList = 2048, kRound = kPickThreads * 8, kShortRow = 32768;
 constexpr double kBinsPerNat = 2047.0 / 24.0;
 
 struct RowTop { float m; int at; };
 struct SampleShape { uint32_t top, ntop, bins, nbins, find, nfind; };       // chunks of a row for the first three launches: entries, how many
+// What the borders of a row are found by, and the bins that they may lie in
+struct Wanted { uint32_t most; bool by_k, by_p, by_m; double share, reach, u; int bk, p0, p1, bm, d0, d1; };
 struct SampleWork {
     RowTop *tops;                  // [row][chunk]
     unsigned long long *sums;      // [row][bin]
     uint32_t *counts;              // [row][bin]
     uint32_t *listed;              // [row]
     unsigned long long *list;      // [row][kList]
+    Wanted *wanted;                // [row]
+    double *before_sum;            // [row][kBinsPad]: of all entries in front of a bin, and of all
+    uint32_t *before_count;        // [row][kBinsPad]
 };
 
 // bits that order as the values do, and back: larger for larger logits
@@ -930,6 +930,14 @@ __device__ __forceinline__ RowTop row_top(const RowTop *tops, uint32_t n, float 
     return t;
 }
 
+// a thread's first entries of lo .. hi - 1
+template <typename T>
+__device__ __forceinline__ Oct<T> first_of(const T *x, uint32_t lo, uint32_t hi) {
+    Oct<T> o;
+    o.fill(x, min(lo + threadIdx.x * 8, hi), hi);
+    return o;
+}
+
 template <typename T>
 __global__ __launch_bounds__(kPickThreads) void sample_bins_kernel(ps_sample_args a, SampleShape sh, SampleWork w) {
     __shared__ unsigned long long bins[kBins];             // sum of weights, and from bit 49 on how many: of 2^13 entries
@@ -948,8 +956,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_bins_kernel(ps_sample_arg
     const uint32_t lo = chunk * sh.bins, hi = min(a.vocab, lo + sh.bins);
     unsigned long long sum[kMine] = {};
     uint32_t count[kMine] = {};
-    Oct<T> next;
-    next.fill(x, min(lo + tid * 8, a.vocab), hi);
+    Oct<T> next = first_of(x, lo, hi);
     for (uint32_t i0 = lo; i0 < hi; i0 += 2 * kRound) {
 #pragma unroll
         for (uint32_t r = 0; r < 2; ++r) {
@@ -1004,8 +1011,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_bins_kernel(ps_sample_arg
         }
 }
 
-// What the borders of a row are found by, and the bins that they may lie in: up to four runs of bins, apart and ascending
-struct Wanted { uint32_t most; bool by_k, by_p, by_m; double share, reach, u; int bk, p0, p1, bm, d0, d1; };
+// up to four runs of bins, apart and ascending
 struct Runs {
     int lo[4], hi[4];
     uint32_t before[5];          // entries of the runs in front
@@ -1153,9 +1159,9 @@ __device__ __forceinline__ Runs runs_of(const Wanted &q, const BinLds &l) {
     }
     return r;
 }
-// every entry lo .. hi - 1 of a row in one of the runs: take(value, index, place)
+// every entry lo .. hi - 1 of a row in one of the runs: take(value, index, place); `next`: first_of these
 template <typename T, class Take>
-__device__ __forceinline__ void each_in(const T *x, uint32_t lo, uint32_t hi, const BinScale &s, const Runs &r, Take take) {
+__device__ __forceinline__ void each_in(const T *x, uint32_t lo, uint32_t hi, const BinScale &s, const Runs &r, Oct<T> next, Take take) {
     float from[4], to[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -1165,9 +1171,6 @@ __device__ __forceinline__ void each_in(const T *x, uint32_t lo, uint32_t hi, co
     }
     constexpr uint32_t kStride = kPickThreads * 8;
     uint32_t i = lo + threadIdx.x * 8;
-    if (i >= hi) return;
-    Oct<T> next;
-    next.fill(x, i, hi);
     for (; i < hi; i += kStride) {
         Oct<T> o = next;
         if (i + kStride < hi) next.fill(x, i + kStride, hi);
@@ -1202,15 +1205,24 @@ __global__ __launch_bounds__(kPickThreads) void sample_find_kernel(ps_sample_arg
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (!(temp > 0.f)) return;
     const FourBins four(w, row);
+    const T *x = static_cast<const T *>(a.logits) + row * a.logits_row;
+    const uint32_t lo = blockIdx.x * sh.find, hi = min(a.vocab, lo + sh.find);
+    const Oct<T> begin = first_of(x, lo, hi);
     const float m = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, l.fbuf, l.ibuf).m;
     if (m == -INFINITY) return;
     if (tid == 0) n = 0;
     __syncthreads();
     const Wanted q = analyse(a, four, row, l);
+    if (blockIdx.x == 0) {                    // the last launch need not work it out again
+        if (tid == 0) w.wanted[row] = q;
+        for (uint32_t b = tid; b <= kBins; b += kPickThreads) {
+            w.before_sum[(size_t)row * kBinsPad + b] = l.sum[b];
+            w.before_count[(size_t)row * kBinsPad + b] = l.count[b];
+        }
+    }
     const Runs r = runs_of(q, l);
     if (r.before[4] > kList) return;
-    const uint32_t lo = blockIdx.x * sh.find, hi = min(a.vocab, lo + sh.find);
-    each_in(static_cast<const T *>(a.logits) + row * a.logits_row, lo, hi, bin_scale(m, temp), r, [&](float v, uint32_t i, const Place &) {
+    each_in(x, lo, hi, bin_scale(m, temp), r, begin, [&](float v, uint32_t i, const Place &) {
         const uint32_t slot = atomicAdd(&n, 1u);
         if (slot < kList) mine[slot] = entry_of(v, i);
     });
@@ -1248,7 +1260,7 @@ struct Picker {
             for (uint32_t i = threadIdx.x; i < n; i += kPickThreads)
                 if (l.bin[i] == b) take(l.list[i]);
         } else {
-            each_in(x, 0, vocab, s, run_of(b), [&](float v, uint32_t i, const Place &) { take(entry_of(v, i)); });
+            each_in(x, 0, vocab, s, run_of(b), first_of(x, 0, vocab), [&](float v, uint32_t i, const Place &) { take(entry_of(v, i)); });
         }
     }
     __device__ __forceinline__ unsigned long long weight_of(unsigned long long e) const { return whole_of(s.place(value_in(e))); }
@@ -1370,11 +1382,25 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     __shared__ PickLds lds;
     BinLds &l = lds.bins;
     const uint32_t row = blockIdx.x, tid = threadIdx.x;
-    const FourBins four(w, row);
-    constexpr uint32_t kEach = kList / kPickThreads;
-    unsigned long long entry[kEach];                  // (those of the list that there are turn out later)
+    const T *x = static_cast<const T *>(a.logits) + row * a.logits_row;
+    // all that earlier launches have left is asked for at once (which entries of the list there are turns out later)
+    constexpr uint32_t kEach = kList / kPickThreads, kMine = kBins / kPickThreads;
+    unsigned long long entry[kEach] = {};
+    double sums[kMine] = {}, all_sum = 0;
+    uint32_t counts[kMine] = {}, all_count = 0;
+    Wanted q{};
+    if (sh.nfind) {
+        q = w.wanted[row];
 #pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) entry[j] = sh.nfind ? w.list[(size_t)row * kList + tid + j * kPickThreads] : 0;
+        for (uint32_t j = 0; j < kEach; ++j) entry[j] = w.list[(size_t)row * kList + tid + j * kPickThreads];
+#pragma unroll
+        for (uint32_t j = 0; j < kMine; ++j) {
+            sums[j] = w.before_sum[(size_t)row * kBinsPad + tid + j * kPickThreads];
+            counts[j] = w.before_count[(size_t)row * kBinsPad + tid + j * kPickThreads];
+        }
+        all_sum = w.before_sum[(size_t)row * kBinsPad + kBins];
+        all_count = w.before_count[(size_t)row * kBinsPad + kBins];
+    }
     const RowTop top = row_top<kPickThreads>(w.tops + (size_t)row * sh.ntop, sh.ntop, l.fbuf, l.ibuf);
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     if (top.m == -INFINITY || !(temp > 0.f)) {
@@ -1385,10 +1411,17 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
         return;
     }
     __syncthreads();
-    const Wanted q = analyse(a, four, row, l);
+    if (sh.nfind) {
+#pragma unroll
+        for (uint32_t j = 0; j < kMine; ++j) { l.sum[tid + j * kPickThreads] = sums[j]; l.count[tid + j * kPickThreads] = counts[j]; }
+        if (tid == 0) { l.sum[kBins] = all_sum; l.count[kBins] = all_count; }
+        __syncthreads();
+    } else {
+        q = analyse(a, FourBins(w, row), row, l);
+    }
     const Runs runs = runs_of(q, l);
     const uint32_t n = runs.before[4];
-    Picker<T> p{static_cast<const T *>(a.logits) + row * a.logits_row, a.vocab, n, n <= kList, bin_scale(top.m, temp), lds};
+    Picker<T> p{x, a.vocab, n, n <= kList, bin_scale(top.m, temp), lds};
     if (p.listed && sh.nfind) {
 #pragma unroll
         for (uint32_t j = 0; j < kEach; ++j) {
@@ -1400,7 +1433,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(ps_sample_arg
     } else if (p.listed) {                            // (a short row: picked out here)
         if (tid == 0) lds.n = 0;
         __syncthreads();
-        each_in(p.x, 0, a.vocab, p.s, runs, [&](float v, uint32_t i, const Place &y) {
+        each_in(p.x, 0, a.vocab, p.s, runs, first_of(p.x, 0, a.vocab), [&](float v, uint32_t i, const Place &y) {
             const uint32_t slot = atomicAdd(&lds.n, 1u);
             if (slot >= kList) return;
             lds.list[slot] = entry_of(v, i);
@@ -1480,6 +1513,10 @@ uint64_t sample_work(const ps_sample_args &a, const SampleShape &sh, uint8_t *ba
     w->counts = reinterpret_cast<uint32_t *>(take((uint64_t)a.n_rows * kBins * 4));
     w->listed = reinterpret_cast<uint32_t *>(take((uint64_t)a.n_rows * 4));
     w->list = reinterpret_cast<unsigned long long *>(take((uint64_t)a.n_rows * kList * 8));
+    const uint64_t found = sh.nfind ? a.n_rows : 0;
+    w->wanted = reinterpret_cast<Wanted *>(take(found * sizeof(Wanted)));
+    w->before_sum = reinterpret_cast<double *>(take(found * kBinsPad * 8));
+    w->before_count = reinterpret_cast<uint32_t *>(take(found * kBinsPad * 4));
     return off;
 }
 
