@@ -112,8 +112,9 @@ def test_append(ty, n, h, d, page, lay):
 
 # ------------------------------------------------------------------ attention
 
-def _attend_case(ty, d, hq, hk, page, toks, lens, groups=(), plens=(), seed=0, sharp=1.0, lay="heads", pad=0, holes=False):
-    """groups: first sequence of each prefix's, then the end.  What no table names, and rows behind a length, hold nan and inf."""
+def _attend_case(ty, d, hq, hk, page, toks, lens, groups=(), plens=(), seed=0, sharp=1.0, lay="heads", pad=0, holes=False, bound=0):
+    """groups: first sequence of each prefix's, then the end.  What no table names, and rows behind a length, hold nan and inf.  bound: of the prefixes,
+    by which work is dealt out (short prefixes of few sequences are walked with the sequences' own positions, others by themselves)."""
     torch, g, rng, dt = _t(), _gen(seed + 5), np.random.default_rng(seed), _dt(ty)
     n = sum(toks) + pad
     q = (torch.randn(n, (hq + 2 * hk) * d, generator=g, device=DEV) * sharp).to(dt)[:, :hq * d].view(n, hq, d)
@@ -141,7 +142,8 @@ def _attend_case(ty, d, hq, hk, page, toks, lens, groups=(), plens=(), seed=0, s
     first = np.concatenate([[0], np.cumsum(toks)]).astype(int).tolist()
     a = dict(q=q, k_pages=kp, v_pages=vp, first=_ints(first), length=_ints(list(lens)), table=_ints(full[0]), max_length=max(lens), max_tokens=max(toks))
     if plens:
-        a.update(group_first=_ints(list(groups)), prefix_length=_ints(list(plens)), prefix_table=_ints(full[1]), max_prefix=max(plens))
+        columns = [order[-1]] * max(0, -(-bound // page) - wide[1])
+        a.update(group_first=_ints(list(groups)), prefix_length=_ints(list(plens)), prefix_table=_ints([r + columns for r in full[1]]), max_prefix=max(list(plens) + [bound]))
     return a, first, full
 
 
@@ -182,15 +184,18 @@ ATTEND = [
     (128, 16, 2, 16, [130, 9, 64], [130, 9, 1000], (), ()), (128, 32, 4, 1024, [2] * 33, [900 + i for i in range(33)], (0, 33), [1500]),
     (64, 1, 1, 16, [1] * 130, [i % 90 + 1 for i in range(130)], (0, 129, 130), [16, 48]), (128, 64, 1, 16, [2, 2], [20, 333], (0, 2), [64]),
     (128, 3, 1, 16, [5] * 30, [i * 13 % 90 + 5 for i in range(30)], (0, 10, 10, 25), [50, 9, 200]),
+    (64, 8, 2, 128, [60, 200], [60, 700], (0, 2), [300]), (128, 8, 2, 256, [40, 33], [40, 500], (), ()), (64, 4, 4, 1024, [100], [2500], (), ()),
+    (128, 6, 2, 64, [7, 2], [90, 64], (0, 1, 2), [128, 640]), (64, 8, 1, 64, [4] * 9, [64 + i for i in range(9)], (0, 5, 9), [64, 129]),
 ]
 
 
 @pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("bound", [0, 1000])
 @pytest.mark.parametrize("case", range(len(ATTEND)))
-def test_attention(ty, case):
+def test_attention(ty, case, bound):
     from paper_2604_26334_amd import binding as B
     d, hq, hk, page, toks, lens, groups, plens = ATTEND[case]
-    a, first, full = _attend_case(ty, d, hq, hk, page, toks, lens, groups, plens, case, sharp=(1.0, 4.0)[case % 2], lay=("heads", "rows")[case // 2 % 2])
+    a, first, full = _attend_case(ty, d, hq, hk, page, toks, lens, groups, plens, case, sharp=(1.0, 4.0)[case % 2], lay=("heads", "rows")[case // 2 % 2], bound=bound)
     out = B.page_attention(**a)
     _check_attend(a, out, first, full, toks, lens, groups, plens, ty)
     assert _same_bits(out, B.page_attention(**a))
@@ -211,32 +216,34 @@ def test_attention_over_long_contexts(ty, d, hq, hk, page, toks, lens, plens):
     _check_attend(a, B.page_attention(**a), first, full, toks, lens, groups, plens, ty)
 
 
-def test_empty_rows_are_zero():
+@pytest.mark.parametrize("bound", [0, 1000])
+def test_empty_rows_are_zero(bound):
     """Tokens without a position, sequences of length 0 and prefixes of length 0; pages that name nothing."""
     from paper_2604_26334_amd import binding as B
     for toks, lens, groups, plens in (([1, 2, 3, 1], [0, 1, 2, 5], (), ()), ([2, 3, 1], [0, 1, 3], (0, 1, 3), [0, 40]), ([40, 50], [0, 30], (0, 1), [0]),
                                       ([60, 1], [10, 0], (0, 2), [33]), ([1, 1], [0, 0], (), ())):
-        a, first, full = _attend_case("f16", 64, 4, 2, 16, toks, lens, groups, plens, 4)
+        a, first, full = _attend_case("f16", 64, 4, 2, 16, toks, lens, groups, plens, 4, bound=bound)
         out = B.page_attention(**a)
         _check_attend(a, out, first, full, toks, lens, groups, plens, "f16")
         if not plens:
             assert bool((out[:max(0, toks[0] - lens[0])] == 0).all())
     for seed in range(4):
         toks, lens, groups, plens = ([1, 1, 2, 1], [17, 100, 40, 16], (0, 2), [90]) if seed % 2 else ([50, 30], [50, 99], (0, 2), [64])
-        a, first, full = _attend_case("f16", 128, 4, 2, 16, toks, lens, groups, plens, seed, holes=True)
+        a, first, full = _attend_case("f16", 128, 4, 2, 16, toks, lens, groups, plens, seed, holes=True, bound=bound)
         _check_attend(a, B.page_attention(**a), first, full, toks, lens, groups, plens, "f16")
     a["table"].fill_(-1)
     a["prefix_table"].fill_(99999)
     assert bool((B.page_attention(**a) == 0).all())
 
 
+@pytest.mark.parametrize("bound", [0, 1000])
 @pytest.mark.parametrize("hq,toks", [(4, [1, 3, 8]), (16, [2, 1, 4]), (4, [40, 3, 70])])
-def test_hidden_positions_may_hold_anything(hq, toks):
+def test_hidden_positions_may_hold_anything(hq, toks, bound):
     """A position that a token does not see does not count, whatever its key and value hold; one that it sees does."""
     from paper_2604_26334_amd import binding as B
     torch = _t()
     lens = [t + 20 for t in toks]
-    a, first, full = _attend_case("f16", 128, hq, 2, 16, toks, lens, (0, 2), [50], 6)
+    a, first, full = _attend_case("f16", 128, hq, 2, 16, toks, lens, (0, 2), [50], 6, bound=bound)
     clean = B.page_attention(**a)
     p = lens[2] - toks[2] // 2                 # an own position of the last sequence in the middle of its new tokens
     i = p - (lens[2] - toks[2])                # the first token that sees it
@@ -252,13 +259,14 @@ def test_hidden_positions_may_hold_anything(hq, toks):
                 assert not bool(torch.isfinite(out[first[2] + i:]).any())
 
 
+@pytest.mark.parametrize("bound", [0, 1000])
 @pytest.mark.parametrize("toks", [[1, 1, 1], [2] * 20, [60, 9]])
-def test_keys_that_are_no_numbers_reach_every_token_that_sees_them(toks):
+def test_keys_that_are_no_numbers_reach_every_token_that_sees_them(toks, bound):
     from paper_2604_26334_amd import binding as B
     torch = _t()
     for where in ("prefix", "own"):
         for lo, hi in ((0, 16), (0, 64), (64, 192), (0, 400), (384, 400)):
-            a, first, full = _attend_case("f16", 64, 4, 2, 16, toks, [400 + t for t in toks], (0, len(toks)), [400], 3)
+            a, first, full = _attend_case("f16", 64, 4, 2, 16, toks, [400 + t for t in toks], (0, len(toks)), [400], 3, bound=bound)
             for i in range(lo, hi):
                 row = full[1][0] if where == "prefix" else full[0][0]
                 a["k_pages"][row[i // 16], 1, i % 16] = float("nan")
@@ -267,20 +275,22 @@ def test_keys_that_are_no_numbers_reach_every_token_that_sees_them(toks):
             assert bool(fine[:, :2].all()) and not bool(fine[:rows, 2:].any()) and bool(fine[rows:].all()), (where, lo, hi)
 
 
+@pytest.mark.parametrize("bound", [0, 1000])
 @pytest.mark.parametrize("toks", [[1, 2], [40, 3]])
 @pytest.mark.parametrize("scale", [-0.09, 0.0, 1.3])
-def test_attention_with_any_scale(toks, scale):
+def test_attention_with_any_scale(toks, scale, bound):
     from paper_2604_26334_amd import binding as B
-    a, first, full = _attend_case("bf16", 128, 4, 2, 16, toks, [333, 40], (0, 2), [99], 6)
+    a, first, full = _attend_case("bf16", 128, 4, 2, 16, toks, [333, 40], (0, 2), [99], 6, bound=bound)
     _check_attend(a, B.page_attention(**a, scale=scale), first, full, toks, [333, 40], (0, 2), [99], "bf16", scale)
 
 
-def test_attention_of_padded_batches_and_bounded_values():
+@pytest.mark.parametrize("bound", [0, 1000])
+def test_attention_of_padded_batches_and_bounded_values(bound):
     """Rows behind the last sequence keep what they hold; lengths, offsets and groups out of range are bounded as documented."""
     from paper_2604_26334_amd import binding as B
     torch = _t()
     toks, lens, groups, plens = [5, 0, 4], [20, 3, 30], (0, 2), [70]
-    a, first, full = _attend_case("f16", 128, 4, 2, 16, toks, lens, groups, plens, 5, pad=7)
+    a, first, full = _attend_case("f16", 128, 4, 2, 16, toks, lens, groups, plens, 5, pad=7, bound=bound)
     out = torch.full((16, 4, 128), 3.0, dtype=torch.float16, device=DEV)
     B.page_attention(**a, out=out)
     _check_attend(a, out, first, full, toks, lens, groups, plens, "f16")
@@ -292,7 +302,7 @@ def test_attention_of_padded_batches_and_bounded_values():
     B.page_attention(**b, out=out)
     # (the first of five tokens sees 19 - 5 + 1 positions; the fifth is not answered)
     want = torch.full_like(out, 3.0)
-    B.page_attention(**dict(b, length=_ints([19, 0, 0]), prefix_length=_ints([33]), max_tokens=5), out=want)
+    B.page_attention(**dict(b, length=_ints([19, 0, 0]), prefix_length=_ints([33]), max_tokens=5, max_prefix=a["max_prefix"]), out=want)
     assert bool((out[4] == 3).all()) and bool((out[9:] == 3).all())
     err = (out[:4].float() - want[:4].float()).abs().max()
     # (two results, each off by half a step of a value up to 5 and of the values' spread, up to 10, and by fp32's sums: 32 half steps)
@@ -473,6 +483,31 @@ def test_calls_at_once_on_streams_of_their_own():
     for i, (out, (token, kept)) in enumerate(got):
         want = work[i % 2]
         assert _same_bits(out, want[3]) and torch.equal(token, want[4][0]) and torch.equal(kept, want[4][1]), i
+
+
+def test_a_workspace_may_hold_anything():
+    """What a workspace holds before a call does not show in the results, and nothing behind the bytes that were asked for is written."""
+    import ctypes as C
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    for toks, lens, groups, plens, bound in (([1, 2, 1] * 5, [700, 33, 1] * 5, (0, 9, 15), [900, 40], 0), ([3] * 4, [50, 3, 900, 2000], (0, 2), [70], 1000),
+                                             ([60, 2], [60, 3000], (0, 1), [500], 0), ([1] * 9, [0] * 9, (3, 6), [600], 0)):
+        a, _, _ = _attend_case("f16", 64, 8, 2, 16, toks, lens, groups, plens, 7, bound=bound)
+        want = B.page_attention(**a)
+        for fill in (0, 255, 127):
+            work = torch.full((1 << 26,), fill, dtype=torch.uint8, device=DEV)
+            assert _same_bits(B.page_attention(**a, workspace=work), want)
+    for n, V in ((7, 3000), (5, 90000)):
+        x, u = (torch.randn(n, V, generator=_gen(V), device=DEV) * 2).half(), torch.rand(n, generator=_gen(V), device=DEV)
+        x[1], x[2] = float("-inf"), 1.0
+        s = dict(temperature=torch.tensor([1.0, 1.0, 1.0, 0.0, 0.5] + [2.0] * (n - 5), device=DEV), top_p=torch.full((n,), 0.9, device=DEV), top_k=_ints([100] * n))
+        want = B.sample(x, u, **s)
+        need = C.c_uint64()
+        assert B.lib().ps_sample_workspace(C.byref(B.ps_sample_args(type=0, n_rows=n, vocab=V)), C.byref(need)) == 0
+        for fill in (0, 255, 127):
+            work = torch.full((need.value + 4096,), fill, dtype=torch.uint8, device=DEV)
+            got = B.sample(x, u, **s, workspace=work)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool((work[need.value:] == fill).all())
 
 
 def test_attention_into_a_part_of_a_larger_tensor():
