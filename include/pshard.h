@@ -849,7 +849,8 @@ int32_t ps_page_attention(const ps_page_attention_args *args, void *workspace, u
  * Weights are right to 2e-11 of each (those below e^-24 of the largest to 2^-31 of e^-24) and added as whole numbers, runs of them in 64 bits
  * and always alike, so a row's result is the same in any call, batch, stride or type that holds its values.
  *  type F16, BF16 or F32; rows [n_rows][vocab], logits_row elements apart, alignment of an element is enough; vocab 1 .. 2^24;
- *  n_rows <= 65535.  token, kept [n_rows]; kept (n of each row) may be NULL.  ps_sample_workspace: about 65 KB a row; 256-byte aligned. */
+ *  n_rows <= 65535.  token, kept [n_rows]; kept (n of each row) may be NULL.  A stack's next tokens: over the buffer of
+ *  ps_stack_set_logits_out, on its compute stream behind ps_stack_forward.  ps_sample_workspace: about 65 KB a row; 256-byte aligned. */
 typedef struct ps_sample_args {
     uint32_t type, n_rows, vocab, reserved;
     const void *logits;

@@ -673,3 +673,34 @@ def test_a_step_on_another_stream_and_replayed():
     a["table"].copy_(table0)
     for x, y in zip(list(_step(a, B)) + [a["pool"], a["table"]], replayed):
         assert _same_bits(x, y)
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+def test_a_stacks_next_tokens(mode):
+    """A stack's logits, drawn from on its compute stream behind each forward, without a wait between them."""
+    import synth_inputs as S
+    from paper_2604_26334_amd import binding as B
+    from tests import harness as Hn
+    from tests.test_gpu_head import _budgets, _load_all
+    torch = _t()
+    M, V = 16, 1040
+    cfg = dict(Hn.small_dense_cfg(2), vocab=V)
+    plan = B.Plan(cfg, _budgets(cfg, M, [1.0])[0], M)
+    st = B.Stack(plan)
+    st.set_decode_mode(mode)
+    _load_all(st, cfg, Hn.WeightCache(cfg, 9), S.head_matrix(9, cfg))
+    xin = torch.from_numpy(np.ascontiguousarray(S.activations(9, 0, M, cfg["hidden"]))).to(st.device)
+    xout, logits = torch.empty_like(xin), torch.full((M, V), 7.0, dtype=torch.float16, device=st.device)
+    u = torch.rand(M, generator=_gen(1), device=DEV)
+    s = dict(temperature=torch.full((M,), 0.8, device=DEV), top_k=_ints([40] * M), top_p=torch.full((M,), 0.95, device=DEV))
+    st.set_logits_out(logits, 0, M)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        st.forward(xin, xout)
+        with torch.cuda.stream(st.compute):
+            token, kept = B.sample(logits, u, **s)
+        st.synchronize()
+        _check_sample(logits, u, token, kept, **s)
+        assert int(kept.max()) <= 40 and len(set(token.tolist())) > 1
+    st.close()
+    plan.close()
