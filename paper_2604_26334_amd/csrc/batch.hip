@@ -142,11 +142,11 @@ template <int D> __device__ __forceinline__ uint32_t v_slot(uint32_t row) { retu
 template <int D> __device__ __forceinline__ uint32_t k_slot(uint32_t row) { return D == 128 ? row & 15u : row >> 1 & 7u; }
 
 struct PageDeal {
-    uint32_t shared;             // 1: prefixes for all their tokens at once; 0: blocks of 128 rows of a sequence
-    uint32_t nt;                 // rows of a sequence, in 16 (shared)
+    uint32_t shared;             // 1: prefixes for all their tokens at once; 0: with each sequence's own positions
+    uint32_t nt;                 // rows of a sequence, in 16; 0: in blocks of 128
     uint32_t blocks;             // of 128 rows: of all groups at most (shared), of a sequence
     uint32_t psplit, plen;       // runs of a prefix, positions of a run (shared)
-    uint32_t osplit, olen;       // runs of own positions (shared), or of a sequence's steps
+    uint32_t osplit, olen;       // runs of own positions (shared), or of a sequence's tiles (nt) or steps
     uint32_t direct;             // no records: the result itself
 };
 template <int D, int NT> constexpr uint32_t few_lds() { return std::max<uint32_t>(4 * kTile * D * 2, 4 * NT * 16 * (D + 4) * 4 + 4 * NT * 16 * 2 * 4) + 16; }
@@ -197,11 +197,11 @@ __device__ __forceinline__ void add_wild(const ps_page_attention_args &a, const 
     }
 }
 
-// Rows of `set` (up to NT x 16) over positions lo .. hi - 1 of a span (lo a multiple of 32).  Row rho sees positions below limit0 + rho / group.
-// `window` holds the table's entries from the wave's first tile on.
-template <typename T, int D, int NT>
-__device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const RowSet &set, const Span &span, uint32_t shift, uint32_t hk, int lo, int hi, int limit0,
-                                         PageWindow window, uint32_t records, uint32_t z, float *part, unsigned char *lds) {
+// Rows of `set` (up to NT x 16) over tiles lo .. hi - 1 of a span's positions up to `end`, of which row rho sees those below limit0 + rho / group; `window` holds
+// the table's entries from the wave's first tile on.  kBoth: over tiles of `prefix`, which every row sees, and then those of the span.
+template <typename T, int D, int NT, bool kBoth>
+__device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const RowSet &set, const Span &prefix, const Span &span, uint32_t shift, uint32_t hk, int lo, int hi, int end,
+                                         int limit0, PageWindow window, uint32_t records, uint32_t z, float *part, unsigned char *lds) {
     using M = Mfma<T>;
     using v8 = typename M::v8;
     constexpr int KK = D / 32, DT = D / 16, RB = NT * 16, OP = D + 4;
@@ -215,12 +215,19 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
     const uint32_t vrow = lane / kRowPieces;
     u4_t kreg[2][KK], vreg[kVLoads];
     uint32_t gone = 0;                         // halves of the requested tile that no page holds
-    int P0 = lo + (int)wave * (int)kTile;
-    auto request = [&](int P) {
+    const int np = kBoth ? (prefix.len + (int)kTile - 1) / (int)kTile : 0;
+    int held = kBoth ? -1 : 1;                 // which table the window is of
+    auto request = [&](int tile) {
+        const bool mine = !kBoth || tile >= np;
+        const int P = (tile - (mine ? np : 0)) * (int)kTile, last = (mine ? end : prefix.len) - 1;
+        if (held != (int)mine || ((P + 31) >> shift) - window.base >= 64) {
+            window.fill(mine ? span : prefix, P >> shift, a.n_pages);
+            held = mine;
+        }
         gone = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int number = window(min(P + h * 16, hi - 1) >> shift);
+            const int number = window(min(P + h * 16, last) >> shift);
             if (number < 0) gone |= 1u << h;
             const PageRows rows(a, kc, vc, number, P + h * 16, mask);
 #pragma unroll
@@ -232,10 +239,8 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
             }
         }
     };
-    auto move_window = [&](int P) {
-        if (((P + 31) >> shift) - window.base >= 64) window.fill(span, P >> shift, a.n_pages);
-    };
-    if (P0 < hi) request(P0);
+    int tile = lo + (int)wave;
+    if (tile < hi) request(tile);
     if (tid == 0) *wild = 0;
     __syncthreads();
 
@@ -272,7 +277,9 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
         for (int dt = 0; dt < DT; ++dt) vread[dt] = row * (D * 2) + (((2 * dt + ((i & 3) >> 1)) ^ v_slot<D>(row)) << 4) + (i & 1) * 8;
     }
     const int wild0 = max(limit0, 0) & ~(int)(kTile - 1);        // from here on not every row sees every position
-    for (; P0 < hi; P0 += 4 * (int)kTile) {
+    for (; tile < hi; tile += 4) {
+        const bool mine = !kBoth || tile >= np;
+        const int P0 = (tile - (mine ? np : 0)) * (int)kTile, stop = mine ? end : prefix.len;
         const uint32_t missing = gone;
         f4_t S[NT][2];
 #pragma unroll
@@ -283,15 +290,15 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
             for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) S[t][h] = M::mul(__builtin_bit_cast(v8, kreg[h][kk]), q[t][kk], S[t][h]);
-        if (missing || P0 + (int)kTile > hi) {
+        if (missing || P0 + (int)kTile > stop) {
             asm volatile("");
 #pragma unroll
             for (uint32_t u = 0; u < kVLoads; ++u) {
                 const uint32_t row = u * (64 / kRowPieces) + vrow;
-                vreg[u] = P0 + (int)row < hi && !(missing >> (2 * u / kVLoads) & 1) ? vreg[u] : u4_t{0, 0, 0, 0};
+                vreg[u] = P0 + (int)row < stop && !(missing >> (2 * u / kVLoads) & 1) ? vreg[u] : u4_t{0, 0, 0, 0};
             }
         }
-        if (P0 >= wild0) {
+        if (mine && P0 >= wild0) {
             bool odd = false;
 #pragma unroll
             for (uint32_t u = 0; u < kVLoads; ++u) odd |= made_finite<T>(vreg[u]);
@@ -299,15 +306,12 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
         }
 #pragma unroll
         for (uint32_t u = 0; u < kVLoads; ++u) *reinterpret_cast<u4_t *>(stage + u * 1024 + lane * 16) = vreg[u];
-        if (P0 + 4 * (int)kTile < hi) {
-            move_window(P0 + 4 * (int)kTile);
-            request(P0 + 4 * (int)kTile);
-        }
-        if (missing || P0 + (int)kTile > min(hi, limit0)) {
+        if (tile + 4 < hi) request(tile + 4);
+        if (missing || P0 + (int)kTile > stop || (mine && P0 + (int)kTile > limit0)) {
             asm volatile("");
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const int last = min(hi, limit[t]) - P0 - 4 * (int)c;
+                const int last = (mine ? min(stop, limit[t]) : stop) - P0 - 4 * (int)c;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) S[t][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < last && !(missing >> (e >> 2) & 1) ? S[t][e >> 2][e & 3] : -INFINITY;
             }
@@ -354,7 +358,7 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
             for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[e], o[e]);
         }
         const uint32_t tok = rho / G, h = hk * G + rho % G;
-        if (*wild) add_wild<T>(a, span, shift, hk, max(lo, wild0), min(hi, limit0 + (int)tok), d0, o);
+        if (*wild) add_wild<T>(a, span, shift, hk, max((lo - np) * (int)kTile, wild0), min(min((hi - np) * (int)kTile, end), limit0 + (int)tok), d0, o);
         const size_t token = (size_t)set.token0 + tok;
         if (records) {
             float *dst = part + ((token * a.n_q_heads + h) * records + z) * OP;
@@ -678,7 +682,7 @@ __global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_a
         if (g.set.rows <= NT * 16) {
             PageWindow window;
             window.fill(span, (lo + (int)(wave * kTile)) >> shift, a.n_pages);
-            rows_few<T, D, NT>(a, g.set, span, shift, hk, lo, hi, len, window, records, z, part, lds);
+            rows_few<T, D, NT, false>(a, g.set, Span{nullptr, 0, 0}, span, shift, hk, lo / (int)kTile, (hi + (int)kTile - 1) / (int)kTile, hi, hi, window, records, z, part, lds);
         } else rows_many<T, D, false>(a, g.set, g.block * 128, Span{span.table, span.entries, hi}, Span{nullptr, 0, 0}, shift, hk, lo / (int)kStep, (hi + (int)kStep - 1) / (int)kStep, 0, records, z, part, lds);
     } else {
         const uint32_t unit = (run - prefix8) * 8 + blockIdx.x % 8, z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads;
@@ -690,8 +694,28 @@ __global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_a
         const int len = length_of(a, s), lo = (int)min((uint64_t)z * d.olen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)len);
         if (t.answered == 0 || (lo >= hi && records)) return;
         const uint32_t G = a.n_q_heads / a.n_kv_heads;
-        rows_few<T, D, NT>(a, RowSet{t.row0, t.answered * G, G}, Span{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), len}, shift, hk, lo, hi, len - t.n + 1, window, records, d.psplit + z, part, lds);
+        const Span own{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), len};
+        rows_few<T, D, NT, false>(a, RowSet{t.row0, t.answered * G, G}, Span{nullptr, 0, 0}, own, shift, hk, lo / (int)kTile, (hi + (int)kTile - 1) / (int)kTile, hi, len - t.n + 1, window, records,
+                                  d.psplit + z, part, lds);
     }
+}
+
+// Few rows a sequence and a short prefix: the sequence's own workgroups walk its tiles, the prefix's first.  Where 128 rows' places are mostly empty, this
+// kernel's reads are ahead by a tile in every wave; latencies bound it (3 sequences, 4 / 2 heads of 128, 77 + 40 positions: 8.5 us on the GPU, as a
+// block of 128 rows 13.6), then memory (16 sequences, 32 / 8 heads of 128, 500 + 3000: 30.7 us a call, 4.5 TB/s, for 40.8).
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(256, 2) void page_few_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, float *part) {
+    const uint32_t unit = blockIdx.x, z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads, G = a.n_q_heads / a.n_kv_heads;
+    const SeqTokens t = tokens_of(a, s);
+    const Span own{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), length_of(a, s)};
+    const Behind p = prefix_behind(a, s);
+    if (t.answered == 0) return;
+    const Span prefix = p.prefix < 0 ? Span{nullptr, 0, 0} : Span{a.prefix_table + p.prefix * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), p.len};
+    const int tiles = (prefix.len + (int)kTile - 1) / (int)kTile + (own.len + (int)kTile - 1) / (int)kTile;
+    const int lo = (int)min((uint64_t)z * d.olen, (uint64_t)tiles), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)tiles);
+    if (lo >= hi && !d.direct) return;
+    rows_few<T, D, NT, true>(a, RowSet{t.row0, t.answered * G, G}, prefix, own, shift, hk, lo, hi, own.len, own.len - t.n + 1, PageWindow{-1, 0}, d.direct ? 0 : d.osplit, z, part,
+                             reinterpret_cast<unsigned char *>(page_lds));
 }
 
 template <typename T, int D>
@@ -727,7 +751,7 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
     const int len = length_of(a, s), plen = prefix_behind(a, s).len;
     if (h >= a.n_q_heads || (int)i >= t.answered) return;
     const uint32_t np = d.shared && plen ? (plen + d.plen - 1) / d.plen : 0;
-    const uint32_t positions = d.shared ? len : (plen + kStep - 1) / kStep + (len + kStep - 1) / kStep;
+    const uint32_t unit = d.nt ? kTile : kStep, positions = d.shared ? len : (plen + unit - 1) / unit + (len + unit - 1) / unit;
     const uint32_t n = np + (positions + d.olen - 1) / d.olen;
     const size_t token = (size_t)t.row0 + i;
     const float *r0 = part + (token * a.n_q_heads + h) * (d.psplit + d.osplit) * OP;
@@ -1549,9 +1573,9 @@ PageDeal page_deal(const ps_page_attention_args &a) {
     const uint32_t G = a.n_q_heads / a.n_kv_heads;
     const uint64_t tokens = std::min(a.max_tokens, a.n_tokens), rows = tokens * G;
     const bool prefixes = a.n_prefix && a.max_prefix;
-    // a short prefix of few sequences is not worth a launch of its own results: 3 sequences, 4 / 2 heads, 77 + 40 positions 14 us for 17, 16 of 32 / 8
-    // heads, 500 + 500 21 for 26 (but 64 of 250 + 250 25 for 22)
-    const bool small = prefixes && (uint64_t)a.n_seq * a.n_kv_heads <= 128 && a.max_prefix <= 512;
+    // Prefixes of few positions in all are read again for each sequence sooner than joined from results of their own: 16 sequences, 32 / 8 heads of 128,
+    // 500 + 500 positions 16.5 us for 25.8, 1000 + 500 19.3 for 22.3, 2000 + 100 21.8 for 20.6; 64 sequences, 250 + 250 18.3 for 21.2, 1000 + 500 35.5 for 27.9
+    const bool small = prefixes && (uint64_t)a.n_seq * a.n_kv_heads * a.max_prefix <= 196608;
     d.shared = rows <= kFewRows && !small;
     auto cut = [](uint64_t units, uint64_t want, uint64_t whole, uint64_t least, uint64_t multiple, uint32_t *n, uint32_t *len) {
         const uint64_t most = std::max<uint64_t>(1, whole / least), runs = std::min(std::max<uint64_t>(1, want / std::max<uint64_t>(1, units)), most);
@@ -1566,10 +1590,17 @@ PageDeal page_deal(const ps_page_attention_args &a) {
         if (prefixes) cut((uint64_t)d.blocks * a.n_kv_heads, own_us * 4 > prefix_us ? 256 : 512, a.max_prefix, 256, kStep, &d.psplit, &d.plen);
         cut((uint64_t)a.n_seq * a.n_kv_heads, a.n_seq > 1 ? 512 : 1024, a.max_length, 128, 4 * kTile, &d.osplit, &d.olen);
         d.direct = d.psplit == 0 && d.osplit == 1;
+    } else if (rows <= kFewRows) {
+        d.nt = rows <= 16 ? 1 : 2;
+        d.blocks = 1;
+        const uint64_t tiles = (prefixes ? (a.max_prefix + kTile - 1) / kTile : 0) + (a.max_length + kTile - 1) / kTile;
+        // (up to 1024 positions in one run: without a merge 16.5 us for 17.3, 16 sequences of 500 + 500; longer ones in runs of 512: 500 + 3000 30.7 us for 34.6)
+        cut((uint64_t)a.n_seq * a.n_kv_heads, 512, tiles, tiles <= 32 ? 32 : 16, 4, &d.osplit, &d.olen);
+        d.direct = d.osplit == 1;
     } else {
         d.blocks = (uint32_t)((rows + 127) / 128);
         const uint64_t steps = (prefixes ? (a.max_prefix + kStep - 1) / kStep : 0) + (a.max_length + kStep - 1) / kStep;
-        // (up to four steps in one run: without a merge 16 us for 19, 16 sequences of 100 + 100)
+        // (up to four steps in one run: without a merge 17.6 us for 19, 16 sequences of 16 tokens behind 100 + 100)
         cut((uint64_t)a.n_seq * a.n_kv_heads * d.blocks, 512, steps, steps <= 4 ? 4 : 2, 1, &d.osplit, &d.olen);
         d.direct = d.osplit == 1;
     }
@@ -1615,6 +1646,15 @@ hipError_t launch_rows(const ps_page_attention_args &a, const PageDeal &d, uint3
     hipLaunchKernelGGL((page_rows_kernel<T, D>), dim3(own8 * 8), dim3(256), many_lds<D>(), st, a, d, log2_of(a.page), part);
     return hipGetLastError();
 }
+template <typename T, int D, int NT>
+hipError_t launch_few(const ps_page_attention_args &a, const PageDeal &d, float *part, hipStream_t st) {
+    static std::atomic<uint64_t> done;
+    constexpr uint32_t lds = few_lds<D, NT>();
+    const hipError_t e = take_lds(&page_few_kernel<T, D, NT>, lds, done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((page_few_kernel<T, D, NT>), dim3(a.n_seq * a.n_kv_heads * d.osplit), dim3(256), lds, st, a, d, log2_of(a.page), part);
+    return hipGetLastError();
+}
 template <typename T, int D>
 hipError_t launch_page_attention(const ps_page_attention_args &call, float *part, hipStream_t st) {
     ps_page_attention_args a = call;
@@ -1626,7 +1666,9 @@ hipError_t launch_page_attention(const ps_page_attention_args &call, float *part
     if (a.max_prefix == 0) a.prefix_width = 0;
     uint64_t prefix8, own8;
     page_groups(a, d, &prefix8, &own8);
-    const hipError_t e = !d.shared ? launch_rows<T, D>(a, d, (uint32_t)own8, part, st)
+    const hipError_t e = !d.shared && d.nt == 1 ? launch_few<T, D, 1>(a, d, part, st)
+                         : !d.shared && d.nt == 2 ? launch_few<T, D, 2>(a, d, part, st)
+                         : !d.shared ? launch_rows<T, D>(a, d, (uint32_t)own8, part, st)
                          : d.nt == 1 ? launch_shared<T, D, 1>(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st)
                                      : launch_shared<T, D, 2>(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st);
     if (e != hipSuccess || d.direct) return e;

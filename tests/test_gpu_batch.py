@@ -114,7 +114,8 @@ def test_append(ty, n, h, d, page, lay):
 
 def _attend_case(ty, d, hq, hk, page, toks, lens, groups=(), plens=(), seed=0, sharp=1.0, lay="heads", pad=0, holes=False, bound=0):
     """groups: first sequence of each prefix's, then the end.  What no table names, and rows behind a length, hold nan and inf.  bound: of the prefixes,
-    by which work is dealt out (short prefixes of few sequences are walked with the sequences' own positions, others by themselves)."""
+    by which work is dealt out (prefixes of up to 196608 positions over all sequences and kv heads are walked with the sequences' own positions, longer ones by
+    themselves)."""
     torch, g, rng, dt = _t(), _gen(seed + 5), np.random.default_rng(seed), _dt(ty)
     n = sum(toks) + pad
     q = (torch.randn(n, (hq + 2 * hk) * d, generator=g, device=DEV) * sharp).to(dt)[:, :hq * d].view(n, hq, d)
@@ -190,7 +191,7 @@ ATTEND = [
 
 
 @pytest.mark.parametrize("ty", ["f16", "bf16"])
-@pytest.mark.parametrize("bound", [0, 1000])
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
 @pytest.mark.parametrize("case", range(len(ATTEND)))
 def test_attention(ty, case, bound):
     from paper_2604_26334_amd import binding as B
@@ -203,7 +204,8 @@ def test_attention(ty, case, bound):
 
 @pytest.mark.parametrize("ty", ["f16", "bf16"])
 @pytest.mark.parametrize("d,hq,hk,page,toks,lens,plens", [(128, 32, 8, 16, [1] * 5, [700, 1, 33, 64, 5000], [4097]), (64, 8, 2, 64, [1], [70001], []),
-                                                          (128, 8, 2, 32, [24, 24], [300, 24], [9000]), (64, 16, 2, 16, [2] * 17, [50] * 17, [20003])])
+                                                          (128, 8, 2, 32, [24, 24], [300, 24], [9000]), (64, 16, 2, 16, [2] * 17, [50] * 17, [20003]),
+                                                          (128, 32, 8, 16, [1] * 24, [1 + 70 * i for i in range(24)], [4097]), (128, 24, 2, 64, [2, 1], [900, 1], [12321])])
 def test_attention_over_long_contexts(ty, d, hq, hk, page, toks, lens, plens):
     """Sharp scores; positions at the boundaries of tiles, pages and splits are each some token's favourite."""
     from paper_2604_26334_amd import binding as B
@@ -216,7 +218,7 @@ def test_attention_over_long_contexts(ty, d, hq, hk, page, toks, lens, plens):
     _check_attend(a, B.page_attention(**a), first, full, toks, lens, groups, plens, ty)
 
 
-@pytest.mark.parametrize("bound", [0, 1000])
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
 def test_empty_rows_are_zero(bound):
     """Tokens without a position, sequences of length 0 and prefixes of length 0; pages that name nothing."""
     from paper_2604_26334_amd import binding as B
@@ -236,7 +238,7 @@ def test_empty_rows_are_zero(bound):
     assert bool((B.page_attention(**a) == 0).all())
 
 
-@pytest.mark.parametrize("bound", [0, 1000])
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
 @pytest.mark.parametrize("hq,toks", [(4, [1, 3, 8]), (16, [2, 1, 4]), (4, [40, 3, 70])])
 def test_hidden_positions_may_hold_anything(hq, toks, bound):
     """A position that a token does not see does not count, whatever its key and value hold; one that it sees does."""
@@ -259,7 +261,7 @@ def test_hidden_positions_may_hold_anything(hq, toks, bound):
                 assert not bool(torch.isfinite(out[first[2] + i:]).any())
 
 
-@pytest.mark.parametrize("bound", [0, 1000])
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
 @pytest.mark.parametrize("toks", [[1, 1, 1], [2] * 20, [60, 9]])
 def test_keys_that_are_no_numbers_reach_every_token_that_sees_them(toks, bound):
     from paper_2604_26334_amd import binding as B
@@ -275,7 +277,7 @@ def test_keys_that_are_no_numbers_reach_every_token_that_sees_them(toks, bound):
             assert bool(fine[:, :2].all()) and not bool(fine[:rows, 2:].any()) and bool(fine[rows:].all()), (where, lo, hi)
 
 
-@pytest.mark.parametrize("bound", [0, 1000])
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
 @pytest.mark.parametrize("toks", [[1, 2], [40, 3]])
 @pytest.mark.parametrize("scale", [-0.09, 0.0, 1.3])
 def test_attention_with_any_scale(toks, scale, bound):
@@ -284,7 +286,7 @@ def test_attention_with_any_scale(toks, scale, bound):
     _check_attend(a, B.page_attention(**a, scale=scale), first, full, toks, [333, 40], (0, 2), [99], "bf16", scale)
 
 
-@pytest.mark.parametrize("bound", [0, 1000])
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
 def test_attention_of_padded_batches_and_bounded_values(bound):
     """Rows behind the last sequence keep what they hold; lengths, offsets and groups out of range are bounded as documented."""
     from paper_2604_26334_amd import binding as B
