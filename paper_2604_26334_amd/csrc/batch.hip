@@ -24,26 +24,29 @@ constexpr int kMostPositions = 1 << 30;
 // of a token 4.4 us, 1000 sequences of up to 130 tokens 6.8.
 constexpr uint32_t kTableThreads = 512;
 
+// a + b, but at most `most` (each of the three 0 .. 2^30: two of them pass the signed range)
+__device__ __forceinline__ int capped(int a, int b, int most) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)most); }
+
 // running sums in front of each of v[0 .. n), ends at `most` (v: non-negative, at most `most` <= 2^30); v[n] becomes the total
 __device__ __forceinline__ void running(int *v, uint32_t n, int most, int *buf) {
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (n + kTableThreads - 1) / kTableThreads;
     const uint32_t lo = min(n, tid * per), hi = min(n, lo + per);
     int sum = 0;
-    for (uint32_t i = lo; i < hi; ++i) sum = min(sum + v[i], most);
+    for (uint32_t i = lo; i < hi; ++i) sum = capped(sum, v[i], most);
     int upto = sum;
     for (int o = 1; o < 64; o <<= 1) {
         const int t = __shfl_up(upto, o, 64);
-        if ((int)lane >= o) upto = min(upto + t, most);
+        if ((int)lane >= o) upto = capped(upto, t, most);
     }
     if (lane == 63) buf[wave] = upto;
     const int prior = __shfl_up(upto, 1, 64);
     int from = lane ? prior : 0;
     __syncthreads();
-    for (uint32_t w = 0; w < wave; ++w) from = min(from + buf[w], most);
+    for (uint32_t w = 0; w < wave; ++w) from = capped(from, buf[w], most);
     for (uint32_t i = lo; i < hi; ++i) {
         const int x = v[i];
         v[i] = from;
-        from = min(from + x, most);
+        from = capped(from, x, most);
     }
     if (tid == kTableThreads - 1) v[n] = from;
     __syncthreads();
@@ -60,7 +63,7 @@ __global__ __launch_bounds__(kTableThreads) void page_tables_kernel(ps_page_tabl
     running(first, n, (int)a.n_tokens, buf);
     for (uint32_t s = tid; s < n; s += kTableThreads) {
         const int64_t room = (int64_t)a.width << shift;
-        const int cached = clampi(a.cached[s], 0, kMostPositions), length = min(cached + (first[s + 1] - first[s]), kMostPositions);
+        const int cached = clampi(a.cached[s], 0, kMostPositions), length = capped(cached, first[s + 1] - first[s], kMostPositions);
         const int held = (int)((min((int64_t)cached, room) + page - 1) >> shift), full = (int)((min((int64_t)length, room) + page - 1) >> shift);
         need[s] = full - held;
         if (blockIdx.x == 0) { a.first[s] = first[s]; a.length[s] = length; }
