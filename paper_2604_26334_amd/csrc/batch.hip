@@ -546,9 +546,9 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
                 float mx = -INFINITY;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) mx = fmaxf(mx, fmaxf(fmaxf(S[t][g][0], S[t][g][1]), fmaxf(S[t][g][2], S[t][g][3])));
-                if (__any(mx > m_run[t] + slack)) {
+                if (__any(mx - m_run[t] > slack)) {            // (as `weigh` has it)
                     mx = row_max(mx);
-                    mx = mx > m_run[t] + slack ? mx : m_run[t];
+                    mx = mx - m_run[t] > slack ? mx : m_run[t];
                     const float resc = m_run[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[t] - mx) * c2);
                     m_run[t] = mx;
                     L[t] = L[t] * resc;

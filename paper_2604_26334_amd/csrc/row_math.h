@@ -99,9 +99,10 @@ __device__ __forceinline__ void weigh(const f4_t (&S)[NT][2], float (&m_run)[NT]
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         float mx = fmaxf(fmaxf(fmaxf(S[t][0][0], S[t][0][1]), fmaxf(S[t][0][2], S[t][0][3])), fmaxf(fmaxf(S[t][1][0], S[t][1][1]), fmaxf(S[t][1][2], S[t][1][3])));
-        if (__any(mx > m_run[t] + slack)) {
+        // (the difference is exact where it is close to the slack; a sum rounds, from 2^24 on past what fp16 holds)
+        if (__any(mx - m_run[t] > slack)) {
             mx = row_max(mx);
-            mx = mx > m_run[t] + slack ? mx : m_run[t];
+            mx = mx - m_run[t] > slack ? mx : m_run[t];
             const float resc = m_run[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[t] - mx) * c2);
             m_run[t] = mx;
             L[t] = L[t] * resc;

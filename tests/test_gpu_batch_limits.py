@@ -2,7 +2,10 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_drafts import DEV, _ints, _t
+from oracle import batch as O
+from oracle import drafts as D
+from tests import test_gpu_batch_weights as W
+from tests.test_gpu_drafts import DEV, _dt, _gen, _half_step, _ints, _np, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +41,51 @@ def test_tables_of_as_many_tokens_as_there_may_be(cached, new):
     assert np.array_equal(position[there].cpu().numpy(), j.astype(np.int32))
     entry = np.minimum(j // page, width - 1)
     assert np.array_equal(slot[there].cpu().numpy(), np.where(j // page < width, np.array(rows)[s, entry] * page + j % page, -1))
+
+
+# Scores of 2^29 and of 64 more: neighbours among fp32's numbers there, 8 nats apart at a scale of 1/8.  Sums of two products each, which are exact.
+LARGE = 2.0 ** 29
+
+
+def _large_scores(ty, n, t, d, heads):
+    """Queries [t, heads, d] and keys [n, d] of which the first 16 positions score 2^29, two in each later tile 2^29 + 64 and all others 0"""
+    torch = _t()
+    q, k = torch.zeros(t, heads, d, dtype=_dt(ty), device=DEV), torch.zeros(n, d, dtype=_dt(ty), device=DEV)
+    q[..., 0], q[..., 1] = 16384.0, 8.0
+    k[:16, 0] = 32768.0
+    for p in range(128, n, 16):
+        k[p + 2, 0], k[p + 2, 1] = 32768.0, 8.0
+    return q, k, torch.randn(n, d, generator=_gen(n), device=DEV).to(_dt(ty))
+
+
+def _near_weights(out, ref, v, ty):
+    """Half a step of the result, and of the weights against their sum (the spread of the values each); the exponential's argument, up to 12 in powers of two, and
+    the exponential in fp32: less than 2^-19 of a weight."""
+    off = np.abs(_np(out) - ref)
+    assert np.isfinite(_np(out)).all()
+    assert (off <= np.abs(ref) * _half_step(ty) + 2 * np.abs(_np(v)).max() * (_half_step(ty) + 2.0 ** -19)).all(), off.max()
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("bound", [0, 200000])
+@pytest.mark.parametrize("d,t,prefix", [(64, 1, 0), (128, 2, 0), (128, 20, 0), (64, 40, 0), (128, 1, 400), (64, 20, 400), (128, 40, 400)])
+def test_large_scores_next_to_each_other(ty, bound, d, t, prefix):
+    """Weights stay in their type's range however large the scores are.  512 heads, so that no run ends between the two kinds of keys."""
+    torch = _t()
+    q, k, v = _large_scores(ty, 400, t, d, 512)
+    k, v = (torch.cat((x, torch.zeros(t, d, dtype=x.dtype, device=DEV))) for x in (k, v))
+    ref = O.attention(_np(q[:, :1]), _np(k)[None], _np(v)[None], np.ones(400 + t, bool), 400, 0.125)
+    _near_weights(W._call(q, k, v, prefix, 0.125, bound), ref, v, ty)
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("d,t", [(64, 1), (128, 20), (64, 40)])
+def test_large_scores_next_to_each_other_behind_a_tree(ty, d, t):
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    q, k, v = _large_scores(ty, 400, t, d, 512)
+    new = torch.zeros(t, 1, d, dtype=_dt(ty), device=DEV)
+    out = B.tree_attention(q, new.expand(t, 512, d), new.expand(t, 512, d), k.expand(1, 512, 400, d), v.expand(1, 512, 400, d), _ints([0, t]), _ints([400]),
+                           _ints([-1] + [0] * (t - 1)), max_context=400, max_tree=t, scale=0.125)
+    ref = D.tree_attention(_np(q[:, :1]), _np(new), _np(new), _np(k)[None], _np(v)[None], 400, [-1] + [0] * (t - 1), 0.125)
+    _near_weights(out, ref, v, ty)
