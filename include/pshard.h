@@ -818,7 +818,7 @@ int32_t ps_page_append(const ps_page_append_args *args, void *stream);
  *  [n_pages][n_kv_heads][page][head_dim], all with the strides below (any order of pages, heads and rows); every address and
  *  stride in bytes a multiple of 16, a page's rows (and 32 rows) span less than 4 GiB, pages lie less than 64 GiB apart.  max_length <= width * page, max_prefix <= prefix_width * page
  *  and max_tokens: bounds on length, prefix_length and a sequence's tokens (what lies beyond is left out: tokens beyond max_tokens
- *  are not written); work is dealt out by them.  n_prefix <= 4096, n_seq <= 65535; out may not overlap any input.
+ *  are not written); work and workspace are dealt out by them, and rows of the token arrays beyond n_seq * max_tokens cost nothing.  n_prefix <= 4096, n_seq <= 65535; out may not overlap any input.
  * Scores, softmax and sums in fp32; the weights of the value product are rounded to `type`, and their sum is taken of the rounded
  * ones (fp16: in steps of at least 2^-34 of the largest).  A call repeated gives the same bits; under other bounds or batches sums are
  * taken in other runs.  ps_page_attention_workspace: bytes for these arguments (a function of sizes alone); 256-byte aligned. */

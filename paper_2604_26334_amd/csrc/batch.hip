@@ -151,15 +151,40 @@ struct PageDeal {
     uint32_t psplit, plen;       // runs of a prefix, positions of a run (shared)
     uint32_t osplit, olen;       // runs of own positions (shared), or of a sequence's tiles (nt) or steps
     uint32_t direct;             // no records: the result itself
+    // Tokens that may be answered, for each of which there is a place for records.  The arrays may have room for more (rows behind the last sequence, tokens
+    // beyond max_tokens): by_seq, places are then numbered by sequence and number in it, and a prefix's workgroups, as many as the tokens that may be answered fill,
+    // look for blocks from `blocks` on, up to `most`.
+    uint32_t tokens, by_seq, most;
 };
 template <int D, int NT> constexpr uint32_t few_lds() { return std::max<uint32_t>(4 * kTile * D * 2, 4 * NT * 16 * (D + 4) * 4 + 4 * NT * 16 * 2 * 4) + 16; }
 template <int D> constexpr uint32_t many_lds() { return 2 * 2 * kStep * D * 2 + 16; }
 
-struct RowSet { int token0; uint32_t rows, group; };             // rows of consecutive tokens, `group` query heads each
+struct RowSet {                                                  // rows of consecutive tokens, `group` query heads each
+    int token0;
+    uint32_t rows, group;
+    uint32_t seq0, seqs;                                         // whose tokens they are (by_seq, of a group)
+};
 struct Span {                                                    // positions that one table names
     const int32_t *table;
     int entries, len;                                            // entries of the table, positions
 };
+
+// By sequence and number in it, the place of a token's records; -1: it has none.  (Below n_seq * max_tokens, whatever `first` holds)
+__device__ __forceinline__ int place_of(const ps_page_attention_args &a, const RowSet &set, int token) {
+    uint32_t s = set.seq0;                    // the last one that begins at or in front of the token: one with tokens
+    for (uint32_t n = set.seqs; n > 1;) {
+        const uint32_t half = n / 2;
+        const bool behind = clampi(a.first[s + half], 0, (int)a.n_tokens) <= token;
+        s = behind ? s + half : s;
+        n = behind ? n - half : half;
+    }
+    const int i = token - clampi(a.first[s], 0, (int)a.n_tokens);
+    return i >= 0 && (uint32_t)i < a.max_tokens ? (int)(s * a.max_tokens) + i : -1;
+}
+// The records as those of a sequence's tokens are found in them: token row0's at the sequence's first place
+__device__ __forceinline__ float *records_of(const ps_page_attention_args &a, const PageDeal &d, uint32_t s, int row0, uint32_t floats, float *part) {
+    return part + ((int64_t)s * a.max_tokens - row0) * a.n_q_heads * (int64_t)(d.psplit + d.osplit) * floats;
+}
 
 // page numbers of a table, 64 at a time, one a lane; -1: none
 struct PageWindow {
@@ -201,8 +226,8 @@ __device__ __forceinline__ void add_wild(const ps_page_attention_args &a, const 
 }
 
 // Rows of `set` (up to NT x 16) over tiles lo .. hi - 1 of a span's positions up to `end`, of which row rho sees those below limit0 + rho / group; `window` holds
-// the table's entries from the wave's first tile on.  kBoth: over tiles of `prefix`, which every row sees, and then those of the span.
-template <typename T, int D, int NT, bool kBoth>
+// the table's entries from the wave's first tile on.  kBoth: over tiles of `prefix`, which every row sees, and then those of the span.  kSeek: records by place_of.
+template <typename T, int D, int NT, bool kBoth, bool kSeek = false>
 __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const RowSet &set, const Span &prefix, const Span &span, uint32_t shift, uint32_t hk, int lo, int hi, int end,
                                          int limit0, PageWindow window, uint32_t records, uint32_t z, float *part, unsigned char *lds) {
     using M = Mfma<T>;
@@ -364,7 +389,9 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
         if (*wild) add_wild<T>(a, span, shift, hk, max((lo - np) * (int)kTile, wild0), min(min((hi - np) * (int)kTile, end), limit0 + (int)tok), d0, o);
         const size_t token = (size_t)set.token0 + tok;
         if (records) {
-            float *dst = part + ((token * a.n_q_heads + h) * records + z) * OP;
+            const int place = kSeek ? place_of(a, set, (int)token) : 0;
+            if (place < 0) continue;
+            float *dst = part + (((kSeek ? (size_t)place : token) * a.n_q_heads + h) * records + z) * OP;
             *reinterpret_cast<f4_t *>(dst + d0) = f4_t{o[0], o[1], o[2], o[3]};
             if (d0 == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(mx * c2, l);
         } else {
@@ -377,8 +404,8 @@ __device__ __forceinline__ void rows_few(const ps_page_attention_args &a, const 
 }
 
 // Rows row0 .. row0 + 127 of `set` over steps lo .. hi - 1: those of `prefix` (which every row sees), then those of `own` (row rho sees
-// positions below limit0 + rho / group).  kOwn false: a prefix alone.
-template <typename T, int D, bool kOwn>
+// positions below limit0 + rho / group).  kOwn false: a prefix alone.  kSeek: records by place_of.
+template <typename T, int D, bool kOwn, bool kSeek = false>
 __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const RowSet &set, uint32_t row0, const Span &prefix, const Span &own, uint32_t shift, uint32_t hk,
                                           int lo, int hi, int limit0, uint32_t records, uint32_t z, float *part, unsigned char *lds) {
     using M = Mfma<T>;
@@ -596,7 +623,9 @@ __device__ __forceinline__ void rows_many(const ps_page_attention_args &a, const
             }
         }
         if (records) {
-            float *dst = part + ((token * a.n_q_heads + head[t]) * records + z) * OP;
+            const int place = kSeek ? place_of(a, set, (int)token) : 0;
+            if (place < 0) continue;
+            float *dst = part + (((kSeek ? (size_t)place : token) * a.n_q_heads + head[t]) * records + z) * OP;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4_t *>(dst + 16 * dt + 4 * c) = O[t][dt];
             if (c == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(m_run[t] * c2, L[t][0]);
@@ -657,16 +686,18 @@ __device__ __forceinline__ GroupBlock group_block(const ps_page_attention_args &
         if (past) {
             const int at = __ffsll((unsigned long long)past) - 1;
             const uint32_t before = base + __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at);
-            return {{__builtin_amdgcn_readlane(t0, at), (uint32_t)__builtin_amdgcn_readlane(n, at) * G, G}, p0 + at, flat - before};
+            return {{__builtin_amdgcn_readlane(t0, at), (uint32_t)__builtin_amdgcn_readlane(n, at) * G, G, 0, 0}, p0 + at, flat - before};
         }
         base += __builtin_amdgcn_readlane(upto, 63);
     }
-    return {{0, 0, G}, 0, 0};
+    return {{0, 0, G, 0, 0}, 0, 0};
 }
 
 extern __shared__ u4_t page_lds[];
 
-template <typename T, int D, int NT>
+// kSeek, here and below: where the arrays have room for more tokens than may be answered (what it takes costs registers in the others: here 256 for 241, and the
+// prompts' blocks 205 us for 200)
+template <typename T, int D, int NT, bool kSeek>
 __global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, uint32_t prefix8, float *part) {
     unsigned char *const lds = reinterpret_cast<unsigned char *>(page_lds);
     const uint32_t records = d.direct ? 0 : d.psplit + d.osplit, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -676,17 +707,29 @@ __global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_a
         // blocks of the same positions follow one another on one XCD, whose L2 they share
         const uint32_t unit = run / d.blocks * 8 + blockIdx.x % 8;
         if (unit >= a.n_kv_heads * d.psplit) return;
-        const GroupBlock g = group_block(a, run % d.blocks);
-        if (g.set.rows == 0) return;
-        const uint32_t z = unit % d.psplit, hk = unit / d.psplit;
-        const int len = prefix_length_of(a, g.prefix), lo = (int)min((uint64_t)z * d.plen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.plen, (uint64_t)len);
-        if (lo >= hi) return;
-        const Span span{a.prefix_table + g.prefix * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), len};
-        if (g.set.rows <= NT * 16) {
-            PageWindow window;
-            window.fill(span, (lo + (int)(wave * kTile)) >> shift, a.n_pages);
-            rows_few<T, D, NT, false>(a, g.set, Span{nullptr, 0, 0}, span, shift, hk, lo / (int)kTile, (hi + (int)kTile - 1) / (int)kTile, hi, hi, window, records, z, part, lds);
-        } else rows_many<T, D, false>(a, g.set, g.block * 128, Span{span.table, span.entries, hi}, Span{nullptr, 0, 0}, shift, hk, lo / (int)kStep, (hi + (int)kStep - 1) / (int)kStep, 0, records, z, part, lds);
+        for (uint32_t block = run % d.blocks;;) {
+            GroupBlock g = group_block(a, block);
+            if (g.set.rows == 0) return;
+            if (kSeek) {
+                g.set.seq0 = clampi(a.group_first[g.prefix], 0, (int)a.n_seq - 1);
+                g.set.seqs = max(1, clampi(a.group_first[g.prefix + 1], 0, (int)a.n_seq) - (int)g.set.seq0);
+            }
+            const uint32_t z = unit % d.psplit, hk = unit / d.psplit;
+            const int len = prefix_length_of(a, g.prefix), lo = (int)min((uint64_t)z * d.plen, (uint64_t)len), hi = (int)min((uint64_t)lo + d.plen, (uint64_t)len);
+            if (!kSeek && lo >= hi) return;
+            if (lo < hi) {
+                const Span span{a.prefix_table + g.prefix * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), len};
+                if (g.set.rows <= NT * 16) {
+                    PageWindow window;
+                    window.fill(span, (lo + (int)(wave * kTile)) >> shift, a.n_pages);
+                    rows_few<T, D, NT, false, kSeek>(a, g.set, Span{nullptr, 0, 0}, span, shift, hk, lo / (int)kTile, (hi + (int)kTile - 1) / (int)kTile, hi, hi, window, records, z, part, lds);
+                } else rows_many<T, D, false, kSeek>(a, g.set, g.block * 128, Span{span.table, span.entries, hi}, Span{nullptr, 0, 0}, shift, hk, lo / (int)kStep,
+                                                     (hi + (int)kStep - 1) / (int)kStep, 0, records, z, part, lds);
+            }
+            block += d.blocks;
+            if (!kSeek || block >= d.most) return;
+            __syncthreads();            // (the next block's rows come to lie where this one's results were put together)
+        }
     } else {
         const uint32_t unit = (run - prefix8) * 8 + blockIdx.x % 8, z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads;
         if (s >= a.n_seq) return;
@@ -698,15 +741,15 @@ __global__ __launch_bounds__(256, 2) void page_shared_kernel(ps_page_attention_a
         if (t.answered == 0 || (lo >= hi && records)) return;
         const uint32_t G = a.n_q_heads / a.n_kv_heads;
         const Span own{a.table + s * a.table_seq, (int)min(a.width, 0x7FFFFFFFu), len};
-        rows_few<T, D, NT, false>(a, RowSet{t.row0, t.answered * G, G}, Span{nullptr, 0, 0}, own, shift, hk, lo / (int)kTile, (hi + (int)kTile - 1) / (int)kTile, hi, len - t.n + 1, window, records,
-                                  d.psplit + z, part, lds);
+        rows_few<T, D, NT, false>(a, RowSet{t.row0, t.answered * G, G, 0, 0}, Span{nullptr, 0, 0}, own, shift, hk, lo / (int)kTile, (hi + (int)kTile - 1) / (int)kTile, hi, len - t.n + 1, window, records,
+                                  d.psplit + z, kSeek ? records_of(a, d, s, t.row0, D + 4, part) : part, lds);
     }
 }
 
 // Few rows a sequence and a short prefix: the sequence's own workgroups walk its tiles, the prefix's first.  Where 128 rows' places are mostly empty, this
 // kernel's reads are ahead by a tile in every wave; latencies bound it (3 sequences, 4 / 2 heads of 128, 77 + 40 positions: 8.5 us on the GPU, as a
 // block of 128 rows 13.6), then memory (16 sequences, 32 / 8 heads of 128, 500 + 3000: 30.7 us a call, 4.5 TB/s, for 40.8).
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool kSeek>
 __global__ __launch_bounds__(256, 2) void page_few_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, float *part) {
     const uint32_t unit = blockIdx.x, z = unit % d.osplit, hk = unit / d.osplit % a.n_kv_heads, s = unit / d.osplit / a.n_kv_heads, G = a.n_q_heads / a.n_kv_heads;
     const SeqTokens t = tokens_of(a, s);
@@ -717,11 +760,11 @@ __global__ __launch_bounds__(256, 2) void page_few_kernel(ps_page_attention_args
     const int tiles = (prefix.len + (int)kTile - 1) / (int)kTile + (own.len + (int)kTile - 1) / (int)kTile;
     const int lo = (int)min((uint64_t)z * d.olen, (uint64_t)tiles), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)tiles);
     if (lo >= hi && !d.direct) return;
-    rows_few<T, D, NT, true>(a, RowSet{t.row0, t.answered * G, G}, prefix, own, shift, hk, lo, hi, own.len, own.len - t.n + 1, PageWindow{-1, 0}, d.direct ? 0 : d.osplit, z, part,
+    rows_few<T, D, NT, true>(a, RowSet{t.row0, t.answered * G, G, 0, 0}, prefix, own, shift, hk, lo, hi, own.len, own.len - t.n + 1, PageWindow{-1, 0}, d.direct ? 0 : d.osplit, z, kSeek ? records_of(a, d, s, t.row0, D + 4, part) : part,
                              reinterpret_cast<unsigned char *>(page_lds));
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kSeek>
 __global__ __launch_bounds__(256, 2) void page_rows_kernel(ps_page_attention_args a, PageDeal d, uint32_t shift, float *part) {
     unsigned char *const lds = reinterpret_cast<unsigned char *>(page_lds);
     const uint32_t units = a.n_seq * a.n_kv_heads * d.osplit;
@@ -733,13 +776,13 @@ __global__ __launch_bounds__(256, 2) void page_rows_kernel(ps_page_attention_arg
     const Behind p = prefix_behind(a, s);
     if (block * 128 >= t.answered * G) return;
     const Span prefix = p.prefix < 0 ? Span{nullptr, 0, 0} : Span{a.prefix_table + p.prefix * a.prefix_seq, (int)min(a.prefix_width, 0x7FFFFFFFu), p.len};
-    const RowSet set{t.row0, t.answered * G, G};
+    const RowSet set{t.row0, t.answered * G, G, 0, 0};
     const int np = (prefix.len + (int)kStep - 1) / (int)kStep, limit0 = own.len - t.n + 1;
     const int last = min(own.len, limit0 + (int)(min(block * 128 + 127, set.rows - 1) / G));
     const int steps = np + (max(last, 0) + (int)kStep - 1) / (int)kStep;
     const int lo = (int)min((uint64_t)z * d.olen, (uint64_t)steps), hi = (int)min((uint64_t)lo + d.olen, (uint64_t)steps);
     // (a run that none of the block's rows sees leaves records of nothing)
-    rows_many<T, D, true>(a, set, block * 128, prefix, own, shift, hk, lo, hi, limit0, d.direct ? 0 : d.osplit, z, part, lds);
+    rows_many<T, D, true>(a, set, block * 128, prefix, own, shift, hk, lo, hi, limit0, d.direct ? 0 : d.osplit, z, kSeek ? records_of(a, d, s, t.row0, D + 4, part) : part, lds);
 }
 
 // D / 4 lanes per (token, query head) put the records of its prefix's and of its sequence's runs together, in their order: value sums, then maximum
@@ -756,8 +799,8 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
     const uint32_t np = d.shared && plen ? (plen + d.plen - 1) / d.plen : 0;
     const uint32_t unit = d.nt ? kTile : kStep, positions = d.shared ? len : (plen + unit - 1) / unit + (len + unit - 1) / unit;
     const uint32_t n = np + (positions + d.olen - 1) / d.olen;
-    const size_t token = (size_t)t.row0 + i;
-    const float *r0 = part + (token * a.n_q_heads + h) * (d.psplit + d.osplit) * OP;
+    const size_t token = (size_t)t.row0 + i, place = d.by_seq ? (size_t)s * a.max_tokens + i : token;
+    const float *r0 = part + (place * a.n_q_heads + h) * (d.psplit + d.osplit) * OP;
     float mx = -INFINITY, l = 0.f;
     f4_t o{0.f, 0.f, 0.f, 0.f};
     for (uint32_t z0 = 0; z0 < n; z0 += 8) {
@@ -1580,6 +1623,9 @@ PageDeal page_deal(const ps_page_attention_args &a) {
     // 500 + 500 positions 16.5 us for 25.8, 1000 + 500 19.3 for 22.3, 2000 + 100 21.8 for 20.6; 64 sequences, 250 + 250 18.3 for 21.2, 1000 + 500 35.5 for 27.9
     const bool small = prefixes && (uint64_t)a.n_seq * a.n_kv_heads * a.max_prefix <= 196608;
     d.shared = rows <= kFewRows && !small;
+    // (1024 rows for 64 sequences of a token each, 32 / 8 heads behind 32761: dealt out by 1024 the prefix was one run of 16 workgroups, 620 us for 109)
+    d.tokens = (uint32_t)std::min<uint64_t>(a.n_tokens, a.n_seq * tokens);
+    d.by_seq = d.tokens < a.n_tokens;
     auto cut = [](uint64_t units, uint64_t want, uint64_t whole, uint64_t least, uint64_t multiple, uint32_t *n, uint32_t *len) {
         const uint64_t most = std::max<uint64_t>(1, whole / least), runs = std::min(std::max<uint64_t>(1, want / std::max<uint64_t>(1, units)), most);
         *len = (uint32_t)std::max<uint64_t>(multiple, ((whole + runs - 1) / runs + multiple - 1) / multiple * multiple);
@@ -1587,9 +1633,11 @@ PageDeal page_deal(const ps_page_attention_args &a) {
     };
     if (d.shared) {
         d.nt = rows <= 16 ? 1 : 2;
-        d.blocks = prefixes ? (uint32_t)(((uint64_t)a.n_tokens * G + 127ull * a.n_prefix) / 128) : 0;
+        auto blocks = [&](uint64_t n) { return prefixes ? (uint32_t)((n * G + 127ull * a.n_prefix) / 128) : 0; };
+        d.blocks = blocks(d.tokens);
+        d.most = blocks(a.n_tokens);
         // about how long each part takes by itself, at 700 TFLOP/s and 5 TB/s
-        const double prefix_us = (double)a.n_tokens * a.n_q_heads * a.max_prefix * a.head_dim * 4 / 700e6, own_us = (double)a.n_seq * a.n_kv_heads * a.max_length * a.head_dim * 4 / 5e6;
+        const double prefix_us = (double)d.tokens * a.n_q_heads * a.max_prefix * a.head_dim * 4 / 700e6, own_us = (double)a.n_seq * a.n_kv_heads * a.max_length * a.head_dim * 4 / 5e6;
         if (prefixes) cut((uint64_t)d.blocks * a.n_kv_heads, own_us * 4 > prefix_us ? 256 : 512, a.max_prefix, 256, kStep, &d.psplit, &d.plen);
         cut((uint64_t)a.n_seq * a.n_kv_heads, a.n_seq > 1 ? 512 : 1024, a.max_length, 128, 4 * kTile, &d.osplit, &d.olen);
         d.direct = d.psplit == 0 && d.osplit == 1;
@@ -1610,7 +1658,7 @@ PageDeal page_deal(const ps_page_attention_args &a) {
     return d;
 }
 uint64_t page_workspace(const ps_page_attention_args &a, const PageDeal &d) {
-    return d.direct ? 0 : align_up((uint64_t)a.n_tokens * a.n_q_heads * (d.psplit + d.osplit) * (a.head_dim + 4) * 4, kAlign);
+    return d.direct ? 0 : align_up((uint64_t)d.tokens * a.n_q_heads * (d.psplit + d.osplit) * (a.head_dim + 4) * 4, kAlign);
 }
 // workgroups of the merge for a token
 uint32_t merge_groups(const ps_page_attention_args &a) { const uint32_t heads = 1024 / a.head_dim; return (a.n_q_heads + heads - 1) / heads; }
@@ -1632,31 +1680,39 @@ hipError_t take_lds(K kernel, uint32_t lds, std::atomic<uint64_t> &done) {
     if (e == hipSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
     return e;
 }
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool kSeek>
 hipError_t launch_shared(const ps_page_attention_args &a, const PageDeal &d, uint32_t prefix8, uint32_t own8, float *part, hipStream_t st) {
     static std::atomic<uint64_t> done;
     constexpr uint32_t lds = std::max(few_lds<D, NT>(), many_lds<D>());
-    const hipError_t e = take_lds(&page_shared_kernel<T, D, NT>, lds, done);
+    const hipError_t e = take_lds(&page_shared_kernel<T, D, NT, kSeek>, lds, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((page_shared_kernel<T, D, NT>), dim3((prefix8 + own8) * 8), dim3(256), lds, st, a, d, log2_of(a.page), prefix8, part);
+    hipLaunchKernelGGL((page_shared_kernel<T, D, NT, kSeek>), dim3((prefix8 + own8) * 8), dim3(256), lds, st, a, d, log2_of(a.page), prefix8, part);
     return hipGetLastError();
 }
-template <typename T, int D>
+template <typename T, int D, bool kSeek>
 hipError_t launch_rows(const ps_page_attention_args &a, const PageDeal &d, uint32_t own8, float *part, hipStream_t st) {
     static std::atomic<uint64_t> done;
-    const hipError_t e = take_lds(&page_rows_kernel<T, D>, many_lds<D>(), done);
+    const hipError_t e = take_lds(&page_rows_kernel<T, D, kSeek>, many_lds<D>(), done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((page_rows_kernel<T, D>), dim3(own8 * 8), dim3(256), many_lds<D>(), st, a, d, log2_of(a.page), part);
+    hipLaunchKernelGGL((page_rows_kernel<T, D, kSeek>), dim3(own8 * 8), dim3(256), many_lds<D>(), st, a, d, log2_of(a.page), part);
     return hipGetLastError();
 }
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool kSeek>
 hipError_t launch_few(const ps_page_attention_args &a, const PageDeal &d, float *part, hipStream_t st) {
     static std::atomic<uint64_t> done;
     constexpr uint32_t lds = few_lds<D, NT>();
-    const hipError_t e = take_lds(&page_few_kernel<T, D, NT>, lds, done);
+    const hipError_t e = take_lds(&page_few_kernel<T, D, NT, kSeek>, lds, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((page_few_kernel<T, D, NT>), dim3(a.n_seq * a.n_kv_heads * d.osplit), dim3(256), lds, st, a, d, log2_of(a.page), part);
+    hipLaunchKernelGGL((page_few_kernel<T, D, NT, kSeek>), dim3(a.n_seq * a.n_kv_heads * d.osplit), dim3(256), lds, st, a, d, log2_of(a.page), part);
     return hipGetLastError();
+}
+template <typename T, int D, bool kSeek>
+hipError_t launch_walk(const ps_page_attention_args &a, const PageDeal &d, float *part, hipStream_t st) {
+    uint64_t prefix8, own8;
+    page_groups(a, d, &prefix8, &own8);
+    if (d.shared) return (d.nt == 1 ? launch_shared<T, D, 1, kSeek> : launch_shared<T, D, 2, kSeek>)(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st);
+    if (d.nt) return (d.nt == 1 ? launch_few<T, D, 1, kSeek> : launch_few<T, D, 2, kSeek>)(a, d, part, st);
+    return launch_rows<T, D, kSeek>(a, d, (uint32_t)own8, part, st);
 }
 template <typename T, int D>
 hipError_t launch_page_attention(const ps_page_attention_args &call, float *part, hipStream_t st) {
@@ -1667,13 +1723,7 @@ hipError_t launch_page_attention(const ps_page_attention_args &call, float *part
     if (a.n_pages == 0) a.max_length = a.max_prefix = 0;
     if (a.max_length == 0) a.width = 0;
     if (a.max_prefix == 0) a.prefix_width = 0;
-    uint64_t prefix8, own8;
-    page_groups(a, d, &prefix8, &own8);
-    const hipError_t e = !d.shared && d.nt == 1 ? launch_few<T, D, 1>(a, d, part, st)
-                         : !d.shared && d.nt == 2 ? launch_few<T, D, 2>(a, d, part, st)
-                         : !d.shared ? launch_rows<T, D>(a, d, (uint32_t)own8, part, st)
-                         : d.nt == 1 ? launch_shared<T, D, 1>(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st)
-                                     : launch_shared<T, D, 2>(a, d, (uint32_t)prefix8, (uint32_t)own8, part, st);
+    const hipError_t e = d.by_seq && !d.direct ? launch_walk<T, D, true>(a, d, part, st) : launch_walk<T, D, false>(a, d, part, st);
     if (e != hipSuccess || d.direct) return e;
     hipLaunchKernelGGL((page_merge_kernel<T, D>), dim3(a.n_seq * a.max_tokens * merge_groups(a)), dim3(256), 0, st, a, d, part);
     return hipGetLastError();

@@ -4,8 +4,9 @@ import pytest
 
 from oracle import batch as O
 from oracle import drafts as D
+from tests import test_gpu_batch as T
 from tests import test_gpu_batch_weights as W
-from tests.test_gpu_drafts import DEV, _dt, _gen, _half_step, _ints, _np, _t
+from tests.test_gpu_drafts import DEV, _dt, _gen, _half_step, _ints, _np, _same_bits, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +90,61 @@ def test_large_scores_next_to_each_other_behind_a_tree(ty, d, t):
                            _ints([-1] + [0] * (t - 1)), max_context=400, max_tree=t, scale=0.125)
     ref = D.tree_attention(_np(q[:, :1]), _np(new), _np(new), _np(k)[None], _np(v)[None], 400, [-1] + [0] * (t - 1), 0.125)
     _near_weights(out, ref, v, ty)
+
+
+# sequences' tokens, own lengths, groups, prefixes
+ROOM = [([1] * 64, [1 + 7 * i for i in range(64)], (0, 64), [900]), ([2] * 30, [2 + 31 * i for i in range(30)], (0, 9, 25), [300, 77]), ([1], [5000], (), ()),
+        ([4] * 9, [300] * 9, (0, 9), [200]), ([40] * 3, [40, 700, 300], (0, 2), [130]), ([1] * 5, [900] * 5, (), ())]
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
+@pytest.mark.parametrize("case", range(len(ROOM)))
+def test_room_for_more_tokens_changes_nothing(ty, bound, case):
+    """Rows behind the last sequence, however many: the same bits, in the same workspace, and these rows as they were."""
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    toks, lens, groups, plens = ROOM[case]
+    a, first, full = T._attend_case(ty, 128, 8, 2, 16, toks, lens, groups, plens, case, bound=bound)
+    want = B.page_attention(**a)
+    T._check_attend(a, want, first, full, toks, lens, groups, plens, ty)
+    n = sum(toks)
+    for pad, at in ((1, 0), (1000, 0), (1000, 37), (20000, 19999)):             # (the first sequence may begin anywhere)
+        q = torch.full((n + pad, 8, 128), float("nan"), dtype=a["q"].dtype, device=DEV)
+        q[at:at + n] = a["q"]
+        out, work = torch.full_like(q, 3.0), torch.full((1 << 26,), 255, dtype=torch.uint8, device=DEV)
+        B.page_attention(**dict(a, q=q, first=a["first"] + at), out=out, workspace=work)
+        assert _same_bits(out[at:at + n], want), (pad, at)
+        assert bool((out[:at] == 3).all()) and bool((out[at + n:] == 3).all())
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
+@pytest.mark.parametrize("hq,most,groups,plens", [(8, 1, (0, 40), [500]), (8, 3, (0, 13, 37), [500, 70]), (4, 2, (3, 4, 20, 40), [90, 16, 333]), (16, 4, (0, 40), [300]), (64, 1, (0, 20), [200]),
+                                                  (8, 8, (0, 40), [400]), (8, 12, (0, 40), [100]), (8, 1, (), ())])
+def test_sequences_of_more_tokens_than_are_answered(ty, bound, hq, most, groups, plens):
+    """More tokens in the arrays than sequences may have: the first max_tokens of each are answered, the others keep what they hold, and nothing behind the
+    workspace that was asked for is written."""
+    import ctypes as C
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    toks = [(5, 1, 17, 0, 2, 9, 3)[i % 7] for i in range(40)]
+    lens = [t + i * 5 for i, t in enumerate(toks)]
+    a, first, full = T._attend_case(ty, 64, hq, 2, 16, toks, lens, groups, plens, most, bound=bound)
+    want = B.page_attention(**a)
+    T._check_attend(a, want, first, full, toks, lens, groups, plens, ty)
+    p = len(plens)
+    sizes = B.ps_page_attention_args(type=0 if ty == "f16" else 1, n_seq=40, n_tokens=sum(toks), n_q_heads=hq, n_kv_heads=2, head_dim=64, page=16, n_pages=a["k_pages"].shape[0],
+                                     width=a["table"].shape[1], n_prefix=p, prefix_width=a["prefix_table"].shape[1] if p else 0, max_length=a["max_length"], max_prefix=a.get("max_prefix", 0),
+                                     max_tokens=most, scale=0.125)
+    need = C.c_uint64()
+    assert B.lib().ps_page_attention_workspace(C.byref(sizes), C.byref(need)) == 0
+    work = torch.full((need.value + (1 << 24),), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full_like(want, 3.0)
+    B.page_attention(**dict(a, max_tokens=most), out=out, workspace=work)
+    assert bool((work[need.value:] == 255).all())
+    for s, t in enumerate(toks):
+        kept = slice(first[s] + min(t, most), first[s + 1])
+        assert bool((out[kept] == 3).all()), s
+        out[kept] = want[kept]
+    T._check_attend(a, out, first, full, toks, lens, groups, plens, ty)
