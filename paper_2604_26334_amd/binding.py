@@ -1063,12 +1063,12 @@ def page_append(k, v, k_pages, v_pages, slot):
 
 
 def page_attention(q, k_pages, v_pages, first, length, table, max_length, max_tokens, group_first=None, prefix_length=None, prefix_table=None,
-                   max_prefix=0, scale=None, out=None, workspace=None):
+                   max_prefix=None, scale=None, out=None, workspace=None):
     """ps_page_attention.  q [tokens, q heads, dim], k_pages, v_pages [pages, kv heads, page, dim] of one type (last dimension contiguous;
     addresses and other strides multiples of 16 bytes); first int32 [sequences + 1], length int32 [sequences], table int32 [sequences, width];
     group_first int32 [prefixes + 1], prefix_length int32 [prefixes], prefix_table int32 [prefixes, width], or all three None.  max_length,
-    max_prefix, max_tokens: bounds on length, prefix_length and the tokens of a sequence.  Returns out [tokens, q heads, dim]: the given
-    tensor, or a new one (whose rows of no sequence hold anything)."""
+    max_prefix, max_tokens: bounds on length, prefix_length and the tokens of a sequence (max_prefix None: what prefix_table has room for).
+    Returns out [tokens, q heads, dim]: the given tensor, or a new one (whose rows of no sequence hold anything)."""
     import torch
     _want(q.dim() == 3 and k_pages.dim() == 4 and table.dim() == 2, "q is [tokens, heads, dim], pages [pages, heads, page, dim], table [sequences, width]")
     n, hq, d = q.shape
@@ -1086,6 +1086,8 @@ def page_attention(q, k_pages, v_pages, first, length, table, max_length, max_to
         p, pw = prefix_table.shape
         _same("prefix_table", prefix_table, (p, pw), i32, dev)
         ps = _rows("prefix_table", prefix_table)[0]
+    if max_prefix is None:
+        max_prefix = min(pw * page, 1 << 30)
     out = _like("out", out, q)
     sq, so, ck, cv = _rows("q", q), _rows("out", out), _rows("k_pages", k_pages), _rows("v_pages", v_pages)
     a = ps_page_attention_args(
