@@ -846,7 +846,7 @@ int32_t ps_page_attention(const ps_page_attention_args *args, void *workspace, u
  * weights.  T = temperature[row] (NULL: 1); T <= 0 or not a number: the first entry of the order.  top_k, top_p and min_p may be NULL
  * (all kept); top_p or min_p that is no number keeps all.  u in [0, 1): below counts as 0, anything else as 1 - 2^-24.  A logit that is no number counts as -inf, +inf as the largest
  * finite number; a row of -inf alone gives token -1, of none kept.
- * Weights are right to 2e-11 of each (those below e^-24 of the largest to 2^-31 of e^-24) and added as whole numbers, runs of them in 64 bits
+ * Weights are right to 2e-11 of each (those below e^-24 of the largest to 2^-22 of e^-24, 9e-18 of the largest) and added as whole numbers, runs of them in 64 bits
  * and always alike, so a row's result is the same in any call, batch, stride or type that holds its values.
  *  type F16, BF16 or F32; rows [n_rows][vocab], logits_row elements apart, alignment of an element is enough; vocab 1 .. 2^24;
  *  n_rows <= 65535.  token, kept [n_rows]; kept (n of each row) may be NULL.  A stack's next tokens: over the buffer of

@@ -877,8 +877,9 @@ __device__ __forceinline__ float value_in(unsigned long long entry) { return val
 
 // How far an entry lies behind the largest one, in bins: the nearest whole number and what remains, by adding 1.5 2^52 (a conversion takes as long as four
 // operations).  Its weight, relative to that of its bin's middle, in whole numbers of 2^-35: exp(-rest / 85.3) as a polynomial of degree 4 (off by
-// 6e-14 of it, the rounding by 1.5e-11).  In the last bin, which is all from 24 nats on, by the 32-bit exponential in steps of 2^-31: all of it weighs
-// at most e^-24 of the largest entry for each of its own.
+// 6e-14 of it, the rounding by 1.5e-11).  In the last bin, which is all from 24 nats on, by the 32-bit exponential in steps of 2^-31: right to 2^-22 of e^-24
+// (a step of the exponential and of its argument, 1.8e-7 at most), 9e-18 of the largest entry's weight for each, where 2^24 of them would be 1.5e-10 and the nearest entries' own
+// rounding is 1.5e-11.  In 64 bits, or as the product of two table entries, 256 rows of 128256 take 43 and 6 us more.
 constexpr double kWhole = 6755399441055744.0;
 struct Place {
     int n;

@@ -148,3 +148,23 @@ def test_sequences_of_more_tokens_than_are_answered(ty, bound, hq, most, groups,
         assert bool((out[kept] == 3).all()), s
         out[kept] = want[kept]
     T._check_attend(a, out, first, full, toks, lens, groups, plens, ty)
+
+
+@pytest.mark.parametrize("back", [24.0, 24.3, 25.0, 26.5])
+def test_weights_far_behind_the_largest(back):
+    """One entry at 0 (its weight is exact) and 2^22 - 1 alike `back` nats behind, weights of which may be off by 2^-22 e^-24: top-p keeps the first r with
+    1 + (r - 1) w >= p (1 + N w), that is p N - (1 - p) / w behind the first; and an entry is drawn where its share lies."""
+    from paper_2604_26334_amd import binding as B
+    torch, V = _t(), 1 << 22
+    x = torch.full((1, V), -back, device=DEV)
+    x[0, 12345] = 0.0
+    N, w, e = V - 1, float(np.exp(-float(np.float32(back)))), 2.0 ** -22 * float(np.exp(-24.0))
+    for part in (0.25, 0.5, 0.9):
+        p = float(np.float32(1 - part * N * w))
+        token, kept = B.sample(x, torch.zeros(1, device=DEV), top_p=torch.tensor([p], device=DEV))
+        lo, hi = (1 + np.ceil(p * N - (1 - p) / (w + d)) for d in (-e, e))
+        assert int(token) == 12345 and lo - 1 <= int(kept) <= hi + 1, (part, lo, int(kept), hi)
+    u = float(np.float32(1 - 0.5 * N * w))
+    token, kept = B.sample(x, torch.tensor([u], device=DEV))
+    lo, hi = (u * N - (1 - u) / (w + d) for d in (-e, e))          # entries of the far ones in front of the drawn one
+    assert int(kept) == V and lo - 2 <= int(token) <= hi + 2, (lo, int(token), hi)
