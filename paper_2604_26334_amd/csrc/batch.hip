@@ -890,6 +890,7 @@ struct Place {
 struct BinScale {
     double m, rate, least;
     float top, coarse;
+    bool rough;                  // `about` says where an entry lies
     __device__ __forceinline__ Place place(float v) const {
         const double d = fmax((double)v - m, least), t = fma(d, -rate, kWhole);
         return {(int)(uint32_t)__builtin_bit_cast(uint64_t, t), fma(d, -rate, kWhole - t)};
@@ -897,8 +898,10 @@ struct BinScale {
     __device__ __forceinline__ float about(float v) const { return fminf((top - v) * coarse, (float)kBins); }     // a place to within 0.01
 };
 __device__ __forceinline__ BinScale bin_scale(float m, float temp) {
-    const double rate = kBinsPerNat / (double)fminf(temp, 1e30f);
-    return {(double)m, rate, -1e6 / rate, m, (float)fmin(rate, 1e30)};
+    // (any temperature above 0: of 1e-45 the rate is 6e46, of an infinite one 0.  What a difference of two logits times the rate is in 32 bits says
+    // nothing where the rate or, under a small rate, the difference passes their range)
+    const double rate = kBinsPerNat / (double)temp;
+    return {(double)m, rate, fmax(-1e6 / rate, -1e300), m, (float)fmin(rate, 1e30), rate >= 1e-25 && rate <= 1e30};
 }
 __device__ __forceinline__ unsigned long long whole_far(int n, double rest) {
     const float back = (float)(n - ((int)kBins - 1)) + (float)rest;
@@ -1237,8 +1240,8 @@ __device__ __forceinline__ void each_in(const T *x, uint32_t lo, uint32_t hi, co
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const bool some = r.lo[j] <= r.hi[j];
-        from[j] = some ? (float)r.lo[j] - 1.f : INFINITY;
-        to[j] = !some ? -INFINITY : r.hi[j] == (int)kBins - 1 ? INFINITY : (float)r.hi[j] + 1.f;
+        from[j] = !some ? INFINITY : !s.rough ? -INFINITY : (float)r.lo[j] - 1.f;
+        to[j] = !some ? -INFINITY : !s.rough || r.hi[j] == (int)kBins - 1 ? INFINITY : (float)r.hi[j] + 1.f;
     }
     constexpr uint32_t kStride = kPickThreads * 8;
     uint32_t i = lo + threadIdx.x * 8;

@@ -168,3 +168,23 @@ def test_weights_far_behind_the_largest(back):
     token, kept = B.sample(x, torch.tensor([u], device=DEV))
     lo, hi = (u * N - (1 - u) / (w + d) for d in (-e, e))          # entries of the far ones in front of the drawn one
     assert int(kept) == V and lo - 2 <= int(token) <= hi + 2, (lo, int(token), hi)
+
+
+@pytest.mark.parametrize("V", [300, 50000])
+@pytest.mark.parametrize("temp,size", [(1e-35, 1e-34), (1e-40, 1e-39), (1e-30, 1e-30), (2e-29, 1e-28), (1e-45, 1.0), (1e26, 2e27), (2e27, 1e28), (1e35, 2e35), (3.4e38, 8e37), (float("inf"), 8e37),
+                                    (float("inf"), 1.0)])
+def test_sample_at_temperatures_of_any_size(temp, size, V):
+    """Temperatures and logits at the ends of fp32's range, subnormal ones among them, some logits at the ends of it themselves."""
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    x = (torch.randn(6, V, generator=_gen(V), device=DEV) * size).clamp(-3.4e38, 3.4e38)
+    if size > 1e30:
+        x[1, 7], x[2, 9], x[2, 11] = torch.finfo(torch.float32).max, torch.finfo(torch.float32).min, float("inf")
+    x[3, 5:60] = float("-inf")
+    u = torch.rand(6, generator=_gen(1), device=DEV)
+    t = torch.full((6,), temp, device=DEV)
+    assert float(t[0]) > 0
+    for s in (dict(), dict(top_k=_ints([20, 1, 0, 100, V, 3])), dict(top_p=torch.tensor([0.9, 0.5, 0.99, 0.9, 0.1, 0.7], device=DEV)),
+              dict(top_k=_ints([200] * 6), top_p=torch.full((6,), 0.8, device=DEV), min_p=torch.full((6,), 0.02, device=DEV))):
+        token, kept = B.sample(x, u, temperature=t, **s)
+        T._check_sample(x, u, token, kept, temperature=t, **s)
