@@ -188,3 +188,25 @@ def test_sample_at_temperatures_of_any_size(temp, size, V):
               dict(top_k=_ints([200] * 6), top_p=torch.full((6,), 0.8, device=DEV), min_p=torch.full((6,), 0.02, device=DEV))):
         token, kept = B.sample(x, u, temperature=t, **s)
         T._check_sample(x, u, token, kept, temperature=t, **s)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_a_steps_attention_sees_what_its_tables_and_rows_say(seed):
+    """Tables, rows to pages and attention of one step, the latter against the oracle over the pages as the step left them and the queries as it made
+    them: within the roundings of the attention alone, so that a position too many or too few shows."""
+    from paper_2604_26334_amd import binding as B
+    a = T._step_case(10 + seed)
+    pool0, table0, toks = a["pool"].clone(), a["table"].tolist(), a["new"].tolist()
+    first, length, position, slot, taken, q, k, out, logits, token, kept = T._step(a, B)
+    want = O.page_tables(a["cached"].tolist(), toks, table0, a["free"].tolist(), 1, 16, a["pages"], a["n"], a["offset"].tolist())
+    assert a["table"].tolist() == want[0] and slot.tolist()[:len(want[4])] == want[4]
+    # the rows of the step's tokens, bit for bit, and no others
+    for t, at in enumerate(want[4]):
+        pool0[at // 16, 0, :, at % 16], pool0[at // 16, 1, :, at % 16] = k[t], a["v"][t]
+    assert _same_bits(a["pool"], pool0)
+    seen = dict(q=q, k_pages=a["pool"][:, 0], v_pages=a["pool"][:, 1])
+    full = [want[0], a["prefix_table"].tolist()]
+    T._check_attend(seen, out, want[1], full, toks, want[2], (0, 4), [50], "f16")
+    for lens, plens in (([n - 1 for n in want[2]], [50]), ([n + 1 for n in want[2]], [50]), (want[2], [49])):       # (the check can tell)
+        with pytest.raises(AssertionError):
+            T._check_attend(seen, out, want[1], full, toks, lens, (0, 4), plens, "f16")
