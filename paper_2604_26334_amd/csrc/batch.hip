@@ -134,8 +134,9 @@ __global__ __launch_bounds__(256) void page_append_kernel(ps_page_append_args a,
 // same time, and a merge of their records.  More tokens: blocks of 128 rows walk prefix and own positions one after the other.
 // Measured: own positions alone, 48 sequences of up to 8190 (16 / 8 heads of 64) 102 us = 5.3 TB/s; 64 sequences behind a prefix of 32761 (32 / 8
 // heads), own lengths up to 1000, 91 us: about 60 for the prefix's products and 34 for the own positions' bytes when each runs alone; prompts, 2 of 2048
-// tokens behind 16384 positions, 798 TFLOP/s, 8 of 512 behind 2048 198 us = 750: the matrix cores are busy 41 % of the time and the vector
-// instructions of the softmax, which share their issue port, 47 %.
+// tokens behind 16384 positions, 798 TFLOP/s, 8 of 512 behind 2048 198 to 206 us = 720 to 750: the matrix cores are busy 37 % of the CUs' time and the vector
+// instructions of the softmax, which share their issue port, 46 %.
+// All of a call goes one way, by its bounds: 64 sequences behind 32761 (32 / 8 heads, own 1000) take 388 us with 8 tokens each, 32 rows, and 1203 with 9.
 constexpr uint32_t kTile = 32, kStep = 64;
 constexpr uint32_t kFewRows = 32;
 
@@ -836,7 +837,8 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
 }
 
 // ------------------------------------------------------------------------------------ sampling
-// Launches, in order:
+// Launches, in order (three for rows of up to 32768 entries, whose border entries the last one picks out itself: rows of 32768, 256 of them 54 us for 60, 16 the same,
+// a single one 31 for 25):
 //  sample_rows_kernel   a row's chunks: largest logit and where; clears the row's bins
 //  sample_bins_kernel   entries by how far they lie behind the row's largest logit, in bins of 24 / 2047 nats (the last one: all from 24 nats on):
 //                       counts, and sums of weights relative to the bin's middle as whole numbers of 2^-35, so that their order does not matter
@@ -845,8 +847,10 @@ __global__ __launch_bounds__(256) void page_merge_kernel(ps_page_attention_args 
 //  sample_pick_kernel   a workgroup per row finds the borders among them, digit by digit of the logits' bits.  Where they are more than a list holds, in
 //                       passes over the row instead.
 // The sum of the first entries of the order is that of whole bins (64 bits, always added alike) and of a part of one, whose whole numbers are exact.
-// 256 rows of 128256 fp32 logits: 22 + 37 + 39 + 16 us, where each of the first three reads the 131 MB (27 us at a copy's rate); the second has a dozen
+// 256 rows of 128256 fp32 logits: 22 + 35 + 37 + 16 us, where each of the first three reads the 131 MB (27 us at a copy's rate); the second has a dozen
 // 64-bit operations and an addition in LDS for each entry beside.  16 rows 4 + 8 + 13 + 12 us, one of 32000 3 + 5 + 16: latencies.
+// Where the borders' bins hold more than a list does, one workgroup reads its row once for each digit: rows of 128256 equal logits 254 us, of logits closer than 0.01
+// 470 to 550 (with top-k and top-p 530 to 610), 16 rows hardly more, 256 rows 385 and 570 to 630.
 constexpr uint32_t kBins = 2048, kRowThreads = 256, kPickThreads = 512, kBinsPad = kBins + 8, kList = 2048, kRound = kPickThreads * 8, kShortRow = 32768;
 constexpr double kBinsPerNat = 2047.0 / 24.0;
 
