@@ -210,3 +210,54 @@ def test_a_steps_attention_sees_what_its_tables_and_rows_say(seed):
     for lens, plens in (([n - 1 for n in want[2]], [50]), ([n + 1 for n in want[2]], [50]), (want[2], [49])):       # (the check can tell)
         with pytest.raises(AssertionError):
             T._check_attend(seen, out, want[1], full, toks, lens, (0, 4), plens, "f16")
+
+
+@pytest.mark.parametrize("bound", [0, 1000, 200000])
+@pytest.mark.parametrize("most", [2, 40])
+def test_a_captured_step_with_room_for_other_batches(bound, most):
+    """One captured call in arrays with room for more rows, replayed for several batches: each replay gives what an eager call gives, and leaves the rows behind the
+    last sequence alone."""
+    from paper_2604_26334_amd import binding as B
+    torch = _t()
+    room = 12 * most + 500
+    batches = []
+    for seed in range(3):
+        rng = np.random.default_rng(seed)
+        toks = [int(rng.integers(0, most + 1)) for _ in range(12)]
+        lens = [t + int(rng.integers(0, 300)) for t in toks]
+        a, first, full = T._attend_case("f16", 128, 8, 2, 16, toks, lens, (0, 5, 9), [300, 77], seed, bound=bound)
+        batches.append((a, first, full, toks, lens))
+    q = torch.zeros(room, 8, 128, dtype=torch.float16, device=DEV)
+    pages = max(a["k_pages"].shape[0] for a, *_ in batches)
+    kp, vp = (torch.zeros(pages, 2, 16, 128, dtype=torch.float16, device=DEV) for _ in range(2))
+    width, wide = (max(a[n].shape[1] for a, *_ in batches) for n in ("table", "prefix_table"))
+    now = dict(q=q, k_pages=kp, v_pages=vp, first=_ints([0] * 13), length=_ints([0] * 12), table=_ints([[-1] * width] * 12), max_length=max(max(b[4]) for b in batches), max_tokens=most,
+               group_first=_ints([0, 5, 9]), prefix_length=_ints([300, 77]), prefix_table=_ints([[-1] * wide] * 2), max_prefix=max(300, bound))
+
+    def put(a):
+        n = int(a["first"][-1])
+        q.fill_(float("nan"))
+        q[:n] = a["q"]
+        for name in ("k_pages", "v_pages"):
+            now[name][:a[name].shape[0]] = a[name]
+        now["first"].copy_(a["first"])
+        now["length"].copy_(a["length"])
+        now["table"][:, :a["table"].shape[1]] = a["table"]
+        now["prefix_table"][:, :a["prefix_table"].shape[1]] = a["prefix_table"]
+        return n
+    out = torch.full_like(q, 3.0)
+    put(batches[0][0])
+    B.page_attention(**now, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.page_attention(**now, out=out)
+    for i in (0, 1, 2, 0, 2, 1):
+        a, first, full, toks, lens = batches[i]
+        n = put(a)
+        out.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert bool((out[n:] == 3).all())
+        T._check_attend(a, out[:n], first, full, toks, lens, (0, 5, 9), [300, 77], "f16")
+        assert _same_bits(out[:n], B.page_attention(**now)[:n])
